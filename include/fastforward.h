@@ -244,6 +244,150 @@ ff_status ff_rmsnorm(ff_ctx *ctx, int32_t n_tokens, int32_t d_model,
 ff_status ff_residual_add(ff_ctx *ctx, int32_t n_tokens, int32_t d_model,
                           void *h, const void *y);
 
+/* ---- the other half of a layer: attention, positions, norms -------------
+ *
+ * Conventions of these calls, beyond those above: a token's heads lie side by
+ * side in its row, head h at [h * head_dim], and rows lie `*_stride` elements
+ * apart (a multiple of 8, at least the row's width), so q, k and v may be parts
+ * of one projection's output.  Lengths, positions, page tables and slots are
+ * device arrays: nothing is copied from the host, every call may be captured in
+ * a HIP graph, and a replay reads what the arrays hold by then.  Whatever they
+ * hold, no access leaves the tensors that the call was given. */
+
+/* Heads of an attention layer and who sees whom.  Query head h reads key head
+ * h / (n_heads / n_kv_heads).  Limits: head_dim 64 or 128, n_heads a multiple
+ * of n_kv_heads and at most 1024, n_tokens at most 2^30 and n_tokens * n_heads
+ * below 2^31 - 2^16, at most 16384 sequences (FF_ERR_SHAPE); scale > 0 and finite, window
+ * >= 0, a window only with causal (FF_ERR_INVALID_ARG). */
+typedef struct {
+  int32_t n_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t causal;   /* 1: a token sees the keys up to its own position, 0: all of its sequence */
+  int32_t window;   /* > 0: of those only the last `window` (its own position among them) */
+  float scale;      /* of the products q . k, e.g. 1 / sqrt(head_dim) */
+} ff_attention;
+
+/* Keys and values in pages: dev bf16 [n_pages][n_kv_heads][page_size][head_dim]
+ * each.  page_size is a power of two from 8 to 4096. */
+typedef struct {
+  void *k;
+  void *v;
+  int32_t n_pages;
+  int32_t page_size;
+} ff_paged_cache;
+
+/* Rotary positions.  Channel pair i of a head, 0 <= i < rot_dim / 2, turns by
+ * the angle positions[axis[i]][token] * inv_freq[i] (the product and its
+ * reduction are made in float64: far positions keep their digits).  Channels
+ * from rot_dim on stay as they are.  rot_dim is a multiple of 16, at most
+ * head_dim. */
+typedef struct {
+  int32_t rot_dim;
+  int32_t interleaved;    /* 0: pair i = channels i and i + rot_dim / 2; 1: 2 i and 2 i + 1 */
+  int32_t n_axes;         /* 1 to 4 rows of positions (text: 1; images: height and width beside time) */
+  const int32_t *axis;    /* host [rot_dim / 2], entries in [0, n_axes); NULL = all on axis 0 */
+  const float *inv_freq;  /* dev f32 [rot_dim / 2], radians per position */
+} ff_rotary_spec;
+
+enum { FF_NORM_RMS = 1, FF_NORM_LAYER = 2 };
+/* v -> (v - c) / sqrt(mean((v - c)^2) + eps) * (gain + gain_offset) + bias, with
+ * c = 0 (RMS) or mean(v) (LAYER). */
+typedef struct {
+  int32_t kind;        /* FF_NORM_* */
+  float eps;           /* >= 0 */
+  float gain_offset;   /* 1 where weights are stored as gain - 1, else 0 */
+  const void *gain;    /* dev bf16 [d_model], or NULL: a factor of 1 (no offset) */
+  const void *bias;    /* dev bf16 [d_model], or NULL */
+} ff_norm;
+
+/* Norms around a block, with the block's gate and the residual's scale:
+ *   s = h + scale * gate * post(y),  h_out = bf16(s),  x = bf16(pre(s))
+ * in fp32 from the inputs to the two roundings (s is not rounded before pre).
+ *   h          dev bf16 [n_tokens][d_model]
+ *   y          dev [n_tokens][d_model], what the block gave, bf16 or f32 by
+ *              y_dtype (FF_OUT_*); NULL: s = h (post, gate and h_out NULL too)
+ *   post       norm of y, or NULL: y as it is
+ *   gate       dev bf16 [ceil(n_tokens / gate_tokens)][d_model], a row for every
+ *              gate_tokens tokens (1: each its own; n_tokens: one for all; a
+ *              block's length: one for each block), or NULL: 1
+ *   h_out      dev bf16 [n_tokens][d_model], out; may be h; NULL: not stored
+ *   pre, x     norm before the next block and dev bf16 [n_tokens][d_model], out;
+ *              both or neither
+ * Outputs overlap no input except h_out = h.  d_model is a multiple of 8, at
+ * most 16384. */
+ff_status ff_norm_residual(ff_ctx *ctx, int32_t n_tokens, int32_t d_model,
+                           const void *h, const void *y, int32_t y_dtype,
+                           const ff_norm *post, const void *gate,
+                           int32_t gate_tokens, float scale, void *h_out,
+                           const ff_norm *pre, void *x);
+
+/* Turns q and k and puts k and v where attention finds them.
+ *   q, k, v       dev bf16 [n_tokens] rows of n_heads, n_kv_heads, n_kv_heads
+ *                 heads (a->causal, window and scale are ignored)
+ *   positions     dev int32 [n_axes][n_tokens]
+ *   q_out, k_out  dev bf16 rows as q and k, out; q_out may be q and k_out may be
+ *                 k (with the same stride); k_out may be NULL with a cache
+ *   cache, slots  the cache and dev int32 [n_tokens]: token t's key and value go
+ *                 to place slots[t] % page_size of page slots[t] / page_size; a
+ *                 slot outside the cache (negative: a padded token) is not
+ *                 written.  Both NULL: no cache (v may then be NULL).  Tokens'
+ *                 slots differ; of two tokens with the same slot either's values
+ *                 may stay, in part. */
+ff_status ff_rotary(ff_ctx *ctx, const ff_attention *a, const ff_rotary_spec *r,
+                    int32_t n_tokens, const void *q, int64_t q_stride,
+                    const void *k, int64_t k_stride, const void *v,
+                    int64_t v_stride, const int32_t *positions, void *q_out,
+                    int64_t q_out_stride, void *k_out, int64_t k_out_stride,
+                    const ff_paged_cache *cache, const int32_t *slots);
+
+/* Bytes of workspace the two attention calls need at most (fp32 partial sums of
+ * attention split along the keys), whatever the sequences' lengths. */
+ff_status ff_attention_workspace_bytes(const ff_attention *a, int32_t n_tokens,
+                                       int32_t n_seqs, size_t *bytes);
+
+/* Attention over whole prompts: o_t = sum_j p_j v_j, p = softmax_j(scale q_t . k_j)
+ * over the keys j of t's own sequence that a->causal and a->window leave it.
+ *   q, k, v      dev bf16 [n_tokens] rows of n_heads, n_kv_heads, n_kv_heads heads
+ *   seq_starts   dev int32 [n_seqs + 1], ascending: sequence s is rows
+ *                [seq_starts[s], seq_starts[s + 1]), possibly none
+ *   o            dev bf16 [n_tokens] rows of n_heads heads, out; rows of no
+ *                sequence are left as they were
+ *   lse_opt      dev f32 [n_tokens][n_heads] out, or NULL: log sum_j exp(scale q . k_j)
+ * Products and sums are fp32; the softmax weights are rounded to bf16 once, as
+ * operands of the product with v; o is rounded once.  A row that sees no key
+ * gets o = 0 and lse = -inf.  Values of keys that a row does not see never reach
+ * it, infinities and NaN among them.  A call repeated on the same inputs gives
+ * the same bits. */
+ff_status ff_prompt_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens,
+                              int32_t n_seqs, const void *q, int64_t q_stride,
+                              const void *k, int64_t k_stride, const void *v,
+                              int64_t v_stride, const int32_t *seq_starts,
+                              void *o, int64_t o_stride, float *lse_opt);
+
+/* The same for new tokens over a paged cache that holds their keys already: a
+ * chunk of a prompt, a single generated token, or a batch of both.
+ *   q             dev bf16 [n_tokens] rows of n_heads heads
+ *   chunk_starts  dev int32 [n_seqs + 1]: rows of sequence s's new tokens
+ *   context_lens  dev int32 [n_seqs]: keys of sequence s, the new tokens' own
+ *                 (the last of them) included; cut to table_stride * page_size.
+ *                 With fewer keys than new tokens the first tokens see none.
+ *   max_chunk     the longest chunk, as far as the host knows: it chooses the
+ *                 kernels; other lengths are computed right too
+ *   page_table    dev int32 [n_seqs][table_stride]: key j of sequence s is at
+ *                 place j % page_size of page page_table[s][j / page_size].  An
+ *                 entry outside [0, n_pages) that a key needs is read as page 0
+ *                 (with the option "validate": FF_ERR_INDEX instead, also for
+ *                 starts and lengths out of range; the check synchronises, and
+ *                 is refused while the stream is capturing)
+ *   o, lse_opt    as above */
+ff_status ff_chunk_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens,
+                             int32_t n_seqs, const void *q, int64_t q_stride,
+                             const int32_t *chunk_starts, const int32_t *context_lens,
+                             int32_t max_chunk, const ff_paged_cache *cache,
+                             const int32_t *page_table, int32_t table_stride,
+                             void *o, int64_t o_stride, float *lse_opt);
+
 #ifdef __cplusplus
 }
 #endif

@@ -67,7 +67,7 @@ enum {
   FF_STAGE_TOPK = 2,   /* Eq. 14: top-K select                      */
   FF_STAGE_GEMM1 = 3,  /* gathered gate/up GEMM + SiLU*up epilogue  */
   FF_STAGE_GEMM2 = 4,  /* gathered down GEMM + compensation         */
-  FF_STAGE_GLUE = 5,   /* RMSNorm, residual add                     */
+  FF_STAGE_GLUE = 5,   /* RMSNorm, residual add; the calls around the FFN */
   FF_N_STAGES = 6
 };
 ff_status ff_profile_enable(ff_ctx *ctx, int32_t max_records, uint32_t stage_mask);

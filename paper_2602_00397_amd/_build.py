@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libfastforward.so")
-SOURCES = ["ff_api.hip", "ff_predict.hip", "ff_gemm.hip", "ff_gemv.hip", "ff_glue.hip"]
+SOURCES = ["ff_api.hip", "ff_predict.hip", "ff_gemm.hip", "ff_gemv.hip", "ff_glue.hip", "ff_norm.hip", "ff_rotary.hip",
+           "ff_attention.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -47,7 +48,7 @@ def build(verbose: bool = False, extra_flags=()) -> str:
             f.writelines(l + "\n" for l in lines if "[-Rpass-analysis" in l)
         return "\n".join(l for l in lines if "[-Rpass-analysis" not in l)
 
-    with ThreadPoolExecutor(max_workers=min(5, len(SOURCES))) as ex:
+    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
         outs = list(ex.map(one, zip(SOURCES, objs)))
     outs.append(_run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]))
     if verbose:
@@ -81,7 +82,7 @@ def build_host_checks() -> str:
         src, obj = pair
         return _run([HIPCC, *FLAGS, *san, "-c", os.path.join(CSRC, src), "-o", obj])
 
-    with ThreadPoolExecutor(max_workers=min(5, len(SOURCES))) as ex:
+    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
         list(ex.map(one, zip(SOURCES, objs)))
     rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
     clang = os.path.join(rocm, "lib", "llvm", "bin", "clang")
@@ -95,12 +96,12 @@ def build_host_checks() -> str:
 
 
 def build_launch_checks() -> str:
-    """csrc/ff_launch_checks.hip with the predictor's, the GEMMs' and the few-token launchers' object files (as build() left them): the program
+    """csrc/ff_launch_checks.hip with the predictor's, the GEMMs', the few-token and the attention launchers' object files (as build() left them): the program
     records their launches instead of making them, so it needs no GPU."""
     exe = os.path.join(OBJ, "ff_launch_checks")
     obj = os.path.join(OBJ, "ff_launch_checks.o")
     _run([HIPCC, *FLAGS, "-c", os.path.join(CSRC, "ff_launch_checks.hip"), "-o", obj])
-    _run([HIPCC, "--offload-arch=gfx950", obj, *(os.path.join(OBJ, "ff_%s.o" % n) for n in ("predict", "gemm", "gemv")), "-o", exe,
+    _run([HIPCC, "--offload-arch=gfx950", obj, *(os.path.join(OBJ, "ff_%s.o" % n) for n in ("predict", "gemm", "gemv", "attention")), "-o", exe,
           "-Wl,-rpath," + os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "lib")])
     return exe
 

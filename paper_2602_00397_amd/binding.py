@@ -19,6 +19,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libfastforward.so")
 
 ACT = {"silu": 0, "relu": 1, "identity": 2}
+NORM = {"rms": 1, "layer": 2}
 OUT_BF16, OUT_F32 = 0, 1
 
 
@@ -37,6 +38,26 @@ class FfnWeights(C.Structure):
 
 class Compensator(C.Structure):
     _fields_ = [("wc1", C.c_void_p), ("wc2", C.c_void_p), ("act", C.c_int32)]
+
+
+class Attention(C.Structure):
+    """Heads of an attention layer and who sees whom (ff_attention)."""
+    _fields_ = [("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("causal", C.c_int32), ("window", C.c_int32), ("scale", C.c_float)]
+
+
+class PagedCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
+class RotarySpec(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32),
+                ("axis", C.POINTER(C.c_int32)), ("inv_freq", C.c_void_p)]
+
+
+class Norm(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("gain_offset", C.c_float), ("gain", C.c_void_p),
+                ("bias", C.c_void_p)]
 
 
 class FFError(RuntimeError):
@@ -59,7 +80,7 @@ def load_library(build_if_missing: bool = True):
         from . import _build
         _build.build()
     lib = C.CDLL(LIB_PATH)
-    vp, i32, sz = C.c_void_p, C.c_int32, C.c_size_t
+    vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
     P = C.POINTER
     sig = {
         "ff_create": ([P(vp), C.c_int, vp], C.c_int),
@@ -82,6 +103,13 @@ def load_library(build_if_missing: bool = True):
         "ff_profile_read": ([vp, P(C.c_double), P(i32)], C.c_int),
         "ff_rmsnorm": ([vp, i32, i32, vp, C.c_float, vp], C.c_int),
         "ff_residual_add": ([vp, i32, i32, vp, vp], C.c_int),
+        "ff_norm_residual": ([vp, i32, i32, vp, vp, i32, P(Norm), vp, i32, C.c_float, vp, P(Norm), vp], C.c_int),
+        "ff_rotary": ([vp, P(Attention), P(RotarySpec), i32, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64,
+                       P(PagedCache), vp], C.c_int),
+        "ff_attention_workspace_bytes": ([P(Attention), i32, i32, P(sz)], C.c_int),
+        "ff_prompt_attention": ([vp, P(Attention), i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp], C.c_int),
+        "ff_chunk_attention": ([vp, P(Attention), i32, i32, vp, i64, vp, vp, i32, P(PagedCache), vp, i32, vp, i64,
+                                vp], C.c_int),
         "ff_copy": ([vp, vp, vp, sz], C.c_int),
         "ff_mfma_peak": ([vp, i32, i32, P(C.c_double)], C.c_int),
     }
@@ -95,6 +123,7 @@ def load_library(build_if_missing: bool = True):
 EXPORTS = ["ff_create", "ff_destroy", "ff_set_stream", "ff_status_str", "ff_last_error", "ff_workspace_bytes",
            "ff_set_workspace", "ff_set_option", "ff_k_from_sparsity", "ff_layer_budgets", "ff_predict", "ff_predict_static",
            "ff_sparse_ffn", "ff_dense_ffn", "ff_ffn_stack", "ff_rmsnorm", "ff_residual_add",
+           "ff_norm_residual", "ff_rotary", "ff_attention_workspace_bytes", "ff_prompt_attention", "ff_chunk_attention",
            "ff_profile_enable", "ff_profile_read", "ff_copy", "ff_mfma_peak"]
 
 STAGES = ("pool", "mlp", "topk", "gemm1", "gemm2", "glue")
@@ -105,6 +134,24 @@ def _ptr(t: Optional[torch.Tensor]):
         return None
     assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous CUDA tensors"
     return C.c_void_p(t.data_ptr())
+
+
+def _typed(t: Optional[torch.Tensor], dtype, shape=None):
+    """A contiguous tensor's pointer, its type and shape as the call takes them for granted."""
+    if t is None:
+        return None
+    assert t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
+    assert shape is None or tuple(t.shape) == tuple(shape), f"expected shape {tuple(shape)}, got {tuple(t.shape)}"
+    return _ptr(t)
+
+
+def _rows(t: Optional[torch.Tensor], n_rows: int, width: int):
+    """(pointer, stride) of bf16 rows that may lie apart, such as a part of a projection's output."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.dtype == torch.bfloat16 and tuple(t.shape) == (n_rows, width) and t.stride(1) == 1, \
+        f"expected bf16 rows [{n_rows}][{width}] on the GPU, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}"
+    return C.c_void_p(t.data_ptr()), (t.stride(0) if n_rows > 1 else max(t.stride(0), width))
 
 
 def _i32_array(values: Sequence[int]):
@@ -136,6 +183,47 @@ def workspace_bytes(shape: Shape, k_max: int) -> int:
     if st:
         raise FFError(st, "ff_workspace_bytes")
     return out.value
+
+
+def attention_workspace_bytes(heads: Attention, n_tokens: int, n_seqs: int) -> int:
+    out = C.c_size_t()
+    st = load_library().ff_attention_workspace_bytes(C.byref(heads), int(n_tokens), int(n_seqs), C.byref(out))
+    if st:
+        raise FFError(st, "ff_attention_workspace_bytes")
+    return out.value
+
+
+# The descriptions below hold pointers; each keeps the tensors that it was made of alive.
+
+def norm(kind: str, eps: float, gain: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+         gain_offset: float = 0.0) -> Norm:
+    n = Norm(NORM[kind], float(eps), float(gain_offset), _typed(gain, torch.bfloat16), _typed(bias, torch.bfloat16))
+    n.tensors = (gain, bias)
+    return n
+
+
+def rotary(rot_dim: int, inv_freq: torch.Tensor, axis: Optional[Sequence[int]] = None, interleaved: bool = False,
+           n_axes: int = 1) -> RotarySpec:
+    keep = ptr = None
+    if axis is not None:
+        assert len(axis) == rot_dim // 2, f"axis has {len(axis)} entries, {rot_dim // 2} pairs turn"
+        keep, ptr = _i32_array(axis)
+    r = RotarySpec(int(rot_dim), int(interleaved), int(n_axes), ptr, _typed(inv_freq, torch.float32, (rot_dim // 2,)))
+    r.tensors = (keep, inv_freq)
+    return r
+
+
+def paged_cache(k_pages: torch.Tensor, v_pages: torch.Tensor) -> PagedCache:
+    """bf16 [n_pages][n_kv_heads][page_size][head_dim] each."""
+    assert k_pages.dim() == 4 and k_pages.shape == v_pages.shape
+    c = PagedCache(_typed(k_pages, torch.bfloat16), _typed(v_pages, torch.bfloat16), k_pages.shape[0], k_pages.shape[2])
+    c.tensors = (k_pages, v_pages)
+    return c
+
+
+def _check_pages(cache: PagedCache, heads: Attention):
+    assert tuple(cache.tensors[0].shape[1::2]) == (heads.n_kv_heads, heads.head_dim), \
+        f"cache pages {tuple(cache.tensors[0].shape)} are not of {heads.n_kv_heads} heads of {heads.head_dim}"
 
 
 class Context:
@@ -173,7 +261,12 @@ class Context:
         self._check(self.lib.ff_set_option(self._h, name.encode(), int(value)))
 
     def ensure_workspace(self, shape: Shape, k_max: int):
-        need = workspace_bytes(shape, k_max)
+        self._ensure(workspace_bytes(shape, k_max))
+
+    def ensure_attention_workspace(self, heads: Attention, n_tokens: int, n_seqs: int):
+        self._ensure(attention_workspace_bytes(heads, n_tokens, n_seqs))
+
+    def _ensure(self, need: int):
         if self._ws is None or self._ws.numel() < need:
             self._ws = None
             self._ws = torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}")
@@ -229,6 +322,46 @@ class Context:
 
     def rmsnorm(self, h, eps: float, x):
         self._check(self.lib.ff_rmsnorm(self._h, h.shape[0], h.shape[1], _ptr(h), float(eps), _ptr(x)))
+
+    def norm_residual(self, h, y, h_out, x, post: Optional[Norm] = None, gate=None, gate_tokens: int = 1,
+                      scale: float = 1.0, pre: Optional[Norm] = None):
+        bf16 = torch.bfloat16
+        for n in (post, pre):
+            for t in n.tensors if n is not None else ():
+                assert t is None or tuple(t.shape) == (h.shape[1],), "norm weights are one for each channel"
+        assert y is None or y.dtype in (bf16, torch.float32)
+        gate_shape = None if gate is None or gate_tokens < 1 else (-(-h.shape[0] // gate_tokens), h.shape[1])
+        ref = lambda n: C.byref(n) if n is not None else None
+        self._check(self.lib.ff_norm_residual(
+            self._h, h.shape[0], h.shape[1], _typed(h, bf16), _typed(y, y.dtype, h.shape) if y is not None else None,
+            OUT_F32 if y is not None and y.dtype == torch.float32 else OUT_BF16, ref(post), _typed(gate, bf16, gate_shape),
+            int(gate_tokens), float(scale), _typed(h_out, bf16, h.shape), ref(pre), _typed(x, bf16, h.shape)))
+
+    def rotary(self, heads: Attention, rot: RotarySpec, q, k, v, positions, q_out, k_out=None,
+               cache: Optional[PagedCache] = None, slots=None):
+        n, qw, kw = q.shape[0], heads.n_heads * heads.head_dim, heads.n_kv_heads * heads.head_dim
+        if cache is not None:
+            _check_pages(cache, heads)
+        self._check(self.lib.ff_rotary(
+            self._h, C.byref(heads), C.byref(rot), n, *_rows(q, n, qw), *_rows(k, n, kw), *_rows(v, n, kw),
+            _typed(positions, torch.int32, (rot.n_axes, n)), *_rows(q_out, n, qw), *_rows(k_out, n, kw),
+            C.byref(cache) if cache is not None else None, _typed(slots, torch.int32, (n,))))
+
+    def prompt_attention(self, heads: Attention, q, k, v, seq_starts, o, lse=None):
+        n, qw, kw = q.shape[0], heads.n_heads * heads.head_dim, heads.n_kv_heads * heads.head_dim
+        self._check(self.lib.ff_prompt_attention(
+            self._h, C.byref(heads), n, seq_starts.numel() - 1, *_rows(q, n, qw), *_rows(k, n, kw), *_rows(v, n, kw),
+            _typed(seq_starts, torch.int32), *_rows(o, n, qw), _typed(lse, torch.float32, (n, heads.n_heads))))
+
+    def chunk_attention(self, heads: Attention, q, chunk_starts, context_lens, max_chunk: int, cache: PagedCache,
+                        page_table, o, lse=None):
+        n, qw, n_seqs = q.shape[0], heads.n_heads * heads.head_dim, context_lens.numel()
+        _check_pages(cache, heads)
+        self._check(self.lib.ff_chunk_attention(
+            self._h, C.byref(heads), n, n_seqs, *_rows(q, n, qw), _typed(chunk_starts, torch.int32, (n_seqs + 1,)),
+            _typed(context_lens, torch.int32), int(max_chunk), C.byref(cache),
+            _typed(page_table, torch.int32, (n_seqs, page_table.shape[1])), page_table.shape[1], *_rows(o, n, qw),
+            _typed(lse, torch.float32, (n, heads.n_heads))))
 
     def copy(self, dst, src):
         n = src.numel() * src.element_size()

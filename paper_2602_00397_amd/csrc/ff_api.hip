@@ -9,6 +9,7 @@
 #include <cmath>
 #include <new>
 
+#include "ff_attn_plan.h"
 #include "ff_internal.h"
 
 #include <vector>
@@ -405,6 +406,85 @@ int merge_choice(const ff_ctx *ctx, const ff_shape &s, const int32_t *k_per_bloc
   return merge_pays(mg, k_sum / n_blocks / s.d_ffn, few) ? mg : 0;
 }
 
+// The validate option: the flag cleared before a check and read back after it.  The check reads its result back and waits for it:
+// not something a graph can hold.
+ff_status begin_validate(ff_ctx *ctx) {
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  FF_HIP(ctx, hipStreamIsCapturing(ctx->stream, &cap));
+  if (cap != hipStreamCaptureStatusNone)
+    return fail(ctx, FF_ERR_INVALID_ARG, "the validate option synchronises the stream and cannot be captured in a HIP graph");
+  FF_HIP(ctx, hipMemsetAsync(ctx->flag_dev, 0, sizeof(int32_t), ctx->stream));
+  return FF_OK;
+}
+ff_status read_flag(ff_ctx *ctx) {
+  FF_HIP(ctx, hipMemcpyAsync(ctx->flag_host, ctx->flag_dev, sizeof(int32_t), hipMemcpyDeviceToHost, ctx->stream));
+  FF_HIP(ctx, hipStreamSynchronize(ctx->stream));
+  return FF_OK;
+}
+
+// ---- checks of the calls around the FFN
+ff_status check_heads(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens) {
+  if (!a) return fail(ctx, FF_ERR_INVALID_ARG, "attention heads are NULL");
+  if (a->n_heads < 1 || a->n_kv_heads < 1 || a->head_dim < 1 || n_tokens < 1) return fail(ctx, FF_ERR_INVALID_ARG, "sizes must be positive");
+  if (a->head_dim != 64 && a->head_dim != 128) return fail(ctx, FF_ERR_SHAPE, "head_dim (%d) must be 64 or 128", a->head_dim);
+  if (a->n_heads > 1024 || a->n_heads % a->n_kv_heads)
+    return fail(ctx, FF_ERR_SHAPE, "n_heads (%d) must be a multiple of n_kv_heads (%d) and at most 1024", a->n_heads, a->n_kv_heads);
+  if (n_tokens > (1 << 30) || (long)n_tokens * a->n_heads > 0x7fff0000L)
+    return fail(ctx, FF_ERR_SHAPE, "more than 2^30 tokens, or about 2^31 rows (n_tokens * n_heads)");
+  return FF_OK;
+}
+constexpr int kMaxSeqs = 16384;
+ff_status check_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs) {
+  ff_status st = check_heads(ctx, a, n_tokens);
+  if (st != FF_OK) return st;
+  if (n_seqs < 1) return fail(ctx, FF_ERR_INVALID_ARG, "sizes must be positive");
+  if (n_seqs > kMaxSeqs) return fail(ctx, FF_ERR_SHAPE, "more than %d sequences", kMaxSeqs);
+  if (!(a->scale > 0.f) || std::isinf(a->scale)) return fail(ctx, FF_ERR_INVALID_ARG, "scale must be positive and finite");
+  if (a->window < 0 || (a->window > 0 && !a->causal)) return fail(ctx, FF_ERR_INVALID_ARG, "a window (%d) is positive and goes with causal", a->window);
+  return FF_OK;
+}
+// rows of `width` elements, `stride` apart
+ff_status check_rows(ff_ctx *ctx, const char *name, const void *ptr, int64_t stride, int64_t width) {
+  if (!ptr) return fail(ctx, FF_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!aligned16(ptr)) return fail(ctx, FF_ERR_ALIGNMENT, "%s must be 16-byte aligned", name);
+  if (stride < width || stride > (1 << 24)) return fail(ctx, FF_ERR_SHAPE, "stride of %s (%lld) must be in [%lld, 2^24]", name, (long long)stride, (long long)width);
+  if (stride % 8) return fail(ctx, FF_ERR_ALIGNMENT, "stride of %s (%lld) must be a multiple of 8", name, (long long)stride);
+  return FF_OK;
+}
+ff_status check_cache(ff_ctx *ctx, const ff_paged_cache *c) {
+  if (!c || !c->k || !c->v || c->n_pages < 1) return fail(ctx, FF_ERR_INVALID_ARG, "no cache, or one without pages");
+  if (!aligned16(c->k) || !aligned16(c->v)) return fail(ctx, FF_ERR_ALIGNMENT, "cache pages must be 16-byte aligned");
+  if (c->page_size < 8 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)))
+    return fail(ctx, FF_ERR_SHAPE, "page_size (%d) must be a power of two from 8 to 4096", c->page_size);
+  return FF_OK;
+}
+ff_status check_norm(ff_ctx *ctx, const ff_norm *n, NormSpec *out) {
+  *out = NormSpec();
+  if (!n) return FF_OK;
+  if (n->kind != FF_NORM_RMS && n->kind != FF_NORM_LAYER) return fail(ctx, FF_ERR_INVALID_ARG, "unknown norm %d", n->kind);
+  if (!(n->eps >= 0.f) || std::isinf(n->eps) || !std::isfinite(n->gain_offset)) return fail(ctx, FF_ERR_INVALID_ARG, "eps must be >= 0, eps and gain_offset finite");
+  if (!aligned16(n->gain) || !aligned16(n->bias)) return fail(ctx, FF_ERR_ALIGNMENT, "norm weights must be 16-byte aligned");
+  out->kind = n->kind;
+  out->eps = n->eps;
+  out->gain_offset = n->gain_offset;
+  out->gain = static_cast<const bf16_t *>(n->gain);
+  out->bias = static_cast<const bf16_t *>(n->bias);
+  return FF_OK;
+}
+int log2_of(int v) {
+  int s = 0;
+  while ((1 << s) < v) ++s;
+  return s;
+}
+AttnParams attn_params(const ff_attention &a, int32_t n_tokens, int32_t n_seqs) {
+  AttnParams p = {};
+  p.T = n_tokens; p.n_seqs = n_seqs;
+  p.n_heads = a.n_heads; p.n_kv = a.n_kv_heads; p.group = a.n_heads / a.n_kv_heads;
+  p.causal = a.causal != 0; p.window = a.window;
+  p.scale_log2 = a.scale * 1.4426950408889634f;
+  return p;
+}
+
 ff_status check_weights(ff_ctx *ctx, const ff_ffn_weights *w) {
   if (!w || !w->w_gate || !w->w_up || !w->w_down) return fail(ctx, FF_ERR_INVALID_ARG, "FFN weight pointer is NULL");
   if (!aligned16(w->w_gate) || !aligned16(w->w_up) || !aligned16(w->w_down))
@@ -479,7 +559,7 @@ ff_status ff_create(ff_ctx **out, int device, void *hip_stream) {
       st = FF_ERR_DEVICE;
       break;
     }
-    if (ff_gemm_init(lds) != hipSuccess) { st = FF_ERR_DEVICE; break; }
+    if (ff_gemm_init(lds) != hipSuccess || ff_attention_init() != hipSuccess) { st = FF_ERR_DEVICE; break; }
     for (int i = 0; i < kRing && st == FF_OK; ++i) {
       if (hipHostMalloc(reinterpret_cast<void **>(&ctx->ring[i].host), kRingCap * sizeof(int32_t), hipHostMallocDefault) != hipSuccess ||
           hipMalloc(reinterpret_cast<void **>(&ctx->ring[i].dev), kRingCap * sizeof(int32_t)) != hipSuccess ||
@@ -711,15 +791,9 @@ ff_status ff_sparse_ffn(ff_ctx *ctx, const ff_shape *shape, const void *x, const
   KSpec ks;
   if ((st = stage_k(ctx, k_per_block, nB, k_max, uniform, &ks)) != FF_OK) return st;
   if (ctx->validate) {
-    // the check reads its result back and waits for it: not something a graph can hold
-    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-    FF_HIP(ctx, hipStreamIsCapturing(ctx->stream, &cap));
-    if (cap != hipStreamCaptureStatusNone)
-      return fail(ctx, FF_ERR_INVALID_ARG, "the validate option synchronises the stream and cannot be captured in a HIP graph");
-    FF_HIP(ctx, hipMemsetAsync(ctx->flag_dev, 0, sizeof(int32_t), ctx->stream));
+    if ((st = begin_validate(ctx)) != FF_OK) return st;
     FF_HIP(ctx, ff_launch_validate(indices, nB, k_stride, ks, shape->d_ffn, ctx->flag_dev, ctx->stream));
-    FF_HIP(ctx, hipMemcpyAsync(ctx->flag_host, ctx->flag_dev, sizeof(int32_t), hipMemcpyDeviceToHost, ctx->stream));
-    FF_HIP(ctx, hipStreamSynchronize(ctx->stream));
+    if ((st = read_flag(ctx)) != FF_OK) return st;
     if (ctx->flag_host[0] != 0)
       return fail(ctx, FF_ERR_INDEX, "index row of block %d is not ascending, in range and -1 padded", ctx->flag_host[0] - 1);
   }
@@ -782,6 +856,156 @@ ff_status ff_residual_add(ff_ctx *ctx, int32_t n_tokens, int32_t d_model, void *
   if (!aligned16(h) || !aligned16(y)) return fail(ctx, FF_ERR_ALIGNMENT, "h / y must be 16-byte aligned");
   FF_HIP(ctx, hipSetDevice(ctx->device));
   FF_HIP(ctx, ff_launch_residual(static_cast<bf16_t *>(h), static_cast<const bf16_t *>(y), (size_t)n_tokens * d_model, ctx->stream));
+  return FF_OK;
+}
+
+ff_status ff_norm_residual(ff_ctx *ctx, int32_t n_tokens, int32_t d_model, const void *h, const void *y, int32_t y_dtype,
+                           const ff_norm *post, const void *gate, int32_t gate_tokens, float scale, void *h_out,
+                           const ff_norm *pre, void *x) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  if (n_tokens < 1 || d_model < 1) return fail(ctx, FF_ERR_INVALID_ARG, "sizes must be positive");
+  if (d_model % 8 || d_model > kNormMaxModel) return fail(ctx, FF_ERR_SHAPE, "d_model (%d) must be a multiple of 8, at most %d", d_model, kNormMaxModel);
+  if (!h) return fail(ctx, FF_ERR_INVALID_ARG, "h is NULL");
+  if (!y && (post || gate || h_out)) return fail(ctx, FF_ERR_INVALID_ARG, "post, gate and h_out go with y");
+  if ((pre != nullptr) != (x != nullptr)) return fail(ctx, FF_ERR_INVALID_ARG, "pre and x are given both or neither");
+  if (!h_out && !x) return fail(ctx, FF_ERR_INVALID_ARG, "neither h_out nor x is given");
+  if (y && y_dtype != FF_OUT_BF16 && y_dtype != FF_OUT_F32) return fail(ctx, FF_ERR_INVALID_ARG, "unknown y_dtype %d", y_dtype);
+  if (gate && gate_tokens < 1) return fail(ctx, FF_ERR_INVALID_ARG, "gate_tokens (%d) must be positive", gate_tokens);
+  if (y && !std::isfinite(scale)) return fail(ctx, FF_ERR_INVALID_ARG, "scale must be finite");
+  if (!aligned16(h) || !aligned16(y) || !aligned16(gate) || !aligned16(h_out) || !aligned16(x))
+    return fail(ctx, FF_ERR_ALIGNMENT, "h / y / gate / h_out / x must be 16-byte aligned");
+  NormParams p;
+  ff_status st;
+  if ((st = check_norm(ctx, post, &p.post)) != FF_OK || (st = check_norm(ctx, pre, &p.pre)) != FF_OK) return st;
+  p.h = static_cast<const bf16_t *>(h);
+  p.y = y;
+  p.gate = static_cast<const bf16_t *>(gate);
+  p.h_out = static_cast<bf16_t *>(h_out);
+  p.x = static_cast<bf16_t *>(x);
+  p.T = n_tokens; p.d_model = d_model; p.y_f32 = y && y_dtype == FF_OUT_F32; p.gate_tokens = gate ? gate_tokens : 1; p.scale = scale;
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_norm(p, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
+}
+
+ff_status ff_rotary(ff_ctx *ctx, const ff_attention *a, const ff_rotary_spec *r, int32_t n_tokens, const void *q, int64_t q_stride,
+                    const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *positions, void *q_out,
+                    int64_t q_out_stride, void *k_out, int64_t k_out_stride, const ff_paged_cache *cache, const int32_t *slots) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_heads(ctx, a, n_tokens);
+  if (st != FF_OK) return st;
+  if (!r || !r->inv_freq || !positions) return fail(ctx, FF_ERR_INVALID_ARG, "rotary description, frequencies or positions are NULL");
+  if (r->rot_dim < 16 || r->rot_dim % 16 || r->rot_dim > a->head_dim)
+    return fail(ctx, FF_ERR_SHAPE, "rot_dim (%d) must be a multiple of 16 in [16, head_dim]", r->rot_dim);
+  if (r->n_axes < 1 || r->n_axes > 4) return fail(ctx, FF_ERR_SHAPE, "n_axes (%d) must be in [1, 4]", r->n_axes);
+  const int64_t qw = (int64_t)a->n_heads * a->head_dim, kw = (int64_t)a->n_kv_heads * a->head_dim;
+  if ((st = check_rows(ctx, "q", q, q_stride, qw)) != FF_OK || (st = check_rows(ctx, "k", k, k_stride, kw)) != FF_OK ||
+      (st = check_rows(ctx, "q_out", q_out, q_out_stride, qw)) != FF_OK || (k_out && (st = check_rows(ctx, "k_out", k_out, k_out_stride, kw)) != FF_OK))
+    return st;
+  if ((q_out == q && q_out_stride != q_stride) || (k_out == k && k_out_stride != k_stride))
+    return fail(ctx, FF_ERR_INVALID_ARG, "an output in the place of its input has the input's stride");
+  if (!aligned16(positions) || !aligned16(r->inv_freq) || !aligned16(slots)) return fail(ctx, FF_ERR_ALIGNMENT, "positions / inv_freq / slots must be 16-byte aligned");
+  if ((cache != nullptr) != (slots != nullptr)) return fail(ctx, FF_ERR_INVALID_ARG, "cache and slots are given both or neither");
+  if (!cache && !k_out) return fail(ctx, FF_ERR_INVALID_ARG, "neither k_out nor a cache is given");
+  RotaryParams p = {};
+  if (cache) {
+    if ((st = check_cache(ctx, cache)) != FF_OK) return st;
+    if ((st = check_rows(ctx, "v", v, v_stride, kw)) != FF_OK) return st;
+    p.k_pages = static_cast<bf16_t *>(cache->k);
+    p.v_pages = static_cast<bf16_t *>(cache->v);
+    p.page_shift = log2_of(cache->page_size);
+    p.n_slots = (int64_t)cache->n_pages << p.page_shift;
+    p.slots = slots;
+  }
+  for (int i = 0; i < r->rot_dim / 2; ++i) {
+    const int ax = r->axis ? r->axis[i] : 0;
+    if (ax < 0 || ax >= r->n_axes) return fail(ctx, FF_ERR_INVALID_ARG, "axis[%d] = %d not in [0, %d)", i, ax, r->n_axes);
+    p.axis[i >> 4] |= (uint32_t)ax << (2 * (i & 15));
+  }
+  p.q = static_cast<const bf16_t *>(q); p.k = static_cast<const bf16_t *>(k); p.v = static_cast<const bf16_t *>(v);
+  p.q_out = static_cast<bf16_t *>(q_out); p.k_out = static_cast<bf16_t *>(k_out);
+  p.positions = positions; p.inv_freq = r->inv_freq;
+  p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride; p.q_out_stride = q_out_stride; p.k_out_stride = k_out_stride;
+  p.T = n_tokens; p.n_heads = a->n_heads; p.n_kv = a->n_kv_heads; p.head_dim = a->head_dim;
+  p.rot_dim = r->rot_dim; p.interleaved = r->interleaved != 0;
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_rotary(p, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
+}
+
+ff_status ff_attention_workspace_bytes(const ff_attention *a, int32_t n_tokens, int32_t n_seqs, size_t *bytes) {
+  if (!bytes) return FF_ERR_INVALID_ARG;
+  ff_status st = check_attention(nullptr, a, n_tokens, n_seqs);
+  if (st != FF_OK) return st;
+  *bytes = ff_attention_part_bytes(a->n_heads, a->n_kv_heads, a->head_dim, n_tokens, n_seqs);
+  return FF_OK;
+}
+
+ff_status ff_prompt_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs, const void *q, int64_t q_stride,
+                              const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *seq_starts,
+                              void *o, int64_t o_stride, float *lse_opt) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_attention(ctx, a, n_tokens, n_seqs);
+  if (st != FF_OK) return st;
+  const int64_t qw = (int64_t)a->n_heads * a->head_dim, kw = (int64_t)a->n_kv_heads * a->head_dim;
+  if ((st = check_rows(ctx, "q", q, q_stride, qw)) != FF_OK || (st = check_rows(ctx, "k", k, k_stride, kw)) != FF_OK ||
+      (st = check_rows(ctx, "v", v, v_stride, kw)) != FF_OK || (st = check_rows(ctx, "o", o, o_stride, qw)) != FF_OK)
+    return st;
+  if (!seq_starts) return fail(ctx, FF_ERR_INVALID_ARG, "seq_starts is NULL");
+  if (!aligned16(seq_starts) || !aligned16(lse_opt)) return fail(ctx, FF_ERR_ALIGNMENT, "seq_starts / lse must be 16-byte aligned");
+  AttnParams p = attn_params(*a, n_tokens, n_seqs);
+  p.q = static_cast<const bf16_t *>(q); p.k = static_cast<const bf16_t *>(k); p.v = static_cast<const bf16_t *>(v);
+  p.o = static_cast<bf16_t *>(o); p.lse = lse_opt; p.starts = seq_starts;
+  p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride; p.o_stride = o_stride;
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_attention(p, a->head_dim, n_tokens, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
+}
+
+ff_status ff_chunk_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs, const void *q, int64_t q_stride,
+                             const int32_t *chunk_starts, const int32_t *context_lens, int32_t max_chunk, const ff_paged_cache *cache,
+                             const int32_t *page_table, int32_t table_stride, void *o, int64_t o_stride, float *lse_opt) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_attention(ctx, a, n_tokens, n_seqs);
+  if (st != FF_OK) return st;
+  const int64_t qw = (int64_t)a->n_heads * a->head_dim;
+  if ((st = check_rows(ctx, "q", q, q_stride, qw)) != FF_OK || (st = check_rows(ctx, "o", o, o_stride, qw)) != FF_OK) return st;
+  if ((st = check_cache(ctx, cache)) != FF_OK) return st;
+  if (!chunk_starts || !context_lens || !page_table) return fail(ctx, FF_ERR_INVALID_ARG, "chunk_starts, context_lens or page_table is NULL");
+  if (!aligned16(chunk_starts) || !aligned16(context_lens) || !aligned16(page_table) || !aligned16(lse_opt))
+    return fail(ctx, FF_ERR_ALIGNMENT, "chunk_starts / context_lens / page_table / lse must be 16-byte aligned");
+  if (max_chunk < 1 || max_chunk > n_tokens) return fail(ctx, FF_ERR_INVALID_ARG, "max_chunk (%d) must be in [1, n_tokens]", max_chunk);
+  if (table_stride < 1) return fail(ctx, FF_ERR_INVALID_ARG, "table_stride (%d) must be positive", table_stride);
+  AttnParams p = attn_params(*a, n_tokens, n_seqs);
+  p.q = static_cast<const bf16_t *>(q); p.k = static_cast<const bf16_t *>(cache->k); p.v = static_cast<const bf16_t *>(cache->v);
+  p.o = static_cast<bf16_t *>(o); p.lse = lse_opt;
+  p.starts = chunk_starts; p.lens = context_lens; p.table = page_table;
+  p.q_stride = q_stride; p.o_stride = o_stride;
+  p.table_stride = table_stride; p.page_shift = log2_of(cache->page_size); p.n_pages = cache->n_pages;
+  const size_t need = ff_attention_need(p, a->head_dim, max_chunk);
+  if (need > 0) {
+    if (!ctx->ws) return fail(ctx, FF_ERR_WORKSPACE, "no workspace set (ff_set_workspace)");
+    if (ctx->ws_bytes < need) return fail(ctx, FF_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", ctx->ws_bytes, need);
+    p.part = static_cast<float *>(ctx->ws);
+    p.part_bytes = ctx->ws_bytes;
+  }
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  if (ctx->validate) {
+    if ((st = begin_validate(ctx)) != FF_OK) return st;
+    FF_HIP(ctx, ff_launch_validate_pages(p, ctx->flag_dev, ctx->stream));
+    if ((st = read_flag(ctx)) != FF_OK) return st;
+    if (ctx->flag_host[0] != 0)
+      return fail(ctx, FF_ERR_INDEX, "sequence %d has a chunk, a length or a page out of range", ctx->flag_host[0] - 1);
+  }
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_attention(p, a->head_dim, max_chunk, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
   return FF_OK;
 }
 

@@ -280,3 +280,34 @@ hipError_t ff_launch_merge_lists(const int32_t *idx, int k_stride, KSpec ks, int
                                  hipStream_t s);
 hipError_t ff_launch_validate(const int32_t *idx, int n_blocks, int k_stride, KSpec k,
                               int d_ffn, int32_t *flag, hipStream_t s);
+
+// ---- norms around a block ----------------------------------------------------
+constexpr int kNormMaxModel = 16384;
+struct NormSpec {
+  int32_t kind = 0;   // FF_NORM_*, 0 = none
+  float eps = 0.f, gain_offset = 0.f;
+  const bf16_t *gain = nullptr, *bias = nullptr;
+};
+struct NormParams {
+  const bf16_t *h;
+  const void *y;        // bf16 or f32 by y_f32, or nullptr
+  const bf16_t *gate;   // or nullptr
+  bf16_t *h_out, *x;    // either may be nullptr
+  int32_t T, d_model, y_f32, gate_tokens;
+  float scale;
+  NormSpec post, pre;
+};
+hipError_t ff_launch_norm(const NormParams &p, hipStream_t s);
+
+// ---- rotary positions and the cache write ------------------------------------
+struct RotaryParams {
+  const bf16_t *q, *k, *v;
+  bf16_t *q_out, *k_out;         // k_out or nullptr
+  bf16_t *k_pages, *v_pages;     // or nullptr
+  const int32_t *positions, *slots;
+  const float *inv_freq;
+  int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride, n_slots;
+  int32_t T, n_heads, n_kv, head_dim, rot_dim, interleaved, page_shift;
+  uint32_t axis[4];              // two bits for each of up to 64 pairs
+};
+hipError_t ff_launch_rotary(const RotaryParams &p, hipStream_t s);

@@ -9,6 +9,7 @@
 #include <set>
 #include <vector>
 
+#include "ff_attn_plan.h"
 #include "ff_internal.h"
 
 struct Launch {
@@ -19,16 +20,18 @@ struct Launch {
   Gemm2Params g2;
   dim3 dims;
   const double *pooled;     // where a pooling kernel writes
+  AttnPlan plan;
 };
 static std::vector<Launch> g_log;
 static int g_fail = 0, g_calls = 0;
-static bool g_down = false, g_few = false, g_pred = false;   // whose launches are being recorded
+static bool g_down = false, g_few = false, g_pred = false, g_attn = false;   // whose launches are being recorded
 static size_t g_pool_at = 0;                                 // which of the predictor's is the pooling kernel
 
 extern "C" hipError_t hipLaunchKernel(const void *fn, dim3 grid, dim3 block, void **args, size_t lds, hipStream_t) {
-  Launch l = {fn, grid.x * grid.y * grid.z, block.x, lds, {}, {}, grid, nullptr};
+  Launch l = {fn, grid.x * grid.y * grid.z, block.x, lds, {}, {}, grid, nullptr, {}};
   if (g_pred && g_log.size() == g_pool_at) memcpy(&l.pooled, args[3], sizeof(l.pooled));
-  if (g_few || g_pred) {}                                                  // (the grid says enough)
+  if (g_attn) memcpy(static_cast<void *>(&l.plan), args[1], sizeof(l.plan));
+  else if (g_few || g_pred) {}                                                  // (the grid says enough)
   else if (g_down) memcpy(static_cast<void *>(&l.g2), args[0], sizeof(l.g2));
   else memcpy(static_cast<void *>(&l.g1), args[0], sizeof(l.g1));
   g_log.push_back(l);
@@ -461,6 +464,92 @@ static void check_topk_map() {
   CHECK(topk_map(1.0, 1.0).none && topk_map(0.0, INFINITY).none && topk_map(-INFINITY, 0.0).none && topk_map(0.0, NAN).none && topk_map(NAN, 0.0).none, "no range");
 }
 
+// Attention: the launches that a call makes, and what their workgroups find when lengths, starts and windows are anything at all.
+// Every tile, piece and key lies within the tensors; where the lengths are valid, the items fit into the launch and into the
+// workspace, a sequence's rows are all covered by one kernel, and a tile's pieces cover what its rows see.
+static void check_attention() {
+  uint32_t rnd = 12345;
+  const auto below = [&](int n) { rnd = rnd * 1664525u + 1013904223u; return (int)((rnd >> 8) % (unsigned)n); };
+  static float room[1];
+  g_attn = true;
+  for (int round = 0; round < 6000; ++round) {
+    static const int groups[] = {1, 3, 4, 7, 8, 20};
+    const bool valid = round % 3 != 0, paged = round % 4 != 1;
+    const int group = groups[below(6)], n_kv = 1 + below(8), n_seqs = 1 + below(round % 7 == 0 ? 200 : 6), hd = below(2) ? 64 : 128;
+    std::vector<int32_t> starts(n_seqs + 1), lens(n_seqs);
+    AttnParams p = {};
+    p.page_shift = 3 + below(7);
+    p.table_stride = 1 + below(60);
+    int t = 0, longest = 1;
+    for (int s = 0; s < n_seqs; ++s) {
+      starts[s] = t;
+      const int n = below(3) == 0 ? below(3) : below(1 << (1 + below(9)));
+      t += n;
+      longest = std::max(longest, n);
+      lens[s] = below(p.table_stride << p.page_shift);
+    }
+    starts[n_seqs] = t;
+    p.T = std::max(1, t + below(3));
+    if (!valid)
+      for (int i = 0; i < 1 + n_seqs / 2; ++i) {
+        static const int odd[] = {-1, -2147483647 - 1, 2147483647, 1 << 30, 77};
+        starts[below(n_seqs + 1)] = odd[below(5)];
+        lens[below(n_seqs)] = odd[below(5)];
+      }
+    p.starts = starts.data();
+    p.lens = paged ? lens.data() : nullptr;
+    p.table = paged ? starts.data() : nullptr;         // (never read: there is one)
+    p.n_seqs = n_seqs; p.n_kv = n_kv; p.group = group; p.n_heads = n_kv * group; p.n_pages = 10;
+    p.causal = below(5) != 0;
+    p.window = p.causal && below(3) == 0 ? (below(4) ? 1 + below(1000) : 2147483647) : 0;
+    p.part = room;
+    const int hint = below(3) ? std::min(longest, p.T) : 1 + below(p.T);
+    p.part_bytes = ff_attention_part_bytes(p.n_heads, n_kv, hd, p.T, n_seqs);
+    CHECK(ff_attention_need(p, hd, hint) <= p.part_bytes, "group %d kv %d T %d seqs %d hint %d: %zu", group, n_kv, p.T, n_seqs, hint, p.part_bytes);
+    g_log.clear();
+    ++g_calls;
+    CHECK(ff_launch_attention(p, hd, hint, nullptr) == hipSuccess && !g_log.empty(), "round %d", round);
+    std::vector<long> covered(n_seqs, 0);
+    for (const Launch &l : g_log) {
+      const AttnPlan &pl = l.plan;
+      if (l.threads == 256 && l.grid == (unsigned)(((long)p.T * p.n_heads + 3) / 4) && &l == &g_log.back() && pl.max_items != (int)l.grid) continue;   // (joins the pieces)
+      CHECK(l.lds <= kLds && l.grid == (unsigned)pl.max_items, "round %d: %u workgroups, %zu bytes", round, l.grid, l.lds);
+      float steps = 0.f;
+      for (int s = 0; s < n_seqs; ++s) steps += price_of(p, pl, seq_of(p, s));
+      const int kpp = pl.target > 0 ? piece_keys_for(p, pl, steps) : kUnsplit;
+      CHECK(kpp > 0 && kpp % kTileKeys == 0, "round %d: pieces of %d", round, kpp);
+      long items = 0;
+      bool split = false;
+      for (int s = 0; s < n_seqs; ++s) {
+        const Seq q = seq_of(p, s);
+        CHECK(q.t0 >= 0 && q.n >= 0 && q.t0 + (long)q.n <= p.T && q.keys >= 0 && q.keys <= (paged ? most_keys(p) : q.n), "round %d sequence %d", round, s);
+        const int tiles = tiles_of(p, pl, q.n), pieces = seq_pieces(p, pl, q, kpp);
+        items += (long)tiles * pieces;
+        covered[s] += (long)tiles * pl.tile_rows;
+        for (int i = 0; i < tiles; ++i) {
+          const Range r = tile_range(p, q, i, pl.tile_rows);
+          const int n = pieces_of(r, kpp);
+          split = split || n > 1;
+          CHECK(r.lo >= 0 && r.lo % kTileKeys == 0 && r.hi <= q.keys && n >= 1 && n <= pieces, "round %d tile %d: keys %d to %d, %d of %d pieces", round, i, r.lo, r.hi, n, pieces);
+          CHECK(r.lo + (long)n * kpp >= r.hi && (n == 1 || r.lo + (long)(n - 1) * kpp < r.hi), "round %d tile %d", round, i);
+          const int last = std::min((i + 1) * pl.tile_rows, q.n * group) - 1;
+          for (int row : {i * pl.tile_rows, (i * pl.tile_rows + last) / 2, last}) {
+            const Range g = row_range(p, q, row);
+            CHECK(g.lo >= 0 && g.lo <= g.hi && (g.lo == g.hi || (g.lo >= r.lo && g.hi <= r.hi)), "round %d row %d sees %d to %d, tile %d to %d", round, row, g.lo, g.hi, r.lo, r.hi);
+          }
+        }
+      }
+      CHECK(!valid || items * n_kv <= pl.max_items, "round %d: %ld items, %d workgroups", round, items * n_kv, pl.max_items);
+      CHECK(!split || (pl.target > 0 && (pl.part_at + (size_t)pl.max_items * pl.tile_rows * (hd + 2)) * sizeof(float) <= p.part_bytes), "round %d: room", round);
+    }
+    for (int s = 0; s < n_seqs; ++s) {
+      const Seq q = seq_of(p, s);
+      CHECK(covered[s] >= (long)q.n * group && covered[s] < (long)q.n * group + 256 && (q.n > 0 || covered[s] == 0), "round %d sequence %d: %ld rows of %ld", round, s, covered[s], (long)q.n * group);
+    }
+  }
+  g_attn = false;
+}
+
 int main() {
   if (ff_gemm_init(kLds) != hipSuccess) return 1;
   for (int T : {9, 70, 300, 700, 2000, 8192})
@@ -482,6 +571,7 @@ int main() {
   check_few_tokens();
   check_pooling();
   check_topk_map();
+  check_attention();
   printf("launch checks: %d calls, %d wrong\n", g_calls, g_fail);
   return g_fail != 0;
 }
