@@ -56,6 +56,7 @@ class RotarySpec(C.Structure):
 
 
 class Norm(C.Structure):
+    tensors, width = (None, None), None
     _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("gain_offset", C.c_float), ("gain", C.c_void_p),
                 ("bias", C.c_void_p)]
 
@@ -137,21 +138,25 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _typed(t: Optional[torch.Tensor], dtype, shape=None):
-    """A contiguous tensor's pointer, its type and shape as the call takes them for granted."""
+    """Address of a contiguous tensor that has the type and shape that the call takes for granted (plain integers, and few steps:
+    for single tokens the marshalling is most of a call)."""
     if t is None:
         return None
-    assert t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
-    assert shape is None or tuple(t.shape) == tuple(shape), f"expected shape {tuple(shape)}, got {tuple(t.shape)}"
-    return _ptr(t)
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise AssertionError(f"expected a contiguous {dtype} tensor{'' if shape is None else f' {tuple(shape)}'} on the GPU, "
+                             f"got {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
+    return t.data_ptr()
 
 
 def _rows(t: Optional[torch.Tensor], n_rows: int, width: int):
-    """(pointer, stride) of bf16 rows that may lie apart, such as a part of a projection's output."""
+    """(address, stride) of bf16 rows that may lie apart, such as a part of a projection's output."""
     if t is None:
         return None, 0
-    assert t.is_cuda and t.dtype == torch.bfloat16 and tuple(t.shape) == (n_rows, width) and t.stride(1) == 1, \
-        f"expected bf16 rows [{n_rows}][{width}] on the GPU, got {t.dtype} {tuple(t.shape)} with strides {t.stride()}"
-    return C.c_void_p(t.data_ptr()), (t.stride(0) if n_rows > 1 else max(t.stride(0), width))
+    stride = t.stride()
+    if t.dtype is not torch.bfloat16 or not t.is_cuda or t.shape != (n_rows, width) or stride[1] != 1:
+        raise AssertionError(f"expected bf16 rows [{n_rows}][{width}] on the GPU, got {t.dtype} {tuple(t.shape)} on {t.device} "
+                             f"with strides {stride}")
+    return t.data_ptr(), stride[0] if n_rows > 1 or stride[0] > width else width
 
 
 def _i32_array(values: Sequence[int]):
@@ -197,8 +202,9 @@ def attention_workspace_bytes(heads: Attention, n_tokens: int, n_seqs: int) -> i
 
 def norm(kind: str, eps: float, gain: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
          gain_offset: float = 0.0) -> Norm:
-    n = Norm(NORM[kind], float(eps), float(gain_offset), _typed(gain, torch.bfloat16), _typed(bias, torch.bfloat16))
-    n.tensors = (gain, bias)
+    width = gain.numel() if gain is not None else bias.numel() if bias is not None else None
+    n = Norm(NORM[kind], float(eps), float(gain_offset), *(_typed(t, torch.bfloat16, (width,)) for t in (gain, bias)))
+    n.tensors, n.width = (gain, bias), width
     return n
 
 
@@ -222,8 +228,9 @@ def paged_cache(k_pages: torch.Tensor, v_pages: torch.Tensor) -> PagedCache:
 
 
 def _check_pages(cache: PagedCache, heads: Attention):
-    assert tuple(cache.tensors[0].shape[1::2]) == (heads.n_kv_heads, heads.head_dim), \
-        f"cache pages {tuple(cache.tensors[0].shape)} are not of {heads.n_kv_heads} heads of {heads.head_dim}"
+    _, n_kv, _, head_dim = cache.tensors[0].shape
+    if n_kv != heads.n_kv_heads or head_dim != heads.head_dim:
+        raise AssertionError(f"cache pages {tuple(cache.tensors[0].shape)} are not of {heads.n_kv_heads} heads of {heads.head_dim}")
 
 
 class Context:
@@ -325,43 +332,49 @@ class Context:
 
     def norm_residual(self, h, y, h_out, x, post: Optional[Norm] = None, gate=None, gate_tokens: int = 1,
                       scale: float = 1.0, pre: Optional[Norm] = None):
-        bf16 = torch.bfloat16
-        for n in (post, pre):
-            for t in n.tensors if n is not None else ():
-                assert t is None or tuple(t.shape) == (h.shape[1],), "norm weights are one for each channel"
-        assert y is None or y.dtype in (bf16, torch.float32)
-        gate_shape = None if gate is None or gate_tokens < 1 else (-(-h.shape[0] // gate_tokens), h.shape[1])
-        ref = lambda n: C.byref(n) if n is not None else None
-        self._check(self.lib.ff_norm_residual(
-            self._h, h.shape[0], h.shape[1], _typed(h, bf16), _typed(y, y.dtype, h.shape) if y is not None else None,
-            OUT_F32 if y is not None and y.dtype == torch.float32 else OUT_BF16, ref(post), _typed(gate, bf16, gate_shape),
-            int(gate_tokens), float(scale), _typed(h_out, bf16, h.shape), ref(pre), _typed(x, bf16, h.shape)))
+        bf16, shape = torch.bfloat16, h.shape
+        n, d = shape
+        for w in (post, pre):
+            if w is not None and w.width is not None and w.width != d:
+                raise AssertionError(f"norm weights of {w.width} channels for rows of {d}")
+        y_f32 = y is not None and y.dtype is torch.float32
+        st = self.lib.ff_norm_residual(
+            self._h, n, d, _typed(h, bf16), _typed(y, torch.float32 if y_f32 else bf16, shape), OUT_F32 if y_f32 else OUT_BF16,
+            post, _typed(gate, bf16, None if gate_tokens < 1 else (-(-n // gate_tokens), d)), gate_tokens, scale,
+            _typed(h_out, bf16, shape), pre, _typed(x, bf16, shape))
+        if st:
+            self._check(st)
 
     def rotary(self, heads: Attention, rot: RotarySpec, q, k, v, positions, q_out, k_out=None,
                cache: Optional[PagedCache] = None, slots=None):
         n, qw, kw = q.shape[0], heads.n_heads * heads.head_dim, heads.n_kv_heads * heads.head_dim
         if cache is not None:
             _check_pages(cache, heads)
-        self._check(self.lib.ff_rotary(
-            self._h, C.byref(heads), C.byref(rot), n, *_rows(q, n, qw), *_rows(k, n, kw), *_rows(v, n, kw),
-            _typed(positions, torch.int32, (rot.n_axes, n)), *_rows(q_out, n, qw), *_rows(k_out, n, kw),
-            C.byref(cache) if cache is not None else None, _typed(slots, torch.int32, (n,))))
+        st = self.lib.ff_rotary(
+            self._h, heads, rot, n, *_rows(q, n, qw), *_rows(k, n, kw), *_rows(v, n, kw),
+            _typed(positions, torch.int32, (rot.n_axes, n)), *_rows(q_out, n, qw), *_rows(k_out, n, kw), cache,
+            _typed(slots, torch.int32, (n,)))
+        if st:
+            self._check(st)
 
     def prompt_attention(self, heads: Attention, q, k, v, seq_starts, o, lse=None):
         n, qw, kw = q.shape[0], heads.n_heads * heads.head_dim, heads.n_kv_heads * heads.head_dim
-        self._check(self.lib.ff_prompt_attention(
-            self._h, C.byref(heads), n, seq_starts.numel() - 1, *_rows(q, n, qw), *_rows(k, n, kw), *_rows(v, n, kw),
-            _typed(seq_starts, torch.int32), *_rows(o, n, qw), _typed(lse, torch.float32, (n, heads.n_heads))))
+        st = self.lib.ff_prompt_attention(
+            self._h, heads, n, seq_starts.numel() - 1, *_rows(q, n, qw), *_rows(k, n, kw), *_rows(v, n, kw),
+            _typed(seq_starts, torch.int32), *_rows(o, n, qw), _typed(lse, torch.float32, (n, heads.n_heads)))
+        if st:
+            self._check(st)
 
     def chunk_attention(self, heads: Attention, q, chunk_starts, context_lens, max_chunk: int, cache: PagedCache,
                         page_table, o, lse=None):
-        n, qw, n_seqs = q.shape[0], heads.n_heads * heads.head_dim, context_lens.numel()
+        n, qw, (n_seqs, table_stride) = q.shape[0], heads.n_heads * heads.head_dim, page_table.shape
         _check_pages(cache, heads)
-        self._check(self.lib.ff_chunk_attention(
-            self._h, C.byref(heads), n, n_seqs, *_rows(q, n, qw), _typed(chunk_starts, torch.int32, (n_seqs + 1,)),
-            _typed(context_lens, torch.int32), int(max_chunk), C.byref(cache),
-            _typed(page_table, torch.int32, (n_seqs, page_table.shape[1])), page_table.shape[1], *_rows(o, n, qw),
-            _typed(lse, torch.float32, (n, heads.n_heads))))
+        st = self.lib.ff_chunk_attention(
+            self._h, heads, n, n_seqs, *_rows(q, n, qw), _typed(chunk_starts, torch.int32, (n_seqs + 1,)),
+            _typed(context_lens, torch.int32, (n_seqs,)), max_chunk, cache, _typed(page_table, torch.int32), table_stride,
+            *_rows(o, n, qw), _typed(lse, torch.float32, (n, heads.n_heads)))
+        if st:
+            self._check(st)
 
     def copy(self, dst, src):
         n = src.numel() * src.element_size()

@@ -54,6 +54,7 @@ struct ff_ctx {
   int staged_slot = -1, staged_n = 0;   // the slot staged last and its length: the same values again need no new copy
   int32_t *flag_dev = nullptr;
   int32_t *flag_host = nullptr;
+  int32_t *counters = nullptr;     // of attention's pieces, zero between calls
   Profiler prof;
   char err[320] = {0};
 };
@@ -568,7 +569,9 @@ ff_status ff_create(ff_ctx **out, int device, void *hip_stream) {
     }
     if (st != FF_OK) break;
     if (hipMalloc(reinterpret_cast<void **>(&ctx->flag_dev), 256) != hipSuccess ||
-        hipHostMalloc(reinterpret_cast<void **>(&ctx->flag_host), 256, hipHostMallocDefault) != hipSuccess)
+        hipHostMalloc(reinterpret_cast<void **>(&ctx->flag_host), 256, hipHostMallocDefault) != hipSuccess ||
+        hipMalloc(reinterpret_cast<void **>(&ctx->counters), kAttnCounters * sizeof(int32_t)) != hipSuccess ||
+        hipMemset(ctx->counters, 0, kAttnCounters * sizeof(int32_t)) != hipSuccess || hipDeviceSynchronize() != hipSuccess)
       st = FF_ERR_DEVICE;
   } while (0);
   if (st != FF_OK) {
@@ -590,6 +593,7 @@ ff_status ff_destroy(ff_ctx *ctx) {
   }
   if (ctx->flag_dev) (void)hipFree(ctx->flag_dev);
   if (ctx->flag_host) (void)hipHostFree(ctx->flag_host);
+  if (ctx->counters) (void)hipFree(ctx->counters);
   prof_free(ctx);
   delete ctx;
   return FF_OK;
@@ -987,6 +991,7 @@ ff_status ff_chunk_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_token
   p.o = static_cast<bf16_t *>(o); p.lse = lse_opt;
   p.starts = chunk_starts; p.lens = context_lens; p.table = page_table;
   p.q_stride = q_stride; p.o_stride = o_stride;
+  p.counters = ctx->counters;
   p.table_stride = table_stride; p.page_shift = log2_of(cache->page_size); p.n_pages = cache->n_pages;
   const size_t need = ff_attention_need(p, a->head_dim, max_chunk);
   if (need > 0) {

@@ -15,12 +15,14 @@
 #include "ff_attn_plan.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 
@@ -75,51 +77,66 @@ __device__ __forceinline__ void copied(int i, int lane, int &key, int &chunk) {
 
 // ---- which part of which sequence a workgroup computes -----------------------------------------------------------------
 
-// How long a piece is, from the work of the whole call; every wavefront finds the same.
-__device__ __forceinline__ int piece_keys(const AttnParams &p, const AttnPlan &pl) {
-  if (pl.target <= 0) return kUnsplit;
+// Running sums over the 64 lanes (lane 63: all of them), by DPP: some 8 cycles a step, where a shuffle through LDS takes over 100.
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T dpp(T v) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+template <class T>
+__device__ __forceinline__ T lane_sums(T v) {
+  v += dpp<0x111, 0xf>(v);     // the lane before in the row of 16, then 2, 4 and 8 before
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  v += dpp<0x142, 0xa>(v);     // rows 1 and 3: the last lane of the row before
+  v += dpp<0x143, 0xc>(v);     // rows 2 and 3: lane 31
+  return v;
+}
+// Sequence number lane + s0, which the first 64 lanes of a call's sequences keep in `first`.
+__device__ __forceinline__ Seq lane_seq(const AttnParams &p, int s0, const Seq &first) {
+  const int s = s0 + (threadIdx.x & 63);
+  if (s0 == 0) return first;
+  return s < p.n_seqs ? seq_of(p, s) : Seq{0, 0, 0};
+}
+// How long a piece is and how many (tile, piece) there are, from the work of the whole call; every wavefront finds the same.
+struct Cut { int keys, items; Seq first; };
+__device__ __forceinline__ Cut cut_of(const AttnParams &p, const AttnPlan &pl) {
+  Cut c = {kUnsplit, 0, {0, 0, 0}};
   const int lane = threadIdx.x & 63;
-  float steps = 0.f;
-  for (int s0 = 0; s0 < p.n_seqs; s0 += 64)
-    if (s0 + lane < p.n_seqs) steps += price_of(p, pl, seq_of(p, s0 + lane));
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) steps += __shfl_xor(steps, off);
-  return __builtin_amdgcn_readfirstlane(piece_keys_for(p, pl, steps));
+  if (lane < p.n_seqs) c.first = seq_of(p, lane);
+  if (pl.target > 0) {
+    float steps = 0.f;
+    for (int s0 = 0; s0 < p.n_seqs; s0 += 64) steps += price_of(p, pl, lane_seq(p, s0, c.first));
+    c.keys = __builtin_amdgcn_readfirstlane(piece_keys_for(p, pl, __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lane_sums(steps)), 63))));
+  }
+  for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
+    const Seq q = lane_seq(p, s0, c.first);
+    c.items += tiles_of(p, pl, q.n) * seq_pieces(p, pl, q, c.keys);
+  }
+  c.items = __builtin_amdgcn_readlane(lane_sums(c.items), 63);
+  return c;
 }
 
 struct Item {
-  bool found;
   int s, tile, piece, kvh;   // piece of tile of sequence s, key head kvh
   int n_tiles, n_pieces;     // of the sequence (a tile may have fewer pieces)
   int first;                 // number of the sequence's first (tile, piece)
   Seq seq;
 };
-// The (tile, piece) number x, counted over the sequences, or, with by_seq, the first one of sequence x.
-__device__ __forceinline__ Item find_item(const AttnParams &p, const AttnPlan &pl, int keys_per_piece, int x, bool by_seq) {
+// The sequence of (tile, piece) number x, counted over the sequences in pieces of `keys`, or, with BY_SEQ, sequence x.
+template <bool BY_SEQ>
+__device__ __forceinline__ Item find_seq(const AttnParams &p, const AttnPlan &pl, int keys, const Seq &first, int x) {
   const int lane = threadIdx.x & 63;
-  Item it;
-  it.found = false;
+  Item it = {};
   int base = 0;
   for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
-    Seq q = {0, 0, 0};
-    int tiles = 0, pieces = 1;
-    if (s0 + lane < p.n_seqs) {
-      q = seq_of(p, s0 + lane);
-      tiles = tiles_of(p, pl, q.n);
-      pieces = seq_pieces(p, pl, q, keys_per_piece);
-    }
-    const int mine = tiles * pieces;
-    int incl = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(incl, d);
-      if (lane >= d) incl += up;
-    }
+    const Seq q = lane_seq(p, s0, first);
+    const int tiles = tiles_of(p, pl, q.n), pieces = seq_pieces(p, pl, q, keys);
+    const int mine = tiles * pieces, incl = lane_sums(mine);
     const int excl = base + incl - mine;
-    const unsigned long long hit = __ballot(by_seq ? s0 + lane == x : x >= excl && x < excl + mine);
+    const unsigned long long hit = __ballot(BY_SEQ ? s0 + lane == x : x >= excl && x < excl + mine);
     if (hit) {
       const int l = __builtin_ctzll(hit);
-      it.found = true;
       it.s = s0 + l;
       it.first = __builtin_amdgcn_readlane(excl, l);
       it.n_tiles = __builtin_amdgcn_readlane(tiles, l);
@@ -133,21 +150,24 @@ __device__ __forceinline__ Item find_item(const AttnParams &p, const AttnPlan &p
   }
   return it;
 }
-// Workgroup number -> item.  Key heads go innermost (workgroups id mod 8 share an XCD, so its L2 keeps one head's keys where there
-// are eight), then the tiles of one piece, the last first: under a causal mask those have the most keys.
-__device__ __forceinline__ Item work_of(const AttnParams &p, const AttnPlan &pl, int keys_per_piece, int id) {
+// Item number -> what to compute.  Key heads go innermost (workgroups id mod 8 share an XCD, so its L2 keeps one head's keys where
+// there are eight), then the tiles of one piece, the last first: under a causal mask those have the most keys.
+__device__ __forceinline__ Item work_of(const AttnParams &p, const AttnPlan &pl, const Cut &cut, int id) {
   const int x = id / p.n_kv;
-  Item it = find_item(p, pl, keys_per_piece, x, false);
-  if (it.found) {
-    const int local = x - it.first;
-    it.kvh = id - x * p.n_kv;
-    it.piece = local / it.n_tiles;
-    it.tile = it.n_tiles - 1 - (local - it.piece * it.n_tiles);
-  }
+  Item it = find_seq<false>(p, pl, cut.keys, cut.first, x);
+  const int local = x - it.first;
+  it.kvh = id - x * p.n_kv;
+  if (it.n_tiles == 0) return it;       // (sums beyond 32 bits, of lengths that no valid call has)
+  it.piece = local / it.n_tiles;
+  it.tile = it.n_tiles - 1 - (local - it.piece * it.n_tiles);
   return it;
 }
+__device__ __forceinline__ int items_of(const AttnParams &p, const AttnPlan &pl, const Cut &cut) {
+  return min(cut.items * p.n_kv, pl.max_items);     // (chunks that overlap may have more than there is room for)
+}
 
-// partial sums of a piece: tile_rows rows of HD sums, then tile_rows pairs of maximum and sum
+// Partial sums of a piece: tile_rows times HD sums, then tile_rows pairs of maximum and sum.  The few-row kernel's sums lie by rows,
+// the other's as its lanes hold them: 1 KB for four values of each lane, 32 rows together.
 template <int HD>
 __device__ __forceinline__ float *part_of(const AttnPlan &pl, int x, int kvh, int n_kv) {
   return pl.part + ((size_t)x * n_kv + kvh) * ((size_t)pl.tile_rows * (HD + 2));
@@ -181,39 +201,76 @@ __device__ __forceinline__ KeySource<PAGED> key_source(const AttnParams &p, cons
   }
   return ks;
 }
-// Copies number i of the tile that starts at key j (a multiple of 32) to LDS: 1 KB of K and 1 KB of V.  Keys from `end` on are
-// replaced by the last one.  The keys of one copy (4 or 8, aligned) are in one page.
-template <int HD, bool PAGED>
-__device__ __forceinline__ void copy_keys(const KeySource<PAGED> &ks, int i, int j, int end, uint32_t lds_k, uint32_t lds_v, int lane) {
-  constexpr int KPI = 512 / HD;
-  int key, chunk;
-  copied<HD>(i, lane, key, chunk);
-  const int first = min(j + i * KPI, end - 1);      // (wave-uniform)
-  const int mine = min(j + key, end - 1);
-  if (PAGED) {
-    // (by a scalar load: the wait for it is not one for the copies before it)
-    int page = *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(ks.table + (first >> ks.shift)));
-    page = __builtin_amdgcn_readfirstlane((unsigned)page < (unsigned)ks.n_pages ? page : 0);
-    const size_t at = (size_t)page * ks.page_elems;
-    const uint32_t off = (uint32_t)(((mine & ((1 << ks.shift) - 1)) * HD + chunk * 8) * 2);
-    gload_lds16_at(ks.k + at, off, lds_k + i * 1024);
-    gload_lds16_at(ks.v + at, off, lds_v + i * 1024);
-  } else {
-    const uint8_t *kb = reinterpret_cast<const uint8_t *>(ks.k) + (size_t)first * ks.k_pitch;
-    const uint8_t *vb = reinterpret_cast<const uint8_t *>(ks.v) + (size_t)first * ks.v_pitch;
-    gload_lds16_at(kb, (uint32_t)(mine - first) * ks.k_pitch + chunk * 16, lds_k + i * 1024);
-    gload_lds16_at(vb, (uint32_t)(mine - first) * ks.v_pitch + chunk * 16, lds_v + i * 1024);
+// Copies `first` to `first` + NI - 1 of a tile of TILE keys, 1 KB each, as one wavefront makes them.  The keys of one copy (4 or 8,
+// aligned) are in one page.
+template <int HD, bool PAGED, int NI, int TILE>
+struct Copier {
+  static constexpr int KPI = 512 / HD;
+  KeySource<PAGED> ks;
+  int first, end;
+  uint32_t k_off[NI], v_off[NI];     // of this lane, from the copy's first key
+  __device__ __forceinline__ Copier(const KeySource<PAGED> &src, int first_copy, int end_key, int lane) : ks(src), first(first_copy), end(end_key) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      int key, chunk;
+      copied<HD>(first + i, lane, key, chunk);
+      k_off[i] = (uint32_t)(key - (first + i) * KPI) * ks.k_pitch + chunk * 16;
+      v_off[i] = PAGED ? k_off[i] : (uint32_t)(key - (first + i) * KPI) * ks.v_pitch + chunk * 16;
+    }
   }
-}
+  // the tile that starts at key j, a multiple of 32; keys from `end` on are replaced by the last one
+  template <bool VALUES>
+  __device__ __forceinline__ void copy(int j, uint32_t lds, int lane) const {
+    const bf16_t *src = VALUES ? ks.v : ks.k;
+    const uint32_t pitch = VALUES ? ks.v_pitch : ks.k_pitch;
+    const bool full = j + TILE <= end;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int key0 = full ? j + (first + i) * KPI : min(j + (first + i) * KPI, end - 1);
+      uint32_t off = VALUES ? v_off[i] : k_off[i];
+      if (!full) {
+        int key, chunk;
+        copied<HD>(first + i, lane, key, chunk);
+        off = (uint32_t)(min(j + key, end - 1) - key0) * pitch + chunk * 16;
+      }
+      const uint8_t *base;
+      if (PAGED) {
+        // (by a scalar load: the wait for it is not one for the copies before it)
+        int page = *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(ks.table + (key0 >> ks.shift)));
+        page = __builtin_amdgcn_readfirstlane((unsigned)page < (unsigned)ks.n_pages ? page : 0);
+        base = reinterpret_cast<const uint8_t *>(src + (size_t)page * ks.page_elems) + (uint32_t)(key0 & ((1 << ks.shift) - 1)) * (HD * 2);
+      } else {
+        base = reinterpret_cast<const uint8_t *>(src) + (uint64_t)(uint32_t)key0 * pitch;
+      }
+      gload_lds16_at(base, off, lds + (first + i) * 1024);
+    }
+  }
+};
 
+// The largest of a lane's scores.  v_max3 takes two at a time, where fmaxf first quiets each of its arguments.  The compiler does not
+// count the wait states between an MFMA and inline asm that reads what it wrote (18 after the longest): the first asm has them, and
+// the others depend on it.
+__device__ __forceinline__ float max_score(const f32x16_t (&s)[2]) {
+  float mx;
+  asm("s_nop 15\n\ts_nop 3\n\tv_max3_f32 %0, %1, %2, %3" : "=v"(mx) : "v"(s[0][0]), "v"(s[1][0]), "v"(s[0][1]));
+#pragma unroll
+  for (int i = 1; i < 15; ++i) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(mx) : "v"(s[1][i]), "v"(s[0][i + 1]));
+  asm("v_max_f32 %0, %0, %1" : "+v"(mx) : "v"(s[1][15]));
+  return mx;
+}
 // infinities and NaN of a pair of bf16 values set to 0; `any` collects whether there were some
 __device__ __forceinline__ uint32_t finite_pair(uint32_t w, uint32_t &any) {
   const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
   any |= lo | hi;
   return w & ~(lo | hi);
 }
-__device__ __forceinline__ float lds_bf16(uint32_t addr) {
-  return __uint_as_float((uint32_t)(*reinterpret_cast<const __attribute__((address_space(3))) uint16_t *>(addr)) << 16);
+__device__ __forceinline__ void lds_bf16x4(uint32_t addr, float (&v)[4]) {
+  const u32x2_t w = *reinterpret_cast<const __attribute__((address_space(3))) u32x2_t *>(addr);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
 }
 
 // natural log of the sum that belongs to a maximum (in powers of two of the scaled products) and a sum
@@ -223,347 +280,532 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 
 // ---- few rows: single tokens of a generation step ------------------------------------------------------------------------
 // HBM-bound: every key is read once for at most 16 NB rows.  Four wavefronts, each with keys of its own (32 at a time, every
-// fourth 32 of the piece), its own two stages of LDS and its own softmax state, without barriers until they join at the end.
+// fourth 32 of the piece), its own 32 keys of LDS and its own softmax state, without barriers until they join at the end: K of the
+// next keys is on its way while V of these is waited for, and the other way round.  Workgroups take pieces in turn, two of them
+// on a CU, so one streams while the other starts or joins.  The last piece of a tile to end joins all of them, in order.
+constexpr int kFewWaves = 4, kFewGrid = 512;
+
+// The sums of a piece go past this XCD's L2 (relaxed atomics of device scope: a release fence would write back all of it).
+__device__ __forceinline__ void part_store(float *at, float a, float b) {
+  const f32x2_t v = {a, b};
+  __hip_atomic_store(reinterpret_cast<uint64_t *>(at), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2_t part_load(const float *at) {
+  return __builtin_bit_cast(f32x2_t, __hip_atomic_load(reinterpret_cast<const uint64_t *>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
 template <int HD, int NB>
-__global__ __launch_bounds__(256) void ff_attn_few_kernel(AttnParams p, AttnPlan pl) {
+__global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnParams p, AttnPlan pl) {
   constexpr int KS = HD / 32, DB = HD / 16, NI = 32 * HD * 2 / 1024;
-  constexpr uint32_t kHalf = 32 * HD * 2, kStage = 2 * kHalf;
+  constexpr uint32_t kHalf = 32 * HD * 2;
   constexpr int kRows = 16 * NB, kPitch = HD + 4;
   extern __shared__ __align__(256) uint8_t lds[];
+  __shared__ int last_s;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l16 = lane & 15, quad = lane >> 4;
-  const int kpp = piece_keys(p, pl);
-  const Item it = work_of(p, pl, kpp, blockIdx.x);
-  if (!it.found) return;
-  const int n_rows = it.seq.n * p.group, row0 = it.tile * kRows;
-  const Range range = tile_range(p, it.seq, it.tile, kRows);
-  const int n_pieces = pieces_of(range, kpp);
-  if (it.piece >= n_pieces) return;
-  const int beg = range.lo + it.piece * kpp, end = min(range.hi, beg + kpp);
-  const KeySource<true> ks = key_source<HD, true>(p, it);
-  const uint32_t ring = lds_addr_of(lds) + wave * 2 * kStage;
+  const uint32_t k_at = lds_addr_of(lds) + wave * 2 * kHalf, v_at = k_at + kHalf;
+  // where this lane's operands lie in a tile (the swizzle repeats after 16 keys)
+  uint32_t k_off[KS], v_off[DB];
+#pragma unroll
+  for (int c = 0; c < KS; ++c) k_off[c] = k_at + chunk_at<HD>(l16, c * 4 + quad);
+#pragma unroll
+  for (int d = 0; d < DB; ++d) v_off[d] = v_at + chunk_at<HD>(quad * 4 + (l16 >> 2), d * 2 + ((l16 & 3) >> 1)) + (l16 & 1) * 8;
 
-  // the rows' own limits, and the part of the tile's keys that all of them see
-  Range see[NB];
-  u32x4_t q[NB][KS];
-  int all_lo = 0, all_hi = 0x7fffffff;
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int r = min(row0 + b * 16 + l16, n_rows - 1);
-    see[b] = row_range(p, it.seq, r);
-    see[b].hi = min(see[b].hi, end);
-    all_lo = max(all_lo, see[b].lo);
-    all_hi = min(all_hi, see[b].hi);
-    const bf16_t *src = p.q + (int64_t)(it.seq.t0 + r / p.group) * p.q_stride + (it.kvh * p.group + r % p.group) * HD + quad * 8;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) q[b][s] = *reinterpret_cast<const u32x4_t *>(src + s * 32);
-  }
-#pragma unroll
-  for (int off = 8; off > 0; off >>= 1) {
-    all_lo = max(all_lo, __shfl_xor(all_lo, off));
-    all_hi = min(all_hi, __shfl_xor(all_hi, off));
-  }
-  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+  const Cut cut = cut_of(p, pl);
+  const int n_items = items_of(p, pl, cut);
+  for (int id = blockIdx.x; id < n_items; id += gridDim.x) {
+    const Item it = work_of(p, pl, cut, id);
+    if (it.n_tiles == 0) continue;
+    const int n_rows = it.seq.n * p.group, row0 = it.tile * kRows;
+    const Range range = tile_range(p, it.seq, it.tile, kRows);
+    const int n_pieces = pieces_of(range, cut.keys);
+    if (it.piece >= n_pieces) continue;
+    const int beg = range.lo + it.piece * cut.keys, end = range.hi - beg > cut.keys ? beg + cut.keys : range.hi;
+    const Copier<HD, true, NI, 32> copier(key_source<HD, true>(p, it), 0, end, lane);
 
-  f32x4_t o[NB][DB];
-  float m[NB], l[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    m[b] = kNoMax;
-    l[b] = 0.f;
-#pragma unroll
-    for (int d = 0; d < DB; ++d) o[b][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
-
-  auto copy_tile = [&](int j, uint32_t stage) {
-#pragma unroll
-    for (int i = 0; i < NI; ++i) copy_keys<HD, true>(ks, i, j, end, stage, stage + kHalf, lane);
-  };
-  int j = beg + wave * 32;
-  uint32_t stage = ring;
-  wait_copies<0>();                       // (q is here: only copies are counted from now on)
-  if (j < end) copy_tile(j, stage);
-  for (; j < end; j += 128) {
-    const bool more = j + 128 < end;
-    if (more) {
-      copy_tile(j + 128, stage ^ ring ^ (ring + kStage));
-      wait_copies<2 * NI>();
-    } else {
-      wait_copies<0>();
-    }
-    // S^T: 32 keys by the rows
-    f32x4_t s[NB][2];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      u32x4_t kf[KS];
-#pragma unroll
-      for (int c = 0; c < KS; ++c) kf[c] = lds_read16(stage + chunk_at<HD>(kt * 16 + l16, c * 4 + quad));
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        s[b][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < KS; ++c) s[b][kt] = mfma16(kf[c], q[b][c], s[b][kt]);
-      }
-    }
-    const bool masked = j < all_lo || j + 32 > all_hi;
-    u32x4_t pk[NB];
+    // the rows' own limits, and the part of the tile's keys that all of them see
+    Range see[NB];
+    u32x4_t q[NB][KS];
+    int all_lo = 0, all_hi = 0x7fffffff;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      if (masked) {
+      const int r = min(row0 + b * 16 + l16, n_rows - 1);
+      see[b] = row_range(p, it.seq, r);
+      see[b].hi = min(see[b].hi, end);
+      all_lo = max(all_lo, see[b].lo);
+      all_hi = min(all_hi, see[b].hi);
+      const bf16_t *src = p.q + (int64_t)(it.seq.t0 + r / p.group) * p.q_stride + (it.kvh * p.group + r % p.group) * HD + quad * 8;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = j + kt * 16 + quad * 4 + i;
-            s[b][kt][i] = key >= see[b].lo && key < see[b].hi ? s[b][kt][i] : -INFINITY;
-          }
-      }
-      float mx = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])),
-                       fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32)) * p.scale_log2;
-      if (__any(mx > m[b] + kLazy)) {
-        const float m_new = fmaxf(m[b], mx), a = __builtin_amdgcn_exp2f(m[b] - m_new);
-        m[b] = m_new;
-        l[b] *= a;
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[b][d][i] *= a;
-      }
-      float e[8];
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        e[x] = __builtin_amdgcn_exp2f(fmaf(s[b][x >> 2][x & 3], p.scale_log2, -m[b]));
-        l[b] += e[x];
-      }
-      pk[b] = u32x4_t{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
+      for (int s = 0; s < KS; ++s) q[b][s] = *reinterpret_cast<const u32x4_t *>(src + s * 32);
     }
-    // O^T += V^T P^T
-    uint32_t odd = 0;
+    int j = beg + wave * 32;
+    if (j < end) copier.template copy<false>(j, k_at, lane);
 #pragma unroll
-    for (int d = 0; d < DB; ++d) {
-      const int c = d * 2 + ((l16 & 3) >> 1);
-      u32x2_t v0 = lds_read_tr(stage + kHalf + chunk_at<HD>(quad * 4 + (l16 >> 2), c) + (l16 & 1) * 8);
-      u32x2_t v1 = lds_read_tr(stage + kHalf + chunk_at<HD>(16 + quad * 4 + (l16 >> 2), c) + (l16 & 1) * 8);
-      u32x4_t vf = {v0[0], v0[1], v1[0], v1[1]};
-      if (masked) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) vf[x] = finite_pair(vf[x], odd);
-      }
-#pragma unroll
-      for (int b = 0; b < NB; ++b) o[b][d] = mfma16(vf, pk[b], o[b][d]);
+    for (int off = 8; off > 0; off >>= 1) {
+      all_lo = max(all_lo, __shfl_xor(all_lo, off));
+      all_hi = min(all_hi, __shfl_xor(all_hi, off));
     }
-    if (masked && __any(odd != 0)) {
-      // infinities and NaN among the values (0 in the product): they reach the rows that see their key, and no other
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[b][s]));   // (arrived: no wait for it among the copies' later on)
+    if (j < end) copier.template copy<true>(j, v_at, lane);
+
+    f32x4_t o[NB][DB];
+    float m[NB], l[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      m[b] = kNoMax;
+      l[b] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[b][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    for (; j < end; j += 32 * kFewWaves) {
+      const bool more = j + 32 * kFewWaves < end;
+      wait_copies<NI>();                    // K is here, V on its way
+      // S^T: 32 keys by the rows
+      f32x4_t s[NB][2];
+      u32x4_t kf[2][KS];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int c = 0; c < KS; ++c) kf[kt][c] = lds_read16(k_off[c] + kt * 16 * HD * 2);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K is in registers: its place is free
+      if (more) copier.template copy<false>(j + 32 * kFewWaves, k_at, lane);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          s[b][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < KS; ++c) s[b][kt] = mfma16(kf[kt][c], q[b][c], s[b][kt]);
+        }
+      const bool masked = j < all_lo || j + 32 > all_hi;
+      u32x4_t pk[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        if (masked) {
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int key = j + kt * 16 + quad * 4 + i;
+              s[b][kt][i] = key >= see[b].lo && key < see[b].hi ? s[b][kt][i] : -INFINITY;
+            }
+        }
+        float mx = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])),
+                         fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32)) * p.scale_log2;
+        if (__any(mx > m[b] + kLazy)) {
+          const float m_new = fmaxf(m[b], mx), a = __builtin_amdgcn_exp2f(m[b] - m_new);
+          m[b] = m_new;
+          l[b] *= a;
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[b][d][i] *= a;
+        }
+        float e[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          e[x] = __builtin_amdgcn_exp2f(fmaf(s[b][x >> 2][x & 3], p.scale_log2, -m[b]));
+          l[b] += e[x];
+        }
+        pk[b] = u32x4_t{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
+      }
+      if (more) wait_copies<NI>();          // V is here, the next K on its way
+      else wait_copies<0>();
+      // O^T += V^T P^T
+      if (!masked) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const u32x2_t v0 = lds_read_tr(v_off[d]), v1 = lds_read_tr(v_off[d] + 16 * HD * 2);
+          const u32x4_t vf = {v0[0], v0[1], v1[0], v1[1]};
+#pragma unroll
+          for (int b = 0; b < NB; ++b) o[b][d] = mfma16(vf, pk[b], o[b][d]);
+        }
+      } else {
+        uint32_t odd = 0;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const u32x2_t v0 = lds_read_tr(v_off[d]), v1 = lds_read_tr(v_off[d] + 16 * HD * 2);
+          const u32x4_t vf = {finite_pair(v0[0], odd), finite_pair(v0[1], odd), finite_pair(v1[0], odd), finite_pair(v1[1], odd)};
+#pragma unroll
+          for (int b = 0; b < NB; ++b) o[b][d] = mfma16(vf, pk[b], o[b][d]);
+        }
+        if (__any(odd != 0)) {
+          // infinities and NaN among the values (0 in the product): they reach the rows that see their key, and no other
 #pragma unroll 1
-      for (int x = 0; x < 32; ++x) {
+          for (int x = 0; x < 32; ++x) {
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int ch = d * 16 + quad * 4 + i;
-            const float v = lds_bf16(stage + kHalf + chunk_at<HD>(x, ch >> 3) + (ch & 7) * 2);
-            if (!(fabsf(v) < INFINITY))
+            for (int d = 0; d < DB; ++d) {
+              float v[4];
+              lds_bf16x4(v_at + chunk_at<HD>(x, d * 2 + (quad >> 1)) + (quad & 1) * 8, v);
 #pragma unroll
               for (int b = 0; b < NB; ++b)
-                if (j + x >= see[b].lo && j + x < see[b].hi) o[b][d][i] += v;
+                if (j + x >= see[b].lo && j + x < see[b].hi)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+                    if (!(fabsf(v[i]) < INFINITY)) o[b][d][i] += v[i];
+            }
           }
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V is in registers
+      if (more) copier.template copy<true>(j + 32 * kFewWaves, v_at, lane);
+    }
+
+    // join the four wavefronts' sums
+    float *joined = reinterpret_cast<float *>(lds);                        // [4][kRows][kPitch]
+    float *ml = joined + kFewWaves * kRows * kPitch;                       // [4][kRows][2]
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      l[b] += __shfl_xor(l[b], 16);
+      l[b] += __shfl_xor(l[b], 32);
+      const int r = b * 16 + l16;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+        *reinterpret_cast<f32x4_t *>(joined + (wave * kRows + r) * kPitch + d * 16 + quad * 4) = o[b][d];
+      if (quad == 0) {
+        ml[(wave * kRows + r) * 2] = m[b];
+        ml[(wave * kRows + r) * 2 + 1] = l[b];
       }
     }
-    stage = stage ^ ring ^ (ring + kStage);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // nothing of this stage is still being read when it is filled again
-  }
-
-  // join the four wavefronts' sums
-  float *joined = reinterpret_cast<float *>(lds);                        // [4][kRows][kPitch]
-  float *ml = joined + 4 * kRows * kPitch;                               // [4][kRows][2]
-  __syncthreads();
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    l[b] += __shfl_xor(l[b], 16);
-    l[b] += __shfl_xor(l[b], 32);
-    const int r = b * 16 + l16;
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-      *reinterpret_cast<f32x4_t *>(joined + (wave * kRows + r) * kPitch + d * 16 + quad * 4) = o[b][d];
-    if (quad == 0) {
-      ml[(wave * kRows + r) * 2] = m[b];
-      ml[(wave * kRows + r) * 2 + 1] = l[b];
-    }
-  }
-  __syncthreads();
-  const bool whole = n_pieces == 1;
-  float *part = whole ? nullptr : part_of<HD>(pl, it.first + it.piece * it.n_tiles + it.n_tiles - 1 - it.tile, it.kvh, p.n_kv);
-  for (int i = threadIdx.x; i < kRows * (HD / 4); i += 256) {
-    const int r = i / (HD / 4), c = (i % (HD / 4)) * 4;
-    if (row0 + r >= n_rows) break;
-    float mw[4], top = kNoMax, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      mw[w] = ml[(w * kRows + r) * 2];
-      top = fmaxf(top, mw[w]);
-    }
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float a = __builtin_amdgcn_exp2f(mw[w] - top);
-      sum = fmaf(ml[(w * kRows + r) * 2 + 1], a, sum);
-      const f32x4_t x = *reinterpret_cast<const f32x4_t *>(joined + (w * kRows + r) * kPitch + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = fmaf(x[e], a, acc[e]);
-    }
-    if (whole) {
+    __syncthreads();
+    const int rows_here = min(kRows, n_rows - row0);
+    const bool whole = n_pieces == 1;
+    // (tile, piece) numbers of this tile: x0, x0 + n_tiles, ...
+    const int x0 = it.first + it.n_tiles - 1 - it.tile;
+    const auto out = [&](int r, int c, float a, float b, float top, float sum) __attribute__((always_inline)) {
       const int row = row0 + r;
       const int64_t t = it.seq.t0 + row / p.group;
       const int head = it.kvh * p.group + row % p.group;
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-      *reinterpret_cast<u32x2_t *>(p.o + t * p.o_stride + head * HD + c) =
-          u32x2_t{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+      *reinterpret_cast<uint32_t *>(p.o + t * p.o_stride + head * HD + c) = pack_bf16x2(a * inv, b * inv);
       if (c == 0 && p.lse) p.lse[t * p.n_heads + head] = lse_of(top, sum);
-    } else {
-      *reinterpret_cast<f32x4_t *>(part + r * HD + c) = acc;
-      if (c == 0) {
-        part[kRows * HD + r * 2] = top;
-        part[kRows * HD + r * 2 + 1] = sum;
+    };
+    float *part = whole ? nullptr : part_of<HD>(pl, x0 + it.piece * it.n_tiles, it.kvh, p.n_kv);
+    for (int i = threadIdx.x; i < rows_here * (HD / 2); i += 64 * kFewWaves) {
+      const int r = i / (HD / 2), c = (i % (HD / 2)) * 2;
+      float mw[kFewWaves], top = kNoMax, sum = 0.f, a = 0.f, b = 0.f;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) {
+        mw[w] = ml[(w * kRows + r) * 2];
+        top = fmaxf(top, mw[w]);
+      }
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(mw[w] - top);
+        sum = fmaf(ml[(w * kRows + r) * 2 + 1], f, sum);
+        const f32x2_t x = *reinterpret_cast<const f32x2_t *>(joined + (w * kRows + r) * kPitch + c);
+        a = fmaf(x[0], f, a);
+        b = fmaf(x[1], f, b);
+      }
+      if (whole) {
+        out(r, c, a, b, top, sum);
+      } else {
+        part_store(part + r * HD + c, a, b);
+        if (c == 0) part_store(part + kRows * HD + r * 2, top, sum);
       }
     }
+    if (!whole) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // this wavefront's sums have arrived
+      __syncthreads();
+      int *counter = p.counters + x0 * p.n_kv + it.kvh;
+      if (threadIdx.x == 0) {
+        last_s = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n_pieces - 1;
+        if (last_s) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call expects it
+      }
+      __syncthreads();
+      if (last_s) {
+        const size_t step = (size_t)it.n_tiles * p.n_kv * ((size_t)kRows * (HD + 2));
+        const float *src = part_of<HD>(pl, x0, it.kvh, p.n_kv);
+        for (int i = threadIdx.x; i < rows_here * (HD / 2); i += 64 * kFewWaves) {
+          const int r = i / (HD / 2), c = (i % (HD / 2)) * 2;
+          // eight pieces' loads on their way at a time; their sums in a running maximum's scale, in the pieces' order
+          float top = kNoMax, sum = 0.f, a = 0.f, b = 0.f;
+          for (int k0 = 0; k0 < n_pieces; k0 += 8) {
+            f32x2_t x[8], w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float *from = src + (size_t)min(k0 + k, n_pieces - 1) * step;
+              w[k] = part_load(from + kRows * HD + r * 2);
+              x[k] = part_load(from + r * HD + c);
+            }
+            float higher = top;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) higher = fmaxf(higher, w[k][0]);
+            const float f0 = __builtin_amdgcn_exp2f(top - higher);
+            sum *= f0; a *= f0; b *= f0;
+            top = higher;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              if (k0 + k >= n_pieces) break;
+              const float f = __builtin_amdgcn_exp2f(w[k][0] - top);
+              sum = fmaf(w[k][1], f, sum);
+              a = fmaf(x[k][0], f, a);
+              b = fmaf(x[k][1], f, b);
+            }
+          }
+          out(r, c, a, b, top, sum);
+        }
+      }
+    }
+    __syncthreads();                        // nothing of this piece is still being read when the next one's copies land
   }
 }
 
 // ---- many rows: prompts and chunks of them --------------------------------------------------------------------------------
-// MFMA-bound.  WAVES wavefronts of 32 rows each share the key tiles of 64 in two stages of LDS.
-template <int HD, int WAVES, bool PAGED>
-__global__ __launch_bounds__(WAVES * 64) void ff_attn_tile_kernel(AttnParams p, AttnPlan pl) {
-  constexpr int KS = HD / 16, DB = HD / 32, NI = kTileKeys * HD * 2 / 1024 / WAVES;
-  constexpr uint32_t kHalf = kTileKeys * HD * 2, kStage = 2 * kHalf;
-  constexpr int kRows = 32 * WAVES;
+// MFMA-bound.  RW wavefronts of 32 rows share the key tiles of 64; with KW = 2 there are two such groups of wavefronts, which take
+// every other tile, for half as many rows, and join at the end.  Two stages of LDS for K and two for V: in step i, Q K of tile i
+// and P V of tile i - 1 are one run of MFMAs, whose operands are read six MFMAs ahead, and the softmax of tile i follows, while the
+// copies of K of tile i + 1 and V of tile i land.  One barrier a step: a SIMD's two wavefronts drift apart within it, and one's
+// exponentials go through the vector unit while the matrix pipe works for the other, whose MFMAs have priority.
+template <int HD, int RW, int KW, bool PAGED>
+__global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p, AttnPlan pl) {
+  constexpr int KS = HD / 16, DB = HD / 32, NI = kTileKeys * HD * 2 / 1024 / RW;
+  constexpr uint32_t kHalf = kTileKeys * HD * 2;
+  constexpr int kRows = 32 * RW, kStep = kTileKeys * KW;
   extern __shared__ __align__(256) uint8_t lds[];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % RW, kw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / RW;
+  const int lane = threadIdx.x & 63;
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15, grp = lane >> 4;
-  const int kpp = piece_keys(p, pl);
-  const Item it = work_of(p, pl, kpp, blockIdx.x);
-  if (!it.found) return;
+  const Cut cut = cut_of(p, pl);
+  if ((int)blockIdx.x >= items_of(p, pl, cut)) return;
+  const Item it = work_of(p, pl, cut, blockIdx.x);
+  if (it.n_tiles == 0) return;
+  const int kpp = cut.keys;
   const int n_rows = it.seq.n * p.group, row0 = it.tile * kRows + wave * 32;
   const Range range = tile_range(p, it.seq, it.tile, kRows);
   const int n_pieces = pieces_of(range, kpp);
   if (it.piece >= n_pieces) return;
-  const int beg = range.lo + it.piece * kpp, end = min(range.hi, beg + kpp);
-  const KeySource<PAGED> ks = key_source<HD, PAGED>(p, it);
-  const uint32_t ring = lds_addr_of(lds);
+  const int beg = range.lo + it.piece * kpp, end = range.hi - beg > kpp ? beg + kpp : range.hi;
+  const Copier<HD, PAGED, NI, kTileKeys> copier(key_source<HD, PAGED>(p, it), wave * NI, end, lane);
+  const uint32_t ring_k = lds_addr_of(lds) + kw * 4 * kHalf, ring_v = ring_k + 2 * kHalf;
 
-  const int row = min(row0 + l32, n_rows - 1);
+  // (out before the rows' own arithmetic and loads)
+  if (beg < end) copier.template copy<false>(beg + kw * kTileKeys, ring_k, lane);
+  int row = min(row0 + l32, n_rows - 1);
   Range see = row_range(p, it.seq, row);
   see.hi = min(see.hi, end);
-  const int head = it.kvh * p.group + row % p.group;
-  const int64_t t = it.seq.t0 + row / p.group;
   u32x4_t q[KS];
+  {
+    const bf16_t *src = p.q + (int64_t)(it.seq.t0 + row / p.group) * p.q_stride + (it.kvh * p.group + row % p.group) * HD + half * 8;
 #pragma unroll
-  for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const u32x4_t *>(p.q + t * p.q_stride + head * HD + s * 16 + half * 8);
+    for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const u32x4_t *>(src + s * 16);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));   // (arrived: no wait for it among the copies' later on)
+  }
   // (limits grow with the row: the first and the last row of the wavefront have the extremes)
   const int lo_first = __builtin_amdgcn_readlane(see.lo, 0), lo_last = __builtin_amdgcn_readlane(see.lo, 31);
-  const int hi_first = __builtin_amdgcn_readlane(see.hi, 0), hi_last = __builtin_amdgcn_readlane(see.hi, 31);
+  const int hi_first = __builtin_amdgcn_readlane(see.hi, 0);
+  const int hi_last = row0 < n_rows ? __builtin_amdgcn_readlane(see.hi, 31) : 0;     // (no rows: no tile is seen)
 
   f32x16_t o[DB];
+  u32x4_t pk[4];
   float m = kNoMax, l = 0.f;
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-  auto copy_tile = [&](int j, uint32_t stage) {
+  // where this lane's operands lie in a tile: chunk c of the key that is its row of K, and 8 bytes of each of two keys for V^T, from
+  // which the other keys' are 32 and 16 keys further (the swizzle repeats after 16)
+  uint32_t k_off[KS], v_off[DB][2];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) copy_keys<HD, PAGED>(ks, wave * NI + i, j, end, stage, stage + kHalf, lane);
+  for (int c = 0; c < KS; ++c) k_off[c] = chunk_at<HD>(l32, c * 2 + half);
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+      v_off[d][r] = chunk_at<HD>(half * 4 + (l16 >> 2) + 8 * r, d * 4 + (grp & 1) * 2 + ((l16 & 3) >> 1)) + (l16 & 1) * 8;
+
+  // Q K of the tile in LDS at `k_at`
+  auto scores = [&](f32x16_t (&s)[2], uint32_t k_at) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < KS; ++c) s[kb] = mfma32(lds_read16(k_at + k_off[c] + kb * 32 * HD * 2), q[c], s[kb]);
+    }
   };
-  uint32_t stage = ring;
-  wait_copies<0>();
-  if (beg < end) copy_tile(beg, stage);
-  for (int j = beg; j < end; j += kTileKeys) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // this tile is here, and nobody reads the other stage any more
-    if (j + kTileKeys < end) copy_tile(j + kTileKeys, stage ^ ring ^ (ring + kStage));
-    if (j < hi_last && j + kTileKeys > lo_first && row0 < n_rows) {
-      f32x16_t s[2];
+  // scores of the tile at key j -> weights, in the rows' running maximum's scale
+  auto weights = [&](f32x16_t (&s)[2], int j, auto masked) __attribute__((always_inline)) {
+    if (masked) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+        for (int i = 0; i < 16; ++i) {
+          const int key = j + half * 4 - see.lo + (kb * 32 + (i & 3) + 8 * (i >> 2));
+          s[kb][i] = (unsigned)key < (unsigned)(see.hi - see.lo) ? s[kb][i] : -INFINITY;
+        }
+    }
+    float mx = max_score(s);
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * p.scale_log2;
+    if (__any(mx > m + kLazy)) {
+      const float m_new = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= a;
 #pragma unroll
-        for (int c = 0; c < KS; ++c) s[kb] = mfma32(lds_read16(stage + chunk_at<HD>(kb * 32 + l32, c * 2 + half)), q[c], s[kb]);
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= a;
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(fmaf(s[x >> 1][(x & 1) * 8 + i], p.scale_log2, -m));
+        l += e[i];
       }
-      const bool masked = j < lo_last || j + kTileKeys > hi_first;
-      if (masked) {
+      pk[x] = u32x4_t{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
+    }
+  };
+  // P V of the tile at key j, whose values are in LDS at `v_at`, some of which a row may not see
+  auto values = [&](int j, uint32_t v_at) __attribute__((always_inline)) {
+    uint32_t odd = 0;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+    for (int x = 0; x < 4; ++x)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = j + kb * 32 + half * 4 + (i & 3) + 8 * (i >> 2);
-            s[kb][i] = key >= see.lo && key < see.hi ? s[kb][i] : -INFINITY;
-          }
+      for (int d = 0; d < DB; ++d) {
+        const u32x2_t v0 = lds_read_tr(v_at + v_off[d][0] + x * 16 * HD * 2);
+        const u32x2_t v1 = lds_read_tr(v_at + v_off[d][1] + x * 16 * HD * 2);
+        u32x4_t vf = {v0[0], v0[1], v1[0], v1[1]};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vf[e] = finite_pair(vf[e], odd);
+        o[d] = mfma32(vf, pk[x], o[d]);
+        __builtin_amdgcn_sched_barrier(0);     // (few registers, where speed does not matter)
       }
-      float mx = s[0][0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[0][i]);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[1][i]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32)) * p.scale_log2;
-      if (__any(mx > m + kLazy)) {
-        const float m_new = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - m_new);
-        m = m_new;
-        l *= a;
+    if (__any(odd != 0)) {
+      // infinities and NaN among the values (0 in the product): they reach the rows that see their key, and no other
+#pragma unroll 1
+      for (int x = 0; x < kTileKeys; ++x) {
+        const bool seen = j + x >= see.lo && j + x < see.hi;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] *= a;
-      }
-      u32x4_t pk[4];
+          for (int g = 0; g < 4; ++g) {
+            float v[4];
+            lds_bf16x4(v_at + chunk_at<HD>(x, d * 4 + g) + half * 8, v);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        float e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          e[i] = __builtin_amdgcn_exp2f(fmaf(s[x >> 1][(x & 1) * 8 + i], p.scale_log2, -m));
-          l += e[i];
-        }
-        pk[x] = u32x4_t{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
-      }
-      uint32_t odd = 0;
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const int c = d * 4 + (grp & 1) * 2 + ((l16 & 3) >> 1), key = x * 16 + half * 4 + (l16 >> 2);
-          const u32x2_t v0 = lds_read_tr(stage + kHalf + chunk_at<HD>(key, c) + (l16 & 1) * 8);
-          const u32x2_t v1 = lds_read_tr(stage + kHalf + chunk_at<HD>(key + 8, c) + (l16 & 1) * 8);
-          u32x4_t vf = {v0[0], v0[1], v1[0], v1[1]};
-          if (masked) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) vf[e] = finite_pair(vf[e], odd);
+            for (int i = 0; i < 4; ++i)
+              if (seen && !(fabsf(v[i]) < INFINITY)) o[d][g * 4 + i] += v[i];
           }
-          o[d] = mfma32(vf, pk[x], o[d]);
-        }
-      if (masked && __any(odd != 0)) {
-        // infinities and NaN among the values (0 in the product): they reach the rows that see their key, and no other
-#pragma unroll 1
-        for (int x = 0; x < kTileKeys; ++x) {
-          const bool seen = j + x >= see.lo && j + x < see.hi;
-#pragma unroll
-          for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int ch = d * 32 + half * 4 + (i & 3) + 8 * (i >> 2);
-              const float v = lds_bf16(stage + kHalf + chunk_at<HD>(x, ch >> 3) + (ch & 7) * 2);
-              if (seen && !(fabsf(v) < INFINITY)) o[d][i] += v;
-            }
-        }
       }
     }
-    stage = stage ^ ring ^ (ring + kStage);
-  }
+  };
+  // both products of a phase, for tiles that every row sees whole: each operand is read D MFMAs before its own
+  auto products = [&](f32x16_t (&s)[2], uint32_t v_at, uint32_t k_at) __attribute__((always_inline)) {
+    constexpr int NV = 4 * DB, N = NV + 2 * KS, D = 6;
+    u32x4_t f[D];
+    auto load = [&](int n) __attribute__((always_inline)) {
+      if (n < NV) {
+        const u32x2_t v0 = lds_read_tr(v_at + v_off[n % DB][0] + (n / DB) * 16 * HD * 2);
+        const u32x2_t v1 = lds_read_tr(v_at + v_off[n % DB][1] + (n / DB) * 16 * HD * 2);
+        f[n % D] = u32x4_t{v0[0], v0[1], v1[0], v1[1]};
+      } else {
+        f[n % D] = lds_read16(k_at + k_off[(n - NV) / 2] + (n - NV) % 2 * 32 * HD * 2);
+      }
+    };
+#pragma unroll
+    for (int n = 0; n < D; ++n) load(n);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (n < NV) {
+        o[n % DB] = mfma32(f[n % D], pk[n / DB], o[n % DB]);
+      } else {
+        const int kb = (n - NV) % 2, c = (n - NV) / 2;
+        if (c == 0)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+        s[kb] = mfma32(f[n % D], q[c], s[kb]);
+      }
+      if (n + D < N) load(n + D);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  const auto is_seen = [&](int j) { return j < hi_last && j + kTileKeys > lo_first; };
 
+  if (beg < end) {
+    // Step i: K of tile i is in stage i % 2, V of tile i - 1 in the other.  The copies that go out at its start fill the stages that
+    // step i - 1 read, and have landed when it ends.  (Copies past the end bring the last key again.)
+    const auto begin = [&](int j, uint32_t at) __attribute__((always_inline)) {
+      copier.template copy<false>(j + kStep, ring_k + (kHalf - at), lane);
+      copier.template copy<true>(j, ring_v + at, lane);
+    };
+    const auto step_end = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    const int start = beg + kw * kTileKeys;
+    const int whole_lo = max(start, lo_last), whole_hi = hi_first;   // tiles between these are seen whole by every row of the wavefront
+    // (all wavefronts make the same number of steps)
+    const int last = beg + (end - beg + kStep - 1) / kStep * kStep + kw * kTileKeys;
+    uint32_t at = 0;
+    step_end();
+    for (int j = start;; j += kStep, at = kHalf - at) {
+      for (; j - kStep >= whole_lo && j + kTileKeys <= whole_hi; j += kStep, at = kHalf - at) {
+        f32x16_t s[2];
+        begin(j, at);
+        __builtin_amdgcn_s_setprio(1);
+        products(s, ring_v + kHalf - at, ring_k + at);
+        __builtin_amdgcn_s_setprio(0);
+        weights(s, j, std::false_type());
+        step_end();
+      }
+      f32x16_t s[2];
+      const bool seen = j < last && is_seen(j);
+      begin(j, at);
+      if (j > start && is_seen(j - kStep)) values(j - kStep, ring_v + kHalf - at);
+      if (seen) {
+        scores(s, ring_k + at);
+        weights(s, j, std::true_type());
+      }
+      step_end();
+      if (j >= last) break;
+    }
+  }
   l += __shfl_xor(l, 32);
-  if (row0 + l32 >= n_rows) return;
+  if (KW > 1) {
+    // the second group's sums, through LDS, into the first's
+    constexpr int kPitch = HD + 4;
+    float *other = reinterpret_cast<float *>(lds) + (wave * 32 + l32) * kPitch;
+    float *ml = reinterpret_cast<float *>(lds) + kRows * kPitch + (wave * 32 + l32) * 2;
+    __syncthreads();
+    if (kw == 1) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4_t *>(other + d * 32 + g * 8 + half * 4) = f32x4_t{o[d][g * 4], o[d][g * 4 + 1], o[d][g * 4 + 2], o[d][g * 4 + 3]};
+      if (half == 0) {
+        ml[0] = m;
+        ml[1] = l;
+      }
+    }
+    __syncthreads();
+    if (kw == 1) return;
+    const float top = fmaxf(m, ml[0]), a = __builtin_amdgcn_exp2f(m - top), b = __builtin_amdgcn_exp2f(ml[0] - top);
+    m = top;
+    l = l * a + ml[1] * b;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(other + d * 32 + g * 8 + half * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[d][g * 4 + i] = fmaf(o[d][g * 4 + i], a, x[i] * b);
+      }
+  }
   if (n_pieces == 1) {
+    if (row0 + l32 >= n_rows) return;
+    asm volatile("" : "+v"(row));      // (its token and head are found again here: four registers less in the loop)
+    const int head = it.kvh * p.group + row % p.group;
+    const int64_t t = it.seq.t0 + row / p.group;
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     bf16_t *dst = p.o + t * p.o_stride + head * HD;
 #pragma unroll
@@ -576,68 +818,74 @@ __global__ __launch_bounds__(WAVES * 64) void ff_attn_tile_kernel(AttnParams p, 
   } else {
     float *part = part_of<HD>(pl, it.first + it.piece * it.n_tiles + it.n_tiles - 1 - it.tile, it.kvh, p.n_kv);
     const int r = wave * 32 + l32;
+    float *mine = part + wave * 32 * HD + lane * 4;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4_t *>(part + r * HD + d * 32 + g * 8 + half * 4) =
-            f32x4_t{o[d][g * 4], o[d][g * 4 + 1], o[d][g * 4 + 2], o[d][g * 4 + 3]};
-    if (half == 0) {
-      part[kRows * HD + r * 2] = m;
-      part[kRows * HD + r * 2 + 1] = l;
-    }
+        *reinterpret_cast<f32x4_t *>(mine + (d * 4 + g) * 256) = f32x4_t{o[d][g * 4], o[d][g * 4 + 1], o[d][g * 4 + 2], o[d][g * 4 + 3]};
+    if (half == 0) *reinterpret_cast<f32x2_t *>(part + kRows * HD + r * 2) = f32x2_t{m, l};
   }
 }
 
 // ---- rows split along the keys: their pieces joined, in order ------------------------------------------------------------
-// One wavefront to a (token, head).
+// One wavefront to 1 KB of every piece: 32 rows, eight channels.
 template <int HD>
-__global__ __launch_bounds__(256) void ff_attn_join_kernel(AttnParams p, AttnPlan few, AttnPlan tile) {
-  const int lane = threadIdx.x & 63;
-  const long id = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t = (int)(id / p.n_heads), head = (int)(id % p.n_heads);
-  if (t >= p.T) return;
-  // the sequence whose rows hold the token
-  int s = -1;
-  for (int s0 = 0; s0 < p.n_seqs && s < 0; s0 += 64) {
-    bool mine = false;
-    if (s0 + lane < p.n_seqs) {
-      const Seq q = seq_of(p, s0 + lane);
-      mine = t >= q.t0 && t < q.t0 + q.n;
-    }
-    const unsigned long long hit = __ballot(mine);
-    if (hit) s = s0 + __builtin_ctzll(hit);
-  }
-  if (s < 0) return;
-  const Seq q = seq_of(p, s);
-  const bool is_few = tiles_of(p, few, q.n) > 0;
-  const AttnPlan &pl = is_few ? few : tile;
-  if (pl.target <= 0) return;
-  const int kpp = piece_keys(p, pl);
-  const Item it = find_item(p, pl, kpp, s, true);
-  const int kvh = head / p.group, row = (t - it.seq.t0) * p.group + head % p.group;
-  const int tl = row / pl.tile_rows, r = row - tl * pl.tile_rows;
-  const int n = pieces_of(tile_range(p, it.seq, tl, pl.tile_rows), kpp);
-  const int x0 = it.first + it.n_tiles - 1 - tl;
+__global__ __launch_bounds__(256) void ff_attn_join_kernel(AttnParams p, AttnPlan pl) {
+  const Cut cut = cut_of(p, pl);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int runs = pl.tile_rows / 32 * (HD / 8);                // of 1 KB in a tile
+  const int id = (int)blockIdx.x * 4 / runs, run = (int)blockIdx.x * 4 % runs + wave;
+  const int x = id / p.n_kv, kvh = id - x * p.n_kv;
+  // (tiles are counted as they would be without pieces)
+  const Item whole = find_seq<false>(p, pl, kUnsplit, cut.first, x);
+  if (whole.n_tiles == 0) return;
+  const int tile = x - whole.first;
+  const int n = pieces_of(tile_range(p, whole.seq, tile, pl.tile_rows), cut.keys);
+  if (n <= 1) return;
+  const Item it = find_seq<true>(p, pl, cut.keys, cut.first, whole.s);
+  const int x0 = it.first + it.n_tiles - 1 - tile;
   // (chunks that overlap may have more pieces than there were workgroups and room for)
-  if (n <= 1 || it.n_tiles == 0 || ((long)x0 + (long)(n - 1) * it.n_tiles + 1) * p.n_kv > pl.max_items) return;
-  float top = kNoMax;
-  for (int i = lane; i < n; i += 64) top = fmaxf(top, part_of<HD>(pl, x0 + i * it.n_tiles, kvh, p.n_kv)[pl.tile_rows * HD + r * 2]);
+  if (((long)x0 + (long)(n - 1) * it.n_tiles + 1) * p.n_kv > pl.max_items) return;
+  const int r = run / (HD / 8) * 32 + (lane & 31), c = run % (HD / 8) * 8 + (lane >> 5) * 4;
+  const int row = tile * pl.tile_rows + r;
+  if (row >= it.seq.n * p.group) return;
+  const size_t step = (size_t)it.n_tiles * p.n_kv * ((size_t)pl.tile_rows * (HD + 2));
+  const float *src = part_of<HD>(pl, x0, kvh, p.n_kv);
+  float top = kNoMax, sum = 0.f;
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  for (int k0 = 0; k0 < n; k0 += 8) {                 // eight pieces' loads on their way at a time
+    f32x4_t v[8];
+    f32x2_t w[8];
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-  float sum = 0.f, acc[HD / 64] = {};
-  for (int i = 0; i < n; ++i) {
-    const float *part = part_of<HD>(pl, x0 + i * it.n_tiles, kvh, p.n_kv);
-    const float a = __builtin_amdgcn_exp2f(part[pl.tile_rows * HD + r * 2] - top);
-    sum = fmaf(part[pl.tile_rows * HD + r * 2 + 1], a, sum);
+    for (int k = 0; k < 8; ++k) {
+      const float *from = src + (size_t)min(k0 + k, n - 1) * step;
+      w[k] = *reinterpret_cast<const f32x2_t *>(from + pl.tile_rows * HD + r * 2);
+      v[k] = *reinterpret_cast<const f32x4_t *>(from + run * 256 + lane * 4);
+    }
+    float higher = top;
 #pragma unroll
-    for (int e = 0; e < HD / 64; ++e) acc[e] = fmaf(part[r * HD + lane * (HD / 64) + e], a, acc[e]);
+    for (int k = 0; k < 8; ++k) higher = fmaxf(higher, w[k][0]);
+    const float f0 = __builtin_amdgcn_exp2f(top - higher);
+    top = higher;
+    sum *= f0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] *= f0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (k0 + k >= n) break;
+      const float f = __builtin_amdgcn_exp2f(w[k][0] - top);
+      sum = fmaf(w[k][1], f, sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[k][e], f, acc[e]);
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  bf16_t *dst = p.o + (int64_t)t * p.o_stride + head * HD;
-  if (HD == 128) *reinterpret_cast<uint32_t *>(dst + lane * 2) = pack_bf16x2(acc[0] * inv, acc[HD / 64 - 1] * inv);
-  else dst[lane] = f32_to_bf16(acc[0] * inv);
-  if (lane == 0 && p.lse) p.lse[(int64_t)t * p.n_heads + head] = lse_of(top, sum);
+  const int64_t t = it.seq.t0 + row / p.group;
+  const int head = kvh * p.group + row % p.group;
+  *reinterpret_cast<u32x2_t *>(p.o + t * p.o_stride + head * HD + c) =
+      u32x2_t{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+  if (c == 0 && p.lse) p.lse[t * p.n_heads + head] = lse_of(top, sum);
 }
 
 // one wavefront per sequence
@@ -646,7 +894,7 @@ __global__ __launch_bounds__(64) void ff_attn_validate_kernel(AttnParams p, int3
   const int a = p.starts[s], b = p.starts[s + 1];
   bool bad = a < 0 || b < a || b > p.T || p.lens[s] < 0 || p.lens[s] > most_keys(p);
   const Seq q = seq_of(p, s);
-  const int first = p.window > 0 ? max(0, q.keys - q.n + 1 - p.window) >> p.page_shift : 0;
+  const int first = p.window > 0 ? max(0, q.keys - q.n + 1 - min(p.window, kMaxKeys)) >> p.page_shift : 0;
   const int pages = q.n > 0 ? (int)(((long)q.keys + (1 << p.page_shift) - 1) >> p.page_shift) : 0;
   for (int i = first + lane; i < pages; i += 64) {
     const int page = p.table[(size_t)s * p.table_stride + i];
@@ -655,13 +903,16 @@ __global__ __launch_bounds__(64) void ff_attn_validate_kernel(AttnParams p, int3
   if (__any(bad) && lane == 0) atomicMax(flag, s + 1);
 }
 
-constexpr int kFewWaves = 4;
 size_t few_lds(int hd, int nb) {
-  const size_t ring = (size_t)kFewWaves * 2 * 2 * 32 * hd * 2;
+  const size_t ring = (size_t)kFewWaves * 2 * 32 * hd * 2;
   const size_t join = (size_t)kFewWaves * 16 * nb * (hd + 4 + 2) * 4;
   return std::max(ring, join);
 }
-size_t tile_lds(int hd) { return (size_t)2 * 2 * kTileKeys * hd * 2; }
+size_t tile_lds(int hd, int rw, int kw) {
+  const size_t ring = (size_t)kw * 4 * kTileKeys * hd * 2;
+  const size_t join = kw > 1 ? (size_t)32 * rw * (hd + 4 + 2) * 4 : 0;
+  return std::max(ring, join);
+}
 
 template <int HD>
 hipError_t raise_limits() {
@@ -671,52 +922,54 @@ hipError_t raise_limits() {
   };
   raise(reinterpret_cast<const void *>(ff_attn_few_kernel<HD, 1>), few_lds(HD, 1));
   raise(reinterpret_cast<const void *>(ff_attn_few_kernel<HD, 2>), few_lds(HD, 2));
-  raise(reinterpret_cast<const void *>(ff_attn_few_kernel<HD, 4>), few_lds(HD, 4));
-  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 4, true>), tile_lds(HD));
-  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 8, true>), tile_lds(HD));
-  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 4, false>), tile_lds(HD));
-  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 8, false>), tile_lds(HD));
+  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 4, 2, true>), tile_lds(HD, 4, 2));
+  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 8, 1, true>), tile_lds(HD, 8, 1));
+  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 4, 2, false>), tile_lds(HD, 4, 2));
+  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 8, 1, false>), tile_lds(HD, 8, 1));
   return e;
 }
 
 // How the call is cut.  rows of a sequence = new tokens times heads of a group.
 struct Choice {
   AttnPlan few, tile;
-  int nb = 0, waves = 0;          // 0: that kernel is not launched
+  int nb = 0, rw = 0;             // 0: that kernel is not launched
+  long tiles = 0;                 // most tiles of the second kernel
   size_t bytes = 0;
 };
-// Items that a plan can have at most: about `target` pieces and one more for each (tile, key head).  Their tiles: the rows' own and
-// one part-filled tile for each sequence.
-long tiles_bound(long rows, int n_seqs, int n_tokens, int tile_rows) { return rows / tile_rows + std::min(n_seqs, n_tokens); }
-
 Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int max_chunk, bool paged) {
   Choice c;
   const int group = n_heads / n_kv;
-  const long rows = (long)n_tokens * group, chunk_rows = (long)max_chunk * group;
-  const auto set = [&](AttnPlan &pl, int tile_rows, long above, long upto, int target, int min_steps) {
-    const long tiles = tiles_bound(rows, n_seqs, n_tokens, tile_rows);
+  const long rows = (long)n_tokens * group, chunk_rows = (long)max_chunk * group, seqs = std::min(n_seqs, n_tokens);
+  constexpr long kAll = 0x7fffffffffffL;
+  // Items that a plan can have at most: about `target` pieces and one more for each of the tiles and key heads.
+  const auto set = [&](AttnPlan &pl, int tile_rows, long tiles, long above, long upto, int target, int min_steps) {
     pl.tile_rows = tile_rows;
     pl.rows_above = above;
     pl.rows_upto = upto;
     pl.min_steps = min_steps;
-    // rows enough for every CU are not split: whole rows need no second pass
-    pl.target = paged && rows / tile_rows * n_kv < 512 ? target : 0;
+    pl.target = tiles * n_kv + target + 16 <= kAttnCounters ? target : 0;
     pl.max_items = (int)std::min<long>(tiles * n_kv + pl.target + 16, 0x7fffffff);   // (the price of a call is summed in fp32)
     pl.part_at = c.bytes / sizeof(float);
     if (pl.target > 0) c.bytes += (size_t)pl.max_items * tile_rows * (head_dim + 2) * sizeof(float);
   };
-  const long all = 0x7fffffffffffL;
-  if (paged && chunk_rows <= 64) {
-    c.nb = chunk_rows <= 16 ? 1 : (chunk_rows <= 32 ? 2 : 4);
-    set(c.few, 16 * c.nb, 0, all, 1024, 4);
+  // (the rows' own tiles and a part-filled one for each sequence)
+  if (paged && chunk_rows <= 32) {
+    c.nb = chunk_rows <= 16 ? 1 : 2;
+    set(c.few, 16 * c.nb, rows / (16 * c.nb) + seqs, 0, kAll, 2 * kFewGrid, 2);
     return c;
   }
-  c.waves = chunk_rows <= 128 ? 4 : 8;
   const bool both = paged && n_seqs > 1 && group <= 16;     // sequences that generate one token beside chunks
-  set(c.tile, 32 * c.waves, both ? 16 : 0, all, 256, 4);
+  // 256 rows where those fill the CUs
+  c.rw = rows / 256 * n_kv >= 256 ? 8 : 4;
+  const int tile_rows = 32 * c.rw;
+  c.tiles = rows / tile_rows + seqs;
+  // A piece for every CU, two where the rows alone give those: then only sequences longer than the others are split.  Rows enough for
+  // every CU many times over are not: whole rows need no second pass.
+  const long items = rows / tile_rows * n_kv;
+  set(c.tile, tile_rows, c.tiles, both ? 16 : 0, kAll, !paged || items >= 2048 ? 0 : (items < 256 ? 256 : 512), 4);
   if (both) {
     c.nb = 1;
-    set(c.few, 16, 0, 16, 1024, 4);
+    set(c.few, 16, seqs, 0, 16, 2 * kFewGrid, 2);
   }
   return c;
 }
@@ -727,26 +980,23 @@ hipError_t launch(const AttnParams &p, Choice &c, hipStream_t s) {
   c.few.part = p.part + c.few.part_at;
   c.tile.part = p.part + c.tile.part_at;
   if (c.nb) {
-    const dim3 grid((unsigned)c.few.max_items), block(64 * kFewWaves);
+    const dim3 grid((unsigned)std::min(c.few.max_items, kFewGrid)), block(64 * kFewWaves);
     const size_t lds = few_lds(HD, c.nb);
     if (c.nb == 1) hipLaunchKernelGGL((ff_attn_few_kernel<HD, 1>), grid, block, lds, s, p, c.few);
-    else if (c.nb == 2) hipLaunchKernelGGL((ff_attn_few_kernel<HD, 2>), grid, block, lds, s, p, c.few);
-    else hipLaunchKernelGGL((ff_attn_few_kernel<HD, 4>), grid, block, lds, s, p, c.few);
+    else hipLaunchKernelGGL((ff_attn_few_kernel<HD, 2>), grid, block, lds, s, p, c.few);
   }
-  if (c.waves) {
-    const dim3 grid((unsigned)c.tile.max_items), block(64 * c.waves);
-    const size_t lds = tile_lds(HD);
+  if (c.rw) {
+    const dim3 grid((unsigned)c.tile.max_items), block(512);
+    const size_t lds = tile_lds(HD, c.rw, 8 / c.rw);
     if (p.table) {
-      if (c.waves == 4) hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 4, true>), grid, block, lds, s, p, c.tile);
-      else hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 8, true>), grid, block, lds, s, p, c.tile);
+      if (c.rw == 4) hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 4, 2, true>), grid, block, lds, s, p, c.tile);
+      else hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 8, 1, true>), grid, block, lds, s, p, c.tile);
     } else {
-      if (c.waves == 4) hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 4, false>), grid, block, lds, s, p, c.tile);
-      else hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 8, false>), grid, block, lds, s, p, c.tile);
+      if (c.rw == 4) hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 4, 2, false>), grid, block, lds, s, p, c.tile);
+      else hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 8, 1, false>), grid, block, lds, s, p, c.tile);
     }
-  }
-  if (c.few.target > 0 || c.tile.target > 0) {
-    const long waves = (long)p.T * p.n_heads;
-    hipLaunchKernelGGL((ff_attn_join_kernel<HD>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, p, c.few, c.tile);
+    if (c.tile.target > 0)
+      hipLaunchKernelGGL((ff_attn_join_kernel<HD>), dim3((unsigned)(c.tiles * p.n_kv * (c.tile.tile_rows / 32 * (HD / 8) / 4))), dim3(256), 0, s, p, c.tile);
   }
   return hipGetLastError();
 }
@@ -757,8 +1007,8 @@ hipError_t launch(const AttnParams &p, Choice &c, hipStream_t s) {
 size_t ff_attention_part_bytes(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs) {
   const int group = n_heads / n_kv;
   size_t most = 0;
-  for (int rows : {16, 32, 64, 128, 129})
-    most = std::max(most, choose(n_heads, n_kv, head_dim, n_tokens, n_seqs, std::max(1, (rows + (rows > 128 ? group - 1 : 0)) / group), true).bytes);
+  for (int rows : {1, 17, 33})
+    most = std::max(most, choose(n_heads, n_kv, head_dim, n_tokens, n_seqs, (rows + group - 1) / group, true).bytes);
   return most;
 }
 

@@ -20,10 +20,12 @@ struct AttnParams {
   int32_t T, n_seqs, n_heads, n_kv, group, causal, window;
   int32_t table_stride, page_shift, n_pages;
   float scale_log2;              // scale * log2(e)
-  // set by the launcher: room for pieces of rows split along the keys
+  // room for pieces of rows split along the keys
   float *part = nullptr;
   size_t part_bytes = 0;
+  int32_t *counters = nullptr;   // [kAttnCounters], zero: how many pieces of a tile have ended; zero again when the call has
 };
+constexpr int kAttnCounters = 16384;
 // One kernel's share of a call: the sequences with rows (new tokens times heads of a group) in (rows_above, rows_upto], in tiles of
 // tile_rows, split along the keys into about `target` pieces of at least min_steps times 64 keys (0: not split).
 struct AttnPlan {

@@ -512,8 +512,13 @@ static void check_attention() {
     std::vector<long> covered(n_seqs, 0);
     for (const Launch &l : g_log) {
       const AttnPlan &pl = l.plan;
-      if (l.threads == 256 && l.grid == (unsigned)(((long)p.T * p.n_heads + 3) / 4) && &l == &g_log.back() && pl.max_items != (int)l.grid) continue;   // (joins the pieces)
-      CHECK(l.lds <= kLds && l.grid == (unsigned)pl.max_items, "round %d: %u workgroups, %zu bytes", round, l.grid, l.lds);
+      if (l.threads == 256 && pl.tile_rows >= 128) {                                       // (joins the pieces of the launch before)
+        CHECK(l.grid >= (unsigned)((long)t * group / pl.tile_rows * n_kv), "round %d: %u workgroups join", round, l.grid);
+        continue;
+      }
+      // (the few-row kernel's workgroups take items in turn)
+      CHECK(l.lds <= kLds && l.grid == (unsigned)(l.threads == 256 ? std::min(pl.max_items, 512) : pl.max_items), "round %d: %u workgroups, %zu bytes", round, l.grid, l.lds);
+      CHECK(pl.target == 0 || pl.max_items <= kAttnCounters, "round %d: %d counters", round, pl.max_items);
       float steps = 0.f;
       for (int s = 0; s < n_seqs; ++s) steps += price_of(p, pl, seq_of(p, s));
       const int kpp = pl.target > 0 ? piece_keys_for(p, pl, steps) : kUnsplit;
