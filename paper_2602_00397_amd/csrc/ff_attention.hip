@@ -250,14 +250,25 @@ struct Copier {
 // The largest of a lane's scores.  v_max3 takes two at a time, where fmaxf first quiets each of its arguments.  The compiler does not
 // count the wait states between an MFMA and inline asm that reads what it wrote (18 after the longest): the first asm has them, and
 // the others depend on it.
-__device__ __forceinline__ float max_score(const f32x16_t (&s)[2]) {
+__device__ __forceinline__ float max16(const f32x16_t &s) {
   float mx;
-  asm("s_nop 15\n\ts_nop 3\n\tv_max3_f32 %0, %1, %2, %3" : "=v"(mx) : "v"(s[0][0]), "v"(s[1][0]), "v"(s[0][1]));
+  asm("s_nop 15\n\ts_nop 3\n\tv_max3_f32 %0, %1, %2, %3" : "=v"(mx) : "v"(s[0]), "v"(s[1]), "v"(s[2]));
 #pragma unroll
-  for (int i = 1; i < 15; ++i) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(mx) : "v"(s[1][i]), "v"(s[0][i + 1]));
-  asm("v_max_f32 %0, %0, %1" : "+v"(mx) : "v"(s[1][15]));
+  for (int i = 3; i < 15; i += 2) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(mx) : "v"(s[i]), "v"(s[i + 1]));
+  asm("v_max_f32 %0, %0, %1" : "+v"(mx) : "v"(s[15]));
   return mx;
 }
+__device__ __forceinline__ float max_score(const f32x16_t (&s)[2]) { return fmaxf(max16(s[0]), max16(s[1])); }
+// What lane l ^ 32, or l ^ 16, holds beside this lane's value, by the vector unit (a shuffle goes through LDS).
+__device__ __forceinline__ f32x2_t with_half(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return f32x2_t{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ f32x2_t with_row(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return f32x2_t{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ float larger(const f32x2_t &v) { return fmaxf(v[0], v[1]); }
 // infinities and NaN of a pair of bf16 values set to 0; `any` collects whether there were some
 __device__ __forceinline__ uint32_t finite_pair(uint32_t w, uint32_t &any) {
   const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
@@ -298,7 +309,7 @@ template <int HD, int NB>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnParams p, AttnPlan pl) {
   constexpr int KS = HD / 32, DB = HD / 16, NI = 32 * HD * 2 / 1024;
   constexpr uint32_t kHalf = 32 * HD * 2;
-  constexpr int kRows = 16 * NB, kPitch = HD + 4;
+  constexpr int kRows = 16 * NB, kPitch = HD + 4, kBatch = 16;
   extern __shared__ __align__(256) uint8_t lds[];
   __shared__ int last_s;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -397,8 +408,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
         }
         float mx = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])),
                          fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32)) * p.scale_log2;
+        mx = larger(with_half(larger(with_row(mx)))) * p.scale_log2;
         if (__any(mx > m[b] + kLazy)) {
           const float m_new = fmaxf(m[b], mx), a = __builtin_amdgcn_exp2f(m[b] - m_new);
           m[b] = m_new;
@@ -464,8 +474,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
     __syncthreads();
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      l[b] += __shfl_xor(l[b], 16);
-      l[b] += __shfl_xor(l[b], 32);
+      f32x2_t both = with_row(l[b]);
+      both = with_half(both[0] + both[1]);
+      l[b] = both[0] + both[1];
       const int r = b * 16 + l16;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
@@ -526,29 +537,29 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
         const float *src = part_of<HD>(pl, x0, it.kvh, p.n_kv);
         for (int i = threadIdx.x; i < rows_here * (HD / 2); i += 64 * kFewWaves) {
           const int r = i / (HD / 2), c = (i % (HD / 2)) * 2;
-          // eight pieces' loads on their way at a time; their sums in a running maximum's scale, in the pieces' order
+          // kBatch pieces' loads on their way at a time; their sums in a running maximum's scale, in the pieces' order
           float top = kNoMax, sum = 0.f, a = 0.f, b = 0.f;
-          for (int k0 = 0; k0 < n_pieces; k0 += 8) {
-            f32x2_t x[8], w[8];
+          for (int k0 = 0; k0 < n_pieces; k0 += kBatch) {
+            f32x2_t x[kBatch], w[kBatch];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < kBatch; ++k) {
               const float *from = src + (size_t)min(k0 + k, n_pieces - 1) * step;
               w[k] = part_load(from + kRows * HD + r * 2);
               x[k] = part_load(from + r * HD + c);
             }
             float higher = top;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) higher = fmaxf(higher, w[k][0]);
+            for (int k = 0; k < kBatch; ++k) higher = fmaxf(higher, w[k][0]);
             const float f0 = __builtin_amdgcn_exp2f(top - higher);
             sum *= f0; a *= f0; b *= f0;
             top = higher;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              if (k0 + k >= n_pieces) break;
+            for (int k = 0; k < kBatch; ++k) {
+              const bool is = k0 + k < n_pieces;       // (not by a factor of 0: the sums may be infinite)
               const float f = __builtin_amdgcn_exp2f(w[k][0] - top);
-              sum = fmaf(w[k][1], f, sum);
-              a = fmaf(x[k][0], f, a);
-              b = fmaf(x[k][1], f, b);
+              sum = is ? fmaf(w[k][1], f, sum) : sum;
+              a = is ? fmaf(x[k][0], f, a) : a;
+              b = is ? fmaf(x[k][1], f, b) : b;
             }
           }
           out(r, c, a, b, top, sum);
@@ -566,11 +577,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
 // copies of K of tile i + 1 and V of tile i land.  One barrier a step: a SIMD's two wavefronts drift apart within it, and one's
 // exponentials go through the vector unit while the matrix pipe works for the other, whose MFMAs have priority.
 template <int HD, int RW, int KW, bool PAGED>
-__global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p, AttnPlan pl) {
+__global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 2) void ff_attn_tile_kernel(AttnParams p, AttnPlan pl) {
   constexpr int KS = HD / 16, DB = HD / 32, NI = kTileKeys * HD * 2 / 1024 / RW;
   constexpr uint32_t kHalf = kTileKeys * HD * 2;
   constexpr int kRows = 32 * RW, kStep = kTileKeys * KW;
   extern __shared__ __align__(256) uint8_t lds[];
+  __shared__ int odd_s[KW][2];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % RW, kw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / RW;
   const int lane = threadIdx.x & 63;
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15, grp = lane >> 4;
@@ -589,20 +601,20 @@ __global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p
 
   // (out before the rows' own arithmetic and loads)
   if (beg < end) copier.template copy<false>(beg + kw * kTileKeys, ring_k, lane);
-  int row = min(row0 + l32, n_rows - 1);
-  Range see = row_range(p, it.seq, row);
-  see.hi = min(see.hi, end);
+  Range see;
   u32x4_t q[KS];
   {
+    const int row = min(row0 + l32, n_rows - 1);
+    see = row_range(p, it.seq, row);
+    see.hi = min(see.hi, end);
     const bf16_t *src = p.q + (int64_t)(it.seq.t0 + row / p.group) * p.q_stride + (it.kvh * p.group + row % p.group) * HD + half * 8;
 #pragma unroll
     for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const u32x4_t *>(src + s * 16);
 #pragma unroll
     for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));   // (arrived: no wait for it among the copies' later on)
   }
-  // (limits grow with the row: the first and the last row of the wavefront have the extremes)
-  const int lo_first = __builtin_amdgcn_readlane(see.lo, 0), lo_last = __builtin_amdgcn_readlane(see.lo, 31);
-  const int hi_first = __builtin_amdgcn_readlane(see.hi, 0);
+  // (limits grow with the row: the first and the last row have the extremes)
+  const int lo_first = __builtin_amdgcn_readlane(see.lo, 0);
   const int hi_last = row0 < n_rows ? __builtin_amdgcn_readlane(see.hi, 31) : 0;     // (no rows: no tile is seen)
 
   f32x16_t o[DB];
@@ -612,6 +624,12 @@ __global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+  // Tiles that not all rows of the workgroup see whole: their values are looked through for infinities and NaN when they have landed,
+  // by the wavefront that copied them, which leaves the tile's key in the stage's flag if there are any.
+  const int edge_lo = row_range(p, it.seq, min((it.tile + 1) * kRows, n_rows) - 1).lo, edge_hi = min(row_range(p, it.seq, it.tile * kRows).hi, end);
+  const auto is_edge = [&](int j) { return j < edge_lo || j + kTileKeys > edge_hi; };
+  volatile int *const odd_tile = odd_s[kw];
 
   // where this lane's operands lie in a tile: chunk c of the key that is its row of K, and 8 bytes of each of two keys for V^T, from
   // which the other keys' are 32 and 16 keys further (the swizzle repeats after 16)
@@ -645,8 +663,7 @@ __global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p
           s[kb][i] = (unsigned)key < (unsigned)(see.hi - see.lo) ? s[kb][i] : -INFINITY;
         }
     }
-    float mx = max_score(s);
-    mx = fmaxf(mx, __shfl_xor(mx, 32)) * p.scale_log2;
+    const float mx = larger(with_half(max_score(s))) * p.scale_log2;
     if (__any(mx > m + kLazy)) {
       const float m_new = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;
@@ -667,8 +684,19 @@ __global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p
       pk[x] = u32x4_t{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
     }
   };
-  // P V of the tile at key j, whose values are in LDS at `v_at`, some of which a row may not see
-  auto values = [&](int j, uint32_t v_at) __attribute__((always_inline)) {
+  // P V of the tile whose values are in LDS at `v_at`
+  auto values = [&](uint32_t v_at) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const u32x2_t v0 = lds_read_tr(v_at + v_off[d][0] + x * 16 * HD * 2), v1 = lds_read_tr(v_at + v_off[d][1] + x * 16 * HD * 2);
+        o[d] = mfma32(u32x4_t{v0[0], v0[1], v1[0], v1[1]}, pk[x], o[d]);
+      }
+  };
+  // The same for the tile at key j, where some value that a row may not see is an infinity or NaN: 0 in the product, and added
+  // to the rows that see its key, and to no other.
+  auto odd_values = [&](int j, uint32_t v_at) __attribute__((always_inline)) {
     uint32_t odd = 0;
 #pragma unroll
     for (int x = 0; x < 4; ++x)
@@ -683,7 +711,6 @@ __global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p
         __builtin_amdgcn_sched_barrier(0);     // (few registers, where speed does not matter)
       }
     if (__any(odd != 0)) {
-      // infinities and NaN among the values (0 in the product): they reach the rows that see their key, and no other
 #pragma unroll 1
       for (int x = 0; x < kTileKeys; ++x) {
         const bool seen = j + x >= see.lo && j + x < see.hi;
@@ -702,7 +729,7 @@ __global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p
   };
   // both products of a phase, for tiles that every row sees whole: each operand is read D MFMAs before its own
   auto products = [&](f32x16_t (&s)[2], uint32_t v_at, uint32_t k_at) __attribute__((always_inline)) {
-    constexpr int NV = 4 * DB, N = NV + 2 * KS, D = 6;
+    constexpr int NV = 4 * DB, N = NV + 2 * KS, D = HD == 64 ? 4 : 6;
     u32x4_t f[D];
     auto load = [&](int n) __attribute__((always_inline)) {
       if (n < NV) {
@@ -740,49 +767,78 @@ __global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p
       copier.template copy<false>(j + kStep, ring_k + (kHalf - at), lane);
       copier.template copy<true>(j, ring_v + at, lane);
     };
-    const auto step_end = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    const auto step_end = [&](int j, uint32_t at) __attribute__((always_inline)) {
+      if (is_edge(j)) {
+        wait_copies<0>();
+        uint32_t odd = 0;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const u32x4_t v = lds_read16(ring_v + at + (wave * NI + i) * 1024 + lane * 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) (void)finite_pair(v[e], odd);
+        }
+        if (odd) odd_tile[at != 0] = j;
+      }
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    const auto is_odd = [&](int j, uint32_t at) { return is_edge(j) && __builtin_amdgcn_readfirstlane(odd_tile[at != 0]) == j; };
     const int start = beg + kw * kTileKeys;
-    const int whole_lo = max(start, lo_last), whole_hi = hi_first;   // tiles between these are seen whole by every row of the wavefront
     // (all wavefronts make the same number of steps)
     const int last = beg + (end - beg + kStep - 1) / kStep * kStep + kw * kTileKeys;
     uint32_t at = 0;
-    step_end();
+    if (threadIdx.x < 2 * KW) odd_s[threadIdx.x >> 1][threadIdx.x & 1] = -1;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     for (int j = start;; j += kStep, at = kHalf - at) {
-      for (; j - kStep >= whole_lo && j + kTileKeys <= whole_hi; j += kStep, at = kHalf - at) {
+      // both products in one run: of tiles that every row of the workgroup sees whole, then of tiles that some see in part
+      for (; j > start && !is_edge(j - kStep) && !is_edge(j); j += kStep, at = kHalf - at) {
         f32x16_t s[2];
         begin(j, at);
         __builtin_amdgcn_s_setprio(1);
         products(s, ring_v + kHalf - at, ring_k + at);
         __builtin_amdgcn_s_setprio(0);
         weights(s, j, std::false_type());
-        step_end();
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      }
+      for (; j > start && j < last && is_edge(j) && is_seen(j - kStep) && is_seen(j) && !is_odd(j - kStep, kHalf - at); j += kStep, at = kHalf - at) {
+        f32x16_t s[2];
+        begin(j, at);
+        products(s, ring_v + kHalf - at, ring_k + at);
+        weights(s, j, std::true_type());
+        step_end(j, at);
       }
       f32x16_t s[2];
       const bool seen = j < last && is_seen(j);
       begin(j, at);
-      if (j > start && is_seen(j - kStep)) values(j - kStep, ring_v + kHalf - at);
+      if (j > start && is_seen(j - kStep)) {
+        if (is_odd(j - kStep, kHalf - at)) odd_values(j - kStep, ring_v + kHalf - at);
+        else values(ring_v + kHalf - at);
+      }
       if (seen) {
         scores(s, ring_k + at);
         weights(s, j, std::true_type());
       }
-      step_end();
+      step_end(j, at);
       if (j >= last) break;
     }
   }
-  l += __shfl_xor(l, 32);
+  const f32x2_t both = with_half(l);
+  l = both[0] + both[1];
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));        // (the lane's row, token and head are found again here, for fewer registers in the loop)
+  const int end_row = tid & 31, end_half = (tid >> 5) & 1;
   if (KW > 1) {
     // the second group's sums, through LDS, into the first's
     constexpr int kPitch = HD + 4;
-    float *other = reinterpret_cast<float *>(lds) + (wave * 32 + l32) * kPitch;
-    float *ml = reinterpret_cast<float *>(lds) + kRows * kPitch + (wave * 32 + l32) * 2;
+    float *other = reinterpret_cast<float *>(lds) + (wave * 32 + end_row) * kPitch;
+    float *ml = reinterpret_cast<float *>(lds) + kRows * kPitch + (wave * 32 + end_row) * 2;
     __syncthreads();
     if (kw == 1) {
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f32x4_t *>(other + d * 32 + g * 8 + half * 4) = f32x4_t{o[d][g * 4], o[d][g * 4 + 1], o[d][g * 4 + 2], o[d][g * 4 + 3]};
-      if (half == 0) {
+          *reinterpret_cast<f32x4_t *>(other + d * 32 + g * 8 + end_half * 4) = f32x4_t{o[d][g * 4], o[d][g * 4 + 1], o[d][g * 4 + 2], o[d][g * 4 + 3]};
+      if (end_half == 0) {
         ml[0] = m;
         ml[1] = l;
       }
@@ -796,14 +852,14 @@ __global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(other + d * 32 + g * 8 + half * 4);
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(other + d * 32 + g * 8 + end_half * 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[d][g * 4 + i] = fmaf(o[d][g * 4 + i], a, x[i] * b);
       }
   }
   if (n_pieces == 1) {
-    if (row0 + l32 >= n_rows) return;
-    asm volatile("" : "+v"(row));      // (its token and head are found again here: four registers less in the loop)
+    if (row0 + end_row >= n_rows) return;
+    const int row = row0 + end_row;
     const int head = it.kvh * p.group + row % p.group;
     const int64_t t = it.seq.t0 + row / p.group;
     const float inv = l == 0.f ? 0.f : 1.0f / l;
@@ -812,19 +868,19 @@ __global__ __launch_bounds__(RW * KW * 64) void ff_attn_tile_kernel(AttnParams p
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<u32x2_t *>(dst + d * 32 + g * 8 + half * 4) =
+        *reinterpret_cast<u32x2_t *>(dst + d * 32 + g * 8 + end_half * 4) =
             u32x2_t{pack_bf16x2(o[d][g * 4] * inv, o[d][g * 4 + 1] * inv), pack_bf16x2(o[d][g * 4 + 2] * inv, o[d][g * 4 + 3] * inv)};
-    if (half == 0 && p.lse) p.lse[t * p.n_heads + head] = lse_of(m, l);
+    if (end_half == 0 && p.lse) p.lse[t * p.n_heads + head] = lse_of(m, l);
   } else {
     float *part = part_of<HD>(pl, it.first + it.piece * it.n_tiles + it.n_tiles - 1 - it.tile, it.kvh, p.n_kv);
-    const int r = wave * 32 + l32;
-    float *mine = part + wave * 32 * HD + lane * 4;
+    const int r = wave * 32 + end_row;
+    float *mine = part + wave * 32 * HD + (end_half * 32 + end_row) * 4;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *reinterpret_cast<f32x4_t *>(mine + (d * 4 + g) * 256) = f32x4_t{o[d][g * 4], o[d][g * 4 + 1], o[d][g * 4 + 2], o[d][g * 4 + 3]};
-    if (half == 0) *reinterpret_cast<f32x2_t *>(part + kRows * HD + r * 2) = f32x2_t{m, l};
+    if (end_half == 0) *reinterpret_cast<f32x2_t *>(part + kRows * HD + r * 2) = f32x2_t{m, l};
   }
 }
 
@@ -873,11 +929,11 @@ __global__ __launch_bounds__(256) void ff_attn_join_kernel(AttnParams p, AttnPla
     for (int e = 0; e < 4; ++e) acc[e] *= f0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      if (k0 + k >= n) break;
+      const bool is = k0 + k < n;                     // (not by a factor of 0: the sums may be infinite)
       const float f = __builtin_amdgcn_exp2f(w[k][0] - top);
-      sum = fmaf(w[k][1], f, sum);
+      sum = is ? fmaf(w[k][1], f, sum) : sum;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[k][e], f, acc[e]);
+      for (int e = 0; e < 4; ++e) acc[e] = is ? fmaf(v[k][e], f, acc[e]) : acc[e];
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
@@ -952,10 +1008,14 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
     pl.part_at = c.bytes / sizeof(float);
     if (pl.target > 0) c.bytes += (size_t)pl.max_items * tile_rows * (head_dim + 2) * sizeof(float);
   };
+  // One token's keys go to a piece for every CU, and no more: its pieces are joined by one workgroup.  Many tokens' are cut finer, for
+  // their lengths differ.  (4096 keys of 128 channels and more a piece, us with 256 / 512 / 1024 pieces: 8 key heads, one token over
+  // 8191 keys 15.9 / 15.9 / 15.8, over 32768 28.5 / 31.7 / 41.0; 48 tokens over up to 16384 137 / 97 / 94.)
+  const auto few_target = [&](long tiles) { return tiles * n_kv < 128 ? kFewGrid / 2 : 2 * kFewGrid; };
   // (the rows' own tiles and a part-filled one for each sequence)
   if (paged && chunk_rows <= 32) {
     c.nb = chunk_rows <= 16 ? 1 : 2;
-    set(c.few, 16 * c.nb, rows / (16 * c.nb) + seqs, 0, kAll, 2 * kFewGrid, 2);
+    set(c.few, 16 * c.nb, rows / (16 * c.nb) + seqs, 0, kAll, few_target(rows / (16 * c.nb) + seqs), 4);
     return c;
   }
   const bool both = paged && n_seqs > 1 && group <= 16;     // sequences that generate one token beside chunks
@@ -966,10 +1026,10 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
   // A piece for every CU, two where the rows alone give those: then only sequences longer than the others are split.  Rows enough for
   // every CU many times over are not: whole rows need no second pass.
   const long items = rows / tile_rows * n_kv;
-  set(c.tile, tile_rows, c.tiles, both ? 16 : 0, kAll, !paged || items >= 2048 ? 0 : (items < 256 ? 256 : 512), 4);
+  set(c.tile, tile_rows, c.tiles, both ? 16 : 0, kAll, !paged || items >= 2048 ? 0 : (items < 256 && head_dim == 128 ? 256 : 512), 4);
   if (both) {
     c.nb = 1;
-    set(c.few, 16, seqs, 0, 16, 2 * kFewGrid, 2);
+    set(c.few, 16, seqs, 0, 16, few_target(seqs), 4);
   }
   return c;
 }
