@@ -481,6 +481,7 @@ AttnParams attn_params(const ff_attention &a, int32_t n_tokens, int32_t n_seqs) 
   AttnParams p = {};
   p.T = n_tokens; p.n_seqs = n_seqs;
   p.n_heads = a.n_heads; p.n_kv = a.n_kv_heads; p.group = a.n_heads / a.n_kv_heads;
+  p.by_group = fast_div(p.group); p.by_kv = fast_div(p.n_kv);
   p.causal = a.causal != 0; p.window = a.window;
   p.scale_log2 = a.scale * 1.4426950408889634f;
   return p;

@@ -153,7 +153,7 @@ __device__ __forceinline__ Item find_seq(const AttnParams &p, const AttnPlan &pl
 // Item number -> what to compute.  Key heads go innermost (workgroups id mod 8 share an XCD, so its L2 keeps one head's keys where
 // there are eight), then the tiles of one piece, the last first: under a causal mask those have the most keys.
 __device__ __forceinline__ Item work_of(const AttnParams &p, const AttnPlan &pl, const Cut &cut, int id) {
-  const int x = id / p.n_kv;
+  const int x = p.by_kv(id);
   Item it = find_seq<false>(p, pl, cut.keys, cut.first, x);
   const int local = x - it.first;
   it.kvh = id - x * p.n_kv;
@@ -171,6 +171,17 @@ __device__ __forceinline__ int items_of(const AttnParams &p, const AttnPlan &pl,
 template <int HD>
 __device__ __forceinline__ float *part_of(const AttnPlan &pl, int x, int kvh, int n_kv) {
   return pl.part + ((size_t)x * n_kv + kvh) * ((size_t)pl.tile_rows * (HD + 2));
+}
+
+// the token and the head that row r of a sequence is
+__device__ __forceinline__ int64_t row_token(const AttnParams &p, const Seq &q, int r) { return q.t0 + p.by_group(r); }
+__device__ __forceinline__ int row_head(const AttnParams &p, int kvh, int r) { return kvh * p.group + r - p.by_group(r) * p.group; }
+
+// the lane's number, found again where it is asked for: none of the registers of the loops before holds it
+__device__ __forceinline__ int fresh_lane() {
+  int none = 0;
+  asm volatile("" : "+v"(none));
+  return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
 }
 
 // where keys lie
@@ -217,6 +228,12 @@ struct Copier {
       k_off[i] = (uint32_t)(key - (first + i) * KPI) * ks.k_pitch + chunk * 16;
       v_off[i] = PAGED ? k_off[i] : (uint32_t)(key - (first + i) * KPI) * ks.v_pitch + chunk * 16;
     }
+  }
+  // where a key's value lies (a wave-uniform key below `end`)
+  __device__ __forceinline__ const bf16_t *value(int key) const {
+    if (!PAGED) return reinterpret_cast<const bf16_t *>(reinterpret_cast<const uint8_t *>(ks.v) + (uint64_t)(uint32_t)key * ks.v_pitch);
+    const int page = ks.table[key >> ks.shift];
+    return ks.v + (size_t)((unsigned)page < (unsigned)ks.n_pages ? page : 0) * ks.page_elems + (key & ((1 << ks.shift) - 1)) * HD;
   }
   // the tile that starts at key j, a multiple of 32; keys from `end` on are replaced by the last one
   template <bool VALUES>
@@ -271,12 +288,11 @@ __device__ __forceinline__ f32x2_t with_row(float v) {
 __device__ __forceinline__ float larger(const f32x2_t &v) { return fmaxf(v[0], v[1]); }
 // infinities and NaN of a pair of bf16 values set to 0; `any` collects whether there were some
 __device__ __forceinline__ uint32_t finite_pair(uint32_t w, uint32_t &any) {
-  const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-  any |= lo | hi;
-  return w & ~(lo | hi);
+  const uint32_t n = ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;     // an exponent of all ones carries into its half's top bit
+  any |= n;
+  return w & ~((n - (n >> 15)) | n);
 }
-__device__ __forceinline__ void lds_bf16x4(uint32_t addr, float (&v)[4]) {
-  const u32x2_t w = *reinterpret_cast<const __attribute__((address_space(3))) u32x2_t *>(addr);
+__device__ __forceinline__ void bf16x4(const u32x2_t &w, float (&v)[4]) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     v[2 * i] = __uint_as_float(w[i] << 16);
@@ -345,7 +361,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
       see[b].hi = min(see[b].hi, end);
       all_lo = max(all_lo, see[b].lo);
       all_hi = min(all_hi, see[b].hi);
-      const bf16_t *src = p.q + (int64_t)(it.seq.t0 + r / p.group) * p.q_stride + (it.kvh * p.group + r % p.group) * HD + quad * 8;
+      const bf16_t *src = p.q + row_token(p, it.seq, r) * p.q_stride + row_head(p, it.kvh, r) * HD + quad * 8;
 #pragma unroll
       for (int s = 0; s < KS; ++s) q[b][s] = *reinterpret_cast<const u32x4_t *>(src + s * 32);
     }
@@ -453,7 +469,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
               float v[4];
-              lds_bf16x4(v_at + chunk_at<HD>(x, d * 2 + (quad >> 1)) + (quad & 1) * 8, v);
+              const u32x2_t w = *reinterpret_cast<const __attribute__((address_space(3))) u32x2_t *>(v_at + chunk_at<HD>(x, d * 2 + (quad >> 1)) + (quad & 1) * 8);
+              bf16x4(w, v);
 #pragma unroll
               for (int b = 0; b < NB; ++b)
                 if (j + x >= see[b].lo && j + x < see[b].hi)
@@ -493,8 +510,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
     const int x0 = it.first + it.n_tiles - 1 - it.tile;
     const auto out = [&](int r, int c, float a, float b, float top, float sum) __attribute__((always_inline)) {
       const int row = row0 + r;
-      const int64_t t = it.seq.t0 + row / p.group;
-      const int head = it.kvh * p.group + row % p.group;
+      const int64_t t = row_token(p, it.seq, row);
+      const int head = row_head(p, it.kvh, row);
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
       *reinterpret_cast<uint32_t *>(p.o + t * p.o_stride + head * HD + c) = pack_bf16x2(a * inv, b * inv);
       if (c == 0 && p.lse) p.lse[t * p.n_heads + head] = lse_of(top, sum);
@@ -600,14 +617,14 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
   const uint32_t ring_k = lds_addr_of(lds) + kw * 4 * kHalf, ring_v = ring_k + 2 * kHalf;
 
   // (out before the rows' own arithmetic and loads)
-  if (beg < end) copier.template copy<false>(beg + kw * kTileKeys, ring_k, lane);
+  if (beg + kw * kTileKeys < end) copier.template copy<false>(beg + kw * kTileKeys, ring_k, lane);
   Range see;
   u32x4_t q[KS];
   {
     const int row = min(row0 + l32, n_rows - 1);
     see = row_range(p, it.seq, row);
     see.hi = min(see.hi, end);
-    const bf16_t *src = p.q + (int64_t)(it.seq.t0 + row / p.group) * p.q_stride + (it.kvh * p.group + row % p.group) * HD + half * 8;
+    const bf16_t *src = p.q + row_token(p, it.seq, row) * p.q_stride + row_head(p, it.kvh, row) * HD + half * 8;
 #pragma unroll
     for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const u32x4_t *>(src + s * 16);
 #pragma unroll
@@ -625,33 +642,19 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-  // Tiles that not all rows of the workgroup see whole: their values are looked through for infinities and NaN when they have landed,
-  // by the wavefront that copied them, which leaves the tile's key in the stage's flag if there are any.
+  // Tiles that not all rows of the workgroup see whole: their values are looked through for infinities and NaN when they have landed, by
+  // the wavefront that copied them, which puts 0 in their place and leaves the tile's key in the stage's flag if there are any.
   const int edge_lo = row_range(p, it.seq, min((it.tile + 1) * kRows, n_rows) - 1).lo, edge_hi = min(row_range(p, it.seq, it.tile * kRows).hi, end);
   const auto is_edge = [&](int j) { return j < edge_lo || j + kTileKeys > edge_hi; };
   volatile int *const odd_tile = odd_s[kw];
 
-  // where this lane's operands lie in a tile: chunk c of the key that is its row of K, and 8 bytes of each of two keys for V^T, from
-  // which the other keys' are 32 and 16 keys further (the swizzle repeats after 16)
-  uint32_t k_off[KS], v_off[DB][2];
+  // Where this lane's operands lie in a tile: chunk 0 of the key that is its row of K, and 8 bytes of each of two keys for V^T.  Chunk c
+  // is 16 c away by exclusive or (the swizzle is one), the other keys' operands are 32 and 16 keys further (it repeats after 16).
+  const uint32_t k_off = chunk_at<HD>(l32, half);
+  uint32_t v_off[2];
 #pragma unroll
-  for (int c = 0; c < KS; ++c) k_off[c] = chunk_at<HD>(l32, c * 2 + half);
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-      v_off[d][r] = chunk_at<HD>(half * 4 + (l16 >> 2) + 8 * r, d * 4 + (grp & 1) * 2 + ((l16 & 3) >> 1)) + (l16 & 1) * 8;
+  for (int r = 0; r < 2; ++r) v_off[r] = chunk_at<HD>(half * 4 + (l16 >> 2) + 8 * r, (grp & 1) * 2 + ((l16 & 3) >> 1)) + (l16 & 1) * 8;
 
-  // Q K of the tile in LDS at `k_at`
-  auto scores = [&](f32x16_t (&s)[2], uint32_t k_at) __attribute__((always_inline)) {
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
-#pragma unroll
-      for (int c = 0; c < KS; ++c) s[kb] = mfma32(lds_read16(k_at + k_off[c] + kb * 32 * HD * 2), q[c], s[kb]);
-    }
-  };
   // scores of the tile at key j -> weights, in the rows' running maximum's scale
   auto weights = [&](f32x16_t (&s)[2], int j, auto masked) __attribute__((always_inline)) {
     if (masked) {
@@ -684,60 +687,38 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
       pk[x] = u32x4_t{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
     }
   };
-  // P V of the tile whose values are in LDS at `v_at`
-  auto values = [&](uint32_t v_at) __attribute__((always_inline)) {
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        const u32x2_t v0 = lds_read_tr(v_at + v_off[d][0] + x * 16 * HD * 2), v1 = lds_read_tr(v_at + v_off[d][1] + x * 16 * HD * 2);
-        o[d] = mfma32(u32x4_t{v0[0], v0[1], v1[0], v1[1]}, pk[x], o[d]);
-      }
-  };
-  // The same for the tile at key j, where some value that a row may not see is an infinity or NaN: 0 in the product, and added
-  // to the rows that see its key, and to no other.
-  auto odd_values = [&](int j, uint32_t v_at) __attribute__((always_inline)) {
-    uint32_t odd = 0;
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        const u32x2_t v0 = lds_read_tr(v_at + v_off[d][0] + x * 16 * HD * 2);
-        const u32x2_t v1 = lds_read_tr(v_at + v_off[d][1] + x * 16 * HD * 2);
-        u32x4_t vf = {v0[0], v0[1], v1[0], v1[1]};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) vf[e] = finite_pair(vf[e], odd);
-        o[d] = mfma32(vf, pk[x], o[d]);
-        __builtin_amdgcn_sched_barrier(0);     // (few registers, where speed does not matter)
-      }
-    if (__any(odd != 0)) {
+  // The infinities and NaN among the values of the tile at key j, which are 0 in LDS: they reach the rows that see their key, and no other.
+  auto add_odd = [&](int j) __attribute__((always_inline)) {
+    const int far = fresh_lane() >> 5;
 #pragma unroll 1
-      for (int x = 0; x < kTileKeys; ++x) {
-        const bool seen = j + x >= see.lo && j + x < see.hi;
+    for (int key = j; key < min(j + kTileKeys, end); ++key) {
+      const bf16_t *src = copier.value(key) + far * 4;
+      const bool seen = key >= see.lo && key < see.hi;
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+      for (int d = 0; d < DB; ++d)
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            float v[4];
-            lds_bf16x4(v_at + chunk_at<HD>(x, d * 4 + g) + half * 8, v);
+        for (int g = 0; g < 4; ++g) {
+          float v[4];
+          bf16x4(*reinterpret_cast<const u32x2_t *>(src + d * 32 + g * 8), v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (seen && !(fabsf(v[i]) < INFINITY)) o[d][g * 4 + i] += v[i];
-          }
-      }
+          for (int i = 0; i < 4; ++i)
+            if (seen && !(fabsf(v[i]) < INFINITY)) o[d][g * 4 + i] += v[i];
+          __builtin_amdgcn_sched_barrier(0);       // (a few registers at a time)
+        }
     }
   };
-  // both products of a phase, for tiles that every row sees whole: each operand is read D MFMAs before its own
-  auto products = [&](f32x16_t (&s)[2], uint32_t v_at, uint32_t k_at) __attribute__((always_inline)) {
-    constexpr int NV = 4 * DB, N = NV + 2 * KS, D = HD == 64 ? 4 : 6;
+  // P V of the tile whose values are in LDS at `v_at` and Q K of the one whose keys are at `k_at`, or either, in one run: each operand
+  // is read D MFMAs before its own
+  auto products = [&](f32x16_t (&s)[2], uint32_t v_at, uint32_t k_at, auto with_v, auto with_k) __attribute__((always_inline)) {
+    constexpr int NV = with_v ? 4 * DB : 0, N = NV + (with_k ? 2 * KS : 0), D = HD == 64 ? (with_v && with_k ? 4 : 2) : 6;
     u32x4_t f[D];
     auto load = [&](int n) __attribute__((always_inline)) {
       if (n < NV) {
-        const u32x2_t v0 = lds_read_tr(v_at + v_off[n % DB][0] + (n / DB) * 16 * HD * 2);
-        const u32x2_t v1 = lds_read_tr(v_at + v_off[n % DB][1] + (n / DB) * 16 * HD * 2);
+        const u32x2_t v0 = lds_read_tr(((v_at + v_off[0]) ^ (n % DB * 64)) + (n / DB) * 16 * HD * 2);
+        const u32x2_t v1 = lds_read_tr(((v_at + v_off[1]) ^ (n % DB * 64)) + (n / DB) * 16 * HD * 2);
         f[n % D] = u32x4_t{v0[0], v0[1], v1[0], v1[1]};
       } else {
-        f[n % D] = lds_read16(k_at + k_off[(n - NV) / 2] + (n - NV) % 2 * 32 * HD * 2);
+        f[n % D] = lds_read16(((k_at + k_off) ^ ((n - NV) / 2 * 32)) + (n - NV) % 2 * 32 * HD * 2);
       }
     };
 #pragma unroll
@@ -762,22 +743,27 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
 
   if (beg < end) {
     // Step i: K of tile i is in stage i % 2, V of tile i - 1 in the other.  The copies that go out at its start fill the stages that
-    // step i - 1 read, and have landed when it ends.  (Copies past the end bring the last key again.)
+    // step i - 1 read, and have landed when it ends.  (Past the end there are none, but a tile that ends behind it is copied whole:
+    // the last key again.)
     const auto begin = [&](int j, uint32_t at) __attribute__((always_inline)) {
-      copier.template copy<false>(j + kStep, ring_k + (kHalf - at), lane);
-      copier.template copy<true>(j, ring_v + at, lane);
+      if (j + kStep < end) copier.template copy<false>(j + kStep, ring_k + (kHalf - at), lane);
+      if (j < end) copier.template copy<true>(j, ring_v + at, lane);
     };
     const auto step_end = [&](int j, uint32_t at) __attribute__((always_inline)) {
-      if (is_edge(j)) {
+      if (is_edge(j) && j < end) {
         wait_copies<0>();
-        uint32_t odd = 0;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          const u32x4_t v = lds_read16(ring_v + at + (wave * NI + i) * 1024 + lane * 16);
+          const uint32_t mine = ring_v + at + (wave * NI + i) * 1024 + lane * 16;
+          u32x4_t v = lds_read16(mine);
+          uint32_t odd = 0;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) (void)finite_pair(v[e], odd);
+          for (int e = 0; e < 4; ++e) v[e] = finite_pair(v[e], odd);
+          if (odd) {
+            *reinterpret_cast<__attribute__((address_space(3))) u32x4_t *>(mine) = v;
+            odd_tile[at != 0] = j;
+          }
         }
-        if (odd) odd_tile[at != 0] = j;
       }
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
@@ -788,21 +774,24 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
     uint32_t at = 0;
     if (threadIdx.x < 2 * KW) odd_s[threadIdx.x >> 1][threadIdx.x & 1] = -1;
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const auto is_inner = [&](int j) { return j > start && !is_edge(j - kStep) && !is_edge(j) && j + kStep < end; };
     for (int j = start;; j += kStep, at = kHalf - at) {
       // both products in one run: of tiles that every row of the workgroup sees whole, then of tiles that some see in part
-      for (; j > start && !is_edge(j - kStep) && !is_edge(j); j += kStep, at = kHalf - at) {
+      for (; is_inner(j); j += kStep, at = kHalf - at) {
         f32x16_t s[2];
-        begin(j, at);
+        copier.template copy<false>(j + kStep, ring_k + (kHalf - at), lane);
+        copier.template copy<true>(j, ring_v + at, lane);
         __builtin_amdgcn_s_setprio(1);
-        products(s, ring_v + kHalf - at, ring_k + at);
+        products(s, ring_v + kHalf - at, ring_k + at, std::true_type(), std::true_type());
         __builtin_amdgcn_s_setprio(0);
         weights(s, j, std::false_type());
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       }
-      for (; j > start && j < last && is_edge(j) && is_seen(j - kStep) && is_seen(j) && !is_odd(j - kStep, kHalf - at); j += kStep, at = kHalf - at) {
+      for (; j > start && j < last && !is_inner(j) && is_seen(j - kStep) && is_seen(j); j += kStep, at = kHalf - at) {
         f32x16_t s[2];
         begin(j, at);
-        products(s, ring_v + kHalf - at, ring_k + at);
+        products(s, ring_v + kHalf - at, ring_k + at, std::true_type(), std::true_type());
+        if (is_odd(j - kStep, kHalf - at)) add_odd(j - kStep);
         weights(s, j, std::true_type());
         step_end(j, at);
       }
@@ -810,11 +799,11 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
       const bool seen = j < last && is_seen(j);
       begin(j, at);
       if (j > start && is_seen(j - kStep)) {
-        if (is_odd(j - kStep, kHalf - at)) odd_values(j - kStep, ring_v + kHalf - at);
-        else values(ring_v + kHalf - at);
+        products(s, ring_v + kHalf - at, 0, std::true_type(), std::false_type());
+        if (is_odd(j - kStep, kHalf - at)) add_odd(j - kStep);
       }
       if (seen) {
-        scores(s, ring_k + at);
+        products(s, 0, ring_k + at, std::false_type(), std::true_type());
         weights(s, j, std::true_type());
       }
       step_end(j, at);
@@ -823,9 +812,7 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
   }
   const f32x2_t both = with_half(l);
   l = both[0] + both[1];
-  int tid = threadIdx.x;
-  asm volatile("" : "+v"(tid));        // (the lane's row, token and head are found again here, for fewer registers in the loop)
-  const int end_row = tid & 31, end_half = (tid >> 5) & 1;
+  const int end_lane = fresh_lane(), end_row = end_lane & 31, end_half = end_lane >> 5;
   if (KW > 1) {
     // the second group's sums, through LDS, into the first's
     constexpr int kPitch = HD + 4;
@@ -860,21 +847,30 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
   if (n_pieces == 1) {
     if (row0 + end_row >= n_rows) return;
     const int row = row0 + end_row;
-    const int head = it.kvh * p.group + row % p.group;
-    const int64_t t = it.seq.t0 + row / p.group;
+    const int head = row_head(p, it.kvh, row);
+    const int64_t t = row_token(p, it.seq, row);
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     bf16_t *dst = p.o + t * p.o_stride + head * HD;
+    // (a lane has four channels of each eight and the lane 32 further the others: they trade, for 16 bytes of one eight each)
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<u32x2_t *>(dst + d * 32 + g * 8 + end_half * 4) =
-            u32x2_t{pack_bf16x2(o[d][g * 4] * inv, o[d][g * 4 + 1] * inv), pack_bf16x2(o[d][g * 4 + 2] * inv, o[d][g * 4 + 3] * inv)};
+      for (int g = 0; g < 4; g += 2) {
+        u32x4_t v;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const auto r = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[d][g * 4 + 2 * i] * inv, o[d][g * 4 + 2 * i + 1] * inv),
+                                                          pack_bf16x2(o[d][g * 4 + 4 + 2 * i] * inv, o[d][g * 4 + 5 + 2 * i] * inv), false, false);
+          v[i] = r[0];
+          v[2 + i] = r[1];
+        }
+        *reinterpret_cast<u32x4_t *>(dst + d * 32 + (g + end_half) * 8) = v;
+      }
     if (end_half == 0 && p.lse) p.lse[t * p.n_heads + head] = lse_of(m, l);
   } else {
     float *part = part_of<HD>(pl, it.first + it.piece * it.n_tiles + it.n_tiles - 1 - it.tile, it.kvh, p.n_kv);
     const int r = wave * 32 + end_row;
-    float *mine = part + wave * 32 * HD + (end_half * 32 + end_row) * 4;
+    float *mine = part + wave * 32 * HD + end_lane * 4;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -892,7 +888,7 @@ __global__ __launch_bounds__(256) void ff_attn_join_kernel(AttnParams p, AttnPla
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int runs = pl.tile_rows / 32 * (HD / 8);                // of 1 KB in a tile
   const int id = (int)blockIdx.x * 4 / runs, run = (int)blockIdx.x * 4 % runs + wave;
-  const int x = id / p.n_kv, kvh = id - x * p.n_kv;
+  const int x = p.by_kv(id), kvh = id - x * p.n_kv;
   // (tiles are counted as they would be without pieces)
   const Item whole = find_seq<false>(p, pl, kUnsplit, cut.first, x);
   if (whole.n_tiles == 0) return;
@@ -937,8 +933,8 @@ __global__ __launch_bounds__(256) void ff_attn_join_kernel(AttnParams p, AttnPla
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  const int64_t t = it.seq.t0 + row / p.group;
-  const int head = kvh * p.group + row % p.group;
+  const int64_t t = row_token(p, it.seq, row);
+  const int head = row_head(p, kvh, row);
   *reinterpret_cast<u32x2_t *>(p.o + t * p.o_stride + head * HD + c) =
       u32x2_t{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
   if (c == 0 && p.lse) p.lse[t * p.n_heads + head] = lse_of(top, sum);
@@ -1019,8 +1015,10 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
     return c;
   }
   const bool both = paged && n_seqs > 1 && group <= 16;     // sequences that generate one token beside chunks
-  // 256 rows where those fill the CUs
-  c.rw = rows / 256 * n_kv >= 256 ? 8 : 4;
+  // 256 rows where those give every CU more than one tile, 128 rows and two groups of keys below: half as many steps for the longest
+  // tile.  (One causal prompt, 8 key heads of 128 / 64, us with 128 and 256 rows: 1024 tokens 28 and 39 / 20 and 28, 2048 57 and 66 /
+  // 37 and 47, 4096 174 and 150 / 112 and 100; 13 packed prompts of 4099 tokens in all, heads of 64, 40 and 33.)
+  c.rw = rows / 256 * n_kv > 384 ? 8 : 4;
   const int tile_rows = 32 * c.rw;
   c.tiles = rows / tile_rows + seqs;
   // A piece for every CU, two where the rows alone give those: then only sequences longer than the others are split.  Rows enough for

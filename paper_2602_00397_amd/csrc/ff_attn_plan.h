@@ -9,6 +9,23 @@
 
 constexpr int kTileKeys = 64;        // keys of one step; pieces of a split row are multiples of it
 
+// r / d for 0 <= r < 2^31 and a divisor d up to 2^16 that the host knows: a product instead of a division's forty instructions
+// (mul = floor(2^(31 + s) / d) + 1 with s = ceil(log2 d): its excess over 2^(31 + s) / d times r stays below 2^(31 + s) / d).
+struct FastDiv {
+  uint32_t mul = 0;
+  int32_t shift = -1;      // s - 1; -1: d = 1
+  ATTN_FN int operator()(int r) const { return shift < 0 ? r : (int)((uint32_t)(((uint64_t)(uint32_t)r * mul) >> 32) >> shift); }
+};
+inline FastDiv fast_div(int d) {
+  FastDiv f;
+  int s = 0;
+  while ((1 << s) < d) ++s;
+  if (s == 0) return f;
+  f.mul = (uint32_t)((1ull << (31 + s)) / (unsigned)d + 1);
+  f.shift = s - 1;
+  return f;
+}
+
 struct AttnParams {
   const bf16_t *q, *k, *v;       // k, v: rows of a prompt, or pages
   bf16_t *o;
@@ -18,6 +35,7 @@ struct AttnParams {
   const int32_t *table;          // [n_seqs][table_stride], or nullptr
   int64_t q_stride, k_stride, v_stride, o_stride;
   int32_t T, n_seqs, n_heads, n_kv, group, causal, window;
+  FastDiv by_group, by_kv;
   int32_t table_stride, page_shift, n_pages;
   float scale_log2;              // scale * log2(e)
   // room for pieces of rows split along the keys
@@ -61,7 +79,7 @@ ATTN_FN Seq seq_of(const AttnParams &p, int s) {
 }
 // most keys that one row tile of the sequence needs, counted from a multiple of kTileKeys
 ATTN_FN int span_of(const AttnParams &p, int keys, int tile_rows) {
-  const int more = tile_rows / p.group + 1 + kTileKeys;
+  const int more = p.by_group(tile_rows) + 1 + kTileKeys;
   return p.window > 0 && p.window < keys - more ? p.window + more : keys;
 }
 ATTN_FN int tiles_of(const AttnParams &p, const AttnPlan &pl, int n) {
@@ -90,7 +108,7 @@ ATTN_FN Range tile_range(const AttnParams &p, const Seq &q, int tile, int tile_r
   Range r = {0, q.keys};
   if (p.causal) {
     const int rows = q.n * p.group;
-    const int tok_lo = tile * tile_rows / p.group, tok_hi = (attn_min((tile + 1) * tile_rows, rows) - 1) / p.group;
+    const int tok_lo = p.by_group(tile * tile_rows), tok_hi = p.by_group(attn_min((tile + 1) * tile_rows, rows) - 1);
     r.hi = attn_max(0, q.keys - q.n + tok_hi + 1);
     if (p.window > 0) r.lo = attn_max(0, q.keys - q.n + tok_lo + 1 - attn_min(p.window, kMaxKeys)) & ~(kTileKeys - 1);
   }
@@ -100,7 +118,7 @@ ATTN_FN Range tile_range(const AttnParams &p, const Seq &q, int tile, int tile_r
 ATTN_FN Range row_range(const AttnParams &p, const Seq &q, int r) {
   Range g = {0, q.keys};
   if (p.causal) {
-    g.hi = attn_max(0, q.keys - q.n + r / p.group + 1);
+    g.hi = attn_max(0, q.keys - q.n + p.by_group(r) + 1);
     if (p.window > 0) g.lo = attn_max(0, g.hi - attn_min(p.window, kMaxKeys));
   }
   return g;

@@ -471,6 +471,14 @@ static void check_attention() {
   uint32_t rnd = 12345;
   const auto below = [&](int n) { rnd = rnd * 1664525u + 1013904223u; return (int)((rnd >> 8) % (unsigned)n); };
   static float room[1];
+  for (int d = 1; d <= 65536; d = d < 2048 ? d + 1 : d * 2 - (d & 1)) {
+    const FastDiv f = fast_div(d);
+    ++g_calls;
+    for (int i = 0; i < 200; ++i) {
+      const int q = below(0x7fffffff / d), r[] = {i, q * d, q * d + d - 1, 0x7fffffff - i, 0x7fffffff / d * d - (i == 0), below(0x7fffffff)};
+      for (int v : r) CHECK(f(v) == v / d, "%d / %d is not %d", v, d, f(v));
+    }
+  }
   g_attn = true;
   for (int round = 0; round < 6000; ++round) {
     static const int groups[] = {1, 3, 4, 7, 8, 20};
@@ -500,6 +508,7 @@ static void check_attention() {
     p.lens = paged ? lens.data() : nullptr;
     p.table = paged ? starts.data() : nullptr;         // (never read: there is one)
     p.n_seqs = n_seqs; p.n_kv = n_kv; p.group = group; p.n_heads = n_kv * group; p.n_pages = 10;
+    p.by_group = fast_div(group); p.by_kv = fast_div(n_kv);
     p.causal = below(5) != 0;
     p.window = p.causal && below(3) == 0 ? (below(4) ? 1 + below(1000) : 2147483647) : 0;
     p.part = room;
