@@ -309,7 +309,8 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 // HBM-bound: every key is read once for at most 16 NB rows.  Four wavefronts, each with keys of its own (32 at a time, every
 // fourth 32 of the piece), its own 32 keys of LDS and its own softmax state, without barriers until they join at the end: K of the
 // next keys is on its way while V of these is waited for, and the other way round.  Workgroups take pieces in turn, two of them
-// on a CU, so one streams while the other starts or joins.  The last piece of a tile to end joins all of them, in order.
+// on a CU, so one streams while the other starts or joins.  The last piece of a tile to end joins all of them, in order, if the rows
+// are few (pl.join_here), else another launch does.
 constexpr int kFewWaves = 4, kFewGrid = 512;
 
 // The sums of a piece go past this XCD's L2 (relaxed atomics of device scope: a release fence would write back all of it).
@@ -540,7 +541,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
         if (c == 0) part_store(part + kRows * HD + r * 2, top, sum);
       }
     }
-    if (!whole) {
+    if (!whole && pl.join_here) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // this wavefront's sums have arrived
       __syncthreads();
       int *counter = p.counters + x0 * p.n_kv + it.kvh;
@@ -710,7 +711,7 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
   // P V of the tile whose values are in LDS at `v_at` and Q K of the one whose keys are at `k_at`, or either, in one run: each operand
   // is read D MFMAs before its own
   auto products = [&](f32x16_t (&s)[2], uint32_t v_at, uint32_t k_at, auto with_v, auto with_k) __attribute__((always_inline)) {
-    constexpr int NV = with_v ? 4 * DB : 0, N = NV + (with_k ? 2 * KS : 0), D = HD == 64 ? (with_v && with_k ? 4 : 2) : 6;
+    constexpr int NV = with_v ? 4 * DB : 0, N = NV + (with_k ? 2 * KS : 0), D = 4;
     u32x4_t f[D];
     auto load = [&](int n) __attribute__((always_inline)) {
       if (n < NV) {
@@ -881,39 +882,42 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
 }
 
 // ---- rows split along the keys: their pieces joined, in order ------------------------------------------------------------
-// One wavefront to 1 KB of every piece: 32 rows, eight channels.
+// The split tile with number x, counted as tiles would be without pieces: which it is, how many pieces it has (1: nothing to join) and
+// where the first one's sums lie.
+struct Split { Seq seq; int tile, n; size_t step; const float *src; };
 template <int HD>
-__global__ __launch_bounds__(256) void ff_attn_join_kernel(AttnParams p, AttnPlan pl) {
+__device__ __forceinline__ Split find_split(const AttnParams &p, const AttnPlan &pl, int x, int kvh) {
+  Split r = {};
   const Cut cut = cut_of(p, pl);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int runs = pl.tile_rows / 32 * (HD / 8);                // of 1 KB in a tile
-  const int id = (int)blockIdx.x * 4 / runs, run = (int)blockIdx.x * 4 % runs + wave;
-  const int x = p.by_kv(id), kvh = id - x * p.n_kv;
-  // (tiles are counted as they would be without pieces)
   const Item whole = find_seq<false>(p, pl, kUnsplit, cut.first, x);
-  if (whole.n_tiles == 0) return;
-  const int tile = x - whole.first;
-  const int n = pieces_of(tile_range(p, whole.seq, tile, pl.tile_rows), cut.keys);
-  if (n <= 1) return;
+  if (whole.n_tiles == 0) return r;
+  r.seq = whole.seq;
+  r.tile = x - whole.first;
+  r.n = pieces_of(tile_range(p, whole.seq, r.tile, pl.tile_rows), cut.keys);
   const Item it = find_seq<true>(p, pl, cut.keys, cut.first, whole.s);
-  const int x0 = it.first + it.n_tiles - 1 - tile;
+  const int x0 = it.first + it.n_tiles - 1 - r.tile;
   // (chunks that overlap may have more pieces than there were workgroups and room for)
-  if (((long)x0 + (long)(n - 1) * it.n_tiles + 1) * p.n_kv > pl.max_items) return;
-  const int r = run / (HD / 8) * 32 + (lane & 31), c = run % (HD / 8) * 8 + (lane >> 5) * 4;
-  const int row = tile * pl.tile_rows + r;
-  if (row >= it.seq.n * p.group) return;
-  const size_t step = (size_t)it.n_tiles * p.n_kv * ((size_t)pl.tile_rows * (HD + 2));
-  const float *src = part_of<HD>(pl, x0, kvh, p.n_kv);
-  float top = kNoMax, sum = 0.f;
-  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = 0; k0 < n; k0 += 8) {                 // eight pieces' loads on their way at a time
-    f32x4_t v[8];
+  if (((long)x0 + (long)(r.n - 1) * it.n_tiles + 1) * p.n_kv > pl.max_items) r.n = 0;
+  r.step = (size_t)it.n_tiles * p.n_kv * ((size_t)pl.tile_rows * (HD + 2));
+  r.src = part_of<HD>(pl, x0, kvh, p.n_kv);
+  return r;
+}
+// Sums of C channels of row r over its pieces, `at` floats into each; eight pieces' loads on their way at a time
+template <int HD, int C>
+__device__ __forceinline__ void join_pieces(const Split &sp, int tile_rows, int r, int at, float &top, float &sum, float (&acc)[C]) {
+  top = kNoMax;
+  sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < C; ++e) acc[e] = 0.f;
+  for (int k0 = 0; k0 < sp.n; k0 += 8) {
+    float v[8][C];
     f32x2_t w[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float *from = src + (size_t)min(k0 + k, n - 1) * step;
-      w[k] = *reinterpret_cast<const f32x2_t *>(from + pl.tile_rows * HD + r * 2);
-      v[k] = *reinterpret_cast<const f32x4_t *>(from + run * 256 + lane * 4);
+      const float *from = sp.src + (size_t)min(k0 + k, sp.n - 1) * sp.step;
+      w[k] = *reinterpret_cast<const f32x2_t *>(from + tile_rows * HD + r * 2);
+#pragma unroll
+      for (int e = 0; e < C; ++e) v[k][e] = from[at + e];
     }
     float higher = top;
 #pragma unroll
@@ -922,22 +926,57 @@ __global__ __launch_bounds__(256) void ff_attn_join_kernel(AttnParams p, AttnPla
     top = higher;
     sum *= f0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] *= f0;
+    for (int e = 0; e < C; ++e) acc[e] *= f0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const bool is = k0 + k < n;                     // (not by a factor of 0: the sums may be infinite)
+      const bool is = k0 + k < sp.n;                  // (not by a factor of 0: the sums may be infinite)
       const float f = __builtin_amdgcn_exp2f(w[k][0] - top);
       sum = is ? fmaf(w[k][1], f, sum) : sum;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = is ? fmaf(v[k][e], f, acc[e]) : acc[e];
+      for (int e = 0; e < C; ++e) acc[e] = is ? fmaf(v[k][e], f, acc[e]) : acc[e];
     }
   }
+}
+// The tile kernel's: one wavefront to 1 KB of every piece, 32 rows of eight channels.
+template <int HD>
+__global__ __launch_bounds__(256) void ff_attn_join_kernel(AttnParams p, AttnPlan pl) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int runs = pl.tile_rows / 32 * (HD / 8);                // of 1 KB in a tile
+  const int id = (int)blockIdx.x * 4 / runs, run = (int)blockIdx.x * 4 % runs + wave;
+  const int x = p.by_kv(id), kvh = id - x * p.n_kv;
+  const Split sp = find_split<HD>(p, pl, x, kvh);
+  if (sp.n <= 1) return;
+  const int r = run / (HD / 8) * 32 + (lane & 31), c = run % (HD / 8) * 8 + (lane >> 5) * 4;
+  const int row = sp.tile * pl.tile_rows + r;
+  if (row >= sp.seq.n * p.group) return;
+  float top, sum, acc[4];
+  join_pieces<HD, 4>(sp, pl.tile_rows, r, run * 256 + lane * 4, top, sum, acc);
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  const int64_t t = row_token(p, it.seq, row);
+  const int64_t t = row_token(p, sp.seq, row);
   const int head = row_head(p, kvh, row);
   *reinterpret_cast<u32x2_t *>(p.o + t * p.o_stride + head * HD + c) =
       u32x2_t{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
   if (c == 0 && p.lse) p.lse[t * p.n_heads + head] = lse_of(top, sum);
+}
+// The few-row kernel's, where one workgroup would have many rows to join: one wavefront to a row.
+template <int HD>
+__global__ __launch_bounds__(256) void ff_attn_join_rows_kernel(AttnParams p, AttnPlan pl) {
+  constexpr int C = HD / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int id = (int)blockIdx.x * 4 / pl.tile_rows, r = (int)blockIdx.x * 4 % pl.tile_rows + wave;
+  const int x = p.by_kv(id), kvh = id - x * p.n_kv;
+  const Split sp = find_split<HD>(p, pl, x, kvh);
+  const int row = sp.tile * pl.tile_rows + r;
+  if (sp.n <= 1 || row >= sp.seq.n * p.group) return;
+  float top, sum, acc[C];
+  join_pieces<HD, C>(sp, pl.tile_rows, r, r * HD + lane * C, top, sum, acc);
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  const int64_t t = row_token(p, sp.seq, row);
+  const int head = row_head(p, kvh, row);
+  bf16_t *dst = p.o + t * p.o_stride + head * HD + lane * C;
+  if (C == 2) *reinterpret_cast<uint32_t *>(dst) = pack_bf16x2(acc[0] * inv, acc[C - 1] * inv);
+  else *dst = f32_to_bf16(acc[0] * inv);
+  if (lane == 0 && p.lse) p.lse[t * p.n_heads + head] = lse_of(top, sum);
 }
 
 // one wavefront per sequence
@@ -985,7 +1024,7 @@ hipError_t raise_limits() {
 struct Choice {
   AttnPlan few, tile;
   int nb = 0, rw = 0;             // 0: that kernel is not launched
-  long tiles = 0;                 // most tiles of the second kernel
+  long tiles = 0, few_tiles = 0;  // most tiles of each
   size_t bytes = 0;
 };
 Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int max_chunk, bool paged) {
@@ -1008,10 +1047,16 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
   // their lengths differ.  (4096 keys of 128 channels and more a piece, us with 256 / 512 / 1024 pieces: 8 key heads, one token over
   // 8191 keys 15.9 / 15.9 / 15.8, over 32768 28.5 / 31.7 / 41.0; 48 tokens over up to 16384 137 / 97 / 94.)
   const auto few_target = [&](long tiles) { return tiles * n_kv < 128 ? kFewGrid / 2 : 2 * kFewGrid; };
+  // One workgroup joins a tile's pieces where these have few rows in all; a launch more costs 1 to 3 us, and many rows several times
+  // that.  (us joined by the last piece and by a launch: 8 key heads, one token of 4 rows over 8191 keys 15.4 and 16.5, 32768 28.2 and
+  // 31.1; 4 key heads, one token of 7 rows over 16384 keys 24.1 and 20.5, four tokens 56 and 24.)
+  const auto joins_here = [&](long tile_rows, long tiles) { return tile_rows <= 8 && tile_rows * few_target(tiles) <= 256 * tiles * n_kv; };
   // (the rows' own tiles and a part-filled one for each sequence)
   if (paged && chunk_rows <= 32) {
     c.nb = chunk_rows <= 16 ? 1 : 2;
-    set(c.few, 16 * c.nb, rows / (16 * c.nb) + seqs, 0, kAll, few_target(rows / (16 * c.nb) + seqs), 4);
+    c.few_tiles = rows / (16 * c.nb) + seqs;
+    set(c.few, 16 * c.nb, c.few_tiles, 0, kAll, few_target(c.few_tiles), 4);
+    c.few.join_here = joins_here(chunk_rows, c.few_tiles);
     return c;
   }
   const bool both = paged && n_seqs > 1 && group <= 16;     // sequences that generate one token beside chunks
@@ -1027,7 +1072,9 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
   set(c.tile, tile_rows, c.tiles, both ? 16 : 0, kAll, !paged || items >= 2048 ? 0 : (items < 256 && head_dim == 128 ? 256 : 512), 4);
   if (both) {
     c.nb = 1;
+    c.few_tiles = seqs;
     set(c.few, 16, seqs, 0, 16, few_target(seqs), 4);
+    c.few.join_here = joins_here(group, seqs);
   }
   return c;
 }
@@ -1042,6 +1089,8 @@ hipError_t launch(const AttnParams &p, Choice &c, hipStream_t s) {
     const size_t lds = few_lds(HD, c.nb);
     if (c.nb == 1) hipLaunchKernelGGL((ff_attn_few_kernel<HD, 1>), grid, block, lds, s, p, c.few);
     else hipLaunchKernelGGL((ff_attn_few_kernel<HD, 2>), grid, block, lds, s, p, c.few);
+    if (c.few.target > 0 && !c.few.join_here)
+      hipLaunchKernelGGL((ff_attn_join_rows_kernel<HD>), dim3((unsigned)(c.few_tiles * p.n_kv * (c.few.tile_rows / 4))), dim3(256), 0, s, p, c.few);
   }
   if (c.rw) {
     const dim3 grid((unsigned)c.tile.max_items), block(512);

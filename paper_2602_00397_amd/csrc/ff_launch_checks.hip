@@ -519,12 +519,17 @@ static void check_attention() {
     ++g_calls;
     CHECK(ff_launch_attention(p, hd, hint, nullptr) == hipSuccess && !g_log.empty(), "round %d", round);
     std::vector<long> covered(n_seqs, 0);
+    const AttnPlan *before = nullptr;
     for (const Launch &l : g_log) {
       const AttnPlan &pl = l.plan;
-      if (l.threads == 256 && pl.tile_rows >= 128) {                                       // (joins the pieces of the launch before)
-        CHECK(l.grid >= (unsigned)((long)t * group / pl.tile_rows * n_kv), "round %d: %u workgroups join", round, l.grid);
+      if (before && before->tile_rows == pl.tile_rows) {                                   // (joins the pieces of the launch before)
+        long tiles = 0;
+        for (int s = 0; s < n_seqs; ++s) tiles += tiles_of(p, pl, seq_of(p, s).n);
+        CHECK(!valid || (long)l.grid * 4 >= tiles * n_kv * pl.tile_rows / 32, "round %d: %u workgroups join %ld tiles", round, l.grid, tiles);
+        CHECK(!pl.join_here && pl.target > 0, "round %d", round);
         continue;
       }
+      before = &pl;
       // (the few-row kernel's workgroups take items in turn)
       CHECK(l.lds <= kLds && l.grid == (unsigned)(l.threads == 256 ? std::min(pl.max_items, 512) : pl.max_items), "round %d: %u workgroups, %zu bytes", round, l.grid, l.lds);
       CHECK(pl.target == 0 || pl.max_items <= kAttnCounters, "round %d: %d counters", round, pl.max_items);
