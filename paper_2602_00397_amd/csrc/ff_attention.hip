@@ -1066,10 +1066,14 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
   c.rw = rows / 256 * n_kv > 384 ? 8 : 4;
   const int tile_rows = 32 * c.rw;
   c.tiles = rows / tile_rows + seqs;
-  // A piece for every CU, two where the rows alone give those: then only sequences longer than the others are split.  Rows enough for
-  // every CU many times over are not: whole rows need no second pass.
+  // Split into a piece for every CU where whole rows would leave many idle: partial sums written and joined cost some 6 us, and as much
+  // again for twice as many.  With sequences of different lengths the longest may take the launch's whole time, so those are split
+  // up to twice as many items.  (us in 256 pieces and whole, 8 key heads of 128: one chunk of 512 tokens over 8192 keys, 128 items,
+  // 90 and 133; 1024 tokens, 256 items, 157 and 148.  Chunks of up to 500 of 8 heads of 64 with single tokens, 336 items, 76 and 85;
+  // 24 sequences of up to 300 tokens, 590 items, 101 and 84.)
   const long items = rows / tile_rows * n_kv;
-  set(c.tile, tile_rows, c.tiles, both ? 16 : 0, kAll, !paged || items >= 2048 ? 0 : (items < 256 && head_dim == 128 ? 256 : 512), 4);
+  const bool few_items = items < (n_seqs == 1 ? 192 : 384);
+  set(c.tile, tile_rows, c.tiles, both ? 16 : 0, kAll, paged && few_items ? (n_seqs > 1 && head_dim == 64 ? 512 : 256) : 0, 4);
   if (both) {
     c.nb = 1;
     c.few_tiles = seqs;
