@@ -111,7 +111,7 @@ __device__ __forceinline__ Cut cut_of(const AttnParams &p, const AttnPlan &pl) {
   }
   for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
     const Seq q = lane_seq(p, s0, c.first);
-    c.items += tiles_of(p, pl, q.n) * seq_pieces(p, pl, q, c.keys);
+    c.items = (int)min((long)c.items + (long)tiles_of(p, pl, q.n) * seq_pieces(p, pl, q, c.keys), 0x1000000L);
   }
   c.items = __builtin_amdgcn_readlane(lane_sums(c.items), 63);
   return c;
@@ -157,13 +157,15 @@ __device__ __forceinline__ Item work_of(const AttnParams &p, const AttnPlan &pl,
   Item it = find_seq<false>(p, pl, cut.keys, cut.first, x);
   const int local = x - it.first;
   it.kvh = id - x * p.n_kv;
-  if (it.n_tiles == 0) return it;       // (sums beyond 32 bits, of lengths that no valid call has)
+  if (it.n_tiles == 0) return it;       // (no such item)
   it.piece = local / it.n_tiles;
   it.tile = it.n_tiles - 1 - (local - it.piece * it.n_tiles);
   return it;
 }
 __device__ __forceinline__ int items_of(const AttnParams &p, const AttnPlan &pl, const Cut &cut) {
-  return min(cut.items * p.n_kv, pl.max_items);     // (chunks that overlap may have more than there is room for)
+  // (chunks that overlap may have more than there is room for: nothing is computed, and no counter is left behind)
+  const long n = (long)cut.items * p.n_kv;
+  return n <= pl.max_items ? (int)n : 0;
 }
 
 // Partial sums of a piece: tile_rows times HD sums, then tile_rows pairs of maximum and sum.  The few-row kernel's sums lie by rows,
@@ -605,8 +607,9 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
   const int lane = threadIdx.x & 63;
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15, grp = lane >> 4;
   const Cut cut = cut_of(p, pl);
-  if ((int)blockIdx.x >= items_of(p, pl, cut)) return;
-  const Item it = work_of(p, pl, cut, blockIdx.x);
+  const int id = blockIdx.y * gridDim.x + blockIdx.x;
+  if (id >= items_of(p, pl, cut)) return;
+  const Item it = work_of(p, pl, cut, id);
   if (it.n_tiles == 0) return;
   const int kpp = cut.keys;
   const int n_rows = it.seq.n * p.group, row0 = it.tile * kRows + wave * 32;
@@ -1097,7 +1100,9 @@ hipError_t launch(const AttnParams &p, Choice &c, hipStream_t s) {
       hipLaunchKernelGGL((ff_attn_join_rows_kernel<HD>), dim3((unsigned)(c.few_tiles * p.n_kv * (c.few.tile_rows / 4))), dim3(256), 0, s, p, c.few);
   }
   if (c.rw) {
-    const dim3 grid((unsigned)c.tile.max_items), block(512);
+    // (a launch's dimension has 32 bits of threads)
+    const unsigned items = (unsigned)c.tile.max_items, across = std::min(items, 1u << 20);
+    const dim3 grid(across, (items + across - 1) / across), block(512);
     const size_t lds = tile_lds(HD, c.rw, 8 / c.rw);
     if (p.table) {
       if (c.rw == 4) hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 4, 2, true>), grid, block, lds, s, p, c.tile);

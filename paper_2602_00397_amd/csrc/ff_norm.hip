@@ -84,8 +84,8 @@ template <int W, int NCH, bool YF32>
 __global__ __launch_bounds__(256) void ff_norm_kernel(NormParams p) {
   __shared__ float part[4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int t = blockIdx.x * (4 / W) + wave / W;
-  if (t >= p.T) return;                      // (W == 4: the whole workgroup; W == 1: no barriers)
+  const unsigned t = (blockIdx.y * gridDim.x + blockIdx.x) * (4 / W) + wave / W;
+  if (t >= (unsigned)p.T) return;                      // (W == 4: the whole workgroup; W == 1: no barriers)
   const int c0 = ((wave % W) * 64 + lane) * 8;
   const size_t row = (size_t)t * p.d_model;
   uint4 hv[NCH];
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void ff_norm_kernel(NormParams p) {
       }
     }
     if (p.post.kind) apply_norm<W, NCH>(s, p.post, c0, p.d_model, part, wave);
-    const bf16_t *gate = p.gate ? p.gate + (size_t)(t / p.gate_tokens) * p.d_model : nullptr;
+    const bf16_t *gate = p.gate ? p.gate + (size_t)(t / (unsigned)p.gate_tokens) * p.d_model : nullptr;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = c0 + i * W * 512;
@@ -150,7 +150,8 @@ __global__ __launch_bounds__(256) void ff_norm_kernel(NormParams p) {
 
 template <int W, int NCH>
 void launch(const NormParams &p, hipStream_t s) {
-  const dim3 grid((unsigned)((p.T + 4 / W - 1) / (4 / W)));
+  const unsigned groups = ((unsigned)p.T + 4 / W - 1) / (4 / W), across = groups < 1u << 20 ? groups : 1u << 20;
+  const dim3 grid(across, (groups + across - 1) / across);               // (a launch's dimension has 32 bits of threads)
   if (p.y_f32) hipLaunchKernelGGL((ff_norm_kernel<W, NCH, true>), grid, dim3(256), 0, s, p);
   else hipLaunchKernelGGL((ff_norm_kernel<W, NCH, false>), grid, dim3(256), 0, s, p);
 }

@@ -12,7 +12,8 @@ namespace {
 constexpr int kThreads = 256, kBatch = 2;
 __global__ __launch_bounds__(kThreads) void ff_rotary_kernel(RotaryParams p) {
   __shared__ float cs[2][64];
-  const int t = blockIdx.x, pairs = p.rot_dim / 2;
+  const int t = blockIdx.y * gridDim.x + blockIdx.x, pairs = p.rot_dim / 2;
+  if (t >= p.T) return;
   const int64_t slot = p.slots ? p.slots[t] : -1;
   if ((int)threadIdx.x < pairs) {
     const int j = threadIdx.x, axis = (p.axis[j >> 4] >> (2 * (j & 15))) & 3;
@@ -95,6 +96,7 @@ __global__ __launch_bounds__(kThreads) void ff_rotary_kernel(RotaryParams p) {
 }  // namespace
 
 hipError_t ff_launch_rotary(const RotaryParams &p, hipStream_t s) {
-  hipLaunchKernelGGL(ff_rotary_kernel, dim3(p.T), dim3(kThreads), 0, s, p);
+  const unsigned across = (unsigned)p.T < 1u << 20 ? p.T : 1u << 20;     // (a launch's dimension has 32 bits of threads)
+  hipLaunchKernelGGL(ff_rotary_kernel, dim3(across, ((unsigned)p.T + across - 1) / across), dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }

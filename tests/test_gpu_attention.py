@@ -161,6 +161,32 @@ def test_long_prompt_and_many_sequences(ctx):
     p.check("150 sequences")
 
 
+@pytest.mark.parametrize("h", [(64, 64, 64), (64, 64, 128), (80, 40, 64), (48, 16, 128)], ids=lambda h: "%d_%d_%d" % h)
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 300)])
+def test_prompts_with_work_for_every_cu_in_large_tiles(ctx, h, causal, window):
+    """Enough rows that tiles have 256 of them: whole, ragged and part-filled ones, and values that are not finite."""
+    group = h[0] // h[1]
+    t = -(-256 * 500 // h[0])                              # rows / 256 * key heads above 384
+    lengths = [t - 517, 1, 0, 300, 63, 31, 129]
+    p = Prompt(_heads(h, causal, window), lengths, seed=30, behind=3)
+    for row, ch, val in ((t - 518, 5, math.inf), (t - 400, 0, math.nan), (t - 390, 9, -math.inf), (70, 64, math.inf)):
+        p.v[row, ch] = val
+    assert sum(lengths) * group // 256 * h[1] > 384
+    p.run(ctx)
+    p.check(f"{h} causal {causal} window {window}")
+
+
+def test_more_sequences_than_a_launch_has_threads_across(ctx):
+    """2^24 tiles of one row: a single token's output is its value."""
+    n = 16384
+    gen = _gen(31)
+    h = _heads((1024, 1024, 64))
+    q, v = _bf16(gen, n, 65536), _bf16(gen, n, 65536)
+    o = torch.zeros_like(q)
+    ctx.prompt_attention(h, q, q, v, torch.arange(n + 1, dtype=torch.int32, device=DEV), o)
+    assert torch.equal(o.view(torch.int16), v.view(torch.int16))
+
+
 def test_prompt_scale_and_large_logits(ctx):
     # logits up to some thousands: the running maximum moves all the time, and most weights vanish
     p = Prompt(_heads(H8B, scale=3.0), [400], seed=6)
@@ -248,6 +274,47 @@ def test_chunks_of_every_kernel(ctx, h, n):
     c = Chunks(_heads(h), [n], [n + 400], page_size=64, seed=n)
     c.run(ctx)
     c.check(f"chunk {h} {n}")
+
+
+@pytest.mark.parametrize("h", [(64, 64, 64), (64, 64, 128), (48, 16, 128)], ids=lambda h: "%d_%d_%d" % h)
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 300)])
+def test_chunks_with_work_for_every_cu_in_large_tiles(ctx, h, causal, window):
+    t = -(-256 * 500 // h[0])
+    new = [t - 60, 1, 40, 0, 19]
+    c = Chunks(_heads(h, causal, window), new, [t + 200, 333, 40, 5, 7], page_size=32, seed=32, behind=2)
+    for i, key, ch, val in ((0, t + 199, 3, math.inf), (0, t + 100, 7, math.nan), (1, 332, 0, -math.inf), (2, 5, 60, math.inf)):
+        c.v[i][key, 0, ch] = val
+        c.v_pages[c.table[i, key // 32].long(), 0, key % 32, ch] = val
+    c.run(ctx)
+    c.check(f"{h} causal {causal} window {window}")
+
+
+@pytest.mark.parametrize("h", [H8B, H7B, H1B, MQA], ids=lambda h: "%d_%d_%d" % h)
+@pytest.mark.parametrize("n", [1, 3, 4])
+def test_few_rows_over_many_keys_with_values_that_are_not_finite(ctx, h, n):
+    """Pieces joined by the last one of them or by a launch of their own: infinities and NaN reach the rows that see them."""
+    c = Chunks(_heads(h), [n, 1], [9000, 4001], page_size=64, seed=33)
+    for i, key, ch, val in ((0, 8999, 3, math.inf), (0, 9000 - n, 7, math.nan), (0, 17, 0, -math.inf), (0, 5000, 0, math.inf), (1, 4000, 60, math.inf)):
+        c.v[i][key, 0, ch] = val
+        c.v_pages[c.table[i, key // 64].long(), 0, key % 64, ch] = val
+    c.run(ctx)
+    c.check(f"{h} {n} not finite")
+
+
+def test_without_the_log_sums(ctx):
+    for new in ([1, 1], [3, 1], [9, 8], [100, 1]):
+        c = Chunks(_heads(H8B), new, [5000, 300], page_size=64, seed=34)
+        c.run(ctx)
+        first = c.o.clone()
+        c.o.fill_(7.0)
+        ctx.chunk_attention(c.h, c.q, c.starts, c.ctx_lens, c.max_chunk, c.cache, c.table, c.o)
+        assert torch.equal(c.o.view(torch.int16), first.view(torch.int16))
+    p = Prompt(_heads(H1B), [300, 5], seed=35)
+    p.run(ctx)
+    first = p.o.clone()
+    p.o.fill_(7.0)
+    ctx.prompt_attention(p.h, p.q, p.k, p.v, p.starts, p.o)
+    assert torch.equal(p.o.view(torch.int16), first.view(torch.int16))
 
 
 @pytest.mark.parametrize("page_size", [8, 16, 128, 4096])
@@ -458,3 +525,17 @@ def test_lengths_and_pages_out_of_range(ctx):
         c.check("validated")
     finally:
         ctx.set_option("validate", 0)
+
+
+def test_a_call_after_chunks_that_overlap(ctx):
+    """Chunks that overlap are more work than there is room for: whatever such a call leaves in its own rows, the next one is right."""
+    t, n_seqs = 64, 200
+    bad = Chunks(_heads(H8B), [1] * t, [3000] * t, page_size=64, seed=36)
+    lens, table = _int32([3000] * n_seqs), bad.table[:1].repeat(n_seqs, 1).contiguous()
+    ends = [0, t] * (n_seqs // 2) + [0]                     # every other sequence has all the rows
+    ctx.ensure_attention_workspace(bad.h, t, n_seqs)
+    ctx.chunk_attention(bad.h, bad.q, _int32(ends), lens, 1, bad.cache, table, bad.o)
+    for _ in range(2):
+        good = Chunks(_heads(H8B), [1, 1], [9000, 5000], page_size=64, seed=37)
+        good.run(ctx)
+        good.check("after overlapping chunks")

@@ -159,6 +159,28 @@ def _refused(status, call, *args, **kw):
     assert e.value.status == status, e.value
 
 
+def test_more_tokens_than_a_launch_has_threads_across(ctx):
+    """Above 2^24 rows, of a norm and of rotary positions: the last ones and some between."""
+    t = (1 << 24) + 70
+    gen = _gen(10)
+    some = torch.cat([torch.arange(0, t, 99991, device=DEV), torch.arange(t - 200, t, device=DEV)])
+    h = _bf16(gen, t, 8)
+    h_out, x = torch.empty_like(h), torch.empty_like(h)
+    n = _norm(gen, "rms", 8)
+    ctx.norm_residual(h, h, h_out, x, pre=n)
+    s, s_size, x_ref, x_size = _norm_reference(h[some], h[some], None, None, 1, 1.0, n)
+    _close(h_out[some], s, s_size, "rows above 2^24, h")
+    _close(x[some], x_ref, x_size, "rows above 2^24, x")
+    del h, h_out, x
+    q = _bf16(gen, t, 64)
+    q_out, k_out = torch.zeros_like(q), torch.zeros_like(q)
+    pos, freqs = torch.arange(t, dtype=torch.int32, device=DEV)[None].contiguous(), _freqs(64)
+    ctx.rotary(B.Attention(1, 1, 64, 1, 0, 1.0), B.rotary(64, freqs), q, q, None, pos, q_out, k_out=k_out)
+    ref, size = _turned(q[some], 64, 64, pos[:, some], [0] * 32, freqs, False)
+    _close(q_out[some].unflatten(1, (-1, 64)), ref, size, "tokens above 2^24")
+    assert torch.equal(q_out.view(torch.int16), k_out.view(torch.int16))
+
+
 def test_norm_refusals(ctx):
     h = torch.zeros((4, 64), dtype=torch.bfloat16, device=DEV)
     x, n = torch.empty_like(h), B.norm("rms", EPS)
