@@ -434,12 +434,11 @@ ff_status check_heads(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens) {
     return fail(ctx, FF_ERR_SHAPE, "more than 2^30 tokens, or about 2^31 rows (n_tokens * n_heads)");
   return FF_OK;
 }
-constexpr int kMaxSeqs = 16384;
 ff_status check_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs) {
   ff_status st = check_heads(ctx, a, n_tokens);
   if (st != FF_OK) return st;
   if (n_seqs < 1) return fail(ctx, FF_ERR_INVALID_ARG, "sizes must be positive");
-  if (n_seqs > kMaxSeqs) return fail(ctx, FF_ERR_SHAPE, "more than %d sequences", kMaxSeqs);
+  if (n_seqs > kAttnSeqs) return fail(ctx, FF_ERR_SHAPE, "more than %d sequences", kAttnSeqs);
   if (!(a->scale > 0.f) || std::isinf(a->scale)) return fail(ctx, FF_ERR_INVALID_ARG, "scale must be positive and finite");
   if (a->window < 0 || (a->window > 0 && !a->causal)) return fail(ctx, FF_ERR_INVALID_ARG, "a window (%d) is positive and goes with causal", a->window);
   return FF_OK;

@@ -98,22 +98,60 @@ __device__ __forceinline__ Seq lane_seq(const AttnParams &p, int s0, const Seq &
   if (s0 == 0) return first;
   return s < p.n_seqs ? seq_of(p, s) : Seq{0, 0, 0};
 }
-// How long a piece is and how many (tile, piece) there are, from the work of the whole call; every wavefront finds the same.
+// More than 64 sequences are looked at by 64, a wavefront of the workgroup to each 64, and the sums go through LDS; then a workgroup finds
+// an item's sequence in those and one look more.  (2048 single tokens over 200 keys: 652 us with a look at every sequence for every
+// item, 311 so.)
+constexpr int kGroups = kAttnSeqs / 64;
+struct Sums { int items[kGroups]; };      // (tile, piece) of each 64 sequences
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
+__device__ __forceinline__ float last_lane(float v) { return __builtin_bit_cast(float, last_lane(__builtin_bit_cast(int, v))); }
+// (tile, piece) of this lane's sequence.  Sums of 64 of these and of the sums stay in 32 bits, whatever the lengths are: each is held to
+// kMostItems, more than a call has whose tensors fit into the memory.
+constexpr int kMostItems = 1 << 24;
+__device__ __forceinline__ int lane_items(const AttnParams &p, const AttnPlan &pl, const Seq &q, int keys) {
+  return (int)min((long)tiles_of(p, pl, q.n) * seq_pieces(p, pl, q, keys), (long)kMostItems);
+}
+// all (tile, piece) of the call, and with more than 64 sequences each 64's in `sums` (a barrier before and behind)
+template <int W>
+__device__ __forceinline__ int count_items(const AttnParams &p, const AttnPlan &pl, int keys, const Seq &first, Sums &sums) {
+  if (p.n_seqs <= 64) return last_lane(lane_sums(lane_items(p, pl, first, keys)));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n_groups = (p.n_seqs + 63) >> 6;
+  __syncthreads();
+  for (int g = wave; g < n_groups; g += W) {
+    const int sum = lane_sums(lane_items(p, pl, lane_seq(p, g * 64, first), keys));
+    if (lane == 63) sums.items[g] = min(sum, kMostItems);
+  }
+  __syncthreads();
+  int all = 0;
+  for (int g = lane; g < n_groups; g += 64) all += sums.items[g];
+  return last_lane(lane_sums(min(all, kMostItems)));
+}
+// How long a piece is and how many (tile, piece) there are, from the work of the whole call; every wavefront of W finds the same.
 struct Cut { int keys, items; Seq first; };
-__device__ __forceinline__ Cut cut_of(const AttnParams &p, const AttnPlan &pl) {
+template <int W>
+__device__ __forceinline__ Cut cut_of(const AttnParams &p, const AttnPlan &pl, Sums &sums) {
   Cut c = {kUnsplit, 0, {0, 0, 0}};
   const int lane = threadIdx.x & 63;
   if (lane < p.n_seqs) c.first = seq_of(p, lane);
   if (pl.target > 0) {
-    float steps = 0.f;
-    for (int s0 = 0; s0 < p.n_seqs; s0 += 64) steps += price_of(p, pl, lane_seq(p, s0, c.first));
-    c.keys = __builtin_amdgcn_readfirstlane(piece_keys_for(p, pl, __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lane_sums(steps)), 63))));
+    float steps;
+    if (p.n_seqs <= 64) {
+      steps = last_lane(lane_sums(price_of(p, pl, c.first)));
+    } else {
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      float mine = 0.f;
+      for (int s0 = wave * 64; s0 < p.n_seqs; s0 += 64 * W) mine += price_of(p, pl, lane_seq(p, s0, c.first));
+      mine = lane_sums(mine);
+      if (lane == 63) sums.items[wave] = __builtin_bit_cast(int, mine);
+      __syncthreads();
+      steps = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) steps += __builtin_bit_cast(float, sums.items[w]);
+    }
+    c.keys = __builtin_amdgcn_readfirstlane(piece_keys_for(p, pl, steps));
   }
-  for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
-    const Seq q = lane_seq(p, s0, c.first);
-    c.items = (int)min((long)c.items + (long)tiles_of(p, pl, q.n) * seq_pieces(p, pl, q, c.keys), 0x1000000L);
-  }
-  c.items = __builtin_amdgcn_readlane(lane_sums(c.items), 63);
+  c.items = count_items<W>(p, pl, c.keys, c.first, sums);
   return c;
 }
 
@@ -125,36 +163,48 @@ struct Item {
 };
 // The sequence of (tile, piece) number x, counted over the sequences in pieces of `keys`, or, with BY_SEQ, sequence x.
 template <bool BY_SEQ>
-__device__ __forceinline__ Item find_seq(const AttnParams &p, const AttnPlan &pl, int keys, const Seq &first, int x) {
+__device__ __forceinline__ Item find_seq(const AttnParams &p, const AttnPlan &pl, int keys, const Seq &first, const Sums &sums, int x) {
   const int lane = threadIdx.x & 63;
   Item it = {};
-  int base = 0;
-  for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
-    const Seq q = lane_seq(p, s0, first);
-    const int tiles = tiles_of(p, pl, q.n), pieces = seq_pieces(p, pl, q, keys);
-    const int mine = tiles * pieces, incl = lane_sums(mine);
-    const int excl = base + incl - mine;
-    const unsigned long long hit = __ballot(BY_SEQ ? s0 + lane == x : x >= excl && x < excl + mine);
-    if (hit) {
-      const int l = __builtin_ctzll(hit);
-      it.s = s0 + l;
-      it.first = __builtin_amdgcn_readlane(excl, l);
-      it.n_tiles = __builtin_amdgcn_readlane(tiles, l);
-      it.n_pieces = __builtin_amdgcn_readlane(pieces, l);
-      it.seq.t0 = __builtin_amdgcn_readlane(q.t0, l);
-      it.seq.n = __builtin_amdgcn_readlane(q.n, l);
-      it.seq.keys = __builtin_amdgcn_readlane(q.keys, l);
-      return it;
+  int base = 0, s0 = 0;                    // 64 sequences from s0 on, with `base` items before
+  if (p.n_seqs > 64) {
+    const int n_groups = (p.n_seqs + 63) >> 6;
+    bool found = false;
+    for (int g0 = 0; g0 < n_groups && !found; g0 += 64) {
+      const int mine = g0 + lane < n_groups ? sums.items[g0 + lane] : 0, incl = lane_sums(mine);
+      const int excl = base + incl - mine;
+      const unsigned long long hit = __ballot(BY_SEQ ? g0 + lane == x >> 6 : x >= excl && x < excl + mine);
+      found = hit != 0;
+      if (found) {
+        const int l = __builtin_ctzll(hit);
+        s0 = (g0 + l) * 64;
+        base = __builtin_amdgcn_readlane(excl, l);
+      } else {
+        base += last_lane(incl);
+      }
     }
-    base += __builtin_amdgcn_readlane(incl, 63);
+    if (!found) return it;
   }
+  const Seq q = lane_seq(p, s0, first);
+  const int tiles = tiles_of(p, pl, q.n), pieces = seq_pieces(p, pl, q, keys);
+  const int mine = lane_items(p, pl, q, keys), excl = base + lane_sums(mine) - mine;
+  const unsigned long long hit = __ballot(BY_SEQ ? s0 + lane == x : x >= excl && x < excl + mine);
+  if (!hit) return it;
+  const int l = __builtin_ctzll(hit);
+  it.s = s0 + l;
+  it.first = __builtin_amdgcn_readlane(excl, l);
+  it.n_tiles = __builtin_amdgcn_readlane(tiles, l);
+  it.n_pieces = __builtin_amdgcn_readlane(pieces, l);
+  it.seq.t0 = __builtin_amdgcn_readlane(q.t0, l);
+  it.seq.n = __builtin_amdgcn_readlane(q.n, l);
+  it.seq.keys = __builtin_amdgcn_readlane(q.keys, l);
   return it;
 }
 // Item number -> what to compute.  Key heads go innermost (workgroups id mod 8 share an XCD, so its L2 keeps one head's keys where
 // there are eight), then the tiles of one piece, the last first: under a causal mask those have the most keys.
-__device__ __forceinline__ Item work_of(const AttnParams &p, const AttnPlan &pl, const Cut &cut, int id) {
+__device__ __forceinline__ Item work_of(const AttnParams &p, const AttnPlan &pl, const Cut &cut, const Sums &sums, int id) {
   const int x = p.by_kv(id);
-  Item it = find_seq<false>(p, pl, cut.keys, cut.first, x);
+  Item it = find_seq<false>(p, pl, cut.keys, cut.first, sums, x);
   const int local = x - it.first;
   it.kvh = id - x * p.n_kv;
   if (it.n_tiles == 0) return it;       // (no such item)
@@ -331,6 +381,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
   constexpr int kRows = 16 * NB, kPitch = HD + 4, kBatch = 16;
   extern __shared__ __align__(256) uint8_t lds[];
   __shared__ int last_s;
+  __shared__ Sums sums_s;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l16 = lane & 15, quad = lane >> 4;
   const uint32_t k_at = lds_addr_of(lds) + wave * 2 * kHalf, v_at = k_at + kHalf;
@@ -341,10 +392,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
 #pragma unroll
   for (int d = 0; d < DB; ++d) v_off[d] = v_at + chunk_at<HD>(quad * 4 + (l16 >> 2), d * 2 + ((l16 & 3) >> 1)) + (l16 & 1) * 8;
 
-  const Cut cut = cut_of(p, pl);
+  const Cut cut = cut_of<kFewWaves>(p, pl, sums_s);
   const int n_items = items_of(p, pl, cut);
   for (int id = blockIdx.x; id < n_items; id += gridDim.x) {
-    const Item it = work_of(p, pl, cut, id);
+    const Item it = work_of(p, pl, cut, sums_s, id);
     if (it.n_tiles == 0) continue;
     const int n_rows = it.seq.n * p.group, row0 = it.tile * kRows;
     const Range range = tile_range(p, it.seq, it.tile, kRows);
@@ -603,13 +654,14 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
   constexpr int kRows = 32 * RW, kStep = kTileKeys * KW;
   extern __shared__ __align__(256) uint8_t lds[];
   __shared__ int odd_s[KW][2];
+  __shared__ Sums sums_s;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % RW, kw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / RW;
   const int lane = threadIdx.x & 63;
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15, grp = lane >> 4;
-  const Cut cut = cut_of(p, pl);
+  const Cut cut = cut_of<RW * KW>(p, pl, sums_s);
   const int id = blockIdx.y * gridDim.x + blockIdx.x;
   if (id >= items_of(p, pl, cut)) return;
-  const Item it = work_of(p, pl, cut, id);
+  const Item it = work_of(p, pl, cut, sums_s, id);
   if (it.n_tiles == 0) return;
   const int kpp = cut.keys;
   const int n_rows = it.seq.n * p.group, row0 = it.tile * kRows + wave * 32;
@@ -889,18 +941,19 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
 // where the first one's sums lie.
 struct Split { Seq seq; int tile, n; size_t step; const float *src; };
 template <int HD>
-__device__ __forceinline__ Split find_split(const AttnParams &p, const AttnPlan &pl, int x, int kvh) {
+__device__ __forceinline__ Split find_split(const AttnParams &p, const AttnPlan &pl, Sums &sums, int x, int kvh) {
   Split r = {};
-  const Cut cut = cut_of(p, pl);
-  const Item whole = find_seq<false>(p, pl, kUnsplit, cut.first, x);
+  const Cut cut = cut_of<4>(p, pl, sums);
+  if (items_of(p, pl, cut) == 0) return r;
+  count_items<4>(p, pl, kUnsplit, cut.first, sums);
+  const Item whole = find_seq<false>(p, pl, kUnsplit, cut.first, sums, x);
+  count_items<4>(p, pl, cut.keys, cut.first, sums);
   if (whole.n_tiles == 0) return r;
   r.seq = whole.seq;
   r.tile = x - whole.first;
   r.n = pieces_of(tile_range(p, whole.seq, r.tile, pl.tile_rows), cut.keys);
-  const Item it = find_seq<true>(p, pl, cut.keys, cut.first, whole.s);
+  const Item it = find_seq<true>(p, pl, cut.keys, cut.first, sums, whole.s);
   const int x0 = it.first + it.n_tiles - 1 - r.tile;
-  // (chunks that overlap may have more pieces than there were workgroups and room for)
-  if (((long)x0 + (long)(r.n - 1) * it.n_tiles + 1) * p.n_kv > pl.max_items) r.n = 0;
   r.step = (size_t)it.n_tiles * p.n_kv * ((size_t)pl.tile_rows * (HD + 2));
   r.src = part_of<HD>(pl, x0, kvh, p.n_kv);
   return r;
@@ -947,7 +1000,8 @@ __global__ __launch_bounds__(256) void ff_attn_join_kernel(AttnParams p, AttnPla
   const int runs = pl.tile_rows / 32 * (HD / 8);                // of 1 KB in a tile
   const int id = (int)blockIdx.x * 4 / runs, run = (int)blockIdx.x * 4 % runs + wave;
   const int x = p.by_kv(id), kvh = id - x * p.n_kv;
-  const Split sp = find_split<HD>(p, pl, x, kvh);
+  __shared__ Sums sums_s;
+  const Split sp = find_split<HD>(p, pl, sums_s, x, kvh);
   if (sp.n <= 1) return;
   const int r = run / (HD / 8) * 32 + (lane & 31), c = run % (HD / 8) * 8 + (lane >> 5) * 4;
   const int row = sp.tile * pl.tile_rows + r;
@@ -968,7 +1022,8 @@ __global__ __launch_bounds__(256) void ff_attn_join_rows_kernel(AttnParams p, At
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int id = (int)blockIdx.x * 4 / pl.tile_rows, r = (int)blockIdx.x * 4 % pl.tile_rows + wave;
   const int x = p.by_kv(id), kvh = id - x * p.n_kv;
-  const Split sp = find_split<HD>(p, pl, x, kvh);
+  __shared__ Sums sums_s;
+  const Split sp = find_split<HD>(p, pl, sums_s, x, kvh);
   const int row = sp.tile * pl.tile_rows + r;
   if (sp.n <= 1 || row >= sp.seq.n * p.group) return;
   float top, sum, acc[C];

@@ -43,7 +43,7 @@ struct AttnParams {
   size_t part_bytes = 0;
   int32_t *counters = nullptr;   // [kAttnCounters], zero: how many pieces of a tile have ended; zero again when the call has
 };
-constexpr int kAttnCounters = 16384;
+constexpr int kAttnCounters = 16384, kAttnSeqs = 16384;   // most sequences of a call
 // One kernel's share of a call: the sequences with rows (new tokens times heads of a group) in (rows_above, rows_upto], in tiles of
 // tile_rows, split along the keys into about `target` pieces of at least min_steps times 64 keys (0: not split).
 struct AttnPlan {
