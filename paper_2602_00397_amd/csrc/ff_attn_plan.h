@@ -48,7 +48,7 @@ constexpr int kAttnCounters = 16384, kAttnSeqs = 16384;   // most sequences of a
 // tile_rows, split along the keys into about `target` pieces of at least min_steps times 64 keys (0: not split).
 struct AttnPlan {
   int64_t rows_above = 0, rows_upto = -1;
-  int32_t tile_rows = 1, target = 0, min_steps = 1, max_items = 0, join_here = 0;
+  int32_t tile_rows = 1, target = 0, min_steps = 1, max_items = 0, join_here = 0, by_tile = 0;
   size_t part_at = 0;
   float *part = nullptr;
 };
