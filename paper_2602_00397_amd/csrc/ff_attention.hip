@@ -114,7 +114,7 @@ __device__ __forceinline__ int lane_items(const AttnParams &p, const AttnPlan &p
 // all (tile, piece) of the call, and with more than 64 sequences each 64's in `sums` (a barrier before and behind)
 template <int W>
 __device__ __forceinline__ int count_items(const AttnParams &p, const AttnPlan &pl, int keys, const Seq &first, Sums &sums) {
-  if (p.n_seqs <= 64) return last_lane(lane_sums(lane_items(p, pl, first, keys)));
+  if (__builtin_expect(p.n_seqs <= 64, 1)) return last_lane(lane_sums(lane_items(p, pl, first, keys)));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int n_groups = (p.n_seqs + 63) >> 6;
   __syncthreads();
@@ -136,7 +136,7 @@ __device__ __forceinline__ Cut cut_of(const AttnParams &p, const AttnPlan &pl, S
   if (lane < p.n_seqs) c.first = seq_of(p, lane);
   if (pl.target > 0) {
     float steps;
-    if (p.n_seqs <= 64) {
+    if (__builtin_expect(p.n_seqs <= 64, 1)) {
       steps = last_lane(lane_sums(price_of(p, pl, c.first)));
     } else {
       const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -167,7 +167,7 @@ __device__ __forceinline__ Item find_seq(const AttnParams &p, const AttnPlan &pl
   const int lane = threadIdx.x & 63;
   Item it = {};
   int base = 0, s0 = 0;                    // 64 sequences from s0 on, with `base` items before
-  if (p.n_seqs > 64) {
+  if (__builtin_expect(p.n_seqs > 64, 0)) {
     const int n_groups = (p.n_seqs + 63) >> 6;
     bool found = false;
     for (int g0 = 0; g0 < n_groups && !found; g0 += 64) {
@@ -968,7 +968,6 @@ template <int HD>
 __device__ __forceinline__ Split find_split(const AttnParams &p, const AttnPlan &pl, Sums &sums, int x, int kvh) {
   Split r = {};
   const Cut cut = cut_of<4>(p, pl, sums);
-  if (items_of(p, pl, cut) == 0) return r;
   count_items<4>(p, pl, kUnsplit, cut.first, sums);
   const Item whole = find_seq<false>(p, pl, kUnsplit, cut.first, sums, x);
   count_items<4>(p, pl, cut.keys, cut.first, sums);
@@ -978,6 +977,8 @@ __device__ __forceinline__ Split find_split(const AttnParams &p, const AttnPlan 
   r.n = pieces_of(tile_range(p, whole.seq, r.tile, pl.tile_rows), cut.keys);
   const Item it = find_seq<true>(p, pl, cut.keys, cut.first, sums, whole.s);
   const int x0 = it.first + it.n_tiles - 1 - r.tile;
+  // (chunks that overlap may have more pieces than there is room for)
+  if (x0 < 0 || ((long)x0 + (long)(r.n - 1) * it.n_tiles + 1) * p.n_kv > pl.max_items) r.n = 0;
   r.step = (size_t)it.n_tiles * p.n_kv * ((size_t)pl.tile_rows * (HD + 2));
   r.src = part_of<HD>(pl, x0, kvh, p.n_kv);
   return r;

@@ -123,6 +123,39 @@ static void part1_no_gpu(void) {
   EXPECT(ff_rmsnorm(NULL, 4, 128, FAKE(7), 1e-6f, FAKE(9)), FF_ERR_INVALID_ARG);
   EXPECT(ff_residual_add(NULL, 4, 128, FAKE(7), FAKE(9)), FF_ERR_INVALID_ARG);
   EXPECT(ff_copy(NULL, FAKE(7), FAKE(9), 1024), FF_ERR_INVALID_ARG);
+  {
+    const ff_attention heads = {32, 8, 128, 1, 0, 0.1f};
+    ff_attention h;
+    const ff_rotary_spec rot = {64, 0, 1, NULL, (const float *)FAKE(14)};
+    const ff_paged_cache cache = {FAKE(15), FAKE(16), 4, 16};
+    const ff_norm norm = {FF_NORM_RMS, 1e-6f, 0.f, NULL, NULL};
+    size_t few = 0;
+    EXPECT(ff_norm_residual(NULL, 4, 128, FAKE(7), NULL, FF_OUT_BF16, NULL, NULL, 1, 1.f, NULL, &norm, FAKE(9)), FF_ERR_INVALID_ARG);
+    EXPECT(ff_rotary(NULL, &heads, &rot, 4, FAKE(7), 4096, FAKE(8), 1024, FAKE(9), 1024, (const int32_t *)FAKE(10), FAKE(11), 4096, FAKE(12), 1024, &cache,
+                     (const int32_t *)FAKE(13)), FF_ERR_INVALID_ARG);
+    EXPECT(ff_prompt_attention(NULL, &heads, 4, 1, FAKE(7), 4096, FAKE(8), 1024, FAKE(9), 1024, (const int32_t *)FAKE(10), FAKE(11), 4096, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ff_chunk_attention(NULL, &heads, 4, 1, FAKE(7), 4096, (const int32_t *)FAKE(8), (const int32_t *)FAKE(9), 4, &cache, (const int32_t *)FAKE(10), 8, FAKE(11), 4096,
+                              NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ff_attention_workspace_bytes(NULL, 4, 1, &bytes), FF_ERR_INVALID_ARG);
+    EXPECT(ff_attention_workspace_bytes(&heads, 4, 1, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ff_attention_workspace_bytes(&heads, 0, 1, &bytes), FF_ERR_INVALID_ARG);
+    EXPECT(ff_attention_workspace_bytes(&heads, 4, 0, &bytes), FF_ERR_INVALID_ARG);
+    EXPECT(ff_attention_workspace_bytes(&heads, 4, 16385, &bytes), FF_ERR_SHAPE);
+    EXPECT(ff_attention_workspace_bytes(&heads, 2147483647, 1, &bytes), FF_ERR_SHAPE);
+    h = heads; h.head_dim = 80;
+    EXPECT(ff_attention_workspace_bytes(&h, 4, 1, &bytes), FF_ERR_SHAPE);
+    h = heads; h.n_kv_heads = 5;
+    EXPECT(ff_attention_workspace_bytes(&h, 4, 1, &bytes), FF_ERR_SHAPE);
+    h = heads; h.n_heads = 2048;
+    EXPECT(ff_attention_workspace_bytes(&h, 4, 1, &bytes), FF_ERR_SHAPE);
+    EXPECT(ff_attention_workspace_bytes(&heads, 1, 1, &few), FF_OK);
+    EXPECT(ff_attention_workspace_bytes(&heads, 4096, 48, &bytes), FF_OK);
+    if (few == 0 || bytes < few) ++n_fail;
+    h.n_heads = h.n_kv_heads = 1024; h.head_dim = 64;
+    EXPECT(ff_attention_workspace_bytes(&h, 1 << 20, 16384, &bytes), FF_OK);
+    h.n_heads = h.n_kv_heads = 1;
+    EXPECT(ff_attention_workspace_bytes(&h, 1 << 30, 16384, &bytes), FF_OK);
+  }
 }
 
 static void part2_argument_errors(ff_ctx *ctx) {
@@ -258,6 +291,91 @@ static void part2_argument_errors(ff_ctx *ctx) {
   EXPECT(ff_residual_add(ctx, 4, 128, x, NULL), FF_ERR_INVALID_ARG);
   EXPECT(ff_residual_add(ctx, 4, 100, x, y), FF_ERR_SHAPE);
   EXPECT(ff_residual_add(ctx, 4, 128, x, odd), FF_ERR_ALIGNMENT);
+  /* the calls around the FFN: each with one thing wrong */
+  {
+    const ff_attention ok_heads = {4, 2, 64, 1, 0, 0.1f};
+    const ff_norm ok_norm = {FF_NORM_LAYER, 1e-6f, 0.f, NULL, NULL};
+    const ff_paged_cache ok_cache = {FAKE(15), FAKE(16), 4, 16};
+    const int32_t axis_far[32] = {1};
+    const int32_t *pos = (const int32_t *)FAKE(17), *pos_odd = (const int32_t *)((uintptr_t)FAKE(17) + 4);
+    ff_attention a = ok_heads;
+    ff_norm n = ok_norm;
+    ff_paged_cache c = ok_cache;
+    ff_rotary_spec r = {64, 0, 1, NULL, (const float *)FAKE(14)};
+    EXPECT(ff_norm_residual(ctx, 0, 128, x, NULL, FF_OUT_BF16, NULL, NULL, 1, 1.f, NULL, &n, y), FF_ERR_INVALID_ARG);
+    EXPECT(ff_norm_residual(ctx, 4, 100, x, NULL, FF_OUT_BF16, NULL, NULL, 1, 1.f, NULL, &n, y), FF_ERR_SHAPE);
+    EXPECT(ff_norm_residual(ctx, 4, 16392, x, NULL, FF_OUT_BF16, NULL, NULL, 1, 1.f, NULL, &n, y), FF_ERR_SHAPE);
+    EXPECT(ff_norm_residual(ctx, 4, 128, NULL, NULL, FF_OUT_BF16, NULL, NULL, 1, 1.f, NULL, &n, y), FF_ERR_INVALID_ARG);
+    EXPECT(ff_norm_residual(ctx, 4, 128, x, NULL, FF_OUT_BF16, NULL, x, 1, 1.f, NULL, &n, y), FF_ERR_INVALID_ARG);
+    EXPECT(ff_norm_residual(ctx, 4, 128, x, y, FF_OUT_BF16, NULL, NULL, 1, 1.f, NULL, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ff_norm_residual(ctx, 4, 128, x, y, 7, NULL, NULL, 1, 1.f, x, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ff_norm_residual(ctx, 4, 128, x, y, FF_OUT_BF16, NULL, x, 0, 1.f, x, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ff_norm_residual(ctx, 4, 128, x, y, FF_OUT_BF16, NULL, NULL, 1, (float)NAN, x, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ff_norm_residual(ctx, 4, 128, x, odd, FF_OUT_BF16, NULL, NULL, 1, 1.f, x, NULL, NULL), FF_ERR_ALIGNMENT);
+    n.kind = 0;
+    EXPECT(ff_norm_residual(ctx, 4, 128, x, NULL, FF_OUT_BF16, NULL, NULL, 1, 1.f, NULL, &n, y), FF_ERR_INVALID_ARG);
+    n = ok_norm; n.eps = -1.f;
+    EXPECT(ff_norm_residual(ctx, 4, 128, x, NULL, FF_OUT_BF16, NULL, NULL, 1, 1.f, NULL, &n, y), FF_ERR_INVALID_ARG);
+    n = ok_norm; n.gain = odd;
+    EXPECT(ff_norm_residual(ctx, 4, 128, x, y, FF_OUT_F32, &n, NULL, 1, 1.f, x, NULL, NULL), FF_ERR_ALIGNMENT);
+
+#define ROTARY(q, qs, k, ks, v, p, qo, qos, ko, kos, cc, sl) ff_rotary(ctx, &a, &r, 4, q, qs, k, ks, v, 128, p, qo, qos, ko, kos, cc, sl)
+    EXPECT(ff_rotary(ctx, NULL, &r, 4, x, 256, y, 128, y, 128, pos, x, 256, y, 128, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ff_rotary(ctx, &a, NULL, 4, x, 256, y, 128, y, 128, pos, x, 256, y, 128, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ROTARY(x, 256, y, 128, y, NULL, x, 256, y, 128, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ROTARY(NULL, 256, y, 128, y, pos, x, 256, y, 128, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ROTARY(x, 248, y, 128, y, pos, x, 256, y, 128, NULL, NULL), FF_ERR_SHAPE);
+    EXPECT(ROTARY(x, 260, y, 128, y, pos, x, 260, y, 128, NULL, NULL), FF_ERR_ALIGNMENT);
+    EXPECT(ROTARY(x, 256, y, 1 << 25, y, pos, x, 256, y, 1 << 25, NULL, NULL), FF_ERR_SHAPE);
+    EXPECT(ROTARY(x, 264, y, 128, y, pos, x, 256, y, 128, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ROTARY(x, 256, y, 128, y, pos, x, 256, NULL, 128, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ROTARY(x, 256, y, 128, y, pos, x, 256, NULL, 128, &c, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ROTARY(x, 256, y, 128, y, pos_odd, x, 256, y, 128, NULL, NULL), FF_ERR_ALIGNMENT);
+    EXPECT(ROTARY(x, 256, y, 128, NULL, pos, x, 256, NULL, 128, &c, pos), FF_ERR_INVALID_ARG);
+    c.page_size = 24;
+    EXPECT(ROTARY(x, 256, y, 128, y, pos, x, 256, NULL, 128, &c, pos), FF_ERR_SHAPE);
+    r.rot_dim = 72;
+    EXPECT(ROTARY(x, 256, y, 128, y, pos, x, 256, y, 128, NULL, NULL), FF_ERR_SHAPE);
+    r.rot_dim = 64; r.axis = axis_far;
+    EXPECT(ROTARY(x, 256, y, 128, y, pos, x, 256, y, 128, NULL, NULL), FF_ERR_INVALID_ARG);
+    r.n_axes = 5;
+    EXPECT(ROTARY(x, 256, y, 128, y, pos, x, 256, y, 128, NULL, NULL), FF_ERR_SHAPE);
+#undef ROTARY
+
+#define PROMPT(nt, ns, q, qs, k, st, o, l) ff_prompt_attention(ctx, &a, nt, ns, q, qs, k, 128, y, 128, st, o, 256, l)
+    EXPECT(PROMPT(0, 1, x, 256, y, pos, y, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(PROMPT(4, 0, x, 256, y, pos, y, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(PROMPT(4, 16385, x, 256, y, pos, y, NULL), FF_ERR_SHAPE);
+    EXPECT(PROMPT(4, 1, x, 128, y, pos, y, NULL), FF_ERR_SHAPE);
+    EXPECT(PROMPT(4, 1, x, 256, NULL, pos, y, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(PROMPT(4, 1, x, 256, y, NULL, y, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(PROMPT(4, 1, x, 256, odd, pos, y, NULL), FF_ERR_ALIGNMENT);
+    EXPECT(PROMPT(4, 1, x, 256, y, pos, y, (float *)odd), FF_ERR_ALIGNMENT);
+    a.scale = 0.f;
+    EXPECT(PROMPT(4, 1, x, 256, y, pos, y, NULL), FF_ERR_INVALID_ARG);
+    a = ok_heads; a.causal = 0; a.window = 5;
+    EXPECT(PROMPT(4, 1, x, 256, y, pos, y, NULL), FF_ERR_INVALID_ARG);
+    a = ok_heads;
+#undef PROMPT
+
+#define CHUNK(mc, cc, tb, ts, ln) ff_chunk_attention(ctx, &a, 4, 1, x, 256, pos, ln, mc, cc, tb, ts, y, 256, NULL)
+    c = ok_cache;
+    EXPECT(CHUNK(0, &c, pos, 4, pos), FF_ERR_INVALID_ARG);
+    EXPECT(CHUNK(5, &c, pos, 4, pos), FF_ERR_INVALID_ARG);
+    EXPECT(CHUNK(4, NULL, pos, 4, pos), FF_ERR_INVALID_ARG);
+    EXPECT(CHUNK(4, &c, NULL, 4, pos), FF_ERR_INVALID_ARG);
+    EXPECT(CHUNK(4, &c, pos, 0, pos), FF_ERR_INVALID_ARG);
+    EXPECT(CHUNK(4, &c, pos, 4, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(CHUNK(4, &c, pos_odd, 4, pos), FF_ERR_ALIGNMENT);
+    EXPECT(CHUNK(4, &c, pos, 4, pos), FF_ERR_WORKSPACE);
+    c.n_pages = 0;
+    EXPECT(CHUNK(4, &c, pos, 4, pos), FF_ERR_INVALID_ARG);
+    c = ok_cache; c.page_size = 4;
+    EXPECT(CHUNK(4, &c, pos, 4, pos), FF_ERR_SHAPE);
+    c = ok_cache; c.v = odd;
+    EXPECT(CHUNK(4, &c, pos, 4, pos), FF_ERR_ALIGNMENT);
+#undef CHUNK
+  }
   EXPECT(ff_copy(ctx, x, y, 0), FF_ERR_INVALID_ARG);
   EXPECT(ff_copy(ctx, x, y, 100), FF_ERR_INVALID_ARG);
   EXPECT(ff_copy(ctx, NULL, y, 1024), FF_ERR_INVALID_ARG);
@@ -273,7 +391,9 @@ static int part3_real_calls(ff_ctx *ctx) {
   const int32_t nB = 4, ks_ragged[4] = {688, 100, 344, 7}, ks[4] = {344, 344, 344, 344};
   const int32_t kl[2 * 4] = {344, 344, 344, 344, 688, 100, 344, 7};
   void *x = NULL, *wg = NULL, *wu = NULL, *wd = NULL, *w1 = NULL, *w2 = NULL, *wc1 = NULL, *wc2 = NULL, *y = NULL, *ws = NULL, *h = NULL;
-  int32_t *idx = NULL, host_idx[8];
+  void *ws2 = NULL;
+  int32_t *idx = NULL, *pages = NULL, *lens = NULL, host_idx[8];
+  float *lse = NULL;
   size_t need = 0;
   double ms[FF_N_STAGES];
   int32_t cnt[FF_N_STAGES];
@@ -331,6 +451,28 @@ static int part3_real_calls(ff_ctx *ctx) {
   EXPECT(ff_rmsnorm(ctx, (int32_t)T, (int32_t)dm, h, 1e-6f, x), FF_OK);
   EXPECT(ff_residual_add(ctx, (int32_t)T, (int32_t)dm, h, x), FF_OK);
   EXPECT(ff_copy(ctx, y, x, T * dm * 2), FF_OK);
+  {                                     /* the calls around the FFN, over zeros: 4 heads of 64, 2 of them keys', pages of 16 */
+    const ff_attention a = {4, 2, 64, 1, 0, 0.125f};
+    const ff_norm n = {FF_NORM_RMS, 1e-6f, 1.f, w1, NULL};
+    const ff_rotary_spec r = {64, 1, 1, NULL, (const float *)w2};
+    const ff_paged_cache c = {wg, wu, 16, 16};
+    const int32_t tokens = 230, starts[2] = {0, 230};
+    size_t need2 = 0;
+    EXPECT(ff_attention_workspace_bytes(&a, tokens, 1, &need2), FF_OK);
+    DEVBUF(ws2, need2); DEVBUF(pages, 64 * 4); DEVBUF(lens, 2 * 4); DEVBUF(lse, T * 4 * 4);
+    if (hipMemcpy(lens, starts, sizeof(starts), hipMemcpyHostToDevice) != hipSuccess) { rc = 1; goto done; }
+    EXPECT(ff_set_workspace(ctx, ws2, need2), FF_OK);
+    EXPECT(ff_norm_residual(ctx, tokens, 256, h, y, FF_OUT_F32, &n, NULL, 1, 0.5f, h, &n, x), FF_OK);
+    /* (idx holds positions, pages slots: all in range) */
+    EXPECT(ff_rotary(ctx, &a, &r, tokens, x, 256, x, 256, x, 256, idx, h, 256, NULL, 0, NULL, NULL), FF_ERR_INVALID_ARG);
+    EXPECT(ff_rotary(ctx, &a, &r, tokens, x, 256, x, 256, x, 256, idx, h, 256, NULL, 0, &c, idx), FF_OK);
+    EXPECT(ff_prompt_attention(ctx, &a, tokens, 1, h, 256, x, 256, x, 256, lens, y, 256, lse), FF_OK);
+    EXPECT(ff_set_option(ctx, "validate", 1), FF_OK);
+    EXPECT(ff_chunk_attention(ctx, &a, tokens, 1, h, 256, lens, lens + 1, tokens, &c, pages, 64, y, 256, lse), FF_ERR_ALIGNMENT);
+    EXPECT(ff_chunk_attention(ctx, &a, tokens, 1, h, 256, lens, pages, tokens, &c, pages, 64, y, 256, lse), FF_OK);
+    EXPECT(ff_chunk_attention(ctx, &a, tokens, 1, h, 256, lens, pages, 1, &c, pages, 64, y, 256, NULL), FF_OK);
+    EXPECT(ff_set_option(ctx, "validate", 0), FF_OK);
+  }
   if (hipDeviceSynchronize() != hipSuccess) { rc = 1; goto done; }
   if (hipMemcpy(host_idx, idx, sizeof(host_idx), hipMemcpyDeviceToHost) != hipSuccess) { rc = 1; goto done; }
   for (i = 0; i < 8; ++i)
@@ -339,7 +481,7 @@ done:
   (void)ff_set_workspace(ctx, NULL, 0);
   (void)hipDeviceSynchronize();
   hipFree(x); hipFree(h); hipFree(wg); hipFree(wu); hipFree(wd); hipFree(w1); hipFree(w2); hipFree(wc1); hipFree(wc2);
-  hipFree(y); hipFree(idx); hipFree(ws);
+  hipFree(y); hipFree(idx); hipFree(ws); hipFree(ws2); hipFree(pages); hipFree(lens); hipFree(lse);
   return rc;
 }
 
