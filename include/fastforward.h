@@ -252,7 +252,9 @@ ff_status ff_residual_add(ff_ctx *ctx, int32_t n_tokens, int32_t d_model,
  * of one projection's output.  Lengths, positions, page tables and slots are
  * device arrays: nothing is copied from the host, every call may be captured in
  * a HIP graph, and a replay reads what the arrays hold by then.  Whatever they
- * hold, no access leaves the tensors that the call was given. */
+ * hold, no access leaves the tensors that the call was given.  As for the calls
+ * above, two that share a context (its workspace, and counters beside it), a
+ * replay among them, must not run at the same time. */
 
 /* Heads of an attention layer and who sees whom.  Query head h reads key head
  * h / (n_heads / n_kv_heads).  Limits: head_dim 64 or 128, n_heads a multiple
@@ -341,8 +343,9 @@ ff_status ff_rotary(ff_ctx *ctx, const ff_attention *a, const ff_rotary_spec *r,
                     int64_t q_out_stride, void *k_out, int64_t k_out_stride,
                     const ff_paged_cache *cache, const int32_t *slots);
 
-/* Bytes of workspace the two attention calls need at most (fp32 partial sums of
- * attention split along the keys), whatever the sequences' lengths. */
+/* Bytes of workspace that ff_chunk_attention needs at most (fp32 partial sums of
+ * rows split along the keys), whatever the sequences' lengths and max_chunk are.
+ * ff_prompt_attention needs none, nor do the two calls above. */
 ff_status ff_attention_workspace_bytes(const ff_attention *a, int32_t n_tokens,
                                        int32_t n_seqs, size_t *bytes);
 

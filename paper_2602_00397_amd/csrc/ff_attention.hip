@@ -668,9 +668,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
 // ---- many rows: prompts and chunks of them --------------------------------------------------------------------------------
 // MFMA-bound.  RW wavefronts of 32 rows share the key tiles of 64; with KW = 2 there are two such groups of wavefronts, which take
 // every other tile, for half as many rows, and join at the end.  Two stages of LDS for K and two for V: in step i, Q K of tile i
-// and P V of tile i - 1 are one run of MFMAs, whose operands are read six MFMAs ahead, and the softmax of tile i follows, while the
-// copies of K of tile i + 1 and V of tile i land.  One barrier a step: a SIMD's two wavefronts drift apart within it, and one's
-// exponentials go through the vector unit while the matrix pipe works for the other, whose MFMAs have priority.
+// and P V of tile i - 1 are one run of MFMAs, whose operands are read four MFMAs ahead, and the softmax of tile i follows, while the
+// copies of K of tile i + 1 and V of tile i land.  One barrier a step.  A SIMD's two wavefronts take turns: in eight wavefronts of 128
+// channels the second four make the softmax of tile i at the start of step i + 1, so their exponentials go through the vector unit while
+// the matrix pipe works for the first four, and the other way round (8192 tokens of 32 heads over 8 key heads of 128, causal, 520 us
+// without turns, 500 with); elsewhere they drift apart by themselves, and MFMAs have priority.
 template <int HD, int RW, int KW, bool PAGED>
 __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 2) void ff_attn_tile_kernel(AttnParams p, AttnPlan pl) {
   constexpr int KS = HD / 16, DB = HD / 32, NI = kTileKeys * HD * 2 / 1024 / RW;
@@ -857,15 +859,24 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
     const auto is_inner = [&](int j) { return j > start && !is_edge(j - kStep) && !is_edge(j) && j + kStep < end; };
     for (int j = start;; j += kStep, at = kHalf - at) {
       // both products in one run: of tiles that every row of the workgroup sees whole, then of tiles that some see in part
-      for (; is_inner(j); j += kStep, at = kHalf - at) {
+      if (is_inner(j)) {
         f32x16_t s[2];
-        copier.template copy<false>(j + kStep, ring_k + (kHalf - at), lane);
-        copier.template copy<true>(j, ring_v + at, lane);
-        __builtin_amdgcn_s_setprio(1);
-        products(s, ring_v + kHalf - at, ring_k + at, std::true_type(), std::true_type());
-        __builtin_amdgcn_s_setprio(0);
-        weights(s, j, std::false_type());
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const bool late = HD == 128 && RW == 8 && wave >= 4;
+        bool have = false;
+        do {
+          copier.template copy<false>(j + kStep, ring_k + (kHalf - at), lane);
+          copier.template copy<true>(j, ring_v + at, lane);
+          if (late && have) weights(s, j, std::false_type());
+          have = true;
+          __builtin_amdgcn_s_setprio(1);
+          products(s, ring_v + kHalf - at, ring_k + at, std::true_type(), std::true_type());
+          __builtin_amdgcn_s_setprio(0);
+          if (!late) weights(s, j, std::false_type());
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          j += kStep;
+          at = kHalf - at;
+        } while (is_inner(j));
+        if (late) weights(s, j, std::false_type());
       }
       for (; j > start && j < last && !is_inner(j) && is_seen(j - kStep) && is_seen(j); j += kStep, at = kHalf - at) {
         f32x16_t s[2];
