@@ -112,7 +112,8 @@ typedef struct {
 /* ---- context ----------------------------------------------------------- */
 
 /* Creates a context bound to GPU `device` and to `hip_stream` (a hipStream_t,
- * NULL = the default stream).  Allocates only the small pinned staging ring. */
+ * NULL = the default stream).  Allocates only a small pinned staging ring and 64 KB
+ * of counters on the GPU. */
 ff_status ff_create(ff_ctx **out, int device, void *hip_stream);
 ff_status ff_destroy(ff_ctx *ctx);
 /* Rebinds the context to another stream of the same device. */

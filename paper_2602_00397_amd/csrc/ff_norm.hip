@@ -1,7 +1,8 @@
 // Norms around a block with the block's gate and the residual's scale, one pass over the data:
 //   s = h + scale * gate * post(y),  h_out = bf16(s),  x = bf16(pre(s))
 // A token's row stays in registers (fp32) between its one read and its one write, so the bound is HBM: 2 d bytes of h, 2 or 4 d
-// of y, 2 d of each output; gains and gate rows come from L2.
+// of y, 2 d of each output; gains and gate rows come from L2.  16384 rows of 3584, bf16 y and both outputs: 91 us, 5.2 TB/s; a row or
+// a few take 3 us, a launch's latency.
 #include "ff_internal.h"
 
 namespace {
