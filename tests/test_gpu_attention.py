@@ -378,6 +378,79 @@ def test_many_sequences(ctx):
     c.check("130 sequences")
 
 
+@pytest.mark.parametrize("h", [H8B, H7B, TINY], ids=lambda h: "%d_%d_%d" % h)
+def test_many_sequences_of_every_kernel(ctx, h):
+    """More sequences than a wavefront has lanes, with pieces joined in each way."""
+    for n_seqs, new in ((70, lambda i: i % 5), (90, lambda i: (i * 29) % 61), (67, lambda i: 150 if i == 66 else 1)):
+        new = [new(i) for i in range(n_seqs)]
+        lens = [n + (53 * i) % 300 for i, n in enumerate(new)]
+        lens[65] = new[65] + 5000
+        c = Chunks(_heads(h), new, lens, page_size=32, seed=38, behind=1)
+        c.run(ctx)
+        c.check(f"{n_seqs} sequences of up to {max(new)} tokens")
+
+
+def test_thousands_of_sequences(ctx):
+    """Contexts of one key or none: a token's output is that key's value, or zeros; the second of two tokens sees it."""
+    h, n_seqs, ps = _heads((4, 2, 64)), 9000, 8
+    gen = _gen(39)
+    for most in (1, 2, 40):
+        new = [1 + (i % 2 if most > 1 else 0) for i in range(n_seqs)]
+        if most == 40:
+            new[8999] = 40
+        lens = [(i // 2) % 2 for i in range(n_seqs)]
+        t = sum(new)
+        q = _bf16(gen, t, 256)
+        k_pages, v_pages = _bf16(gen, n_seqs, 2, ps, 64), _bf16(gen, n_seqs, 2, ps, 64)
+        table = torch.randperm(n_seqs, device=DEV, generator=gen).to(torch.int32)[:, None].contiguous()
+        starts = _int32(_starts(new))
+        o = torch.full((t + 1, 256), 7.0, dtype=torch.bfloat16, device=DEV)
+        ctx.ensure_attention_workspace(h, t, n_seqs)
+        ctx.chunk_attention(h, q, starts, _int32(lens), most, B.paged_cache(k_pages, v_pages), table, o[:t])
+        last = (starts[1:] - 1).long()
+        want = torch.zeros_like(o[:t])
+        value = v_pages[table[:, 0].long(), :, 0].repeat_interleave(2, dim=1).reshape(n_seqs, 256)
+        want[last] = torch.where(_int32(lens)[:, None] > 0, value, torch.zeros_like(value))
+        assert torch.equal(o[:t].view(torch.int16), want.view(torch.int16)) and bool((o[t:] == 7.0).all()), most
+
+
+def test_chunk_rows_apart(ctx):
+    for h, new in ((H8B, [1, 1]), (H7B, [4, 2]), (H8B, [100, 3]), (H1B, [70, 1])):
+        c = Chunks(_heads(h), new, [5000, 77], page_size=64, seed=40)
+        w = c.q.shape[1]
+        q, o = torch.zeros((c.q.shape[0], w + 24), dtype=torch.bfloat16, device=DEV), torch.full((c.q.shape[0], w + 40), 7.0, dtype=torch.bfloat16, device=DEV)
+        q[:, 16:16 + w] = c.q
+        ctx.ensure_attention_workspace(c.h, c.q.shape[0], 2)
+        ctx.chunk_attention(c.h, q[:, 16:16 + w], c.starts, c.ctx_lens, c.max_chunk, c.cache, c.table, o[:, 8:8 + w], lse=c.lse)
+        assert bool((o[:, :8] == 7.0).all()) and bool((o[:, 8 + w:] == 7.0).all())
+        c.o = o[:, 8:8 + w].contiguous()
+        c.check(f"{h} {new} rows apart")
+
+
+@pytest.mark.parametrize("new", [[1, 1], [4, 2], [9, 8], [100, 3]], ids=str)
+def test_chunks_with_large_logits(ctx, new):
+    for h in (H8B, H1B):
+        c = Chunks(_heads(h, scale=3.0), new, [3000, 500], page_size=64, seed=41)
+        c.q *= 4.0
+        c.run(ctx)
+        c.check(f"{h} {new} large logits")
+
+
+def test_queries_that_are_not_finite_spoil_their_own_rows_only(ctx):
+    for h in (H8B, H1B):
+        for new in ([1, 1], [5, 2], [100, 40]):
+            c = Chunks(_heads(h), new, [3000, 500], page_size=64, seed=42)
+            c.run(ctx)
+            first, d = c.o.clone(), h[2]
+            c.q[1, d:d + 3] = float("nan")                     # head 1 of a token
+            c.q[-1, 5] = float("inf")                          # head 0 of another
+            c.run(ctx)
+            same = torch.ones_like(c.o, dtype=torch.bool)
+            same[1, d:2 * d] = same[-1, :d] = False
+            assert bool(torch.isnan(c.o[~same].float()).all()), f"{h} {new}"
+            assert torch.equal(c.o[same].view(torch.int16), first[same].view(torch.int16)), f"{h} {new}"
+
+
 def test_cache_beyond_32_bit_offsets(ctx):
     """Pages at the end of a cache of more than 4 GiB, in bytes and (2^31) in elements."""
     h, ps = _heads(H8B), 64

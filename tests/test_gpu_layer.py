@@ -305,6 +305,55 @@ def test_rotary_refusals(ctx):
     _refused(1, ctx.rotary, heads, spec, wide[:, :256], k, k, pos, wide.view(-1)[:768].view(3, 256), k_out=k)   # the input's place, other rows
 
 
+def test_captured_norms_and_rotary_positions_follow_their_inputs():
+    """Norm, rotary positions with the cache write and norm again on a stream of their own, captured once and replayed while
+    inputs, positions and slots change, with eager calls in between."""
+    stream = torch.cuda.Stream()
+    ctx = B.Context(0, stream)
+    try:
+        gen, t, d = _gen(11), 37, 512
+        heads, spec = B.Attention(4, 2, 64, 1, 0, 1.0), B.rotary(64, _freqs(64), interleaved=True)
+        h, y, qkv = _bf16(gen, t, d), _randn(gen, t, d), _bf16(gen, t, 512)
+        h_out, x, q_out, n = torch.zeros_like(h), torch.zeros_like(h), torch.zeros((t, 256), dtype=torch.bfloat16, device=DEV), _norm(gen, "layer", d, bias=True)
+        pages = [torch.zeros((6, 2, 8, 64), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        cache, pos, slots = B.paged_cache(*pages), torch.zeros((1, t), dtype=torch.int32, device=DEV), torch.zeros(t, dtype=torch.int32, device=DEV)
+        out = (h_out, x, q_out, *pages)
+
+        def run():
+            ctx.norm_residual(h, y, h_out, x, post=n, gate=h, pre=n, scale=0.5)
+            ctx.rotary(heads, spec, qkv[:, :256], qkv[:, 256:384], qkv[:, 384:], pos, q_out, cache=cache, slots=slots)
+
+        def draw():
+            for v in (h, y, qkv):
+                v.copy_(_randn(gen, *v.shape))
+            pos.copy_(torch.randint(0, 1 << 20, (1, t), device=DEV, generator=gen))
+            slots.copy_(torch.randperm(48, device=DEV, generator=gen)[:t])
+            for v in out:
+                v.zero_()
+            torch.cuda.synchronize()
+
+        draw()
+        run()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            run()
+        for rep in range(4):
+            draw()
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [v.clone() for v in out]
+            for v in out:
+                v.zero_()
+            torch.cuda.synchronize()
+            run()
+            stream.synchronize()
+            assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(got, out)), f"replay {rep}"
+    finally:
+        torch.cuda.synchronize()
+        ctx.close()
+
+
 # ------------------------------------------------------------------ a layer's calls together
 
 def test_a_layer_chunk_by_chunk_equals_the_whole_prompt_and_float64(ctx):
