@@ -1122,7 +1122,8 @@ struct Choice {
   long tiles = 0, few_tiles = 0;  // most tiles of each
   size_t bytes = 0;
 };
-Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int max_chunk, bool paged) {
+// `even`: a prompt's last tiles have not many more keys than the others.
+Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int max_chunk, bool paged, bool even) {
   Choice c;
   const int group = n_heads / n_kv;
   const long rows = (long)n_tokens * group, chunk_rows = (long)max_chunk * group, seqs = std::min(n_seqs, n_tokens);
@@ -1155,10 +1156,16 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
     return c;
   }
   const bool both = paged && n_seqs > 1 && group <= 16;     // sequences that generate one token beside chunks
-  // 256 rows where those give every CU more than one tile, 128 rows and two groups of keys below: half as many steps for the longest
-  // tile.  (One causal prompt, 8 key heads of 128 / 64, us with 128 and 256 rows: 1024 tokens 28 and 39 / 20 and 28, 2048 57 and 66 /
-  // 37 and 47, 4096 174 and 150 / 112 and 100; 13 packed prompts of 4099 tokens in all, heads of 64, 40 and 33.)
-  c.rw = rows / 256 * n_kv > 384 ? 8 : 4;
+  // 256 rows, or 128 rows and two groups of keys: half as many steps for the longest tile, but twice the tiles, and steps that take 1.4
+  // times as long.  256 rows where the others would be more than a tile for every CU, and where one causal prompt's longest tile takes as long as the
+  // launch, where they are themselves.  (us with 128 and 256 rows, 8 key heads of 128 / 64.  One causal prompt of 2048 tokens, 256
+  // tiles of 256 rows: 49 and 55 / 34 and 45, of 2560, 320 tiles, 79 and 70 / 53 and 54, of 4096 157 and 131 / 104 and 93.  In a window of
+  // 512, 1700 tokens, 208 tiles: 37 and 25 / 27 and 20.  Prompts of 512 tokens, two of them, 128 tiles: 18 and 22 / 12 and 16, six 42 and
+  // 31 / 27 and 19; 12 of 120, 176 tiles, 19 and 13 / 13 and 10; 100 and 1500 together, 200 tiles, which the host does not know, 35 and 41 / 25 and 34.
+  // Chunks over longer contexts, which are split along the keys below 192 or 384 tiles of 128 rows: heads of 128, three chunks of 900 tokens, 337
+  // tiles of 256, 79 and 70, two of 1100, 275 tiles, 106 and 97, six of 500, 375 tiles, 158 and 163; heads of 64, whose workgroups are two to a CU,
+  // three of 900 over 9000 keys 121 and 179.)
+  c.rw = rows / 256 * n_kv > (paged ? (head_dim == 128 ? 264 : 384) : even ? 128 : 264) ? 8 : 4;
   const int tile_rows = 32 * c.rw;
   c.tiles = rows / tile_rows + seqs;
   // Split into a piece for every CU where whole rows would leave many idle: partial sums written and joined cost some 6 us, and as much
@@ -1166,7 +1173,7 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
   // up to twice as many items.  (us in 256 pieces and whole, 8 key heads of 128: one chunk of 512 tokens over 8192 keys, 128 items,
   // 90 and 133; 1024 tokens, 256 items, 157 and 148.  Chunks of up to 500 of 8 heads of 64 with single tokens, 336 items, 76 and 85;
   // 24 sequences of up to 300 tokens, 590 items, 101 and 84.)
-  const long items = rows / tile_rows * n_kv;
+  const long items = rows / 128 * n_kv;
   const bool few_items = items < (n_seqs == 1 ? 192 : 384);
   set(c.tile, tile_rows, c.tiles, both ? 16 : 0, kAll, paged && few_items ? (n_seqs > 1 && head_dim == 64 ? 512 : 256) : 0, 4);
   if (both) {
@@ -1216,12 +1223,17 @@ size_t ff_attention_part_bytes(int n_heads, int n_kv, int head_dim, int n_tokens
   const int group = n_heads / n_kv;
   size_t most = 0;
   for (int rows : {1, 17, 33})
-    most = std::max(most, choose(n_heads, n_kv, head_dim, n_tokens, n_seqs, (rows + group - 1) / group, true).bytes);
+    most = std::max(most, choose(n_heads, n_kv, head_dim, n_tokens, n_seqs, (rows + group - 1) / group, true, false).bytes);
   return most;
 }
 
+static Choice choose(const AttnParams &p, int head_dim, int max_chunk) {
+  const bool even = !p.causal || p.n_seqs > 1 || (p.window > 0 && p.window < p.T);
+  return choose(p.n_heads, p.n_kv, head_dim, p.T, p.n_seqs, max_chunk, p.table != nullptr, even);
+}
+
 size_t ff_attention_need(const AttnParams &p, int head_dim, int max_chunk) {
-  return choose(p.n_heads, p.n_kv, head_dim, p.T, p.n_seqs, max_chunk, p.table != nullptr).bytes;
+  return choose(p, head_dim, max_chunk).bytes;
 }
 
 hipError_t ff_attention_init() {
@@ -1230,7 +1242,7 @@ hipError_t ff_attention_init() {
 }
 
 hipError_t ff_launch_attention(const AttnParams &p, int head_dim, int max_chunk, hipStream_t s) {
-  Choice c = choose(p.n_heads, p.n_kv, head_dim, p.T, p.n_seqs, max_chunk, p.table != nullptr);
+  Choice c = choose(p, head_dim, max_chunk);
   // Prompts' longest tiles first while a CU has a few tiles; with many, tiles of one sequence side by side share its keys in L2.  (us by
   // length and by sequence, causal, 8 key heads of 64 / 128: 13 prompts of up to 861 tokens, 616 tiles, 25.7 and 31.0 / 39.6 and
   // 45.7; 16 of 1024, 2176 tiles, 95 and 109 / 204 and 205; 32 of 1024, 4352 tiles, 210 and 214 / 406 and 397.  In a window of 300 the
