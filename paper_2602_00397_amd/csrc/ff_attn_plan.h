@@ -45,7 +45,8 @@ struct AttnParams {
 };
 constexpr int kAttnCounters = 16384, kAttnSeqs = 16384;   // most sequences of a call
 // One kernel's share of a call: the sequences with rows (new tokens times heads of a group) in (rows_above, rows_upto], in tiles of
-// tile_rows, split along the keys into about `target` pieces of at least min_steps times 64 keys (0: not split).
+// tile_rows, split along the keys into about `target` pieces of at least min_steps times 64 keys (0: not split).  join_here: a tile's last piece
+// joins them, no launch of its own.  by_tile: the tiles of all sequences by their number, the last first.
 struct AttnPlan {
   int64_t rows_above = 0, rows_upto = -1;
   int32_t tile_rows = 1, target = 0, min_steps = 1, max_items = 0, join_here = 0, by_tile = 0;
