@@ -127,6 +127,12 @@ __device__ __forceinline__ int count_items(const AttnParams &p, const AttnPlan &
   for (int g = lane; g < n_groups; g += 64) all += sums.items[g];
   return last_lane(lane_sums(min(all, kMostItems)));
 }
+// (rounded: the kernels of one call find the same, whatever the compiler could fuse the product with)
+__device__ __forceinline__ float lane_price(const AttnParams &p, const AttnPlan &pl, const Seq &q) {
+  float price = price_of(p, pl, q);
+  asm("" : "+v"(price));
+  return price;
+}
 // How long a piece is and how many (tile, piece) there are, from the work of the whole call; every wavefront of W finds the same.
 struct Cut { int keys, items; Seq first; };
 template <int W>
@@ -137,17 +143,18 @@ __device__ __forceinline__ Cut cut_of(const AttnParams &p, const AttnPlan &pl, S
   if (pl.target > 0) {
     float steps;
     if (__builtin_expect(p.n_seqs <= 64, 1)) {
-      steps = last_lane(lane_sums(price_of(p, pl, c.first)));
+      steps = last_lane(lane_sums(lane_price(p, pl, c.first)));
     } else {
-      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-      float mine = 0.f;
-      for (int s0 = wave * 64; s0 < p.n_seqs; s0 += 64 * W) mine += price_of(p, pl, lane_seq(p, s0, c.first));
-      mine = lane_sums(mine);
-      if (lane == 63) sums.items[wave] = __builtin_bit_cast(int, mine);
+      // (by 64 and then over those, so that kernels of more and of fewer wavefronts find the same sum in fp32)
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_groups = (p.n_seqs + 63) >> 6;
+      for (int g = wave; g < n_groups; g += W) {
+        const float sum = lane_sums(lane_price(p, pl, lane_seq(p, g * 64, c.first)));
+        if (lane == 63) sums.items[g] = __builtin_bit_cast(int, sum);
+      }
       __syncthreads();
-      steps = 0.f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) steps += __builtin_bit_cast(float, sums.items[w]);
+      float mine = 0.f;
+      for (int g = lane; g < n_groups; g += 64) mine += __builtin_bit_cast(float, sums.items[g]);
+      steps = last_lane(lane_sums(mine));
     }
     c.keys = __builtin_amdgcn_readfirstlane(piece_keys_for(p, pl, steps));
   }
