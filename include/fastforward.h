@@ -345,8 +345,11 @@ ff_status ff_rotary(ff_ctx *ctx, const ff_attention *a, const ff_rotary_spec *r,
                     const ff_paged_cache *cache, const int32_t *slots);
 
 /* Bytes of workspace that ff_chunk_attention needs at most (fp32 partial sums of
- * rows split along the keys), whatever the sequences' lengths and max_chunk are.
- * ff_prompt_attention needs none, nor do the two calls above. */
+ * rows split along the keys) with up to n_tokens tokens and up to n_seqs sequences,
+ * whatever these and the sequences' lengths and max_chunk are: a workspace for the
+ * largest call is enough for every smaller one, and need not be replaced while a
+ * graph holds its address.  ff_prompt_attention needs none, nor do the two calls
+ * above. */
 ff_status ff_attention_workspace_bytes(const ff_attention *a, int32_t n_tokens,
                                        int32_t n_seqs, size_t *bytes);
 

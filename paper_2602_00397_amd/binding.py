@@ -271,6 +271,8 @@ class Context:
         self._ensure(workspace_bytes(shape, k_max))
 
     def ensure_attention_workspace(self, heads: Attention, n_tokens: int, n_seqs: int):
+        """Enough for every chunk_attention call of up to so many tokens and sequences.  (A workspace that grows is another one:
+        captured graphs hold the address of the one that they were captured with.)"""
         self._ensure(attention_workspace_bytes(heads, n_tokens, n_seqs))
 
     def _ensure(self, need: int):

@@ -1122,6 +1122,17 @@ hipError_t raise_limits() {
   return e;
 }
 
+// One token's keys go to a piece for every CU, and no more: its pieces are joined by one workgroup.  Many tokens' are cut finer, for
+// their lengths differ.  (Heads of 128, us with 256 / 512 / 1024 pieces: 8 key heads, one token over
+// 8191 keys 15.9 / 15.9 / 15.8, over 32768 28.5 / 31.7 / 41.0; 48 tokens over up to 16384 137 / 97 / 94.)
+int few_target(long tiles, int n_kv) { return tiles * n_kv < 128 ? kFewGrid / 2 : 2 * kFewGrid; }
+// Items that a plan can have at most: about `target` pieces and one more for each of the tiles and key heads.
+long most_items(long tiles, int n_kv, int target) { return tiles * n_kv + target + 16; }
+size_t item_bytes(int tile_rows, int head_dim) { return (size_t)tile_rows * (head_dim + 2) * sizeof(float); }
+// Chunks with fewer (128-row tile, key head) than this are split along the keys (see choose).
+long few_items(long n_seqs) { return n_seqs == 1 ? 192 : 384; }
+int tile_target(long n_seqs, int head_dim) { return n_seqs > 1 && head_dim == 64 ? 512 : 256; }
+
 // How the call is cut.  rows of a sequence = new tokens times heads of a group.
 struct Choice {
   AttnPlan few, tile;
@@ -1135,30 +1146,25 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
   const int group = n_heads / n_kv;
   const long rows = (long)n_tokens * group, chunk_rows = (long)max_chunk * group, seqs = std::min(n_seqs, n_tokens);
   constexpr long kAll = 0x7fffffffffffL;
-  // Items that a plan can have at most: about `target` pieces and one more for each of the tiles and key heads.
   const auto set = [&](AttnPlan &pl, int tile_rows, long tiles, long above, long upto, int target, int min_steps) {
     pl.tile_rows = tile_rows;
     pl.rows_above = above;
     pl.rows_upto = upto;
     pl.min_steps = min_steps;
-    pl.target = tiles * n_kv + target + 16 <= kAttnCounters ? target : 0;
-    pl.max_items = (int)std::min<long>(tiles * n_kv + pl.target + 16, 0x7fffffff);   // (the price of a call is summed in fp32)
+    pl.target = most_items(tiles, n_kv, target) <= kAttnCounters ? target : 0;
+    pl.max_items = (int)std::min<long>(most_items(tiles, n_kv, pl.target), 0x7fffffff);   // (the price of a call is summed in fp32)
     pl.part_at = c.bytes / sizeof(float);
-    if (pl.target > 0) c.bytes += (size_t)pl.max_items * tile_rows * (head_dim + 2) * sizeof(float);
+    if (pl.target > 0) c.bytes += pl.max_items * item_bytes(tile_rows, head_dim);
   };
-  // One token's keys go to a piece for every CU, and no more: its pieces are joined by one workgroup.  Many tokens' are cut finer, for
-  // their lengths differ.  (Heads of 128, us with 256 / 512 / 1024 pieces: 8 key heads, one token over
-  // 8191 keys 15.9 / 15.9 / 15.8, over 32768 28.5 / 31.7 / 41.0; 48 tokens over up to 16384 137 / 97 / 94.)
-  const auto few_target = [&](long tiles) { return tiles * n_kv < 128 ? kFewGrid / 2 : 2 * kFewGrid; };
   // One workgroup joins a tile's pieces where these have few rows in all; a launch more costs 1 to 3 us, and many rows several times
   // that.  (us joined by the last piece and by a launch: 8 key heads, one token of 4 rows over 8191 keys 15.4 and 16.5, 32768 28.2 and
   // 31.1; 4 key heads, one token of 7 rows over 16384 keys 24.1 and 20.5, four tokens 56 and 24.)
-  const auto joins_here = [&](long tile_rows, long tiles) { return tile_rows <= 8 && tile_rows * few_target(tiles) <= 256 * tiles * n_kv; };
+  const auto joins_here = [&](long tile_rows, long tiles) { return tile_rows <= 8 && tile_rows * few_target(tiles, n_kv) <= 256 * tiles * n_kv; };
   // (the rows' own tiles and a part-filled one for each sequence)
   if (paged && chunk_rows <= 32) {
     c.nb = chunk_rows <= 16 ? 1 : 2;
     c.few_tiles = rows / (16 * c.nb) + seqs;
-    set(c.few, 16 * c.nb, c.few_tiles, 0, kAll, few_target(c.few_tiles), 4);
+    set(c.few, 16 * c.nb, c.few_tiles, 0, kAll, few_target(c.few_tiles, n_kv), 4);
     c.few.join_here = joins_here(chunk_rows, c.few_tiles);
     return c;
   }
@@ -1181,12 +1187,12 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
   // 90 and 133; 1024 tokens, 256 items, 157 and 148.  Chunks of up to 500 of 8 heads of 64 with single tokens, 336 items, 76 and 85;
   // 24 sequences of up to 300 tokens, 590 items, 101 and 84.)
   const long items = rows / 128 * n_kv;
-  const bool few_items = items < (n_seqs == 1 ? 192 : 384);
-  set(c.tile, tile_rows, c.tiles, both ? 16 : 0, kAll, paged && few_items ? (n_seqs > 1 && head_dim == 64 ? 512 : 256) : 0, 4);
+  const bool split = paged && items < few_items(n_seqs);
+  set(c.tile, tile_rows, c.tiles, both ? 16 : 0, kAll, split ? tile_target(n_seqs, head_dim) : 0, 4);
   if (both) {
     c.nb = 1;
     c.few_tiles = seqs;
-    set(c.few, 16, seqs, 0, 16, few_target(seqs), 4);
+    set(c.few, 16, seqs, 0, 16, few_target(seqs, n_kv), 4);
     c.few.join_here = joins_here(group, seqs);
   }
   return c;
@@ -1225,12 +1231,21 @@ hipError_t launch(const AttnParams &p, Choice &c, hipStream_t s) {
 
 }  // namespace
 
-// (whatever the longest chunk is: the most that any choice takes)
+// The most that any call of up to n_tokens tokens and n_seqs sequences takes, whatever its longest chunk is: more tokens or sequences
+// never have less, although a call of very many takes none (choose gives up its split where the items would be more than the counters).
 size_t ff_attention_part_bytes(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs) {
   const int group = n_heads / n_kv;
-  size_t most = 0;
-  for (int rows : {1, 17, 33})
-    most = std::max(most, choose(n_heads, n_kv, head_dim, n_tokens, n_seqs, (rows + group - 1) / group, true, false).bytes);
+  const long rows = (long)n_tokens * group, seqs = std::min(n_seqs, n_tokens);
+  // (a plan that is split has no more items than counters, and a call of fewer tiles no more than one of more)
+  const auto bytes = [&](long tiles, int target, int tile_rows) {
+    return std::min<long>(most_items(tiles, n_kv, target), kAttnCounters) * item_bytes(tile_rows, head_dim);
+  };
+  const auto few = [&](long tiles, int tile_rows) { return bytes(tiles, few_target(tiles, n_kv), tile_rows); };
+  // tiles of 128 rows, the only ones of calls that are split, beside sequences of at most 16 rows
+  const long whole = std::min(rows / 128, (few_items(n_seqs) - 1) / n_kv);
+  size_t most = bytes(whole + seqs, tile_target(n_seqs, head_dim), 128) + (n_seqs > 1 && group <= 16 ? few(seqs, 16) : 0);
+  if (group <= 16) most = std::max(most, few(rows / 16 + seqs, 16));
+  if (group <= 32) most = std::max(most, few(rows / 32 + seqs, 32));
   return most;
 }
 

@@ -479,6 +479,22 @@ static void check_attention() {
       for (int v : r) CHECK(f(v) == v / d, "%d / %d is not %d", v, d, f(v));
     }
   }
+  // A workspace for so many tokens and sequences holds every call of fewer, whatever its longest chunk is.
+  for (int round = 0; round < 40000; ++round) {
+    static const int groups[] = {1, 2, 4, 7, 16, 17, 32, 33, 128}, kvs[] = {1, 2, 4, 8, 32, 64};
+    const int group = groups[below(9)], n_kv = kvs[below(6)], hd = below(2) ? 64 : 128;
+    const int T = 1 + below(1 << below(18)), seqs = 1 + below(1 << below(15));
+    AttnParams p = {};
+    p.n_kv = n_kv; p.group = group; p.n_heads = n_kv * group;
+    p.table = g_idx;                                   // (never read: there is one)
+    p.causal = 1;
+    p.T = below(4) ? 1 + below(T) : T;
+    p.n_seqs = below(4) ? 1 + below(seqs) : seqs;
+    const int hint = below(2) ? 1 + below(std::min(p.T, 1 + 32 / group)) : 1 + below(p.T);
+    const size_t need = ff_attention_need(p, hd, hint), room = ff_attention_part_bytes(p.n_heads, n_kv, hd, T, seqs);
+    ++g_calls;
+    CHECK(need <= room, "group %d kv %d hd %d: %d tokens in %d sequences, hint %d, need %zu, room for %d and %d is %zu", group, n_kv, hd, p.T, p.n_seqs, hint, need, T, seqs, room);
+  }
   g_attn = true;
   for (int round = 0; round < 6000; ++round) {
     static const int groups[] = {1, 3, 4, 7, 8, 20};

@@ -60,6 +60,14 @@ def test_host_only_calls():
     assert B.load_library().ff_status_str(2) == b"unsupported shape"
 
 
+@pytest.mark.parametrize("heads", [(32, 8, 128), (28, 4, 128), (32, 8, 64), (64, 64, 128), (20, 1, 128), (40, 1, 64)])
+def test_attention_workspace_of_more_tokens_or_sequences_is_never_smaller(heads):
+    h = B.Attention(heads[0], heads[1], heads[2], 1, 0, 0.1)
+    tokens, seqs = (1, 3, 64, 512, 1000, 8192, 16384, 32768, 1 << 20), (1, 2, 48, 256, 1500, 16384)
+    need = np.array([[B.attention_workspace_bytes(h, t, s) for s in seqs] for t in tokens], dtype=np.int64)
+    assert (np.diff(need, axis=0) >= 0).all() and (np.diff(need, axis=1) >= 0).all(), need
+
+
 def test_library_depends_on_the_hip_runtime_only():
     """The boundary is plain C: the shared library needs the HIP runtime and the C/C++ runtimes,
     nothing of PyTorch or Python."""

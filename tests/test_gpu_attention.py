@@ -612,3 +612,21 @@ def test_a_call_after_chunks_that_overlap(ctx):
         good = Chunks(_heads(H8B), [1, 1], [9000, 5000], page_size=64, seed=37)
         good.run(ctx)
         good.check("after overlapping chunks")
+
+
+@pytest.mark.parametrize("h", [H8B, H7B, H1B, MHA], ids=lambda h: "%d_%d_%d" % h)
+def test_a_workspace_for_the_largest_call_is_enough_for_smaller_ones(h):
+    """Sized once, for calls that are not split themselves; a call of fewer tokens or sequences finds enough, and the workspace stays."""
+    ctx = B.Context(0)
+    try:
+        ctx.ensure_attention_workspace(_heads(h), 16384, 48)
+        ws = ctx._ws
+        for new, lens in (([1], [9000]), ([5], [3000]), ([130], [4000]), ([1] * 20, list(range(100, 2100, 100))), ([60, 1, 1], [2000, 900, 3000])):
+            c = Chunks(_heads(h), new, lens, page_size=64, seed=41)
+            ctx.chunk_attention(c.h, c.q, c.starts, c.ctx_lens, c.max_chunk, c.cache, c.table, c.o, lse=c.lse)
+            c.check(f"{h} in a workspace for more")
+            c.run(ctx)
+            assert ctx._ws is ws
+    finally:
+        torch.cuda.synchronize()
+        ctx.close()
