@@ -113,7 +113,9 @@ typedef struct {
 
 /* Creates a context bound to GPU `device` and to `hip_stream` (a hipStream_t,
  * NULL = the default stream).  Allocates only a small pinned staging ring and 64 KB
- * of counters on the GPU. */
+ * of counters on the GPU, whose clearing is queued on the stream: nothing is waited
+ * for, and a graph that is replayed on another stream comes behind it as behind any
+ * work of the context. */
 ff_status ff_create(ff_ctx **out, int device, void *hip_stream);
 ff_status ff_destroy(ff_ctx *ctx);
 /* Rebinds the context to another stream of the same device. */

@@ -530,6 +530,22 @@ const char *ff_status_str(int status) {
 
 const char *ff_last_error(const ff_ctx *ctx) { return ctx ? ctx->err : "context is NULL"; }
 
+// In front of the context's calls on its stream, so that creating a context waits for no work of the device.  Where a graph would
+// record that (or the stream may not be used while another one is recorded), on a stream of its own, done on return.
+static hipError_t zero_counters(ff_ctx *ctx) {
+  constexpr size_t bytes = kAttnCounters * sizeof(int32_t);
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(ctx->stream, &cap) == hipSuccess && cap == hipStreamCaptureStatusNone)
+    return hipMemsetAsync(ctx->counters, 0, bytes, ctx->stream);
+  hipStream_t own = nullptr;
+  hipError_t e = hipStreamCreateWithFlags(&own, hipStreamNonBlocking);
+  if (e != hipSuccess) return e;
+  e = hipMemsetAsync(ctx->counters, 0, bytes, own);
+  const hipError_t done = hipStreamSynchronize(own);
+  (void)hipStreamDestroy(own);
+  return e != hipSuccess ? e : done;
+}
+
 ff_status ff_create(ff_ctx **out, int device, void *hip_stream) {
   if (!out) return FF_ERR_INVALID_ARG;
   *out = nullptr;
@@ -571,7 +587,7 @@ ff_status ff_create(ff_ctx **out, int device, void *hip_stream) {
     if (hipMalloc(reinterpret_cast<void **>(&ctx->flag_dev), 256) != hipSuccess ||
         hipHostMalloc(reinterpret_cast<void **>(&ctx->flag_host), 256, hipHostMallocDefault) != hipSuccess ||
         hipMalloc(reinterpret_cast<void **>(&ctx->counters), kAttnCounters * sizeof(int32_t)) != hipSuccess ||
-        hipMemset(ctx->counters, 0, kAttnCounters * sizeof(int32_t)) != hipSuccess || hipDeviceSynchronize() != hipSuccess)
+        zero_counters(ctx) != hipSuccess)
       st = FF_ERR_DEVICE;
   } while (0);
   if (st != FF_OK) {

@@ -630,3 +630,52 @@ def test_a_workspace_for_the_largest_call_is_enough_for_smaller_ones(h):
     finally:
         torch.cuda.synchronize()
         ctx.close()
+
+
+def test_creating_a_context_waits_for_no_other_stream(ctx):
+    """Nor does it wait for its own; the counters are zero when its first call comes."""
+    tick = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    tick[0].record()
+    torch.cuda._sleep(1000000)
+    tick[1].record()
+    torch.cuda.synchronize()
+    cycles = int(1000000 * 300.0 / tick[0].elapsed_time(tick[1]))          # 0.3 s
+    c = Chunks(_heads(H8B), [1], [4000], seed=42)
+    torch.cuda.synchronize()
+    for busy, own in ((torch.cuda.Stream(), torch.cuda.Stream()), (torch.cuda.Stream(),) * 2, (torch.cuda.default_stream(),) * 2):
+        with torch.cuda.stream(busy):
+            torch.cuda._sleep(cycles)
+            done = torch.cuda.Event()
+            done.record()
+        fresh = B.Context(0, stream=own)
+        waited = done.query()
+        torch.cuda.synchronize()
+        assert not waited
+        with torch.cuda.stream(own):
+            c.o.fill_(7.0)
+            c.run(fresh)
+        torch.cuda.synchronize()
+        c.check("in a fresh context")
+        fresh.close()
+
+
+def test_a_context_created_while_its_stream_is_captured(ctx):
+    """In the mode that allows allocations; the graph holds nothing of it, and its first call may come before a replay."""
+    c, x = Chunks(_heads(H8B), [1], [4000], seed=43), torch.ones(1000, device=DEV)
+    graph, own = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=own, capture_error_mode="relaxed"):
+        x.add_(1)
+        fresh = B.Context(0, stream=own)
+    try:
+        for rep in range(3):
+            with torch.cuda.stream(own):
+                c.o.fill_(7.0)
+                c.run(fresh)
+                graph.replay()
+            torch.cuda.synchronize()
+            c.check(f"before replay {rep}")
+            assert bool((x == 2 + rep).all())
+    finally:
+        torch.cuda.synchronize()
+        fresh.close()
