@@ -95,9 +95,9 @@ ATTN_FN float price_of(const AttnParams &p, const AttnPlan &pl, const Seq &q) {
 }
 ATTN_FN int piece_keys_for(const AttnParams &p, const AttnPlan &pl, float steps) {
   const float per = ceilf(steps * (float)p.n_kv / (float)pl.target);
-  return attn_max(pl.min_steps, per < 1.0e6f ? (int)per : 1000000) * kTileKeys;
+  return attn_max(pl.min_steps, per < (float)(kMaxKeys / kTileKeys) ? (int)per : kMaxKeys / kTileKeys) * kTileKeys;
 }
-constexpr int kUnsplit = 0x40000000;
+constexpr int kUnsplit = kMaxKeys;
 // pieces that every tile of the sequence is given (a tile with fewer keys leaves its last ones empty)
 ATTN_FN int seq_pieces(const AttnParams &p, const AttnPlan &pl, const Seq &q, int keys_per_piece) {
   return attn_max(0, span_of(p, q.keys, pl.tile_rows) - 1) / keys_per_piece + 1;

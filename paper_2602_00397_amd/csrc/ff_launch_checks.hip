@@ -585,6 +585,44 @@ static void check_attention() {
   g_attn = false;
 }
 
+// The same for contexts of up to 2^30 keys (sequences may share pages): their pieces are as many as the launch has items.
+static void check_far_contexts() {
+  g_attn = true;
+  static float room[1];
+  for (int n_seqs : {1, 2, 48, 63, 400, 1500})
+    for (int keys : {1 << 20, 1 << 27, 1 << 30})
+      for (int group : {1, 4, 16})
+        for (int hint : {1, 8, 40}) {
+          std::vector<int32_t> starts(n_seqs + 1), lens(n_seqs, keys);
+          for (int s = 0; s <= n_seqs; ++s) starts[s] = s * hint;
+          AttnParams p = {};
+          p.T = n_seqs * hint; p.n_seqs = n_seqs; p.n_kv = 8; p.group = group; p.n_heads = 8 * group; p.n_pages = 10;
+          p.by_group = fast_div(group); p.by_kv = fast_div(8);
+          p.causal = 1;
+          p.page_shift = 12; p.table_stride = 1 << 18;
+          p.starts = starts.data(); p.lens = lens.data(); p.table = starts.data();     // (never read: there is one)
+          p.part = room;
+          p.part_bytes = ff_attention_part_bytes(p.n_heads, 8, 128, p.T, n_seqs);
+          g_log.clear();
+          ++g_calls;
+          CHECK(ff_launch_attention(p, 128, hint, nullptr) == hipSuccess && !g_log.empty(), "%d sequences", n_seqs);
+          for (const Launch &l : g_log) {
+            const AttnPlan &pl = l.plan;
+            float steps = 0.f;
+            for (int s = 0; s < n_seqs; ++s) steps += price_of(p, pl, seq_of(p, s));
+            const int kpp = pl.target > 0 ? piece_keys_for(p, pl, steps) : kUnsplit;
+            long items = 0;
+            for (int s = 0; s < n_seqs; ++s) {
+              const Seq q = seq_of(p, s);
+              items += (long)tiles_of(p, pl, q.n) * seq_pieces(p, pl, q, kpp);
+            }
+            CHECK(kpp > 0 && items * 8 <= pl.max_items, "%d sequences of %d keys, group %d, chunks of %d: pieces of %d keys, %ld items, room for %d", n_seqs, keys, group, hint, kpp,
+                  items * 8, pl.max_items);
+          }
+        }
+  g_attn = false;
+}
+
 int main() {
   if (ff_gemm_init(kLds) != hipSuccess) return 1;
   for (int T : {9, 70, 300, 700, 2000, 8192})
@@ -607,6 +645,7 @@ int main() {
   check_pooling();
   check_topk_map();
   check_attention();
+  check_far_contexts();
   printf("launch checks: %d calls, %d wrong\n", g_calls, g_fail);
   return g_fail != 0;
 }
