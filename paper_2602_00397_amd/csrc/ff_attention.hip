@@ -105,9 +105,7 @@ constexpr int kGroups = kAttnSeqs / 64;
 struct Sums { int items[kGroups]; };      // (tile, piece) of each 64 sequences
 __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 __device__ __forceinline__ float last_lane(float v) { return __builtin_bit_cast(float, last_lane(__builtin_bit_cast(int, v))); }
-// (tile, piece) of this lane's sequence.  Sums of 64 of these and of the sums stay in 32 bits, whatever the lengths are: each is held to
-// kMostItems, more than a call has whose tensors fit into the memory.
-constexpr int kMostItems = 1 << 24;
+// (tile, piece) of this lane's sequence.  Sums of 64 of these and of the sums stay in 32 bits, whatever the lengths are.
 __device__ __forceinline__ int lane_items(const AttnParams &p, const AttnPlan &pl, const Seq &q, int keys) {
   return (int)min((long)tiles_of(p, pl, q.n) * seq_pieces(p, pl, q, keys), (long)kMostItems);
 }
@@ -1160,8 +1158,9 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
   // that.  (us joined by the last piece and by a launch: 8 key heads, one token of 4 rows over 8191 keys 15.4 and 16.5, 32768 28.2 and
   // 31.1; 4 key heads, one token of 7 rows over 16384 keys 24.1 and 20.5, four tokens 56 and 24.)
   const auto joins_here = [&](long tile_rows, long tiles) { return tile_rows <= 8 && tile_rows * few_target(tiles, n_kv) <= 256 * tiles * n_kv; };
-  // (the rows' own tiles and a part-filled one for each sequence)
-  if (paged && chunk_rows <= 32) {
+  // (the rows' own tiles and a part-filled one for each sequence; a call with more of them than are counted has longer chunks than the host
+  // knows)
+  if (paged && chunk_rows <= 32 && rows / 16 + seqs <= kMostItems) {
     c.nb = chunk_rows <= 16 ? 1 : 2;
     c.few_tiles = rows / (16 * c.nb) + seqs;
     set(c.few, 16 * c.nb, c.few_tiles, 0, kAll, few_target(c.few_tiles, n_kv), 4);

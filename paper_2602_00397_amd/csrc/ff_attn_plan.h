@@ -44,6 +44,7 @@ struct AttnParams {
   int32_t *counters = nullptr;   // [kAttnCounters], zero: how many pieces of a tile have ended; zero again when the call has
 };
 constexpr int kAttnCounters = 16384, kAttnSeqs = 16384;   // most sequences of a call
+constexpr int kMostItems = 1 << 24;      // a sequence's (tile, piece), and all of a call's, are counted up to this number
 // One kernel's share of a call: the sequences with rows (new tokens times heads of a group) in (rows_above, rows_upto], in tiles of
 // tile_rows, split along the keys into about `target` pieces of at least min_steps times 64 keys (0: not split).  join_here: a tile's last piece
 // joins them, no launch of its own.  by_tile: the tiles of all sequences by their number, the last first.

@@ -623,6 +623,40 @@ static void check_far_contexts() {
   g_attn = false;
 }
 
+// Calls of up to 2^30 tokens, whatever the host took for the longest chunk: a sequence has no more tiles than a kernel counts.
+static void check_most_rows() {
+  g_attn = true;
+  static float room[1];
+  for (int heads : {1, 2, 5, 16})
+    for (int T = 1 << 20; T <= 1 << 30; T *= 2)
+      for (int hint : {1, 2, 16, 40, 1 << 20})
+        for (int n_seqs : {1, 2, 16384}) {
+          if ((long)T * heads > 0x7fff0000L) continue;
+          std::vector<int32_t> starts(n_seqs + 1, T), lens(n_seqs, 1000);
+          starts[0] = 0;
+          AttnParams p = {};
+          p.T = T; p.n_seqs = n_seqs; p.n_kv = 1; p.group = p.n_heads = heads; p.n_pages = 10;
+          p.by_group = fast_div(heads); p.by_kv = fast_div(1);
+          p.page_shift = 8; p.table_stride = 8;
+          p.starts = starts.data(); p.lens = lens.data(); p.table = starts.data();     // (never read: there is one)
+          p.part = room;
+          p.part_bytes = ff_attention_part_bytes(heads, 1, 64, T, n_seqs);
+          CHECK(ff_attention_need(p, 64, hint) <= p.part_bytes, "%d tokens, hint %d", T, hint);
+          g_log.clear();
+          ++g_calls;
+          CHECK(ff_launch_attention(p, 64, hint, nullptr) == hipSuccess && !g_log.empty(), "%d tokens, hint %d", T, hint);
+          long covered = 0;
+          for (const Launch &l : g_log) {
+            const AttnPlan &pl = l.plan;
+            const int tiles = tiles_of(p, pl, T);
+            CHECK(tiles <= kMostItems && tiles <= pl.max_items, "%d tokens of %d heads in %d sequences, hint %d: %d tiles, %d are counted", T, heads, n_seqs, hint, tiles, kMostItems);
+            covered += (long)tiles * pl.tile_rows;
+          }
+          CHECK(covered >= (long)T * heads && covered < (long)T * heads + 256, "%d tokens, hint %d: %ld rows", T, hint, covered);
+        }
+  g_attn = false;
+}
+
 int main() {
   if (ff_gemm_init(kLds) != hipSuccess) return 1;
   for (int T : {9, 70, 300, 700, 2000, 8192})
@@ -646,6 +680,7 @@ int main() {
   check_topk_map();
   check_attention();
   check_far_contexts();
+  check_most_rows();
   printf("launch checks: %d calls, %d wrong\n", g_calls, g_fail);
   return g_fail != 0;
 }
