@@ -366,7 +366,10 @@ ff_status ff_attention_workspace_bytes(const ff_attention *a, int32_t n_tokens,
  * Products and sums are fp32; the softmax weights are rounded to bf16 once, as
  * operands of the product with v; o is rounded once.  A row that sees no key
  * gets o = 0 and lse = -inf.  Values of keys that a row does not see never reach
- * it, infinities and NaN among them.  A call repeated on the same inputs gives
+ * it, infinities and NaN among them.  A channel in which a row sees an infinity is
+ * that infinity while the key's weight is above 2^-100 (NaN with a NaN or the
+ * opposite infinity beside it); of a smaller weight it is the infinity or NaN, by
+ * where the key lies, and never finite.  A call repeated on the same inputs gives
  * the same bits. */
 ff_status ff_prompt_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens,
                               int32_t n_seqs, const void *q, int64_t q_stride,

@@ -679,3 +679,43 @@ def test_a_context_created_while_its_stream_is_captured(ctx):
     finally:
         torch.cuda.synchronize()
         fresh.close()
+
+
+@pytest.mark.parametrize("nats", [60.0, 320.0], ids=["weights of e^-60", "weights of e^-320"])
+@pytest.mark.parametrize("h", [H8B, H1B], ids=lambda h: "%d_%d_%d" % h)
+def test_infinities_of_keys_with_small_weights(ctx, h, nats):
+    """One key takes nearly all the weight.  An infinity among the others' values is in the rows that see it, as itself where its weight
+    is 2^-87 and as itself or NaN where that underflows, in tiles that all rows see whole, at their edges, before and behind that key and in pieces
+    without it; other channels and rows are as without it."""
+    hd, inf = h[2], float("inf")
+
+    def check(o, lse, heads, q, k, v, what):
+        ref = _reference(heads, *(x.unflatten(1, (-1, hd)) if x.dim() == 2 else x for x in (q, k, v)))
+        got = o.double().reshape(ref[0].shape)
+        if nats > 88:
+            got = torch.where(torch.isnan(got) & torch.isinf(ref[0]), ref[0], got)
+        _check(got, lse, ref, hd, k.shape[0], what)
+
+    for causal, window in ((True, 0), (True, 300), (False, 0)):
+        p = Prompt(_heads(h, causal=causal, window=window, scale=1.0), [900], seed=44)
+        p.q.zero_()
+        p.k.zero_()
+        p.q[:, ::hd] = 1.0
+        p.k[400, ::hd] = nats
+        for channel, (key, x) in enumerate(((10, inf), (390, -inf), (399, inf), (401, inf), (600, -inf), (899, inf))):
+            p.v[key, channel::hd] = x
+        p.run(ctx)
+        check(p.o, p.lse, p.h, p.q, p.k, p.v, f"prompt, causal {causal}, window {window}")
+    for new, keys, window in ((1, 9000, 0), (3, 5000, 0), (8, 6000, 1500), (40, 4000, 0), (200, 4000, 0), (200, 4000, 1500)):
+        c = Chunks(_heads(h, window=window, scale=1.0), [new], [keys], page_size=64, seed=45)
+        c.q.zero_()
+        c.q[:, ::hd] = 1.0
+        c.k[0].zero_()
+        c.k[0][keys - 700, :, 0] = nats
+        for channel, key in enumerate((10, keys - 1400, keys - 701, keys - 699, keys - 300, keys - new - 1, keys - new, keys - 1)):
+            c.v[0][key, :, channel] = inf if channel % 2 else -inf
+        j = torch.arange(keys, device=DEV)
+        for pages, x in ((c.k_pages, c.k[0]), (c.v_pages, c.v[0])):
+            pages[c.table[0].long()[j // 64], :, j % 64] = x
+        c.run(ctx)
+        check(c.o, c.lse, c.h, c.q.unflatten(1, (-1, hd)), c.k[0], c.v[0], f"{new} tokens over {keys} keys, window {window}")
