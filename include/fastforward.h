@@ -142,7 +142,8 @@ ff_status ff_set_workspace(ff_ctx *ctx, void *dev_ptr, size_t bytes);
 /* Options: "validate" (0/1, default 0): ff_sparse_ffn first checks on the GPU
  * that every index row is ascending, in range and -1 padded, synchronises,
  * and returns FF_ERR_INDEX instead of launching if not (while the stream is
- * capturing a HIP graph the call returns FF_ERR_INVALID_ARG).  "small_path" (0/1,
+ * capturing a HIP graph the call returns FF_ERR_INVALID_ARG); ff_chunk_attention
+ * checks its starts, lengths and pages in the same way.  "small_path" (0/1,
  * default 1): calls with at most 8 tokens in total (the generation-time
  * regime) use gather-GEMV kernels, which read every selected weight row once
  * at HBM speed, instead of the MFMA tiles; 0 forces the tiles.
@@ -359,7 +360,9 @@ ff_status ff_attention_workspace_bytes(const ff_attention *a, int32_t n_tokens,
  * over the keys j of t's own sequence that a->causal and a->window leave it.
  *   q, k, v      dev bf16 [n_tokens] rows of n_heads, n_kv_heads, n_kv_heads heads
  *   seq_starts   dev int32 [n_seqs + 1], ascending: sequence s is rows
- *                [seq_starts[s], seq_starts[s + 1]), possibly none
+ *                [seq_starts[s], seq_starts[s + 1]), possibly none.  Entries are cut
+ *                to [0, n_tokens], a sequence that ends before it starts has no
+ *                rows, and what rows get that several sequences claim is open
  *   o            dev bf16 [n_tokens] rows of n_heads heads, out; rows of no
  *                sequence are left as they were
  *   lse_opt      dev f32 [n_tokens][n_heads] out, or NULL: log sum_j exp(scale q . k_j)
@@ -380,9 +383,11 @@ ff_status ff_prompt_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_toke
 /* The same for new tokens over a paged cache that holds their keys already: a
  * chunk of a prompt, a single generated token, or a batch of both.
  *   q             dev bf16 [n_tokens] rows of n_heads heads
- *   chunk_starts  dev int32 [n_seqs + 1]: rows of sequence s's new tokens
+ *   chunk_starts  dev int32 [n_seqs + 1]: rows of sequence s's new tokens (as
+ *                 seq_starts)
  *   context_lens  dev int32 [n_seqs]: keys of sequence s, the new tokens' own
- *                 (the last of them) included; cut to table_stride * page_size.
+ *                 (the last of them) included; cut to [0, table_stride * page_size]
+ *                 and 2^30.
  *                 With fewer keys than new tokens the first tokens see none.
  *   max_chunk     the longest chunk, as far as the host knows: it chooses the
  *                 kernels; other lengths are computed right too

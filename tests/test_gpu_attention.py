@@ -719,3 +719,62 @@ def test_infinities_of_keys_with_small_weights(ctx, h, nats):
             pages[c.table[0].long()[j // 64], :, j % 64] = x
         c.run(ctx)
         check(c.o, c.lse, c.h, c.q.unflatten(1, (-1, hd)), c.k[0], c.v[0], f"{new} tokens over {keys} keys, window {window}")
+
+
+def _clamped(starts, s, t):
+    t0 = min(max(starts[s], 0), t)
+    return t0, min(max(starts[s + 1], t0), t)
+
+
+@pytest.mark.parametrize("h", [H8B, H1B], ids=lambda h: "%d_%d_%d" % h)
+@pytest.mark.parametrize("new", [[1, 1], [7, 6], [40, 70], [200, 300]], ids=str)
+def test_what_is_out_of_range_is_clamped_and_touches_nothing_else(ctx, h, new):
+    """Starts, lengths and pages out of range against the clamped ones in float64; margins around the outputs and the cache stay."""
+    hd, qw, lens, t = h[2], h[0] * h[2], [100, 80], sum(new) + 3
+    for what, change in (("nothing", lambda c: None), ("page", lambda c: c.table[1, 0].fill_(1 << 30)), ("negative page", lambda c: c.table[1, 1].fill_(-5)),
+                         ("length", lambda c: c.ctx_lens[0].fill_(1 << 30)), ("negative length", lambda c: c.ctx_lens[0].fill_(-3)),
+                         ("end", lambda c: c.starts[2].fill_(1 << 30)), ("descending starts", lambda c: c.starts[1].fill_(-9)),
+                         ("start", lambda c: c.starts[0].fill_(-(1 << 31))), ("all behind", lambda c: c.starts.fill_(2147483647))):
+        c = Chunks(_heads(h), new, lens, unused=0.0, behind=3, seed=46)
+        change(c)
+        out, lse = torch.full((t + 16, qw + 16), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((t + 16, h[0]), 7.0, device=DEV)
+        c.o, c.lse = out[8:8 + t, 8:8 + qw], lse[8:8 + t]
+        pages = c.k_pages.clone(), c.v_pages.clone()
+        c.run(ctx)
+        torch.cuda.synchronize()
+        starts, n_keys, table = c.starts.tolist(), c.ctx_lens.tolist(), c.table.long()
+        table = torch.where((table < 0) | (table >= c.k_pages.shape[0]), 0, table)
+        left = torch.ones(t, dtype=torch.bool, device=DEV)
+        for s in range(2):
+            t0, t1 = _clamped(starts, s, t)
+            j = torch.arange(min(max(n_keys[s], 0), table.shape[1] * 16), device=DEV)
+            k, v = (x[table[s][j // 16], :, j % 16] for x in pages)
+            _check(c.o[t0:t1], c.lse[t0:t1], _reference(c.h, c.q[t0:t1].unflatten(1, (-1, hd)), k, v), hd, len(j), f"{h} {new} {what}, sequence {s}")
+            left[t0:t1] = False
+        assert bool((c.o[left] == 7.0).all()) and bool((c.lse[left] == 7.0).all()), f"{what}: rows of no sequence"
+        c.o.fill_(7.0)
+        c.lse.fill_(7.0)
+        assert bool((out == 7.0).all()) and bool((lse == 7.0).all()), f"{what}: around the outputs"
+        assert torch.equal(c.k_pages, pages[0]) and torch.equal(c.v_pages, pages[1]), f"{what}: the cache"
+
+
+@pytest.mark.parametrize("h", [H8B, H1B], ids=lambda h: "%d_%d_%d" % h)
+def test_prompts_with_starts_out_of_range(ctx, h):
+    hd, qw, t = h[2], h[0] * h[2], 330
+    for starts in ([-5, 130, 330], [0, 130, 1 << 30], [100, 40, 330], [-(1 << 31), 2147483647, 2147483647], [330, 400, 500], [200, 100, 50]):
+        p = Prompt(_heads(h), [130, 200], seed=47)
+        p.starts.copy_(_int32(starts))
+        out, lse = torch.full((t + 16, qw + 16), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((t + 16, h[0]), 7.0, device=DEV)
+        p.o, p.lse = out[8:8 + t, 8:8 + qw], lse[8:8 + t]
+        p.run(ctx)
+        torch.cuda.synchronize()
+        left = torch.ones(t, dtype=torch.bool, device=DEV)
+        for s in range(2):
+            t0, t1 = _clamped(starts, s, t)
+            part = [x[t0:t1].unflatten(1, (-1, hd)) for x in (p.q, p.k, p.v)]
+            _check(p.o[t0:t1], p.lse[t0:t1], _reference(p.h, *part), hd, t1 - t0, f"{h} starts {starts}, sequence {s}")
+            left[t0:t1] = False
+        assert bool((p.o[left] == 7.0).all()) and bool((p.lse[left] == 7.0).all()), f"{starts}: rows of no sequence"
+        p.o.fill_(7.0)
+        p.lse.fill_(7.0)
+        assert bool((out == 7.0).all()) and bool((lse == 7.0).all()), f"{starts}: around the outputs"
