@@ -263,7 +263,8 @@ ff_status ff_residual_add(ff_ctx *ctx, int32_t n_tokens, int32_t d_model,
 /* Heads of an attention layer and who sees whom.  Query head h reads key head
  * h / (n_heads / n_kv_heads).  Limits: head_dim 64 or 128, n_heads a multiple
  * of n_kv_heads and at most 1024, n_tokens at most 2^30 and n_tokens * n_heads
- * below 2^31 - 2^16, at most 16384 sequences (FF_ERR_SHAPE); scale > 0 and finite, window
+ * below 2^31 - 2^16, at most 16384 sequences (FF_ERR_SHAPE; from some 4000 of a few
+ * keys on, most of the time goes into finding each one's work); scale > 0 and finite, window
  * >= 0, a window only with causal (FF_ERR_INVALID_ARG). */
 typedef struct {
   int32_t n_heads;

@@ -744,6 +744,7 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
   for (int r = 0; r < 2; ++r) v_off[r] = chunk_at<HD>(half * 4 + (l16 >> 2) + 8 * r, (grp & 1) * 2 + ((l16 & 3) >> 1)) + (l16 & 1) * 8;
 
   // scores of the tile at key j -> weights, in the rows' running maximum's scale
+  // (see.lo <= see.hi also where the piece's end cuts the latter: a piece is longer than the limits of a tile's rows are apart)
   auto weights = [&](f32x16_t (&s)[2], int j, auto masked) __attribute__((always_inline)) {
     if (masked) {
 #pragma unroll
@@ -1122,10 +1123,11 @@ hipError_t raise_limits() {
 
 // One token's keys go to a piece for every CU, and no more: its pieces are joined by one workgroup.  Many tokens' are cut finer, for
 // their lengths differ.  (Heads of 128, us with 256 / 512 / 1024 pieces: 8 key heads, one token over
-// 8191 keys 15.9 / 15.9 / 15.8, over 32768 28.5 / 31.7 / 41.0; 48 tokens over up to 16384 137 / 97 / 94.)
+// 8191 keys, whose pieces were 256 / 128 / 64 keys long for it, 15.7 / 19.9 / 33.8, over 32768 28.6 / 32.0 / 44.3; 48 tokens over up to 16384 137 / 97 / 94.)
 int few_target(long tiles, int n_kv) { return tiles * n_kv < 128 ? kFewGrid / 2 : 2 * kFewGrid; }
 // Items that a plan can have at most: about `target` pieces and one more for each of the tiles and key heads.
 long most_items(long tiles, int n_kv, int target) { return tiles * n_kv + target + 16; }
+// (More items than counters: not split.  32768 keys among sequences of 200, 8 key heads of 128: 1400 tokens 273 us, 1600 670.)
 size_t item_bytes(int tile_rows, int head_dim) { return (size_t)tile_rows * (head_dim + 2) * sizeof(float); }
 // Chunks with fewer (128-row tile, key head) than this are split along the keys (see choose).
 long few_items(long n_seqs) { return n_seqs == 1 ? 192 : 384; }
