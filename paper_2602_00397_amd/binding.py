@@ -277,9 +277,8 @@ class Context:
 
     def _ensure(self, need: int):
         if self._ws is None or self._ws.numel() < need:
-            self._ws = None
-            self._ws = torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}")
-            self._check(self.lib.ff_set_workspace(self._h, _ptr(self._ws), self._ws.numel()))
+            self.set_workspace(None)                     # (its address must not stay if there is no memory for the next one)
+            self.set_workspace(torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}"))
 
     def set_workspace(self, ws: Optional[torch.Tensor]):
         self._ws = ws

@@ -778,3 +778,20 @@ def test_prompts_with_starts_out_of_range(ctx, h):
         p.o.fill_(7.0)
         p.lse.fill_(7.0)
         assert bool((out == 7.0).all()) and bool((lse == 7.0).all()), f"{starts}: around the outputs"
+
+
+def test_no_memory_for_a_larger_workspace(ctx):
+    """The one that there was is gone; a call that needs one is refused and does not write where it was."""
+    fresh = B.Context(0)
+    try:
+        c = Chunks(_heads(H8B), [1], [4000], seed=49)
+        c.run(fresh)
+        with pytest.raises(torch.OutOfMemoryError):
+            fresh._ensure(1 << 45)
+        _refused(5, fresh.chunk_attention, c.h, c.q, c.starts, c.ctx_lens, 1, c.cache, c.table, c.o)
+        c.o.fill_(7.0)
+        c.run(fresh)
+        c.check("in a workspace of its own again")
+    finally:
+        torch.cuda.synchronize()
+        fresh.close()
