@@ -240,8 +240,8 @@ class Context:
         self.lib = load_library()
         self.device = device
         self._h = C.c_void_p()
-        s = stream.cuda_stream if stream is not None else torch.cuda.current_stream(device).cuda_stream
-        st = self.lib.ff_create(C.byref(self._h), device, C.c_void_p(s))
+        self._stream = stream if stream is not None else torch.cuda.current_stream(device)
+        st = self.lib.ff_create(C.byref(self._h), device, C.c_void_p(self._stream.cuda_stream))
         if st:
             raise FFError(st, "ff_create: " + self.lib.ff_status_str(st).decode())
         self._ws = None
@@ -263,6 +263,7 @@ class Context:
 
     def set_stream(self, stream: torch.cuda.Stream):
         self._check(self.lib.ff_set_stream(self._h, C.c_void_p(stream.cuda_stream)))
+        self._stream = stream
 
     def set_option(self, name: str, value: int):
         self._check(self.lib.ff_set_option(self._h, name.encode(), int(value)))
@@ -277,7 +278,9 @@ class Context:
 
     def _ensure(self, need: int):
         if self._ws is None or self._ws.numel() < need:
-            self.set_workspace(None)                     # (its address must not stay if there is no memory for the next one)
+            if self._ws is not None:
+                self._ws.record_stream(self._stream)     # (calls in flight there still use it)
+            self.set_workspace(None)                     # (nor may its address stay if there is no memory for the next one)
             self.set_workspace(torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}"))
 
     def set_workspace(self, ws: Optional[torch.Tensor]):

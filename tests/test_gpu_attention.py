@@ -780,6 +780,29 @@ def test_prompts_with_starts_out_of_range(ctx, h):
         assert bool((out == 7.0).all()) and bool((lse == 7.0).all()), f"{starts}: around the outputs"
 
 
+def test_a_workspace_that_grows_leaves_calls_in_flight_alone():
+    """Its memory comes back when the context's stream is through with it, whatever stream it was allocated on."""
+    own = torch.cuda.Stream()
+    ctx = B.Context(0, stream=own)
+    try:
+        c = Chunks(_heads(H8B), [130], [4000], page_size=64, seed=48)
+        ctx.ensure_attention_workspace(c.h, 130, 1)
+        size = ctx._ws.numel()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(own):
+            torch.cuda._sleep(20000000)
+        ctx.chunk_attention(c.h, c.q, c.starts, c.ctx_lens, c.max_chunk, c.cache, c.table, c.o, lse=c.lse)
+        ctx.ensure_attention_workspace(c.h, 2048, 32)
+        assert ctx._ws.numel() > size
+        others = [torch.full((size,), 255, dtype=torch.uint8, device=DEV) for _ in range(2)]
+        torch.cuda.synchronize()
+        c.check("while the workspace grew")
+        del others
+    finally:
+        torch.cuda.synchronize()
+        ctx.close()
+
+
 def test_no_memory_for_a_larger_workspace(ctx):
     """The one that there was is gone; a call that needs one is refused and does not write where it was."""
     fresh = B.Context(0)
