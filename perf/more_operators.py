@@ -10,7 +10,7 @@ A case is a dict of plain values.  By its "op":
             query_block tokens (`keep` earlier pages to a block and key head, the first `first` of them always), and
             ff_selected_attention, over a bf16 cache (scale_tokens 0) or one in 8 bits
   "fork"    a step of a search: n_rows sequences of a page pool forked `beams` times each (ff_pages_fork), all of them grown by a
-            token (ff_pages_grow); `layers` of parts to a page: bf16 keys and values, or (eight) codes, exponents and means
+            token (ff_pages_grow); `layers` of parts to a page: bf16 keys and values, or (eight) codes, scales and means
   "compact" sequences end (ff_pages_free, every `ended`-th of n_rows) and the pages in use move together (ff_pages_compact)
 
 The last two begin each pass with the counts, tables and lengths that the program had before it.  Sizes are those of the benchmark
@@ -189,7 +189,7 @@ def _pairs(n, keys, causal, window):
 def _part_bytes(c):
     """Bytes of one page in every part of a layer."""
     n = c["kv_heads"] * c["page_size"] * c["head_dim"]
-    return [n, n, c["kv_heads"], c["kv_heads"], c["kv_heads"] * c["head_dim"] * 4] if c["eight"] else [2 * n, 2 * n]
+    return [n, n, c["kv_heads"] * 4, c["kv_heads"] * 4, c["kv_heads"] * c["head_dim"] * 4] if c["eight"] else [2 * n, 2 * n]
 
 
 def _pool_tables(c):
@@ -242,7 +242,7 @@ def work(case):
     if c["op"] == "append":
         return {"bytes": t * n_kv * hd * 6, "flops": 8 * t * n_kv * hd}
     code = 1 if c["scale_tokens"] else 2
-    scales = 2 * n_kv / c["scale_tokens"] if c["scale_tokens"] else 0
+    scales = 8 * n_kv / c["scale_tokens"] if c["scale_tokens"] else 0
     if c["op"] == "chunk8":
         keys = sum(min(k, n + c["window"] - 1) if c["window"] else k for n, k in zip(new, ctx))
         pairs = sum(_pairs(n, k, c["causal"], c["window"]) for n, k in zip(new, ctx))
@@ -299,13 +299,13 @@ def _prepare_sequences(c, gen, s):
     keys = _randn(gen, n_pages, n_kv, ps, hd).add_(_randn(gen, n_pages, n_kv, 1, hd)) * torch.exp(0.5 * _randn(gen, hd))
     values = _randn(gen, n_pages, n_kv, ps, hd)
     if st:
-        # a block's exponent is what its largest value asks for
+        # a block's scale is the power of two that its largest value asks for
         for name, x in (("k", keys), ("v", values)):
             x = x.view(n_pages, n_kv, ps // st, st * hd)
             m, e = torch.frexp(x.abs().amax(dim=3))
             e = e - 9 + (m > 0.875).int()
             s[name + "_pages"] = _codes(x * torch.exp2(-e.float())[..., None]).view(n_pages, n_kv, ps, hd)
-            s[name + "_exp"] = (e + 127).to(torch.uint8)
+            s[name + "_scale"] = torch.exp2(e.float())
     else:
         s["k_pages"], s["v_pages"] = keys.to(torch.bfloat16), values.to(torch.bfloat16)
     order = torch.randperm(n_pages, device=DEV, generator=gen).to(torch.int32)
@@ -331,7 +331,7 @@ def _prepare_pool(c, gen, s):
             x = torch.empty((n_pages, n_kv, ps, hd), dtype=torch.bfloat16, device=DEV).normal_(generator=gen)
             parts.append(_codes(x * 64) if c["eight"] else x)
         if c["eight"]:
-            parts += [torch.randint(110, 125, (n_pages, n_kv, 1), device=DEV, generator=gen).to(torch.uint8) for _ in range(2)]
+            parts += [torch.exp2(torch.randint(-17, -2, (n_pages, n_kv, 1), device=DEV, generator=gen).float()) for _ in range(2)]
             parts.append(_randn(gen, n_pages, n_kv, hd))
     s["parts"] = parts
     s["missing"] = _int32([-1])
@@ -366,7 +366,7 @@ def _prepare_own(c, s):
     n_tokens, n_seqs = s["q"].shape[0], c["n_seqs"]
     s["shape"] = B.Attention(c["heads"], c["kv_heads"], c["head_dim"], c.get("causal", True), c.get("window", 0), c["head_dim"] ** -0.5)
     if c["scale_tokens"]:
-        s["cache"] = B.paged_cache8(s["k_pages"], s["v_pages"], s["k_exp"], s["v_exp"])
+        s["cache"] = B.paged_cache8(s["k_pages"], s["v_pages"], s["k_scale"], s["v_scale"])
     else:
         s["cache"] = B.paged_cache(s["k_pages"], s["v_pages"])
     if c["op"] == "append":
@@ -398,7 +398,7 @@ def run(s):
 
 
 def _cache_of(s):
-    return {x: s[x] for x in ("k_pages", "v_pages", "k_exp", "v_exp")}
+    return {x: s[x] for x in ("k_pages", "v_pages", "k_scale", "v_scale")}
 
 
 def _pool_of(s):
@@ -445,27 +445,27 @@ def _plain_append(c, s):
     seq, pos = _tokens(c, s)
     page = s["table"][seq, pos // c["page_size"]].long()
     block, place = page * per_page + pos % c["page_size"] // st, pos % st
-    n_blocks = s["k_exp"].shape[0] * per_page
+    n_blocks = s["k_scale"].shape[0] * per_page
     # the new tokens' first place in each block that gets some
     first = torch.full((n_blocks,), st, device=DEV).scatter_reduce_(0, block, place, "amin")
     touched = torch.nonzero(first < st)[:, 0]
     tp, tb, tf = touched // per_page, touched % per_page, first[touched]
     for name in ("k", "v"):
         x = s[name].reshape(-1, n_kv, hd).float()
-        codes, exps = s[name + "_pages"].view(-1, n_kv, per_page, st, hd), s[name + "_exp"]
+        codes, scales = s[name + "_pages"].view(-1, n_kv, per_page, st, hd), s[name + "_scale"]
         top = torch.zeros((n_blocks, n_kv), device=DEV).scatter_reduce_(0, block[:, None].expand(-1, n_kv), x.abs().amax(dim=2), "amax")[touched]
         m, e = torch.frexp(top)
-        need = torch.where(top > 0, e - 9 + (m > 0.875).int(), torch.full_like(e, -110)).clamp(-110, 119)
-        old = exps[tp, :, tb].int() - 127
+        need = torch.where(top > 0, e - 9 + (m > 0.875).int(), torch.full_like(e, -110)).clamp(-110, 80)
+        need, old = torch.exp2(need.float()), scales[tp, :, tb]
         now = torch.where((tf == 0)[:, None], need, torch.maximum(old, need))
-        # older tokens of a block whose exponent grows
+        # older tokens of a block whose scale grows
         raw = codes.view(torch.uint8)[tp, :, tb].view(E4M3)
-        again = _codes(raw.float() * torch.exp2((old - now).float())[:, :, None, None])
+        again = _codes(raw.float() * (old / now)[:, :, None, None])
         kept = torch.arange(st, device=DEV) < tf[:, None]
         codes.view(torch.uint8)[tp, :, tb] = torch.where(kept[:, None, :, None], again.view(torch.uint8), raw.view(torch.uint8))
-        exps[tp, :, tb] = (now + 127).to(torch.uint8)
-        scale = torch.exp2(127.0 - exps[page, :, block % per_page].float())
-        codes.view(torch.uint8)[page, :, block % per_page, place] = _codes(x * scale[:, :, None]).view(torch.uint8)
+        scales[tp, :, tb] = now
+        scale = scales[page, :, block % per_page]
+        codes.view(torch.uint8)[page, :, block % per_page, place] = _codes(x / scale[:, :, None]).view(torch.uint8)
     return _cache_of(s)
 
 
@@ -473,9 +473,9 @@ def _gathered(c, s, name, pages):
     """Keys or values of pages [...][n], float32 [...][n * page_size][kv_heads][head_dim] (entries below 0: any page)."""
     pages = pages.clamp(min=0).long()
     if c["scale_tokens"]:
-        codes, exps = s[name + "_pages"].view(torch.uint8)[pages].view(E4M3).float(), s[name + "_exp"][pages]
+        codes, scales = s[name + "_pages"].view(torch.uint8)[pages].view(E4M3).float(), s[name + "_scale"][pages]
         shape = codes.shape
-        x = codes.view(*shape[:-2], -1, c["scale_tokens"], shape[-1]) * torch.exp2(exps.float() - 127.0)[..., None, None]
+        x = codes.view(*shape[:-2], -1, c["scale_tokens"], shape[-1]) * scales[..., None, None]
         x = x.view(shape)
     else:
         x = s[name + "_pages"][pages].float()
@@ -609,7 +609,7 @@ def _of_own_head(c, s, name, tables, head):
     if c["scale_tokens"]:
         x = s[name + "_pages"].view(torch.uint8)[pages, h].view(E4M3).float()
         shape = x.shape
-        scale = torch.exp2(s[name + "_exp"][pages, h].float() - 127.0)
+        scale = s[name + "_scale"][pages, h]
         x = (x.view(*shape[:3], -1, c["scale_tokens"], shape[-1]) * scale[..., None, None]).view(shape)
     else:
         x = s[name + "_pages"][pages, h].float()
@@ -691,22 +691,22 @@ def exact(case, seed):
 
 def _decoded(s, name):
     """The values that a cache stands for, from the codes' bits, float64 [n_pages][kv_heads][page_size][hd]."""
-    if name + "_exp" not in s:
+    if name + "_scale" not in s:
         return s[name + "_pages"].double()
     byte = s[name + "_pages"].view(torch.uint8).int()
     sign, e, m = 1 - 2 * (byte >> 7), (byte >> 3) & 15, byte & 7
     x = torch.ldexp(torch.where(e > 0, 8 + m, m).double() * sign, e.clamp(min=1) - 10)
-    exps = s[name + "_exp"].int() - 127
-    return torch.ldexp(x, exps.repeat_interleave(x.shape[2] // exps.shape[2], dim=2)[..., None])
+    scales = s[name + "_scale"].double()
+    return x * scales.repeat_interleave(x.shape[2] // scales.shape[2], dim=2)[..., None]
 
 
 def _exact_append(c, s):
-    """Codes before they are rounded to 8 bits, and the exponents."""
+    """Codes before they are rounded to 8 bits, and the scales."""
     st, hd, ps = c["scale_tokens"], c["head_dim"], c["page_size"]
     out = {}
     table = s["table"].tolist()
     for name in ("k", "v"):
-        exps = s[name + "_exp"].int() - 127
+        exps = torch.frexp(s[name + "_scale"])[1] - 1
         values = torch.ldexp(_decoded(s, name), -exps.repeat_interleave(st, dim=2)[..., None])
         new_all = s[name].double().reshape(-1, c["kv_heads"], hd).transpose(0, 1)
         t = 0
@@ -717,7 +717,7 @@ def _exact_append(c, s):
                 page, b, p = table[i][at // ps], at % ps // st, at % ps
                 x = new_all[:, t:t + end - at]
                 top = x.abs().amax(dim=(1, 2))
-                need = torch.where(top > 0, torch.ceil(torch.log2(top.clamp(min=1e-300) / 448.0)), -110.0).clamp(-110, 119).int()
+                need = torch.where(top > 0, torch.ceil(torch.log2(top.clamp(min=1e-300) / 448.0)), -110.0).clamp(-110, 80).int()
                 old = exps[page, :, b]
                 now = need if at % st == 0 else torch.maximum(old, need)
                 if at % st:
@@ -726,7 +726,7 @@ def _exact_append(c, s):
                 exps[page, :, b] = now
                 t += end - at
                 at = end
-        out[name + "_pages"], out[name + "_exp"] = values, (exps + 127).to(torch.uint8)
+        out[name + "_pages"], out[name + "_scale"] = values, torch.ldexp(torch.ones_like(exps, dtype=torch.float64), exps)
     return out
 
 
