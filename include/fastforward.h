@@ -284,6 +284,25 @@ typedef struct {
   int32_t page_size;
 } ff_paged_cache;
 
+/* The same in 8 bits: dev e4m3 [n_pages][n_kv_heads][page_size][head_dim] each (OCP
+ * e4m3: no infinities, 0x7f and 0xff are NaN), with a scale for every scale_tokens
+ * tokens of a page and head, dev f32 [n_pages][n_kv_heads][page_size / scale_tokens]
+ * each.  What is cached is code * scale.  Scales are powers of two from 2^-110 to
+ * 2^80, so that every such product is a bf16 number and attention's sums of them stay
+ * in fp32's range; of other scales only the exponent counts, products beyond bf16's
+ * range are infinite or lose digits, sums may be infinite, and a scale that is infinite or
+ * NaN makes NaN.  page_size is a power of two from 16 to
+ * 4096, scale_tokens one from 8 to 128 and at most page_size. */
+typedef struct {
+  void *k;
+  void *v;
+  float *k_scale;
+  float *v_scale;
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t scale_tokens;
+} ff_paged_cache8;
+
 /* Rotary positions.  Channel pair i of a head, 0 <= i < rot_dim / 2, turns by
  * the angle positions[axis[i]][token] * inv_freq[i] (the product and its
  * reduction are made in float64: far positions keep their digits).  Channels
@@ -405,6 +424,38 @@ ff_status ff_chunk_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_token
                              int32_t max_chunk, const ff_paged_cache *cache,
                              const int32_t *page_table, int32_t table_stride,
                              void *o, int64_t o_stride, float *lse_opt);
+
+/* Keys and values of new tokens into a cache in 8 bits, at the end of their
+ * sequences' (what rotary does for a bf16 cache; it turns k first, without a cache).
+ *   k, v          dev bf16 [n_tokens] rows of n_kv_heads heads (of a only the heads
+ *                 count)
+ *   chunk_starts, context_lens, page_table, table_stride   as for ff_chunk_attention:
+ *                 sequence s's new tokens are the last of its context_lens[s] keys.
+ *                 Tokens whose position would be negative, or whose page is outside
+ *                 [0, n_pages), are not written
+ * A block of scale_tokens tokens whose first place is written gets the least scale
+ * for which its largest value stays within 448 (2^-110 at least, 2^80 at most);
+ * one that is added to keeps the larger of its scale and that of the new tokens,
+ * and if it grows, the tokens before the new ones are rounded again with
+ * it.  Infinities and NaN become NaN and do not count for the scale; finite values beyond
+ * 448 * 2^80 become that.  Places behind the last new token are left as they are.  Two sequences of
+ * a call that add to the same page leave either's values in it, in part. */
+ff_status ff_cache8_append(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens,
+                           int32_t n_seqs, const void *k, int64_t k_stride,
+                           const void *v, int64_t v_stride,
+                           const int32_t *chunk_starts, const int32_t *context_lens,
+                           const ff_paged_cache8 *cache, const int32_t *page_table,
+                           int32_t table_stride);
+
+/* ff_chunk_attention over a cache in 8 bits: the same arguments otherwise, the same
+ * results as over a bf16 cache of the products code * scale, but for the order of
+ * fp32 sums.  Workspace: ff_attention_workspace_bytes. */
+ff_status ff_chunk_attention8(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens,
+                              int32_t n_seqs, const void *q, int64_t q_stride,
+                              const int32_t *chunk_starts, const int32_t *context_lens,
+                              int32_t max_chunk, const ff_paged_cache8 *cache,
+                              const int32_t *page_table, int32_t table_stride,
+                              void *o, int64_t o_stride, float *lse_opt);
 
 #ifdef __cplusplus
 }

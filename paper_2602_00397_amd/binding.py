@@ -50,6 +50,11 @@ class PagedCache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
 
 
+class PagedCache8(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("scale_tokens", C.c_int32)]
+
+
 class RotarySpec(C.Structure):
     _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32),
                 ("axis", C.POINTER(C.c_int32)), ("inv_freq", C.c_void_p)]
@@ -111,6 +116,9 @@ def load_library(build_if_missing: bool = True):
         "ff_prompt_attention": ([vp, P(Attention), i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp], C.c_int),
         "ff_chunk_attention": ([vp, P(Attention), i32, i32, vp, i64, vp, vp, i32, P(PagedCache), vp, i32, vp, i64,
                                 vp], C.c_int),
+        "ff_cache8_append": ([vp, P(Attention), i32, i32, vp, i64, vp, i64, vp, vp, P(PagedCache8), vp, i32], C.c_int),
+        "ff_chunk_attention8": ([vp, P(Attention), i32, i32, vp, i64, vp, vp, i32, P(PagedCache8), vp, i32, vp, i64,
+                                 vp], C.c_int),
         "ff_copy": ([vp, vp, vp, sz], C.c_int),
         "ff_mfma_peak": ([vp, i32, i32, P(C.c_double)], C.c_int),
     }
@@ -125,6 +133,7 @@ EXPORTS = ["ff_create", "ff_destroy", "ff_set_stream", "ff_status_str", "ff_last
            "ff_set_workspace", "ff_set_option", "ff_k_from_sparsity", "ff_layer_budgets", "ff_predict", "ff_predict_static",
            "ff_sparse_ffn", "ff_dense_ffn", "ff_ffn_stack", "ff_rmsnorm", "ff_residual_add",
            "ff_norm_residual", "ff_rotary", "ff_attention_workspace_bytes", "ff_prompt_attention", "ff_chunk_attention",
+           "ff_cache8_append", "ff_chunk_attention8",
            "ff_profile_enable", "ff_profile_read", "ff_copy", "ff_mfma_peak"]
 
 STAGES = ("pool", "mlp", "topk", "gemm1", "gemm2", "glue")
@@ -227,7 +236,20 @@ def paged_cache(k_pages: torch.Tensor, v_pages: torch.Tensor) -> PagedCache:
     return c
 
 
-def _check_pages(cache: PagedCache, heads: Attention):
+def paged_cache8(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor) -> PagedCache8:
+    """e4m3 [n_pages][n_kv_heads][page_size][head_dim] each, and float32 [n_pages][n_kv_heads][page_size / scale_tokens] each."""
+    assert k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_scale.dim() == 3
+    n_pages, n_kv, page_size, _ = k_pages.shape
+    blocks = k_scale.shape[2]
+    if blocks == 0 or page_size % blocks or k_scale.shape[:2] != (n_pages, n_kv):
+        raise AssertionError(f"scales {tuple(k_scale.shape)} do not go with pages {tuple(k_pages.shape)}")
+    c = PagedCache8(_typed(k_pages, torch.float8_e4m3fn), _typed(v_pages, torch.float8_e4m3fn), _typed(k_scale, torch.float32),
+                    _typed(v_scale, torch.float32, k_scale.shape), n_pages, page_size, page_size // blocks)
+    c.tensors = (k_pages, v_pages, k_scale, v_scale)
+    return c
+
+
+def _check_pages(cache, heads: Attention):
     _, n_kv, _, head_dim = cache.tensors[0].shape
     if n_kv != heads.n_kv_heads or head_dim != heads.head_dim:
         raise AssertionError(f"cache pages {tuple(cache.tensors[0].shape)} are not of {heads.n_kv_heads} heads of {heads.head_dim}")
@@ -374,6 +396,26 @@ class Context:
         n, qw, (n_seqs, table_stride) = q.shape[0], heads.n_heads * heads.head_dim, page_table.shape
         _check_pages(cache, heads)
         st = self.lib.ff_chunk_attention(
+            self._h, heads, n, n_seqs, *_rows(q, n, qw), _typed(chunk_starts, torch.int32, (n_seqs + 1,)),
+            _typed(context_lens, torch.int32, (n_seqs,)), max_chunk, cache, _typed(page_table, torch.int32), table_stride,
+            *_rows(o, n, qw), _typed(lse, torch.float32, (n, heads.n_heads)))
+        if st:
+            self._check(st)
+
+    def cache8_append(self, heads: Attention, k, v, chunk_starts, context_lens, cache: PagedCache8, page_table):
+        n, kw, (n_seqs, table_stride) = k.shape[0], heads.n_kv_heads * heads.head_dim, page_table.shape
+        _check_pages(cache, heads)
+        st = self.lib.ff_cache8_append(
+            self._h, heads, n, n_seqs, *_rows(k, n, kw), *_rows(v, n, kw), _typed(chunk_starts, torch.int32, (n_seqs + 1,)),
+            _typed(context_lens, torch.int32, (n_seqs,)), cache, _typed(page_table, torch.int32), table_stride)
+        if st:
+            self._check(st)
+
+    def chunk_attention8(self, heads: Attention, q, chunk_starts, context_lens, max_chunk: int, cache: PagedCache8,
+                         page_table, o, lse=None):
+        n, qw, (n_seqs, table_stride) = q.shape[0], heads.n_heads * heads.head_dim, page_table.shape
+        _check_pages(cache, heads)
+        st = self.lib.ff_chunk_attention8(
             self._h, heads, n, n_seqs, *_rows(q, n, qw), _typed(chunk_starts, torch.int32, (n_seqs + 1,)),
             _typed(context_lens, torch.int32, (n_seqs,)), max_chunk, cache, _typed(page_table, torch.int32), table_stride,
             *_rows(o, n, qw), _typed(lse, torch.float32, (n, heads.n_heads)))

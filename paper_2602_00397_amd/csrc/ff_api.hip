@@ -434,11 +434,15 @@ ff_status check_heads(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens) {
     return fail(ctx, FF_ERR_SHAPE, "more than 2^30 tokens, or about 2^31 rows (n_tokens * n_heads)");
   return FF_OK;
 }
+ff_status check_seqs(ff_ctx *ctx, int32_t n_seqs) {
+  if (n_seqs < 1) return fail(ctx, FF_ERR_INVALID_ARG, "sizes must be positive");
+  if (n_seqs > kAttnSeqs) return fail(ctx, FF_ERR_SHAPE, "more than %d sequences", kAttnSeqs);
+  return FF_OK;
+}
 ff_status check_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs) {
   ff_status st = check_heads(ctx, a, n_tokens);
   if (st != FF_OK) return st;
-  if (n_seqs < 1) return fail(ctx, FF_ERR_INVALID_ARG, "sizes must be positive");
-  if (n_seqs > kAttnSeqs) return fail(ctx, FF_ERR_SHAPE, "more than %d sequences", kAttnSeqs);
+  if ((st = check_seqs(ctx, n_seqs)) != FF_OK) return st;
   if (!(a->scale > 0.f) || std::isinf(a->scale)) return fail(ctx, FF_ERR_INVALID_ARG, "scale must be positive and finite");
   if (a->window < 0 || (a->window > 0 && !a->causal)) return fail(ctx, FF_ERR_INVALID_ARG, "a window (%d) is positive and goes with causal", a->window);
   return FF_OK;
@@ -456,6 +460,17 @@ ff_status check_cache(ff_ctx *ctx, const ff_paged_cache *c) {
   if (!aligned16(c->k) || !aligned16(c->v)) return fail(ctx, FF_ERR_ALIGNMENT, "cache pages must be 16-byte aligned");
   if (c->page_size < 8 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)))
     return fail(ctx, FF_ERR_SHAPE, "page_size (%d) must be a power of two from 8 to 4096", c->page_size);
+  return FF_OK;
+}
+bool is_power(int32_t v) { return v > 0 && (v & (v - 1)) == 0; }
+ff_status check_cache8(ff_ctx *ctx, const ff_paged_cache8 *c) {
+  if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || c->n_pages < 1) return fail(ctx, FF_ERR_INVALID_ARG, "no cache, or one without pages or scales");
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_scale) || !aligned16(c->v_scale))
+    return fail(ctx, FF_ERR_ALIGNMENT, "cache pages and scales must be 16-byte aligned");
+  if (!is_power(c->page_size) || c->page_size < 16 || c->page_size > 4096)
+    return fail(ctx, FF_ERR_SHAPE, "page_size (%d) must be a power of two from 16 to 4096", c->page_size);
+  if (!is_power(c->scale_tokens) || c->scale_tokens < 8 || c->scale_tokens > kMaxScaleTokens || c->scale_tokens > c->page_size)
+    return fail(ctx, FF_ERR_SHAPE, "scale_tokens (%d) must be a power of two from 8 to %d and at most page_size", c->scale_tokens, kMaxScaleTokens);
   return FF_OK;
 }
 ff_status check_norm(ff_ctx *ctx, const ff_norm *n, NormSpec *out) {
@@ -484,6 +499,67 @@ AttnParams attn_params(const ff_attention &a, int32_t n_tokens, int32_t n_seqs) 
   p.causal = a.causal != 0; p.window = a.window;
   p.scale_log2 = a.scale * 1.4426950408889634f;
   return p;
+}
+
+// New tokens of sequences whose keys are in pages: starts, lengths and tables (`tables` to a sequence: 1, or one for each key head).
+ff_status check_chunks(ff_ctx *ctx, const int32_t *starts, const int32_t *lens, const int32_t *table, int32_t table_stride) {
+  if (!starts || !lens || !table) return fail(ctx, FF_ERR_INVALID_ARG, "starts, lengths or page table is NULL");
+  if (!aligned16(starts) || !aligned16(lens) || !aligned16(table)) return fail(ctx, FF_ERR_ALIGNMENT, "starts / lengths / page table must be 16-byte aligned");
+  if (table_stride < 1) return fail(ctx, FF_ERR_INVALID_ARG, "table_stride (%d) must be positive", table_stride);
+  return FF_OK;
+}
+void set_chunks(AttnParams *p, const int32_t *starts, const int32_t *lens, const int32_t *table, int32_t table_stride, int tables) {
+  p->starts = starts; p->lens = lens; p->table = table; p->table_stride = table_stride;
+  p->seq_tables = (int64_t)tables * table_stride;
+  p->head_tables = tables > 1 ? table_stride : 0;
+}
+void set_cache(AttnParams *p, const ff_paged_cache &c) {
+  p->k = static_cast<const bf16_t *>(c.k); p->v = static_cast<const bf16_t *>(c.v);
+  p->page_shift = log2_of(c.page_size); p->n_pages = c.n_pages;
+}
+void set_cache8(AttnParams *p, const ff_paged_cache8 &c) {
+  p->k = static_cast<const bf16_t *>(c.k); p->v = static_cast<const bf16_t *>(c.v);      // (codes: one byte each)
+  p->k_scale = c.k_scale; p->v_scale = c.v_scale;
+  p->page_shift = log2_of(c.page_size); p->scale_shift = log2_of(c.scale_tokens); p->n_pages = c.n_pages;
+}
+// Attention over pages of either kind (one of the two is given); `tables` of page tables to a sequence.
+ff_status attend_pages(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs, const void *q, int64_t q_stride,
+                       const int32_t *starts, const int32_t *lens, int32_t max_chunk, const ff_paged_cache *cache, const ff_paged_cache8 *cache8,
+                       const int32_t *table, int32_t table_stride, int tables, void *o, int64_t o_stride, float *lse) {
+  ff_status st = check_attention(ctx, a, n_tokens, n_seqs);
+  if (st != FF_OK) return st;
+  const int64_t qw = (int64_t)a->n_heads * a->head_dim;
+  if ((st = check_rows(ctx, "q", q, q_stride, qw)) != FF_OK || (st = check_rows(ctx, "o", o, o_stride, qw)) != FF_OK) return st;
+  if ((st = cache8 ? check_cache8(ctx, cache8) : check_cache(ctx, cache)) != FF_OK) return st;
+  if ((st = check_chunks(ctx, starts, lens, table, table_stride)) != FF_OK) return st;
+  if (!aligned16(lse)) return fail(ctx, FF_ERR_ALIGNMENT, "lse must be 16-byte aligned");
+  if (max_chunk < 1 || max_chunk > n_tokens) return fail(ctx, FF_ERR_INVALID_ARG, "max_chunk (%d) must be in [1, n_tokens]", max_chunk);
+  AttnParams p = attn_params(*a, n_tokens, n_seqs);
+  p.q = static_cast<const bf16_t *>(q); p.o = static_cast<bf16_t *>(o); p.lse = lse;
+  p.q_stride = q_stride; p.o_stride = o_stride;
+  p.counters = ctx->counters;
+  if (cache8) set_cache8(&p, *cache8);
+  else set_cache(&p, *cache);
+  set_chunks(&p, starts, lens, table, table_stride, tables);
+  const size_t need = ff_attention_need(p, a->head_dim, max_chunk);
+  if (need > 0) {
+    if (!ctx->ws) return fail(ctx, FF_ERR_WORKSPACE, "no workspace set (ff_set_workspace)");
+    if (ctx->ws_bytes < need) return fail(ctx, FF_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", ctx->ws_bytes, need);
+    p.part = static_cast<float *>(ctx->ws);
+    p.part_bytes = ctx->ws_bytes;
+  }
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  if (ctx->validate) {
+    if ((st = begin_validate(ctx)) != FF_OK) return st;
+    FF_HIP(ctx, ff_launch_validate_pages(p, ctx->flag_dev, ctx->stream));
+    if ((st = read_flag(ctx)) != FF_OK) return st;
+    if (ctx->flag_host[0] != 0)
+      return fail(ctx, FF_ERR_INDEX, "sequence %d has a chunk, a length or a page out of range", ctx->flag_host[0] - 1);
+  }
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_attention(p, a->head_dim, max_chunk, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
 }
 
 ff_status check_weights(ff_ctx *ctx, const ff_ffn_weights *w) {
@@ -992,42 +1068,42 @@ ff_status ff_chunk_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_token
                              const int32_t *chunk_starts, const int32_t *context_lens, int32_t max_chunk, const ff_paged_cache *cache,
                              const int32_t *page_table, int32_t table_stride, void *o, int64_t o_stride, float *lse_opt) {
   if (!ctx) return FF_ERR_INVALID_ARG;
-  ff_status st = check_attention(ctx, a, n_tokens, n_seqs);
+  return attend_pages(ctx, a, n_tokens, n_seqs, q, q_stride, chunk_starts, context_lens, max_chunk, cache, nullptr, page_table, table_stride, 1,
+                      o, o_stride, lse_opt);
+}
+
+ff_status ff_cache8_append(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs, const void *k, int64_t k_stride,
+                           const void *v, int64_t v_stride, const int32_t *chunk_starts, const int32_t *context_lens,
+                           const ff_paged_cache8 *cache, const int32_t *page_table, int32_t table_stride) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_heads(ctx, a, n_tokens);
   if (st != FF_OK) return st;
-  const int64_t qw = (int64_t)a->n_heads * a->head_dim;
-  if ((st = check_rows(ctx, "q", q, q_stride, qw)) != FF_OK || (st = check_rows(ctx, "o", o, o_stride, qw)) != FF_OK) return st;
-  if ((st = check_cache(ctx, cache)) != FF_OK) return st;
-  if (!chunk_starts || !context_lens || !page_table) return fail(ctx, FF_ERR_INVALID_ARG, "chunk_starts, context_lens or page_table is NULL");
-  if (!aligned16(chunk_starts) || !aligned16(context_lens) || !aligned16(page_table) || !aligned16(lse_opt))
-    return fail(ctx, FF_ERR_ALIGNMENT, "chunk_starts / context_lens / page_table / lse must be 16-byte aligned");
-  if (max_chunk < 1 || max_chunk > n_tokens) return fail(ctx, FF_ERR_INVALID_ARG, "max_chunk (%d) must be in [1, n_tokens]", max_chunk);
-  if (table_stride < 1) return fail(ctx, FF_ERR_INVALID_ARG, "table_stride (%d) must be positive", table_stride);
-  AttnParams p = attn_params(*a, n_tokens, n_seqs);
-  p.q = static_cast<const bf16_t *>(q); p.k = static_cast<const bf16_t *>(cache->k); p.v = static_cast<const bf16_t *>(cache->v);
-  p.o = static_cast<bf16_t *>(o); p.lse = lse_opt;
-  p.starts = chunk_starts; p.lens = context_lens; p.table = page_table;
-  p.q_stride = q_stride; p.o_stride = o_stride;
-  p.counters = ctx->counters;
-  p.table_stride = table_stride; p.page_shift = log2_of(cache->page_size); p.n_pages = cache->n_pages;
-  const size_t need = ff_attention_need(p, a->head_dim, max_chunk);
-  if (need > 0) {
-    if (!ctx->ws) return fail(ctx, FF_ERR_WORKSPACE, "no workspace set (ff_set_workspace)");
-    if (ctx->ws_bytes < need) return fail(ctx, FF_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", ctx->ws_bytes, need);
-    p.part = static_cast<float *>(ctx->ws);
-    p.part_bytes = ctx->ws_bytes;
-  }
+  if ((st = check_seqs(ctx, n_seqs)) != FF_OK) return st;
+  const int64_t kw = (int64_t)a->n_kv_heads * a->head_dim;
+  if ((st = check_rows(ctx, "k", k, k_stride, kw)) != FF_OK || (st = check_rows(ctx, "v", v, v_stride, kw)) != FF_OK) return st;
+  if ((st = check_cache8(ctx, cache)) != FF_OK || (st = check_chunks(ctx, chunk_starts, context_lens, page_table, table_stride)) != FF_OK) return st;
+  Append8Params p = {};
+  p.seqs = attn_params(*a, n_tokens, n_seqs);
+  set_cache8(&p.seqs, *cache);
+  set_chunks(&p.seqs, chunk_starts, context_lens, page_table, table_stride, 1);
+  p.k = static_cast<const bf16_t *>(k); p.v = static_cast<const bf16_t *>(v);
+  p.k_stride = k_stride; p.v_stride = v_stride;
+  p.k_codes = static_cast<uint8_t *>(cache->k); p.v_codes = static_cast<uint8_t *>(cache->v);
+  p.k_scale = cache->k_scale; p.v_scale = cache->v_scale;
   FF_HIP(ctx, hipSetDevice(ctx->device));
-  if (ctx->validate) {
-    if ((st = begin_validate(ctx)) != FF_OK) return st;
-    FF_HIP(ctx, ff_launch_validate_pages(p, ctx->flag_dev, ctx->stream));
-    if ((st = read_flag(ctx)) != FF_OK) return st;
-    if (ctx->flag_host[0] != 0)
-      return fail(ctx, FF_ERR_INDEX, "sequence %d has a chunk, a length or a page out of range", ctx->flag_host[0] - 1);
-  }
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
-  FF_HIP(ctx, ff_launch_attention(p, a->head_dim, max_chunk, ctx->stream));
+  FF_HIP(ctx, ff_launch_append8(p, a->head_dim, ctx->stream));
   prof_end(&ctx->prof, ctx->stream);
   return FF_OK;
+}
+
+ff_status ff_chunk_attention8(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs, const void *q, int64_t q_stride,
+                              const int32_t *chunk_starts, const int32_t *context_lens, int32_t max_chunk, const ff_paged_cache8 *cache,
+                              const int32_t *page_table, int32_t table_stride, void *o, int64_t o_stride, float *lse_opt) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  if (!cache) return fail(ctx, FF_ERR_INVALID_ARG, "no cache, or one without pages or scales");
+  return attend_pages(ctx, a, n_tokens, n_seqs, q, q_stride, chunk_starts, context_lens, max_chunk, nullptr, cache, page_table, table_stride, 1,
+                      o, o_stride, lse_opt);
 }
 
 ff_status ff_copy(ff_ctx *ctx, void *dst, const void *src, size_t bytes) {

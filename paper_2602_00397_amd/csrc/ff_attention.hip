@@ -13,6 +13,7 @@
 // when it has grown by more than 2^8: the exponentials stay below 256, far from fp32's and bf16's limits, and most tiles
 // leave the sums as they are.  P is rounded to bf16 because the MFMA takes no wider operand; its row sum is kept in fp32 of the unrounded values.
 #include "ff_attn_plan.h"
+#include "ff_wave.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -25,6 +26,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+typedef __attribute__((ext_vector_type(2))) int32_t i32x2_t;
 
 constexpr float kNoMax = -3.0e38f;   // a row's maximum before its first key: finite, so no difference of two is a NaN
 constexpr float kLazy = 8.0f;
@@ -41,6 +43,10 @@ __device__ __forceinline__ u32x4_t lds_read16(uint32_t addr) {
 // 16 lanes read four rows of 16 values of 16 bits (lane i the 8 bytes at quarter i % 4 of row i / 4); lane i gets the rows' value i
 __device__ __forceinline__ u32x2_t lds_read_tr(uint32_t addr) {
   return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4_t *>(addr)));
+}
+// 16 lanes read eight rows of 16 bytes (lane i the 8 bytes at half i % 2 of row i / 2); lane i gets the rows' byte i
+__device__ __forceinline__ u32x2_t lds_read_tr8(uint32_t addr) {
+  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<__attribute__((address_space(3))) i32x2_t *>(addr)));
 }
 // asynchronous copy of 16 bytes per lane to LDS from a wave-uniform base and a 32-bit offset (see gload_lds16)
 __device__ __forceinline__ void gload_lds16_at(const void *base, uint32_t offset, uint32_t lds_addr) {
@@ -77,21 +83,6 @@ __device__ __forceinline__ void copied(int i, int lane, int &key, int &chunk) {
 
 // ---- which part of which sequence a workgroup computes -----------------------------------------------------------------
 
-// Running sums over the 64 lanes (lane 63: all of them), by DPP: some 8 cycles a step, where a shuffle through LDS takes over 100.
-template <int CTRL, int ROWS, class T>
-__device__ __forceinline__ T dpp(T v) {
-  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
-}
-template <class T>
-__device__ __forceinline__ T lane_sums(T v) {
-  v += dpp<0x111, 0xf>(v);     // the lane before in the row of 16, then 2, 4 and 8 before
-  v += dpp<0x112, 0xf>(v);
-  v += dpp<0x114, 0xf>(v);
-  v += dpp<0x118, 0xf>(v);
-  v += dpp<0x142, 0xa>(v);     // rows 1 and 3: the last lane of the row before
-  v += dpp<0x143, 0xc>(v);     // rows 2 and 3: lane 31
-  return v;
-}
 // Sequence number lane + s0, which the first 64 lanes of a call's sequences keep in `first`.
 __device__ __forceinline__ Seq lane_seq(const AttnParams &p, int s0, const Seq &first) {
   const int s = s0 + (threadIdx.x & 63);
@@ -103,8 +94,6 @@ __device__ __forceinline__ Seq lane_seq(const AttnParams &p, int s0, const Seq &
 // item, 311 so.)
 constexpr int kGroups = kAttnSeqs / 64;
 struct Sums { int items[kGroups]; };      // (tile, piece) of each 64 sequences
-__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
-__device__ __forceinline__ float last_lane(float v) { return __builtin_bit_cast(float, last_lane(__builtin_bit_cast(int, v))); }
 // (tile, piece) of this lane's sequence.  Sums of 64 of these and of the sums stay in 32 bits, whatever the lengths are.
 __device__ __forceinline__ int lane_items(const AttnParams &p, const AttnPlan &pl, const Seq &q, int keys) {
   return (int)min((long)tiles_of(p, pl, q.n) * seq_pieces(p, pl, q, keys), (long)kMostItems);
@@ -265,7 +254,11 @@ __device__ __forceinline__ int fresh_lane() {
   return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
 }
 
-// where keys lie
+// where keys lie: rows of a prompt, pages in bf16, pages in 8 bits
+enum Source { kRows, kPages, kPages8 };
+__device__ __forceinline__ const int32_t *table_of(const AttnParams &p, const Item &it) {
+  return p.table + it.s * p.seq_tables + (size_t)it.kvh * p.head_tables;
+}
 template <bool PAGED>
 struct KeySource {
   const bf16_t *k, *v;          // PAGED: the head's part of page 0; else the head's part of the sequence's first row
@@ -281,7 +274,7 @@ __device__ __forceinline__ KeySource<PAGED> key_source(const AttnParams &p, cons
     ks.k = p.k + (((size_t)it.kvh << p.page_shift) * HD);
     ks.v = p.v + (((size_t)it.kvh << p.page_shift) * HD);
     ks.page_elems = (uint32_t)((p.n_kv << p.page_shift) * HD);
-    ks.table = p.table + (size_t)it.s * p.table_stride;
+    ks.table = table_of(p, it);
     ks.n_pages = p.n_pages;
     ks.k_pitch = ks.v_pitch = HD * 2;
   } else {
@@ -333,8 +326,7 @@ struct Copier {
       }
       const uint8_t *base;
       if (PAGED) {
-        // (by a scalar load: the wait for it is not one for the copies before it)
-        int page = *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(ks.table + (key0 >> ks.shift)));
+        int page = scalar_load(ks.table + (key0 >> ks.shift));
         page = __builtin_amdgcn_readfirstlane((unsigned)page < (unsigned)ks.n_pages ? page : 0);
         base = reinterpret_cast<const uint8_t *>(src + (size_t)page * ks.page_elems) + (uint32_t)(key0 & ((1 << ks.shift) - 1)) * (HD * 2);
       } else {
@@ -342,6 +334,145 @@ struct Copier {
       }
       gload_lds16_at(base, off, lds + (first + i) * 1024);
     }
+  }
+};
+
+// infinities and NaN of a pair of bf16 values set to 0; `any` collects whether there were some
+__device__ __forceinline__ uint32_t finite_pair(uint32_t w, uint32_t &any) {
+  const uint32_t n = ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;     // an exponent of all ones carries into its half's top bit
+  any |= n;
+  return w & ~((n - (n >> 15)) | n);
+}
+__device__ __forceinline__ void bf16x4(const u32x2_t &w, float (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+// Pages in 8 bits: e4m3 codes with a power of two for every few keys of a page and head.  A code times that power has four bits of
+// mantissa, so it is exact in bf16, and the conversion that multiplies by it (v_cvt_scalef32_pk_bf16_fp8, two values at the
+// rate of an addition) is all that these kernels have beside the others'.
+struct Source8 {
+  const uint8_t *k, *v;        // the head's part of page 0
+  const float *ks, *vs;
+  const int32_t *table;
+  uint32_t page_bytes, page_scales;      // of all heads
+  int shift, scale_shift, n_pages;
+};
+template <int HD>
+__device__ __forceinline__ Source8 source8(const AttnParams &p, const Item &it) {
+  Source8 s;
+  s.shift = p.page_shift;
+  s.scale_shift = p.scale_shift;
+  s.k = reinterpret_cast<const uint8_t *>(p.k) + ((size_t)it.kvh << p.page_shift) * HD;
+  s.v = reinterpret_cast<const uint8_t *>(p.v) + ((size_t)it.kvh << p.page_shift) * HD;
+  s.ks = p.k_scale + ((size_t)it.kvh << (p.page_shift - p.scale_shift));
+  s.vs = p.v_scale + ((size_t)it.kvh << (p.page_shift - p.scale_shift));
+  s.page_bytes = (uint32_t)((p.n_kv << p.page_shift) * HD);
+  s.page_scales = (uint32_t)(p.n_kv << (p.page_shift - p.scale_shift));
+  s.table = table_of(p, it);
+  s.n_pages = p.n_pages;
+  return s;
+}
+// page and place of a wave-uniform key
+__device__ __forceinline__ int page_of(const Source8 &s, int key, int &place) {
+  const int page = scalar_load(s.table + (key >> s.shift));
+  place = key & ((1 << s.shift) - 1);
+  return __builtin_amdgcn_readfirstlane((unsigned)page < (unsigned)s.n_pages ? page : 0);
+}
+template <bool VALUES>
+__device__ __forceinline__ float scale8(const Source8 &s, int page, int place) {
+  return scalar_load((VALUES ? s.vs : s.ks) + (size_t)page * s.page_scales + (place >> s.scale_shift));
+}
+// the lower or upper two of four codes -> a pair of bf16
+template <bool UPPER>
+__device__ __forceinline__ uint32_t decode2(uint32_t codes, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, UPPER));
+}
+__device__ __forceinline__ u32x2_t decode4(uint32_t codes, float scale) { return u32x2_t{decode2<false>(codes, scale), decode2<true>(codes, scale)}; }
+__device__ __forceinline__ u32x4_t decode8(uint32_t a, uint32_t b, float scale) {
+  return u32x4_t{decode2<false>(a, scale), decode2<true>(a, scale), decode2<false>(b, scale), decode2<true>(b, scale)};
+}
+
+// Codes in LDS: 256-byte rows of 2 keys of head_dim 128 or 4 of 64, 16-byte chunks swizzled.  The places are different ones for chunk c
+// of the keys 8 a + b + {0 .. 3}, a = 0 .. 3, b = 0 or 4, which 16 lanes read for K, and of 16 neighbouring keys, which 32 lanes read for V.
+template <int HD>
+__device__ __forceinline__ int swizzle8(int r) {
+  return HD == 128 ? (r & 5) | ((r ^ (r >> 2)) & 2) : ((r ^ (r >> 2)) & 1) | (r & 2);
+}
+template <int HD>
+__device__ __forceinline__ uint32_t chunk8_at(int key, int c) {
+  constexpr int S = HD == 128 ? 1 : 2;            // log2 of the keys of a row
+  return (uint32_t)((key >> S) * 256 + (((((key & ((1 << S) - 1)) << (4 - S)) | c) ^ swizzle8<HD>(key >> S)) << 4));
+}
+// The copies of KEYS (32 or 64) keys in 8 bits to LDS, as one wavefront makes them, 1 KB (8 or 16 keys of one page) each, and their scales, one for
+// each 8 keys.
+template <int HD, int KEYS>
+struct Copier8 {
+  static constexpr int KPI = 1024 / HD, NI = KEYS / KPI;
+  Source8 src;
+  int end;
+  template <bool VALUES>
+  __device__ __forceinline__ void copy(int j, uint32_t lds, int lane, f32x4_t (&scale)[KEYS / 32]) const {
+    const bool full = j + KEYS <= end;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      constexpr int S = HD == 128 ? 1 : 2;
+      const int r = i * 4 + (lane >> 4), c = (lane & 15) ^ swizzle8<HD>(r);
+      const int in_copy = (r << S | c >> (4 - S)) - i * KPI, chunk = c & ((1 << (4 - S)) - 1);
+      const int key0 = full ? j + i * KPI : min(j + i * KPI, end - 1);
+      const int key = full ? in_copy : min(j + i * KPI + in_copy, end - 1) - key0;
+      int place;
+      const int page = page_of(src, key0, place);
+      const uint8_t *base = (VALUES ? src.v : src.k) + (size_t)page * src.page_bytes + (uint32_t)place * HD;
+      gload_lds16_at(base, (uint32_t)(key * HD + chunk * 16), lds + i * 1024);
+      // (key0 is the last key where the copy's keys lie behind it, and then the copy has nothing but it)
+#pragma unroll
+      for (int b = 0; b < KPI / 8; ++b) {
+        const int n = i * (KPI / 8) + b;
+        scale[n >> 2][n & 3] = scale8<VALUES>(src, page, (full ? place : place & -KPI) + b * 8);
+      }
+    }
+  }
+};
+// The keys and values of a tile of 64 on their way from pages in 8 bits to bf16 in LDS, as one of RW wavefronts brings them: NU times 8
+// channels of a key to a lane, 4 or 8 keys at a time, which share a page and a scale.
+template <int HD, int RW>
+struct Stager8 {
+  static constexpr int NU = HD / (8 * RW), KPC = 512 / HD;
+  Source8 src;
+  int first, end;
+  u32x2_t code[2][NU];
+  float scale[2][NU];
+  template <bool VALUES>
+  __device__ __forceinline__ void load(int j, int lane) {
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int at = j + (first + i) * KPC, key0 = min(at, end - 1);
+      const int key = min(at + lane / (HD / 8), end - 1) - key0;
+      int place;
+      const int page = page_of(src, key0, place);
+      scale[VALUES][i] = scale8<VALUES>(src, page, place);
+      const uint8_t *base = (VALUES ? src.v : src.k) + (size_t)page * src.page_bytes + (uint32_t)place * HD;
+      code[VALUES][i] = *reinterpret_cast<const u32x2_t *>(base + (uint32_t)(key * HD + lane % (HD / 8) * 8));
+    }
+  }
+  // `edge`: infinities and NaN become 0; returns whether there were some
+  template <bool VALUES>
+  __device__ __forceinline__ bool store(uint32_t lds, int lane, bool edge) const {
+    uint32_t odd = 0;
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      u32x4_t w = decode8(code[VALUES][i][0], code[VALUES][i][1], scale[VALUES][i]);
+      if (edge)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = finite_pair(w[e], odd);
+      const int key = (first + i) * KPC + lane / (HD / 8);
+      *reinterpret_cast<__attribute__((address_space(3))) u32x4_t *>(lds + chunk_at<HD>(key, lane % (HD / 8))) = w;
+    }
+    return odd != 0;
   }
 };
 
@@ -367,20 +498,6 @@ __device__ __forceinline__ f32x2_t with_row(float v) {
   return f32x2_t{__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
 __device__ __forceinline__ float larger(const f32x2_t &v) { return fmaxf(v[0], v[1]); }
-// infinities and NaN of a pair of bf16 values set to 0; `any` collects whether there were some
-__device__ __forceinline__ uint32_t finite_pair(uint32_t w, uint32_t &any) {
-  const uint32_t n = ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;     // an exponent of all ones carries into its half's top bit
-  any |= n;
-  return w & ~((n - (n >> 15)) | n);
-}
-__device__ __forceinline__ void bf16x4(const u32x2_t &w, float (&v)[4]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-
 // natural log of the sum that belongs to a maximum (in powers of two of the scaled products) and a sum
 __device__ __forceinline__ float lse_of(float m, float l) {
   return l > 0.f || l != l ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
@@ -404,10 +521,13 @@ __device__ __forceinline__ f32x2_t part_load(const float *at) {
   return __builtin_bit_cast(f32x2_t, __hip_atomic_load(reinterpret_cast<const uint64_t *>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 
-template <int HD, int NB>
+// Pages in 8 bits (EIGHT) come 64 keys at a time, as many bytes (32 where two sets' registers would not fit).  Lane (l16, quad) holds 16 channels of a key for two MFMAs, whose
+// channels are in that order in Q too, and eight neighbouring keys of a channel for V^T, by one transposing read.
+template <int HD, int NB, bool EIGHT>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnParams p, AttnPlan pl) {
-  constexpr int KS = HD / 32, DB = HD / 16, NI = 32 * HD * 2 / 1024;
-  constexpr uint32_t kHalf = 32 * HD * 2;
+  constexpr int KS = HD / 32, DB = HD / 16, SETS = EIGHT && !(HD == 128 && NB == 2) ? 2 : 1, KEYS = 32 * SETS;   // of a step, 32 to a set
+  constexpr int NI = KEYS * HD * (EIGHT ? 1 : 2) / 1024;
+  constexpr uint32_t kHalf = 32 * HD * 2, kSet = 32 * HD;
   constexpr int kRows = 16 * NB, kPitch = HD + 4, kBatch = 16;
   extern __shared__ __align__(256) uint8_t lds[];
   __shared__ int last_s;
@@ -415,12 +535,20 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l16 = lane & 15, quad = lane >> 4;
   const uint32_t k_at = lds_addr_of(lds) + wave * 2 * kHalf, v_at = k_at + kHalf;
-  // where this lane's operands lie in a tile (the swizzle repeats after 16 keys)
+  // where this lane's operands lie in a tile (the swizzle repeats after 16 keys, that of codes after 32)
   uint32_t k_off[KS], v_off[DB];
 #pragma unroll
-  for (int c = 0; c < KS; ++c) k_off[c] = k_at + chunk_at<HD>(l16, c * 4 + quad);
+  for (int c = 0; c < KS; ++c) {
+    if (EIGHT) k_off[c] = k_at + chunk8_at<HD>((l16 >> 2) * 8 + (l16 & 3) + (c & 1) * 4, (c >> 1) * 4 + quad);      // chunk c / 2 of the two keys
+    else k_off[c] = k_at + chunk_at<HD>(l16, c * 4 + quad);
+  }
 #pragma unroll
-  for (int d = 0; d < DB; ++d) v_off[d] = v_at + chunk_at<HD>(quad * 4 + (l16 >> 2), d * 2 + ((l16 & 3) >> 1)) + (l16 & 1) * 8;
+  for (int d = 0; d < DB; ++d) {
+    if (EIGHT) v_off[d] = v_at + chunk8_at<HD>(quad * 8 + (l16 >> 1), d) + (l16 & 1) * 8;
+    else v_off[d] = v_at + chunk_at<HD>(quad * 4 + (l16 >> 2), d * 2 + ((l16 & 3) >> 1)) + (l16 & 1) * 8;
+  }
+  // key x of this lane's eight scores of a set
+  const auto key_of = [&](int set, int x) { return EIGHT ? set * 32 + quad * 8 + x : (x >> 2) * 16 + quad * 4 + (x & 3); };
 
   const Cut cut = cut_of<kFewWaves>(p, pl, sums_s);
   const int n_items = items_of(p, pl, cut);
@@ -432,7 +560,24 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
     const int n_pieces = pieces_of(range, cut.keys);
     if (it.piece >= n_pieces) continue;
     const int beg = range.lo + it.piece * cut.keys, end = range.hi - beg > cut.keys ? beg + cut.keys : range.hi;
-    const Copier<HD, true, NI, 32> copier(key_source<HD, true>(p, it), 0, end, lane);
+    std::conditional_t<EIGHT, Copier8<HD, KEYS>, Copier<HD, true, NI, 32>> copier = [&] {
+      if constexpr (EIGHT) return Copier8<HD, KEYS>{source8<HD>(p, it), end};
+      else return Copier<HD, true, NI, 32>(key_source<HD, true>(p, it), 0, end, lane);
+    }();
+    [[maybe_unused]] f32x4_t k_scale[SETS], v_scale[SETS];        // of each eight keys on their way
+    const auto copy_k = [&](int j) __attribute__((always_inline)) {
+      if constexpr (EIGHT) copier.template copy<false>(j, k_at, lane, k_scale);
+      else copier.template copy<false>(j, k_at, lane);
+    };
+    const auto copy_v = [&](int j) __attribute__((always_inline)) {
+      if constexpr (EIGHT) copier.template copy<true>(j, v_at, lane, v_scale);
+      else copier.template copy<true>(j, v_at, lane);
+    };
+    // of those, that of the eight keys that are number b of a set
+    const auto pick = [](f32x4_t scale, int b) __attribute__((always_inline)) {
+      const float lo = b & 1 ? scale[1] : scale[0], hi = b & 1 ? scale[3] : scale[2];
+      return b & 2 ? hi : lo;
+    };
 
     // the rows' own limits, and the part of the tile's keys that all of them see
     Range see[NB];
@@ -445,12 +590,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
       see[b].hi = min(see[b].hi, end);
       all_lo = max(all_lo, see[b].lo);
       all_hi = min(all_hi, see[b].hi);
-      const bf16_t *src = p.q + row_token(p, it.seq, r) * p.q_stride + row_head(p, it.kvh, r) * HD + quad * 8;
+      const bf16_t *src = p.q + row_token(p, it.seq, r) * p.q_stride + row_head(p, it.kvh, r) * HD;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) q[b][s] = *reinterpret_cast<const u32x4_t *>(src + s * 32);
+      for (int s = 0; s < KS; ++s)
+        q[b][s] = *reinterpret_cast<const u32x4_t *>(src + (EIGHT ? (s >> 1) * 64 + quad * 16 + (s & 1) * 8 : s * 32 + quad * 8));
     }
-    int j = beg + wave * 32;
-    if (j < end) copier.template copy<false>(j, k_at, lane);
+    int j = beg + wave * KEYS;
+    if (j < end) copy_k(j);
 #pragma unroll
     for (int off = 8; off > 0; off >>= 1) {
       all_lo = max(all_lo, __shfl_xor(all_lo, off));
@@ -462,7 +608,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[b][s]));   // (arrived: no wait for it among the copies' later on)
-    if (j < end) copier.template copy<true>(j, v_at, lane);
+    if (j < end) copy_v(j);
 
     f32x4_t o[NB][DB];
     float m[NB], l[NB];
@@ -473,41 +619,57 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
 #pragma unroll
       for (int d = 0; d < DB; ++d) o[b][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    for (; j < end; j += 32 * kFewWaves) {
-      const bool more = j + 32 * kFewWaves < end;
+    for (; j < end; j += KEYS * kFewWaves) {
+      const bool more = j + KEYS * kFewWaves < end;
       wait_copies<NI>();                    // K is here, V on its way
-      // S^T: 32 keys by the rows
-      f32x4_t s[NB][2];
-      u32x4_t kf[2][KS];
+      // S^T: the keys of each set, 16 and 16, by the rows
+      f32x4_t s[NB][SETS][2];
+      u32x4_t kf[SETS][2][EIGHT ? KS / 2 : KS];
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+      for (int set = 0; set < SETS; ++set)
 #pragma unroll
-        for (int c = 0; c < KS; ++c) kf[kt][c] = lds_read16(k_off[c] + kt * 16 * HD * 2);
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int c = 0; c < (EIGHT ? KS / 2 : KS); ++c)
+            kf[set][kt][c] = EIGHT ? lds_read16(k_off[c * 2 + kt] + set * kSet) : lds_read16(k_off[c] + kt * 16 * HD * 2);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K is in registers: its place is free
-      if (more) copier.template copy<false>(j + 32 * kFewWaves, k_at, lane);
+      float ks[SETS];
+      if constexpr (EIGHT)
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+        for (int set = 0; set < SETS; ++set) ks[set] = pick(k_scale[set], l16 >> 2);
+      if (more) copy_k(j + KEYS * kFewWaves);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          s[b][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int set = 0; set < SETS; ++set)
 #pragma unroll
-          for (int c = 0; c < KS; ++c) s[b][kt] = mfma16(kf[kt][c], q[b][c], s[b][kt]);
+        for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) s[b][set][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < KS; ++c) {
+            const u32x4_t f = kf[set][kt][EIGHT ? c / 2 : c];
+            const u32x4_t a = EIGHT ? decode8(f[c % 2 * 2], f[c % 2 * 2 + 1], ks[set]) : f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) s[b][set][kt] = mfma16(a, q[b][c], s[b][set][kt]);
+          }
         }
-      const bool masked = j < all_lo || j + 32 > all_hi;
-      u32x4_t pk[NB];
+      const bool masked = j < all_lo || j + KEYS > all_hi;
+      u32x4_t pk[NB][SETS];
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        if (masked) {
+        float mx = -INFINITY;
 #pragma unroll
-          for (int kt = 0; kt < 2; ++kt)
+        for (int set = 0; set < SETS; ++set) {
+          if (masked) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int key = j + kt * 16 + quad * 4 + i;
-              s[b][kt][i] = key >= see[b].lo && key < see[b].hi ? s[b][kt][i] : -INFINITY;
+            for (int x = 0; x < 8; ++x) {
+              const int key = j + key_of(set, x);
+              s[b][set][x >> 2][x & 3] = key >= see[b].lo && key < see[b].hi ? s[b][set][x >> 2][x & 3] : -INFINITY;
             }
+          }
+          const float most = fmaxf(fmaxf(fmaxf(s[b][set][0][0], s[b][set][0][1]), fmaxf(s[b][set][0][2], s[b][set][0][3])),
+                                   fmaxf(fmaxf(s[b][set][1][0], s[b][set][1][1]), fmaxf(s[b][set][1][2], s[b][set][1][3])));
+          mx = set == 0 ? most : fmaxf(mx, most);
         }
-        float mx = fmaxf(fmaxf(fmaxf(s[b][0][0], s[b][0][1]), fmaxf(s[b][0][2], s[b][0][3])),
-                         fmaxf(fmaxf(s[b][1][0], s[b][1][1]), fmaxf(s[b][1][2], s[b][1][3])));
         mx = larger(with_half(larger(with_row(mx)))) * p.scale_log2;
         if (__any(mx > m[b] + kLazy)) {
           const float m_new = fmaxf(m[b], mx), a = __builtin_amdgcn_exp2f(m[b] - m_new);
@@ -518,42 +680,74 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[b][d][i] *= a;
         }
-        float e[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          e[x] = __builtin_amdgcn_exp2f(fmaf(s[b][x >> 2][x & 3], p.scale_log2, -m[b]));
-          l[b] += e[x];
+        for (int set = 0; set < SETS; ++set) {
+          float e[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            e[x] = __builtin_amdgcn_exp2f(fmaf(s[b][set][x >> 2][x & 3], p.scale_log2, -m[b]));
+            l[b] += e[x];
+          }
+          pk[b][set] = u32x4_t{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
         }
-        pk[b] = u32x4_t{pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])};
       }
       if (more) wait_copies<NI>();          // V is here, the next K on its way
       else wait_copies<0>();
       // O^T += V^T P^T
+      [[maybe_unused]] float vs[SETS];
+      if constexpr (EIGHT)
+#pragma unroll
+        for (int set = 0; set < SETS; ++set) vs[set] = pick(v_scale[set], quad);
+      const auto values = [&](int set, int d) __attribute__((always_inline)) {
+        if constexpr (EIGHT) {
+          const u32x2_t v = lds_read_tr8(v_off[d] + set * kSet);
+          return decode8(v[0], v[1], vs[set]);
+        } else {
+          const u32x2_t v0 = lds_read_tr(v_off[d]), v1 = lds_read_tr(v_off[d] + 16 * HD * 2);
+          return u32x4_t{v0[0], v0[1], v1[0], v1[1]};
+        }
+      };
       if (!masked) {
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const u32x2_t v0 = lds_read_tr(v_off[d]), v1 = lds_read_tr(v_off[d] + 16 * HD * 2);
-          const u32x4_t vf = {v0[0], v0[1], v1[0], v1[1]};
+        for (int set = 0; set < SETS; ++set)
 #pragma unroll
-          for (int b = 0; b < NB; ++b) o[b][d] = mfma16(vf, pk[b], o[b][d]);
-        }
+          for (int d = 0; d < DB; ++d) {
+            const u32x4_t vf = values(set, d);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) o[b][d] = mfma16(vf, pk[b][set], o[b][d]);
+          }
       } else {
         uint32_t odd = 0;
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const u32x2_t v0 = lds_read_tr(v_off[d]), v1 = lds_read_tr(v_off[d] + 16 * HD * 2);
-          const u32x4_t vf = {finite_pair(v0[0], odd), finite_pair(v0[1], odd), finite_pair(v1[0], odd), finite_pair(v1[1], odd)};
+        for (int set = 0; set < SETS; ++set)
 #pragma unroll
-          for (int b = 0; b < NB; ++b) o[b][d] = mfma16(vf, pk[b], o[b][d]);
-        }
+          for (int d = 0; d < DB; ++d) {
+            u32x4_t vf = values(set, d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vf[e] = finite_pair(vf[e], odd);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) o[b][d] = mfma16(vf, pk[b][set], o[b][d]);
+          }
         if (__any(odd != 0)) {
           // infinities and NaN among the values (0 in the product): they reach the rows that see their key, and no other
 #pragma unroll 1
-          for (int x = 0; x < 32; ++x) {
+          for (int x = 0; x < KEYS; ++x) {
+            [[maybe_unused]] float scale = 1.f;
+            if constexpr (EIGHT) {
+              int place;
+              const int page = page_of(copier.src, min(j + x, end - 1), place);
+              scale = scale8<true>(copier.src, page, place);
+            }
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
               float v[4];
-              const u32x2_t w = *reinterpret_cast<const __attribute__((address_space(3))) u32x2_t *>(v_at + chunk_at<HD>(x, d * 2 + (quad >> 1)) + (quad & 1) * 8);
+              u32x2_t w;
+              if constexpr (EIGHT) {
+                const uint32_t codes = *reinterpret_cast<const __attribute__((address_space(3))) uint32_t *>(v_at + chunk8_at<HD>(x, d) + quad * 4);
+                w = decode4(codes, scale);
+              } else {
+                w = *reinterpret_cast<const __attribute__((address_space(3))) u32x2_t *>(v_at + chunk_at<HD>(x, d * 2 + (quad >> 1)) + (quad & 1) * 8);
+              }
               bf16x4(w, v);
 #pragma unroll
               for (int b = 0; b < NB; ++b)
@@ -566,7 +760,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
         }
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V is in registers
-      if (more) copier.template copy<true>(j + 32 * kFewWaves, v_at, lane);
+      if (more) copy_v(j + KEYS * kFewWaves);
     }
 
     // join the four wavefronts' sums
@@ -679,8 +873,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
 // channels the second four make the softmax of tile i at the start of step i + 1, so their exponentials go through the vector unit while
 // the matrix pipe works for the first four, and the other way round (8192 tokens of 32 heads over 8 key heads of 128, causal, 520 us
 // without turns, 500 with); elsewhere they drift apart by themselves, and MFMAs have priority.
-template <int HD, int RW, int KW, bool PAGED>
-__global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 2) void ff_attn_tile_kernel(AttnParams p, AttnPlan pl) {
+// Pages in 8 bits go through registers: asked for at a step's start, turned into bf16 and written to their place in LDS at its end.
+template <int HD, int RW, int KW, Source SRC>
+__global__ __launch_bounds__(RW * KW * 64, HD == 64 && (SRC != kRows || KW == 1) ? 4 : 2) void ff_attn_tile_kernel(AttnParams p, AttnPlan pl) {
+  constexpr bool PAGED = SRC != kRows, EIGHT = SRC == kPages8;
   constexpr int KS = HD / 16, DB = HD / 32, NI = kTileKeys * HD * 2 / 1024 / RW;
   constexpr uint32_t kHalf = kTileKeys * HD * 2;
   constexpr int kRows = 32 * RW, kStep = kTileKeys * KW;
@@ -701,11 +897,22 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
   const int n_pieces = pieces_of(range, kpp);
   if (it.piece >= n_pieces) return;
   const int beg = range.lo + it.piece * kpp, end = range.hi - beg > kpp ? beg + kpp : range.hi;
-  const Copier<HD, PAGED, NI, kTileKeys> copier(key_source<HD, PAGED>(p, it), wave * NI, end, lane);
+  std::conditional_t<EIGHT, Stager8<HD, RW>, const Copier<HD, PAGED, NI, kTileKeys>> copier = [&] {
+    if constexpr (EIGHT) return Stager8<HD, RW>{source8<HD>(p, it), wave * (HD / (8 * RW)), end};
+    else return Copier<HD, PAGED, NI, kTileKeys>(key_source<HD, PAGED>(p, it), wave * NI, end, lane);
+  }();
+  const auto copy_k = [&](int j, uint32_t to) __attribute__((always_inline)) {
+    if constexpr (EIGHT) copier.template load<false>(j, lane);
+    else copier.template copy<false>(j, to, lane);
+  };
+  const auto copy_v = [&](int j, uint32_t to) __attribute__((always_inline)) {
+    if constexpr (EIGHT) copier.template load<true>(j, lane);
+    else copier.template copy<true>(j, to, lane);
+  };
   const uint32_t ring_k = lds_addr_of(lds) + kw * 4 * kHalf, ring_v = ring_k + 2 * kHalf;
 
   // (out before the rows' own arithmetic and loads)
-  if (beg + kw * kTileKeys < end) copier.template copy<false>(beg + kw * kTileKeys, ring_k, lane);
+  if (beg + kw * kTileKeys < end) copy_k(beg + kw * kTileKeys, ring_k);
   Range see;
   u32x4_t q[KS];
   {
@@ -781,14 +988,28 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
     const int far = fresh_lane() >> 5;
 #pragma unroll 1
     for (int key = j; key < min(j + kTileKeys, end); ++key) {
-      const bf16_t *src = copier.value(key) + far * 4;
       const bool seen = key >= see.lo && key < see.hi;
+      [[maybe_unused]] const bf16_t *src = nullptr;
+      [[maybe_unused]] const uint8_t *codes = nullptr;
+      [[maybe_unused]] float scale = 1.f;
+      if constexpr (EIGHT) {
+        int place;
+        const int page = page_of(copier.src, key, place);
+        scale = scale8<true>(copier.src, page, place);
+        codes = copier.src.v + (size_t)page * copier.src.page_bytes + (uint32_t)place * HD + far * 4;
+      } else {
+        src = copier.value(key) + far * 4;
+      }
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           float v[4];
-          bf16x4(*reinterpret_cast<const u32x2_t *>(src + d * 32 + g * 8), v);
+          if constexpr (EIGHT) {
+            bf16x4(decode4(*reinterpret_cast<const uint32_t *>(codes + d * 32 + g * 8), scale), v);
+          } else {
+            bf16x4(*reinterpret_cast<const u32x2_t *>(src + d * 32 + g * 8), v);
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (seen && !(fabsf(v[i]) < INFINITY)) o[d][g * 4 + i] += v[i];
@@ -835,11 +1056,14 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
     // step i - 1 read, and have landed when it ends.  (Past the end there are none, but a tile that ends behind it is copied whole:
     // the last key again.)
     const auto begin = [&](int j, uint32_t at) __attribute__((always_inline)) {
-      if (j + kStep < end) copier.template copy<false>(j + kStep, ring_k + (kHalf - at), lane);
-      if (j < end) copier.template copy<true>(j, ring_v + at, lane);
+      if (j + kStep < end) copy_k(j + kStep, ring_k + (kHalf - at));
+      if (j < end) copy_v(j, ring_v + at);
     };
     const auto step_end = [&](int j, uint32_t at) __attribute__((always_inline)) {
-      if (is_edge(j) && j < end) {
+      if constexpr (EIGHT) {
+        if (j + kStep < end) copier.template store<false>(ring_k + (kHalf - at), lane, false);
+        if (j < end && copier.template store<true>(ring_v + at, lane, is_edge(j))) odd_tile[at != 0] = j;
+      } else if (is_edge(j) && j < end) {
         wait_copies<0>();
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
@@ -862,6 +1086,8 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
     const int last = beg + (end - beg + kStep - 1) / kStep * kStep + kw * kTileKeys;
     uint32_t at = 0;
     if (threadIdx.x < 2 * KW) odd_s[threadIdx.x >> 1][threadIdx.x & 1] = -1;
+    if constexpr (EIGHT)
+      if (start < end) copier.template store<false>(ring_k, lane, false);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     const auto is_inner = [&](int j) { return j > start && !is_edge(j - kStep) && !is_edge(j) && j + kStep < end; };
     for (int j = start;; j += kStep, at = kHalf - at) {
@@ -871,14 +1097,18 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (PAGED || KW == 1) ? 4 : 
         const bool late = HD == 128 && RW == 8 && wave >= 4;
         bool have = false;
         do {
-          copier.template copy<false>(j + kStep, ring_k + (kHalf - at), lane);
-          copier.template copy<true>(j, ring_v + at, lane);
+          copy_k(j + kStep, ring_k + (kHalf - at));
+          copy_v(j, ring_v + at);
           if (late && have) weights(s, j, std::false_type());
           have = true;
           __builtin_amdgcn_s_setprio(1);
           products(s, ring_v + kHalf - at, ring_k + at, std::true_type(), std::true_type());
           __builtin_amdgcn_s_setprio(0);
           if (!late) weights(s, j, std::false_type());
+          if constexpr (EIGHT) {
+            copier.template store<false>(ring_k + (kHalf - at), lane, false);
+            copier.template store<true>(ring_v + at, lane, false);
+          }
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
           j += kStep;
           at = kHalf - at;
@@ -1080,16 +1310,17 @@ __global__ __launch_bounds__(256) void ff_attn_join_rows_kernel(AttnParams p, At
   if (lane == 0 && p.lse) p.lse[t * p.n_heads + head] = lse_of(top, sum);
 }
 
-// one wavefront per sequence
+// one wavefront per sequence and table
 __global__ __launch_bounds__(64) void ff_attn_validate_kernel(AttnParams p, int32_t *flag) {
   const int s = blockIdx.x, lane = threadIdx.x;
+  const int32_t *table = p.table + s * p.seq_tables + (size_t)blockIdx.y * p.head_tables;
   const int a = p.starts[s], b = p.starts[s + 1];
   bool bad = a < 0 || b < a || b > p.T || p.lens[s] < 0 || p.lens[s] > most_keys(p);
   const Seq q = seq_of(p, s);
   const int first = p.window > 0 ? max(0, q.keys - q.n + 1 - min(p.window, kMaxKeys)) >> p.page_shift : 0;
   const int pages = q.n > 0 ? (int)(((long)q.keys + (1 << p.page_shift) - 1) >> p.page_shift) : 0;
   for (int i = first + lane; i < pages; i += 64) {
-    const int page = p.table[(size_t)s * p.table_stride + i];
+    const int page = table[i];
     bad = bad || page < 0 || page >= p.n_pages;
   }
   if (__any(bad) && lane == 0) atomicMax(flag, s + 1);
@@ -1112,12 +1343,19 @@ hipError_t raise_limits() {
   auto raise = [&](const void *fn, size_t lds) {
     if (e == hipSuccess) e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   };
-  raise(reinterpret_cast<const void *>(ff_attn_few_kernel<HD, 1>), few_lds(HD, 1));
-  raise(reinterpret_cast<const void *>(ff_attn_few_kernel<HD, 2>), few_lds(HD, 2));
-  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 4, 2, true>), tile_lds(HD, 4, 2));
-  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 8, 1, true>), tile_lds(HD, 8, 1));
-  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 4, 2, false>), tile_lds(HD, 4, 2));
-  raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 8, 1, false>), tile_lds(HD, 8, 1));
+  const auto few = [&](auto eight) {
+    raise(reinterpret_cast<const void *>(ff_attn_few_kernel<HD, 1, eight()>), few_lds(HD, 1));
+    raise(reinterpret_cast<const void *>(ff_attn_few_kernel<HD, 2, eight()>), few_lds(HD, 2));
+  };
+  const auto tile = [&](auto src) {
+    raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 4, 2, src()>), tile_lds(HD, 4, 2));
+    raise(reinterpret_cast<const void *>(ff_attn_tile_kernel<HD, 8, 1, src()>), tile_lds(HD, 8, 1));
+  };
+  few(std::false_type());
+  few(std::true_type());
+  tile(std::integral_constant<Source, kRows>());
+  tile(std::integral_constant<Source, kPages>());
+  tile(std::integral_constant<Source, kPages8>());
   return e;
 }
 
@@ -1207,8 +1445,12 @@ hipError_t launch(const AttnParams &p, Choice &c, hipStream_t s) {
   if (c.nb) {
     const dim3 grid((unsigned)std::min(c.few.max_items, kFewGrid)), block(64 * kFewWaves);
     const size_t lds = few_lds(HD, c.nb);
-    if (c.nb == 1) hipLaunchKernelGGL((ff_attn_few_kernel<HD, 1>), grid, block, lds, s, p, c.few);
-    else hipLaunchKernelGGL((ff_attn_few_kernel<HD, 2>), grid, block, lds, s, p, c.few);
+    const auto few = [&](auto eight) {
+      if (c.nb == 1) hipLaunchKernelGGL((ff_attn_few_kernel<HD, 1, eight()>), grid, block, lds, s, p, c.few);
+      else hipLaunchKernelGGL((ff_attn_few_kernel<HD, 2, eight()>), grid, block, lds, s, p, c.few);
+    };
+    if (p.k_scale) few(std::true_type());
+    else few(std::false_type());
     if (c.few.target > 0 && !c.few.join_here)
       hipLaunchKernelGGL((ff_attn_join_rows_kernel<HD>), dim3((unsigned)(c.few_tiles * p.n_kv * (c.few.tile_rows / 4))), dim3(256), 0, s, p, c.few);
   }
@@ -1217,13 +1459,13 @@ hipError_t launch(const AttnParams &p, Choice &c, hipStream_t s) {
     const unsigned items = (unsigned)c.tile.max_items, across = std::min(items, 1u << 20);
     const dim3 grid(across, (items + across - 1) / across), block(512);
     const size_t lds = tile_lds(HD, c.rw, 8 / c.rw);
-    if (p.table) {
-      if (c.rw == 4) hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 4, 2, true>), grid, block, lds, s, p, c.tile);
-      else hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 8, 1, true>), grid, block, lds, s, p, c.tile);
-    } else {
-      if (c.rw == 4) hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 4, 2, false>), grid, block, lds, s, p, c.tile);
-      else hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 8, 1, false>), grid, block, lds, s, p, c.tile);
-    }
+    const auto tile = [&](auto src) {
+      if (c.rw == 4) hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 4, 2, src()>), grid, block, lds, s, p, c.tile);
+      else hipLaunchKernelGGL((ff_attn_tile_kernel<HD, 8, 1, src()>), grid, block, lds, s, p, c.tile);
+    };
+    if (p.k_scale) tile(std::integral_constant<Source, kPages8>());
+    else if (p.table) tile(std::integral_constant<Source, kPages>());
+    else tile(std::integral_constant<Source, kRows>());
     if (c.tile.target > 0)
       hipLaunchKernelGGL((ff_attn_join_kernel<HD>), dim3((unsigned)(c.tiles * p.n_kv * (c.tile.tile_rows / 32 * (HD / 8) / 4))), dim3(256), 0, s, p, c.tile);
   }
@@ -1275,6 +1517,6 @@ hipError_t ff_launch_attention(const AttnParams &p, int head_dim, int max_chunk,
 }
 
 hipError_t ff_launch_validate_pages(const AttnParams &p, int32_t *flag, hipStream_t s) {
-  hipLaunchKernelGGL(ff_attn_validate_kernel, dim3(p.n_seqs), dim3(64), 0, s, p, flag);
+  hipLaunchKernelGGL(ff_attn_validate_kernel, dim3(p.n_seqs, p.head_tables ? p.n_kv : 1), dim3(64), 0, s, p, flag);
   return hipGetLastError();
 }

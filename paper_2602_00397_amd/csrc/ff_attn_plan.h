@@ -42,6 +42,12 @@ struct AttnParams {
   float *part = nullptr;
   size_t part_bytes = 0;
   int32_t *counters = nullptr;   // [kAttnCounters], zero: how many pieces of a tile have ended; zero again when the call has
+  // the table of sequence s and key head h starts at s * seq_tables + h * head_tables
+  int64_t seq_tables = 0;
+  int32_t head_tables = 0;
+  // pages in 8 bits: k and v are codes, with a scale for every 2^scale_shift keys of a page and head; nullptr: bf16
+  const float *k_scale = nullptr, *v_scale = nullptr;
+  int32_t scale_shift = 0;
 };
 constexpr int kAttnCounters = 16384, kAttnSeqs = 16384;   // most sequences of a call
 constexpr int kMostItems = 1 << 24;      // a sequence's (tile, piece), and all of a call's, are counted up to this number
@@ -60,6 +66,20 @@ hipError_t ff_attention_init();   // raises the kernels' dynamic-LDS limits
 hipError_t ff_launch_attention(const AttnParams &p, int head_dim, int max_chunk, hipStream_t s);
 // flag[0] is set to 1 + a sequence whose start, length or page is out of range.  The caller zeroes flag[0] first.
 hipError_t ff_launch_validate_pages(const AttnParams &p, int32_t *flag, hipStream_t s);
+
+// The write of new tokens into pages in 8 bits: seqs has starts, lens, tables and the pages' shape (scale_shift with it).
+// Of a scale that the write gives.  Its codes' values are normal bf16 numbers, and attention's sums, of up to 2^30 of them with weights up to
+// 2^8 (a row's maximum may lag that far), stay below 2^(9 + 80 + 30 + 8).
+constexpr int kLeastExp8 = -110, kMostExp8 = 80;
+constexpr int kMaxScaleTokens = 128;
+struct Append8Params {
+  AttnParams seqs;
+  const bf16_t *k, *v;
+  int64_t k_stride, v_stride;
+  uint8_t *k_codes, *v_codes;
+  float *k_scale, *v_scale;
+};
+hipError_t ff_launch_append8(const Append8Params &a, int head_dim, hipStream_t s);
 
 ATTN_FN int attn_min(int a, int b) { return a < b ? a : b; }
 ATTN_FN int attn_max(int a, int b) { return a > b ? a : b; }

@@ -1,0 +1,63 @@
+// What the wavefronts of several kernels do alike: sums over lanes, and which sequence of a call an item belongs to.
+#pragma once
+
+#include "ff_attn_plan.h"
+
+// Running sums over the 64 lanes (lane 63: all of them), by DPP: some 8 cycles a step, where a shuffle through LDS takes over 100.
+template <int CTRL, int ROWS, class T>
+__device__ __forceinline__ T dpp(T v) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+template <class T>
+__device__ __forceinline__ T lane_sums(T v) {
+  v += dpp<0x111, 0xf>(v);     // the lane before in the row of 16, then 2, 4 and 8 before
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  v += dpp<0x142, 0xa>(v);     // rows 1 and 3: the last lane of the row before
+  v += dpp<0x143, 0xc>(v);     // rows 2 and 3: lane 31
+  return v;
+}
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
+__device__ __forceinline__ float last_lane(float v) { return __builtin_bit_cast(float, last_lane(__builtin_bit_cast(int, v))); }
+// a wave-uniform value by a scalar load: the wait for it is not one for the copies before it
+template <class T>
+__device__ __forceinline__ T scalar_load(const T *at) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) T *>(reinterpret_cast<uintptr_t>(at));
+}
+
+// Items are counted over the sequences: `count` gives a sequence's.  Item number x (the same in all lanes) is number `at` of sequence s;
+// s < 0: there are fewer.  64 sequences are looked at together, so a call of up to 64 takes one look.
+struct Found { int s, at; Seq seq; };
+template <class Count>
+__device__ __forceinline__ Found find_item(const AttnParams &p, long x, Count count) {
+  const int lane = threadIdx.x & 63;
+  Found f = {-1, 0, {0, 0, 0}};
+  for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
+    const Seq q = s0 + lane < p.n_seqs ? seq_of(p, s0 + lane) : Seq{0, 0, 0};
+    // (a call's tokens keep the sums in 32 bits; starts that do not ascend may not: nothing is found then, or another item)
+    const int mine = count(q), upto = lane_sums(mine);
+    const unsigned long long hit = __ballot(x < (long)(unsigned)upto);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      const int n = __builtin_amdgcn_readlane(mine, l), at = (int)x - (__builtin_amdgcn_readlane(upto, l) - n);
+      if ((unsigned)at < (unsigned)n)
+        f = {s0 + l, at, {__builtin_amdgcn_readlane(q.t0, l), __builtin_amdgcn_readlane(q.n, l), __builtin_amdgcn_readlane(q.keys, l)}};
+      return f;
+    }
+    x -= (unsigned)last_lane(upto);
+  }
+  return f;
+}
+
+// New tokens of a sequence stand at the positions keys - n .. keys - 1 of its cache, as far as these are not negative.
+__device__ __forceinline__ int first_new(const Seq &q) { return q.keys > q.n ? q.keys - q.n : 0; }
+// how many runs of 2^shift positions have new tokens
+__device__ __forceinline__ int runs_of(const Seq &q, int shift) {
+  return q.n > 0 && q.keys > 0 ? ((q.keys - 1) >> shift) - (first_new(q) >> shift) + 1 : 0;
+}
+// most runs of a call: each has a token, and all of a sequence's but two are full
+inline long most_runs(long n_tokens, long n_seqs, int shift) {
+  const long seqs = n_seqs < n_tokens ? n_seqs : n_tokens, runs = (n_tokens >> shift) + 2 * seqs;
+  return runs < n_tokens ? runs : n_tokens;
+}
