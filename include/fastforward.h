@@ -327,6 +327,15 @@ typedef struct {
   const void *bias;    /* dev bf16 [d_model], or NULL */
 } ff_norm;
 
+/* Sparse attention's choice of pages (ff_select_pages).  A sequence's new tokens are
+ * cut into blocks of query_block (1: every token its own).  Limits: query_block and
+ * keep from 1 to 2^20, first from 0 to keep. */
+typedef struct {
+  int32_t query_block;
+  int32_t keep;    /* pages kept of those in front of a block's own */
+  int32_t first;   /* of these the sequence's first so many always */
+} ff_selection;
+
 /* Norms around a block, with the block's gate and the residual's scale:
  *   s = h + scale * gate * post(y),  h_out = bf16(s),  x = bf16(pre(s))
  * in fp32 from the inputs to the two roundings (s is not rounded before pre).
@@ -456,6 +465,77 @@ ff_status ff_chunk_attention8(ff_ctx *ctx, const ff_attention *a, int32_t n_toke
                               int32_t max_chunk, const ff_paged_cache8 *cache,
                               const int32_t *page_table, int32_t table_stride,
                               void *o, int64_t o_stride, float *lse_opt);
+
+/* ---- attention over selected pages ---------------------------------------
+ *
+ * For long contexts: every block of new tokens reads, for each key head, the pages
+ * that a cheap score puts highest, and its own, as the FFN of this library runs over the
+ * neurons that its predictor puts highest.  A step of a layer is ff_page_means (after
+ * its keys are cached), ff_select_pages and ff_selected_attention.  Where a call takes
+ * a cache and a cache8, one of them is NULL. */
+
+/* Means of the keys of pages that have new tokens, over the page's keys so far:
+ *   means         dev f32 [n_pages][n_kv_heads][head_dim]; of other pages as they were
+ *   the rest      as for ff_cache8_append (n_tokens new tokens in all; their keys are
+ *                 in the cache).  A page outside [0, n_pages) is passed over
+ * Sums are float64, rounded once. */
+ff_status ff_page_means(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens,
+                        int32_t n_seqs, const int32_t *chunk_starts,
+                        const int32_t *context_lens, const ff_paged_cache *cache,
+                        const ff_paged_cache8 *cache8, const int32_t *page_table,
+                        int32_t table_stride, float *means);
+
+/* Host arithmetic: most blocks that n_tokens tokens of n_seqs sequences are cut into
+ * (min(n_tokens, n_tokens / query_block + n_seqs)), entries of a block's page table
+ * (keep, and the most pages that a block's own tokens lie in), and the workspace that
+ * ff_select_pages needs for so many blocks. */
+ff_status ff_selection_blocks(const ff_selection *sel, int32_t n_tokens,
+                              int32_t n_seqs, int32_t *n_blocks);
+ff_status ff_selection_pages(const ff_selection *sel, int32_t page_size,
+                             int32_t *block_stride);
+ff_status ff_selection_workspace_bytes(const ff_attention *a, int32_t n_blocks,
+                                       int32_t table_stride, size_t *bytes);
+
+/* Which pages each block reads:
+ *   q, chunk_starts, context_lens, page_table, table_stride   as for ff_chunk_attention
+ *                 (a->causal is 1, a->window 0; the scale does not matter)
+ *   n_pages, page_size, means   of the cache; means as ff_page_means keeps them
+ *   block_starts  dev int32 [n_blocks + 1] out, n_blocks of ff_selection_blocks: block
+ *                 b is rows [block_starts[b], block_starts[b + 1]); blocks behind the
+ *                 last have none
+ *   block_lens    dev int32 [n_blocks] out: keys of the block's pages, up to its last token's own
+ *   block_tables  dev int32 [n_blocks][n_kv_heads][block_stride] out, block_stride of
+ *                 ff_selection_pages: entries of page_table in the order of their
+ *                 positions, then -1.  Of the pages in front of the one that the block's first token
+ *                 is in, min(keep, all) are there: the first `first`, and of the
+ *                 others those with the highest scores, equal ones from the lower position
+ *                 on; then every page from that one to the one of the block's last token
+ * The score of a page for a key head is the sum of the block's queries of that head's
+ * group, times the page's mean key: float64 from the bf16 queries and fp32 means, the
+ * order of the sums fixed by the shapes.  Scores are expected to be finite (a NaN ranks by its bit
+ * pattern).  A page outside [0, n_pages) is scored as page 0 and listed as it is. */
+ff_status ff_select_pages(ff_ctx *ctx, const ff_attention *a, const ff_selection *sel,
+                          int32_t n_tokens, int32_t n_seqs, const void *q,
+                          int64_t q_stride, const int32_t *chunk_starts,
+                          const int32_t *context_lens, int32_t n_pages,
+                          int32_t page_size, const float *means,
+                          const int32_t *page_table, int32_t table_stride,
+                          int32_t *block_starts, int32_t *block_lens,
+                          int32_t *block_tables);
+
+/* Attention of each block over its pages: ff_chunk_attention with the blocks as
+ * sequences and a page table of its own for each key head, [n_blocks][n_kv_heads][
+ * block_stride].  A token sees the block's kept pages whole, and its own pages up to
+ * itself; with keep at least a sequence's pages that is attention over all of them.
+ * a->causal is 1, a->window 0.  max_chunk: the longest block, as far as the host
+ * knows.  Workspace: ff_attention_workspace_bytes(n_tokens, n_blocks). */
+ff_status ff_selected_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens,
+                                int32_t n_blocks, const void *q, int64_t q_stride,
+                                const int32_t *block_starts, const int32_t *block_lens,
+                                int32_t max_chunk, const ff_paged_cache *cache,
+                                const ff_paged_cache8 *cache8,
+                                const int32_t *block_tables, int32_t block_stride,
+                                void *o, int64_t o_stride, float *lse_opt);
 
 #ifdef __cplusplus
 }

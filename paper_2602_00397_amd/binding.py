@@ -55,6 +55,11 @@ class PagedCache8(C.Structure):
                 ("page_size", C.c_int32), ("scale_tokens", C.c_int32)]
 
 
+class Selection(C.Structure):
+    """Which pages blocks of new tokens read (ff_selection)."""
+    _fields_ = [("query_block", C.c_int32), ("keep", C.c_int32), ("first", C.c_int32)]
+
+
 class RotarySpec(C.Structure):
     _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32),
                 ("axis", C.POINTER(C.c_int32)), ("inv_freq", C.c_void_p)]
@@ -119,6 +124,13 @@ def load_library(build_if_missing: bool = True):
         "ff_cache8_append": ([vp, P(Attention), i32, i32, vp, i64, vp, i64, vp, vp, P(PagedCache8), vp, i32], C.c_int),
         "ff_chunk_attention8": ([vp, P(Attention), i32, i32, vp, i64, vp, vp, i32, P(PagedCache8), vp, i32, vp, i64,
                                  vp], C.c_int),
+        "ff_page_means": ([vp, P(Attention), i32, i32, vp, vp, P(PagedCache), P(PagedCache8), vp, i32, vp], C.c_int),
+        "ff_selection_blocks": ([P(Selection), i32, i32, P(i32)], C.c_int),
+        "ff_selection_pages": ([P(Selection), i32, P(i32)], C.c_int),
+        "ff_selection_workspace_bytes": ([P(Attention), i32, i32, P(sz)], C.c_int),
+        "ff_select_pages": ([vp, P(Attention), P(Selection), i32, i32, vp, i64, vp, vp, i32, i32, vp, vp, i32, vp, vp, vp], C.c_int),
+        "ff_selected_attention": ([vp, P(Attention), i32, i32, vp, i64, vp, vp, i32, P(PagedCache), P(PagedCache8), vp, i32, vp, i64,
+                                   vp], C.c_int),
         "ff_copy": ([vp, vp, vp, sz], C.c_int),
         "ff_mfma_peak": ([vp, i32, i32, P(C.c_double)], C.c_int),
     }
@@ -133,7 +145,8 @@ EXPORTS = ["ff_create", "ff_destroy", "ff_set_stream", "ff_status_str", "ff_last
            "ff_set_workspace", "ff_set_option", "ff_k_from_sparsity", "ff_layer_budgets", "ff_predict", "ff_predict_static",
            "ff_sparse_ffn", "ff_dense_ffn", "ff_ffn_stack", "ff_rmsnorm", "ff_residual_add",
            "ff_norm_residual", "ff_rotary", "ff_attention_workspace_bytes", "ff_prompt_attention", "ff_chunk_attention",
-           "ff_cache8_append", "ff_chunk_attention8",
+           "ff_cache8_append", "ff_chunk_attention8", "ff_page_means", "ff_selection_blocks", "ff_selection_pages",
+           "ff_selection_workspace_bytes", "ff_select_pages", "ff_selected_attention",
            "ff_profile_enable", "ff_profile_read", "ff_copy", "ff_mfma_peak"]
 
 STAGES = ("pool", "mlp", "topk", "gemm1", "gemm2", "glue")
@@ -207,6 +220,36 @@ def attention_workspace_bytes(heads: Attention, n_tokens: int, n_seqs: int) -> i
     return out.value
 
 
+def selection(query_block: int, keep: int, first: int = 0) -> Selection:
+    return Selection(int(query_block), int(keep), int(first))
+
+
+def selection_blocks(sel: Selection, n_tokens: int, n_seqs: int) -> int:
+    """Most blocks that so many tokens and sequences are cut into."""
+    out = C.c_int32()
+    st = load_library().ff_selection_blocks(C.byref(sel), int(n_tokens), int(n_seqs), C.byref(out))
+    if st:
+        raise FFError(st, "ff_selection_blocks")
+    return out.value
+
+
+def selection_pages(sel: Selection, page_size: int) -> int:
+    """Entries of a block's page table."""
+    out = C.c_int32()
+    st = load_library().ff_selection_pages(C.byref(sel), int(page_size), C.byref(out))
+    if st:
+        raise FFError(st, "ff_selection_pages")
+    return out.value
+
+
+def selection_workspace_bytes(heads: Attention, n_blocks: int, table_stride: int) -> int:
+    out = C.c_size_t()
+    st = load_library().ff_selection_workspace_bytes(C.byref(heads), int(n_blocks), int(table_stride), C.byref(out))
+    if st:
+        raise FFError(st, "ff_selection_workspace_bytes")
+    return out.value
+
+
 # The descriptions below hold pointers; each keeps the tensors that it was made of alive.
 
 def norm(kind: str, eps: float, gain: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
@@ -255,6 +298,11 @@ def _check_pages(cache, heads: Attention):
         raise AssertionError(f"cache pages {tuple(cache.tensors[0].shape)} are not of {heads.n_kv_heads} heads of {heads.head_dim}")
 
 
+def _either(cache):
+    """(cache, cache8) for the calls that take one of either kind."""
+    return (None, cache) if isinstance(cache, PagedCache8) else (cache, None)
+
+
 class Context:
     """One ff_ctx bound to a torch device and stream; owns its workspace tensor."""
 
@@ -297,6 +345,10 @@ class Context:
         """Enough for every chunk_attention call of up to so many tokens and sequences.  (A workspace that grows is another one:
         captured graphs hold the address of the one that they were captured with.)"""
         self._ensure(attention_workspace_bytes(heads, n_tokens, n_seqs))
+
+    def ensure_selection_workspace(self, heads: Attention, n_blocks: int, table_stride: int):
+        """Enough for every select_pages call of up to so many blocks over page tables of up to so many entries."""
+        self._ensure(selection_workspace_bytes(heads, n_blocks, table_stride))
 
     def _ensure(self, need: int):
         if self._ws is None or self._ws.numel() < need:
@@ -419,6 +471,43 @@ class Context:
             self._h, heads, n, n_seqs, *_rows(q, n, qw), _typed(chunk_starts, torch.int32, (n_seqs + 1,)),
             _typed(context_lens, torch.int32, (n_seqs,)), max_chunk, cache, _typed(page_table, torch.int32), table_stride,
             *_rows(o, n, qw), _typed(lse, torch.float32, (n, heads.n_heads)))
+        if st:
+            self._check(st)
+
+    def page_means(self, heads: Attention, n_tokens: int, chunk_starts, context_lens, cache, page_table, means):
+        n_seqs, table_stride = page_table.shape
+        _check_pages(cache, heads)
+        st = self.lib.ff_page_means(
+            self._h, heads, n_tokens, n_seqs, _typed(chunk_starts, torch.int32, (n_seqs + 1,)),
+            _typed(context_lens, torch.int32, (n_seqs,)), *_either(cache), _typed(page_table, torch.int32), table_stride,
+            _typed(means, torch.float32, (cache.n_pages, heads.n_kv_heads, heads.head_dim)))
+        if st:
+            self._check(st)
+
+    def select_pages(self, heads: Attention, sel: Selection, q, chunk_starts, context_lens, page_size: int, means, page_table,
+                     block_starts, block_lens, block_tables):
+        n, qw, (n_seqs, table_stride) = q.shape[0], heads.n_heads * heads.head_dim, page_table.shape
+        # (of a selection that is not allowed the library says so)
+        allowed = sel.query_block > 0 and sel.keep > 0 and page_size > 0
+        n_blocks = min(n, n // sel.query_block + n_seqs) if allowed else block_lens.numel()
+        shape = (n_blocks, heads.n_kv_heads, sel.keep + (sel.query_block + page_size - 2) // page_size + 1) if allowed else None
+        st = self.lib.ff_select_pages(
+            self._h, heads, sel, n, n_seqs, *_rows(q, n, qw), _typed(chunk_starts, torch.int32, (n_seqs + 1,)),
+            _typed(context_lens, torch.int32, (n_seqs,)), means.shape[0], page_size,
+            _typed(means, torch.float32, (means.shape[0], heads.n_kv_heads, heads.head_dim)), _typed(page_table, torch.int32), table_stride,
+            _typed(block_starts, torch.int32, (n_blocks + 1,)), _typed(block_lens, torch.int32, (n_blocks,)),
+            _typed(block_tables, torch.int32, shape))
+        if st:
+            self._check(st)
+
+    def selected_attention(self, heads: Attention, q, block_starts, block_lens, max_chunk: int, cache, block_tables, o, lse=None):
+        n, qw, (n_blocks, n_kv, block_stride) = q.shape[0], heads.n_heads * heads.head_dim, block_tables.shape
+        _check_pages(cache, heads)
+        st = self.lib.ff_selected_attention(
+            self._h, heads, n, n_blocks, *_rows(q, n, qw), _typed(block_starts, torch.int32, (n_blocks + 1,)),
+            _typed(block_lens, torch.int32, (n_blocks,)), max_chunk, *_either(cache),
+            _typed(block_tables, torch.int32, (n_blocks, heads.n_kv_heads, block_stride)), block_stride, *_rows(o, n, qw),
+            _typed(lse, torch.float32, (n, heads.n_heads)))
         if st:
             self._check(st)
 

@@ -562,6 +562,27 @@ ff_status attend_pages(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int
   return FF_OK;
 }
 
+constexpr int kMostSelected = 1 << 20;
+ff_status check_selection(ff_ctx *ctx, const ff_selection *sel) {
+  if (!sel) return fail(ctx, FF_ERR_INVALID_ARG, "selection is NULL");
+  if (sel->query_block < 1 || sel->query_block > kMostSelected || sel->keep < 1 || sel->keep > kMostSelected || sel->first < 0 || sel->first > sel->keep)
+    return fail(ctx, FF_ERR_SHAPE, "query_block (%d) and keep (%d) must be in [1, %d], first (%d) in [0, keep]", sel->query_block, sel->keep, kMostSelected, sel->first);
+  return FF_OK;
+}
+int selection_blocks(const ff_selection &sel, int32_t n_tokens, int32_t n_seqs) {
+  return (int)std::min<long>(n_tokens, (long)(n_tokens / sel.query_block) + n_seqs);
+}
+int selection_pages(const ff_selection &sel, int32_t page_size) { return sel.keep + (sel.query_block + page_size - 2) / page_size + 1; }
+size_t selection_bytes(int32_t n_kv, int32_t n_blocks, int32_t table_stride) { return (size_t)n_blocks * n_kv * table_stride * sizeof(double); }
+ff_status check_selected(ff_ctx *ctx, const ff_attention *a) {
+  if (!a->causal || a->window != 0) return fail(ctx, FF_ERR_INVALID_ARG, "selected pages go with causal and no window");
+  return FF_OK;
+}
+ff_status check_either(ff_ctx *ctx, const ff_paged_cache *cache, const ff_paged_cache8 *cache8) {
+  if ((cache != nullptr) == (cache8 != nullptr)) return fail(ctx, FF_ERR_INVALID_ARG, "one of cache and cache8 is given");
+  return cache8 ? check_cache8(ctx, cache8) : check_cache(ctx, cache);
+}
+
 ff_status check_weights(ff_ctx *ctx, const ff_ffn_weights *w) {
   if (!w || !w->w_gate || !w->w_up || !w->w_down) return fail(ctx, FF_ERR_INVALID_ARG, "FFN weight pointer is NULL");
   if (!aligned16(w->w_gate) || !aligned16(w->w_up) || !aligned16(w->w_down))
@@ -1104,6 +1125,110 @@ ff_status ff_chunk_attention8(ff_ctx *ctx, const ff_attention *a, int32_t n_toke
   if (!cache) return fail(ctx, FF_ERR_INVALID_ARG, "no cache, or one without pages or scales");
   return attend_pages(ctx, a, n_tokens, n_seqs, q, q_stride, chunk_starts, context_lens, max_chunk, nullptr, cache, page_table, table_stride, 1,
                       o, o_stride, lse_opt);
+}
+
+ff_status ff_page_means(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs, const int32_t *chunk_starts,
+                        const int32_t *context_lens, const ff_paged_cache *cache, const ff_paged_cache8 *cache8, const int32_t *page_table,
+                        int32_t table_stride, float *means) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_heads(ctx, a, n_tokens);
+  if (st != FF_OK) return st;
+  if ((st = check_seqs(ctx, n_seqs)) != FF_OK || (st = check_either(ctx, cache, cache8)) != FF_OK) return st;
+  if ((st = check_chunks(ctx, chunk_starts, context_lens, page_table, table_stride)) != FF_OK) return st;
+  if (!means) return fail(ctx, FF_ERR_INVALID_ARG, "means is NULL");
+  if (!aligned16(means)) return fail(ctx, FF_ERR_ALIGNMENT, "means must be 16-byte aligned");
+  SelectParams p = {};
+  p.seqs = attn_params(*a, n_tokens, n_seqs);
+  if (cache8) set_cache8(&p.seqs, *cache8);
+  else set_cache(&p.seqs, *cache);
+  set_chunks(&p.seqs, chunk_starts, context_lens, page_table, table_stride, 1);
+  p.means = means;
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_page_means(p, a->head_dim, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
+}
+
+ff_status ff_selection_blocks(const ff_selection *sel, int32_t n_tokens, int32_t n_seqs, int32_t *n_blocks) {
+  if (!n_blocks || n_tokens < 1 || n_seqs < 1) return FF_ERR_INVALID_ARG;
+  ff_status st = check_selection(nullptr, sel);
+  if (st != FF_OK) return st;
+  *n_blocks = selection_blocks(*sel, n_tokens, n_seqs);
+  return FF_OK;
+}
+
+ff_status ff_selection_pages(const ff_selection *sel, int32_t page_size, int32_t *block_stride) {
+  if (!block_stride) return FF_ERR_INVALID_ARG;
+  ff_status st = check_selection(nullptr, sel);
+  if (st != FF_OK) return st;
+  if (!is_power(page_size) || page_size < 8 || page_size > 4096) return FF_ERR_SHAPE;
+  *block_stride = selection_pages(*sel, page_size);
+  return FF_OK;
+}
+
+ff_status ff_selection_workspace_bytes(const ff_attention *a, int32_t n_blocks, int32_t table_stride, size_t *bytes) {
+  if (!bytes) return FF_ERR_INVALID_ARG;
+  ff_status st = check_heads(nullptr, a, 1);
+  if (st != FF_OK) return st;
+  if ((st = check_seqs(nullptr, n_blocks)) != FF_OK) return st;
+  if (table_stride < 1) return FF_ERR_INVALID_ARG;
+  *bytes = selection_bytes(a->n_kv_heads, n_blocks, table_stride);
+  return FF_OK;
+}
+
+ff_status ff_select_pages(ff_ctx *ctx, const ff_attention *a, const ff_selection *sel, int32_t n_tokens, int32_t n_seqs, const void *q,
+                          int64_t q_stride, const int32_t *chunk_starts, const int32_t *context_lens, int32_t n_pages, int32_t page_size,
+                          const float *means, const int32_t *page_table, int32_t table_stride, int32_t *block_starts, int32_t *block_lens,
+                          int32_t *block_tables) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_heads(ctx, a, n_tokens);
+  if (st != FF_OK) return st;
+  if ((st = check_seqs(ctx, n_seqs)) != FF_OK || (st = check_selection(ctx, sel)) != FF_OK || (st = check_selected(ctx, a)) != FF_OK) return st;
+  if ((st = check_rows(ctx, "q", q, q_stride, (int64_t)a->n_heads * a->head_dim)) != FF_OK) return st;
+  if ((st = check_chunks(ctx, chunk_starts, context_lens, page_table, table_stride)) != FF_OK) return st;
+  if (!means || !block_starts || !block_lens || !block_tables) return fail(ctx, FF_ERR_INVALID_ARG, "means or a block array is NULL");
+  if (!aligned16(means) || !aligned16(block_starts) || !aligned16(block_lens) || !aligned16(block_tables))
+    return fail(ctx, FF_ERR_ALIGNMENT, "means and block arrays must be 16-byte aligned");
+  if (n_pages < 1) return fail(ctx, FF_ERR_INVALID_ARG, "n_pages (%d) must be positive", n_pages);
+  if (!is_power(page_size) || page_size < 8 || page_size > 4096)
+    return fail(ctx, FF_ERR_SHAPE, "page_size (%d) must be a power of two from 8 to 4096", page_size);
+  SelectParams p = {};
+  p.n_blocks = selection_blocks(*sel, n_tokens, n_seqs);
+  if (p.n_blocks > kAttnSeqs) return fail(ctx, FF_ERR_SHAPE, "more than %d blocks", kAttnSeqs);
+  p.seqs = attn_params(*a, n_tokens, n_seqs);
+  p.seqs.q = static_cast<const bf16_t *>(q);
+  p.seqs.q_stride = q_stride;
+  p.seqs.n_pages = n_pages;
+  p.seqs.page_shift = log2_of(page_size);
+  set_chunks(&p.seqs, chunk_starts, context_lens, page_table, table_stride, 1);
+  p.means = const_cast<float *>(means);
+  p.query_block = sel->query_block; p.keep = sel->keep; p.first = sel->first;
+  p.width = selection_pages(*sel, page_size);
+  p.starts = block_starts; p.lens = block_lens; p.tables = block_tables;
+  if (table_stride > sel->keep) {       // (else every page is kept)
+    const size_t need = selection_bytes(a->n_kv_heads, p.n_blocks, table_stride);
+    if (!ctx->ws) return fail(ctx, FF_ERR_WORKSPACE, "no workspace set (ff_set_workspace)");
+    if (ctx->ws_bytes < need) return fail(ctx, FF_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", ctx->ws_bytes, need);
+    p.scores = static_cast<double *>(ctx->ws);
+  }
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_select_pages(p, a->head_dim, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
+}
+
+ff_status ff_selected_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_blocks, const void *q, int64_t q_stride,
+                                const int32_t *block_starts, const int32_t *block_lens, int32_t max_chunk, const ff_paged_cache *cache,
+                                const ff_paged_cache8 *cache8, const int32_t *block_tables, int32_t block_stride, void *o, int64_t o_stride,
+                                float *lse_opt) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_heads(ctx, a, n_tokens);
+  if (st != FF_OK) return st;
+  if ((st = check_selected(ctx, a)) != FF_OK || (st = check_either(ctx, cache, cache8)) != FF_OK) return st;
+  return attend_pages(ctx, a, n_tokens, n_blocks, q, q_stride, block_starts, block_lens, max_chunk, cache, cache8, block_tables, block_stride,
+                      a->n_kv_heads, o, o_stride, lse_opt);
 }
 
 ff_status ff_copy(ff_ctx *ctx, void *dst, const void *src, size_t bytes) {

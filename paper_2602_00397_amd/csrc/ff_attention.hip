@@ -13,6 +13,7 @@
 // when it has grown by more than 2^8: the exponentials stay below 256, far from fp32's and bf16's limits, and most tiles
 // leave the sums as they are.  P is rounded to bf16 because the MFMA takes no wider operand; its row sum is kept in fp32 of the unrounded values.
 #include "ff_attn_plan.h"
+#include "ff_fp8.h"
 #include "ff_wave.h"
 
 #include <algorithm>
@@ -25,7 +26,6 @@ typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 typedef __attribute__((ext_vector_type(2))) int32_t i32x2_t;
 
 constexpr float kNoMax = -3.0e38f;   // a row's maximum before its first key: finite, so no difference of two is a NaN
@@ -351,9 +351,7 @@ __device__ __forceinline__ void bf16x4(const u32x2_t &w, float (&v)[4]) {
   }
 }
 
-// Pages in 8 bits: e4m3 codes with a power of two for every few keys of a page and head.  A code times that power has four bits of
-// mantissa, so it is exact in bf16, and the conversion that multiplies by it (v_cvt_scalef32_pk_bf16_fp8, two values at the
-// rate of an addition) is all that these kernels have beside the others'.
+// Pages in 8 bits: codes become bf16 on their way to the matrix unit, and the rest is as for pages in bf16.
 struct Source8 {
   const uint8_t *k, *v;        // the head's part of page 0
   const float *ks, *vs;
@@ -386,16 +384,6 @@ template <bool VALUES>
 __device__ __forceinline__ float scale8(const Source8 &s, int page, int place) {
   return scalar_load((VALUES ? s.vs : s.ks) + (size_t)page * s.page_scales + (place >> s.scale_shift));
 }
-// the lower or upper two of four codes -> a pair of bf16
-template <bool UPPER>
-__device__ __forceinline__ uint32_t decode2(uint32_t codes, float scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, UPPER));
-}
-__device__ __forceinline__ u32x2_t decode4(uint32_t codes, float scale) { return u32x2_t{decode2<false>(codes, scale), decode2<true>(codes, scale)}; }
-__device__ __forceinline__ u32x4_t decode8(uint32_t a, uint32_t b, float scale) {
-  return u32x4_t{decode2<false>(a, scale), decode2<true>(a, scale), decode2<false>(b, scale), decode2<true>(b, scale)};
-}
-
 // Codes in LDS: 256-byte rows of 2 keys of head_dim 128 or 4 of 64, 16-byte chunks swizzled.  The places are different ones for chunk c
 // of the keys 8 a + b + {0 .. 3}, a = 0 .. 3, b = 0 or 4, which 16 lanes read for K, and of 16 neighbouring keys, which 32 lanes read for V.
 template <int HD>

@@ -81,6 +81,17 @@ struct Append8Params {
 };
 hipError_t ff_launch_append8(const Append8Params &a, int head_dim, hipStream_t s);
 
+// Which pages blocks of new tokens read.  seqs has starts, lens, tables and the pages' shape; for the means also the cache.
+struct SelectParams {
+  AttnParams seqs;
+  float *means;                  // [n_pages][n_kv][head_dim]; written by the first, read by the others
+  int32_t query_block, keep, first, n_blocks, width;
+  double *scores;                // [n_blocks][n_kv][table_stride]
+  int32_t *starts, *lens, *tables;
+};
+hipError_t ff_launch_page_means(const SelectParams &a, int head_dim, hipStream_t s);
+hipError_t ff_launch_select_pages(const SelectParams &a, int head_dim, hipStream_t s);
+
 ATTN_FN int attn_min(int a, int b) { return a < b ? a : b; }
 ATTN_FN int attn_max(int a, int b) { return a > b ? a : b; }
 ATTN_FN int attn_clamp(int v, int lo, int hi) { return attn_min(attn_max(v, lo), hi); }

@@ -8,11 +8,10 @@
 // HBM-bound for prompts: values are read once, held in registers while their largest is found, and written at half the size.
 #include <algorithm>
 
+#include "ff_fp8.h"
 #include "ff_wave.h"
 
 namespace {
-
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 
 // 448 * 2^e >= top > 448 * 2^(e - 1), within [kLeast, kMost]
 __device__ __forceinline__ int exponent_for(float top) {
@@ -21,16 +20,6 @@ __device__ __forceinline__ int exponent_for(float top) {
   return min(max(e, kLeastExp8), kMostExp8);
 }
 __device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
-// Two values -> two codes in the lower or upper half of `old`.  The conversion rounds to nearest even and gives NaN from 464 on: finite
-// values beyond 448 (of a block whose scale would exceed its limit) become 448 before it, infinities and NaN are NaN.
-template <bool UPPER>
-__device__ __forceinline__ uint32_t encode2(float a, float b, uint32_t old) {
-  const float x = fabsf(a) < INFINITY ? __builtin_amdgcn_fmed3f(a, -448.f, 448.f) : NAN;
-  const float y = fabsf(b) < INFINITY ? __builtin_amdgcn_fmed3f(b, -448.f, 448.f) : NAN;
-  return __builtin_amdgcn_cvt_pk_fp8_f32(x, y, old, UPPER);
-}
-__device__ __forceinline__ uint32_t encode4(const float (&v)[4]) { return encode2<true>(v[2], v[3], encode2<false>(v[0], v[1], 0)); }
-
 // A unit is a block's part of this call for one head of k or v.  W wavefronts share it, 32 tokens to each at most, so that the new
 // values stay in registers between the search for the largest and the conversion.
 constexpr int kThreads = 256;
@@ -100,12 +89,7 @@ __global__ __launch_bounds__(kThreads) void ff_append8_kernel(Append8Params a, l
             u32x2_t *at = reinterpret_cast<u32x2_t *>(codes + (int64_t)t * HD);
             u32x2_t w = *at;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint32_t lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], factor, false));
-              const uint32_t hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], factor, true));
-              const float v[4] = {__uint_as_float(lo << 16), __uint_as_float(lo & 0xffff0000u), __uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)};
-              w[i] = encode4(v);
-            }
+            for (int i = 0; i < 2; ++i) w[i] = encode4(decode2<false>(w[i], factor), decode2<true>(w[i], factor), 1.f);
             *at = w;
           }
         e = max(e, old);
@@ -117,12 +101,7 @@ __global__ __launch_bounds__(kThreads) void ff_append8_kernel(Append8Params a, l
         if (i * W * TPW < n && t < n) {
           u32x2_t w;
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t lo = x[i][2 * j], hi = x[i][2 * j + 1];
-            const float v[4] = {__uint_as_float(lo << 16) * inverse, __uint_as_float(lo & 0xffff0000u) * inverse,
-                                __uint_as_float(hi << 16) * inverse, __uint_as_float(hi & 0xffff0000u) * inverse};
-            w[j] = encode4(v);
-          }
+          for (int j = 0; j < 2; ++j) w[j] = encode4(x[i][2 * j], x[i][2 * j + 1], inverse);
           *reinterpret_cast<u32x2_t *>(codes + t * HD) = w;
         }
       }

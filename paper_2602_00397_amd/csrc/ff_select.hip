@@ -1,0 +1,284 @@
+// Sparse attention's choice: which pages of its sequence's cache a block of new tokens reads, for each key head.
+//
+// A page is scored by its mean key: s = (sum of the block's queries of the key head) . mean, what the block's logits over the page
+// add up to, over the page's length.  Scores are float64, as the FFN predictor's are: the list does not depend on the
+// order of a sum, and the best pages are exactly the best, ties to the earlier page.  The means are kept by the caller and made anew for
+// pages that new tokens come to.
+#include <algorithm>
+
+#include "ff_fp8.h"
+#include "ff_wave.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// ---- mean keys of the pages that have new tokens ------------------------------------------------------------------------------
+// A workgroup to a page and key head: HD / 8 lanes to a key, float64 sums (of up to 4096 bf16 numbers, nearly always exact), one rounding.
+template <int HD, bool EIGHT>
+__global__ __launch_bounds__(kThreads) void ff_page_means_kernel(SelectParams a, long n_items) {
+  constexpr int LPK = HD / 8, GROUPS = kThreads / LPK;
+  __shared__ double sums[GROUPS][HD];
+  const AttnParams &p = a.seqs;
+  const int group = threadIdx.x / LPK, channel = threadIdx.x % LPK * 8;
+  for (long id = blockIdx.x; id < n_items; id += gridDim.x) {
+    const long run = id / p.n_kv;
+    const int kvh = (int)(id - run * p.n_kv);
+    const Found f = find_item(p, run, [&](const Seq &q) { return runs_of(q, p.page_shift); });
+    if (f.s < 0) break;
+    const int number = (first_new(f.seq) >> p.page_shift) + f.at, page = p.table[f.s * p.seq_tables + number];
+    if ((unsigned)page >= (unsigned)p.n_pages) continue;
+    const int live = (int)min((long)f.seq.keys - ((long)number << p.page_shift), 1L << p.page_shift);
+    const size_t head = (size_t)page * p.n_kv + kvh;
+    double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int j = group; j < live; j += GROUPS) {
+      const size_t at = ((head << p.page_shift) + j) * HD + channel;
+      u32x4_t x;
+      if (EIGHT) {
+        const u32x2_t codes = *reinterpret_cast<const u32x2_t *>(reinterpret_cast<const uint8_t *>(p.k) + at);
+        x = decode8(codes[0], codes[1], p.k_scale[(head << (p.page_shift - p.scale_shift)) + (j >> p.scale_shift)]);
+      } else {
+        x = *reinterpret_cast<const u32x4_t *>(p.k + at);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[2 * e] += (double)__uint_as_float(x[e] << 16);
+        acc[2 * e + 1] += (double)__uint_as_float(x[e] & 0xffff0000u);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[group][channel + e] = acc[e];
+    __syncthreads();
+    if (threadIdx.x < HD) {
+      double sum = 0;
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) sum += sums[g][threadIdx.x];
+      a.means[head * HD + threadIdx.x] = (float)(sum / live);
+    }
+    __syncthreads();
+  }
+}
+
+// ---- blocks of new tokens -----------------------------------------------------------------------------------------------------
+struct Block { int s, t0, n, earlier, own, keys; };   // rows; pages in front of its own, its own, and keys of the kept pages and its own
+__device__ __forceinline__ Block block_of(const SelectParams &a, int x) {
+  const AttnParams &p = a.seqs;
+  const Found f = find_item(p, x, [&](const Seq &q) { return (int)(((long)q.n + a.query_block - 1) / a.query_block); });
+  Block b = {f.s, 0, 0, 0, 0, 0};
+  if (f.s < 0) return b;
+  const int at = f.at * a.query_block;
+  b.t0 = f.seq.t0 + at;
+  b.n = min(a.query_block, f.seq.n - at);
+  const int last = f.seq.keys - f.seq.n + at + b.n - 1;     // (below 0: its tokens see nothing)
+  if (last < 0) return b;
+  b.earlier = max(last - b.n + 1, 0) >> p.page_shift;
+  b.own = (last >> p.page_shift) - b.earlier + 1;
+  // (its own pages are the last of the list, and the last of those ends with the block's last token)
+  b.keys = ((min(a.keep, b.earlier) + b.own - 1) << p.page_shift) + (last & ((1 << p.page_shift) - 1)) + 1;
+  return b;
+}
+
+// A workgroup to 64 pages, or several times that, of a block and key head: the queries' sum once, then four lanes to a page.  Blocks with
+// no more earlier pages than are kept need no scores.
+template <int HD>
+__global__ __launch_bounds__(kThreads) void ff_page_scores_kernel(SelectParams a) {
+  constexpr int LPR = HD / 8, GROUPS = kThreads / LPR;
+  __shared__ double part[GROUPS][HD + 2];
+  __shared__ double sum[HD];
+  const AttnParams &p = a.seqs;
+  const int x = blockIdx.y, kvh = blockIdx.x;
+  const Block b = block_of(a, x);
+  if (b.s < 0 || b.earlier <= a.keep || (int)blockIdx.z * 64 >= b.earlier) return;
+  const int group = threadIdx.x / LPR, channel = threadIdx.x % LPR * 8;
+  double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int r = group; r < b.n * p.group; r += GROUPS) {
+    const int t = p.by_group(r);
+    const u32x4_t w = *reinterpret_cast<const u32x4_t *>(p.q + (int64_t)(b.t0 + t) * p.q_stride + (kvh * p.group + r - t * p.group) * HD + channel);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      acc[2 * e] += (double)__uint_as_float(w[e] << 16);
+      acc[2 * e + 1] += (double)__uint_as_float(w[e] & 0xffff0000u);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) part[group][channel + e] = acc[e];
+  __syncthreads();
+  if (threadIdx.x < HD) {
+    double s = 0;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) s += part[g][threadIdx.x];
+    sum[threadIdx.x] = s;
+  }
+  __syncthreads();
+  const int quarter = threadIdx.x & 3;
+  const int32_t *table = p.table + b.s * p.seq_tables;
+  double *scores = a.scores + ((size_t)x * p.n_kv + kvh) * p.table_stride;
+  for (int j0 = blockIdx.z * 64; j0 < b.earlier; j0 += gridDim.z * 64) {
+    const int j = j0 + (threadIdx.x >> 2);
+    int page = table[min(j, b.earlier - 1)];
+    page = (unsigned)page < (unsigned)p.n_pages ? page : 0;
+    const float *mean = a.means + ((size_t)page * p.n_kv + kvh) * HD;
+    float4 m[HD / 16];
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) m[i] = *reinterpret_cast<const float4 *>(mean + i * 16 + quarter * 4);
+    double s = 0;
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) {
+      const double *q = sum + i * 16 + quarter * 4;
+      s += (double)m[i].x * q[0] + (double)m[i].y * q[1] + (double)m[i].z * q[2] + (double)m[i].w * q[3];
+    }
+    s += __shfl_xor(s, 1);
+    s += __shfl_xor(s, 2);
+    if (quarter == 0 && j < b.earlier) scores[j] = s;
+  }
+}
+
+// ---- the best pages, in order ---------------------------------------------------------------------------------------------------
+// A score as a whole number in the scores' order (-0 as +0; NaN by its bits), and pages that are always taken above all.
+__device__ __forceinline__ uint64_t order_of(double s) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
+  return u >> 63 ? ~u : u | 1ull << 63;
+}
+// (of plain min and max, mixed 64-bit types take the double one)
+__device__ __forceinline__ uint64_t lower(uint64_t a, uint64_t b) { return a < b ? a : b; }
+__device__ __forceinline__ uint64_t higher(uint64_t a, uint64_t b) { return a < b ? b : a; }
+constexpr int kBins = 1024, kHeld = 4096;     // numbers that are held in LDS; of more pages they are made again from the scores
+// A workgroup to a block and key head.  The range of the numbers that hold the last one wanted is cut in 1024 until that one's part has
+// no more than are wanted of it (or is one number: then its first pages are); each cut is ten bits of it, so there are at most seven.
+__global__ __launch_bounds__(kThreads) void ff_select_pages_kernel(SelectParams a) {
+  __shared__ uint64_t held[kHeld];
+  __shared__ uint64_t extreme[2][kThreads / 64];
+  __shared__ int bins[kBins], sums[kThreads / 64], found[3];
+  const AttnParams &p = a.seqs;
+  const int x = blockIdx.y, kvh = blockIdx.x;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const Block b = block_of(a, x);
+  const int end = attn_clamp(p.starts[p.n_seqs], 0, p.T);
+  if (kvh == 0 && threadIdx.x == 0) {
+    a.starts[x] = b.s < 0 ? end : b.t0;
+    a.lens[x] = b.keys;
+    if (x == a.n_blocks - 1) a.starts[a.n_blocks] = b.s < 0 ? end : b.t0 + b.n;
+  }
+  int32_t *list = a.tables + ((size_t)x * p.n_kv + kvh) * a.width;
+  const int32_t *table = p.table + (b.s < 0 ? 0 : b.s * p.seq_tables);
+  const int n = b.earlier, kept = min(a.keep, n);
+  for (int i = kept + threadIdx.x; i < a.width; i += kThreads) list[i] = i < kept + b.own ? table[n + i - kept] : -1;
+  if (n <= a.keep) {
+    for (int i = threadIdx.x; i < n; i += kThreads) list[i] = table[i];
+    return;
+  }
+  const double *scores = a.scores + ((size_t)x * p.n_kv + kvh) * p.table_stride;
+  const bool hold = n <= kHeld;
+  const auto number = [&](int i) { return i < a.first ? ~0ull : order_of(scores[i]); };
+  const auto get = [&](int i) { return hold ? held[i] : number(i); };
+  uint64_t lo = ~0ull, hi = 0;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const uint64_t u = number(i);
+    if (hold) held[i] = u;
+    lo = lower(lo, u);
+    hi = higher(hi, u);
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    lo = lower(lo, __shfl_xor((unsigned long long)lo, off));
+    hi = higher(hi, __shfl_xor((unsigned long long)hi, off));
+  }
+  if (lane == 0) {
+    extreme[0][wave] = lo;
+    extreme[1][wave] = hi;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    lo = lower(lo, extreme[0][w]);
+    hi = higher(hi, extreme[1][w]);
+  }
+  int want = kept;               // of those in [lo, hi]; all above are taken
+  for (;;) {
+    const int shift = max(0, 64 - (int)__clzll((long long)(hi - lo | 1)) - 10);
+    for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const uint64_t u = get(i);
+      if (u >= lo && u <= hi) atomicAdd(&bins[(u - lo) >> shift], 1);
+    }
+    __syncthreads();
+    // bins in falling order, four to a thread
+    const int top = kBins - 1 - 4 * (int)threadIdx.x;
+    const int c[4] = {bins[top], bins[top - 1], bins[top - 2], bins[top - 3]};
+    const int mine = c[0] + c[1] + c[2] + c[3], upto = lane_sums(mine);
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int above = upto - mine;
+    for (int w = 0; w < wave; ++w) above += sums[w];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (above < want && want <= above + c[i]) {
+        found[0] = top - i;
+        found[1] = above;
+        found[2] = c[i];
+      }
+      above += c[i];
+    }
+    __syncthreads();
+    lo += (uint64_t)found[0] << shift;
+    hi = lo + lower(hi - lo, ((uint64_t)1 << shift) - 1);
+    want -= found[1];
+    if (shift == 0 || found[2] == want) break;
+  }
+  // a run of pages to a thread: how many are above, how many in the last part, and where its own begin
+  const int per = (n + kThreads - 1) / kThreads, from = min(n, (int)threadIdx.x * per), to = min(n, from + per);
+  int taken = 0, last = 0;
+  for (int i = from; i < to; ++i) {
+    const uint64_t u = get(i);
+    taken += u > hi;
+    last += u >= lo && u <= hi;
+  }
+  __syncthreads();               // (found and sums have been read)
+  const int taken_upto = lane_sums(taken), last_upto = lane_sums(last);
+  if (lane == 63) {
+    sums[wave] = taken_upto;
+    bins[wave] = last_upto;
+  }
+  __syncthreads();
+  int before = last_upto - last, at = taken_upto - taken;
+  for (int w = 0; w < wave; ++w) {
+    at += sums[w];
+    before += bins[w];
+  }
+  for (int i = from; i < to; ++i) {
+    const uint64_t u = get(i);
+    const bool in_last = u >= lo && u <= hi;
+    if (u > hi || (in_last && before < want)) list[at + min(before, want)] = table[i];
+    at += u > hi;
+    before += in_last;
+  }
+}
+
+template <int HD>
+hipError_t means(const SelectParams &a, hipStream_t s) {
+  const long items = most_runs(a.seqs.T, a.seqs.n_seqs, a.seqs.page_shift) * a.seqs.n_kv;
+  const dim3 grid((unsigned)std::min<long>(items, 1 << 20)), block(kThreads);
+  if (a.seqs.k_scale) hipLaunchKernelGGL((ff_page_means_kernel<HD, true>), grid, block, 0, s, a, items);
+  else hipLaunchKernelGGL((ff_page_means_kernel<HD, false>), grid, block, 0, s, a, items);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t ff_launch_page_means(const SelectParams &a, int head_dim, hipStream_t s) {
+  return head_dim == 128 ? means<128>(a, s) : means<64>(a, s);
+}
+
+hipError_t ff_launch_select_pages(const SelectParams &a, int head_dim, hipStream_t s) {
+  const AttnParams &p = a.seqs;
+  if (p.table_stride > a.keep) {
+    // (a sequence's pages are shared out where there are few blocks)
+    const long units = (long)a.n_blocks * p.n_kv;
+    const dim3 grid(p.n_kv, a.n_blocks, (unsigned)std::max(1l, std::min((p.table_stride + 63l) / 64, 1024 / units)));
+    if (head_dim == 128) hipLaunchKernelGGL((ff_page_scores_kernel<128>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((ff_page_scores_kernel<64>), grid, dim3(kThreads), 0, s, a);
+  }
+  hipLaunchKernelGGL(ff_select_pages_kernel, dim3(p.n_kv, a.n_blocks), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}

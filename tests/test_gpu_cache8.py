@@ -27,7 +27,7 @@ def _table():
 def _decode(codes, scales):
     """Pages of codes and their scales -> float64 values."""
     x = _table()[codes.view(torch.uint8).long()]
-    return x * scales.double().repeat_interleave(codes.shape[2] // scales.shape[2], dim=2)[..., None]
+    return x * scales.double().repeat_interleave(codes.shape[-2] // scales.shape[-1], dim=-1)[..., None]
 
 
 def _encode(x):
