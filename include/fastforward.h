@@ -537,6 +537,73 @@ ff_status ff_selected_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_to
                                 const int32_t *block_tables, int32_t block_stride,
                                 void *o, int64_t o_stride, float *lse_opt);
 
+/* ---- pages shared by rows ------------------------------------------------
+ *
+ * Who holds which pages, on the GPU: row r of the table (a sequence, a beam) has
+ * lens[r] tokens, and its first ceil(lens[r] / page_size) entries are pages; entries
+ * behind those are not looked at.  refs[p] counts the entries that hold page p; 0:
+ * the page is free.  The caller begins with zeros (and lens all 0), and from then on these
+ * calls keep the three together.  Everything about a page lies in the pool's parts: k
+ * and v of every layer, scales, means.  Free pages are taken in ascending order, entries of
+ * a call are served in theirs, and nothing depends on timing: the same call on the same state gives
+ * the same tables.  Rows out of range are passed over, lengths are cut to [0,
+ * table_stride * page_size], entries that are no page are not counted and not followed.
+ * Calls that take entries of the same row twice: the last one counts. */
+typedef struct {
+  void *data;            /* dev: page p is the page_bytes bytes from p * page_bytes on */
+  int64_t page_bytes;    /* 1 to 2^32; quickest as a multiple of 16 */
+} ff_page_part;
+/* Limits: n_pages up to 2^28, page_size a power of two from 8 to 4096, n_rows up to
+ * 2^24, table_stride up to 2^20, n_parts from 0 to 4096 (FF_ERR_SHAPE); n of a call from 1 to 2^20. */
+typedef struct {
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_rows;
+  int32_t table_stride;
+  int32_t *refs;               /* dev [n_pages] */
+  int32_t *page_table;         /* dev [n_rows][table_stride] */
+  int32_t *lens;               /* dev [n_rows] */
+  const ff_page_part *parts;   /* host [n_parts] */
+  int32_t n_parts;
+} ff_page_pool;
+
+/* Workspace of the calls below for up to n entries; more entries never take less. */
+ff_status ff_pages_workspace_bytes(const ff_page_pool *pool, int32_t n, size_t *bytes);
+
+/* Copies page from[i] of every part to page to[i] (dev int32 [n] each; i with a page
+ * out of range, or onto itself, is passed over).  A page that is both read and
+ * written, or written twice, ends with either's contents, in part.  Counts and tables stay as they are;
+ * no workspace. */
+ff_status ff_pages_copy(ff_ctx *ctx, const ff_page_pool *pool, int32_t n,
+                        const int32_t *from, const int32_t *to);
+
+/* Row to[i] becomes what row from[i] is before the call, for all i at once (a search
+ * that goes on with some beams in the place of others): full pages are shared, a
+ * part-filled last page is copied to a free one, so that both rows may be added to.
+ * What row to[i] held is given back (and may be taken by the next call, not by this one).  from[i] ==
+ * to[i] leaves the row alone.
+ *   from, to   dev int32 [n] each
+ *   missing    dev int32 [1] out: 0, or by how many the free pages fell short; then
+ *              nothing is changed */
+ff_status ff_pages_fork(ff_ctx *ctx, const ff_page_pool *pool, int32_t n,
+                        const int32_t *from, const int32_t *to, int32_t *missing);
+
+/* Row rows[i] gets the pages for new_lens[i] tokens (free ones, whose contents are
+ * what they were), or gives back those that it has beyond them; lens follow.
+ * missing as above (pages that are given back serve the next call, not this one). */
+ff_status ff_pages_grow(ff_ctx *ctx, const ff_page_pool *pool, int32_t n,
+                        const int32_t *rows, const int32_t *new_lens,
+                        int32_t *missing);
+
+/* Rows give back their pages: their entries become -1, their lengths 0.  No workspace. */
+ff_status ff_pages_free(ff_ctx *ctx, const ff_page_pool *pool, int32_t n,
+                        const int32_t *rows);
+
+/* Moves pages so that those in use are the first ones: *live (dev int32 [1], out) of
+ * them.  In ascending order, each page in use from *live on goes to the next free one
+ * in front; tables and counts follow.  What lies behind stays as it was. */
+ff_status ff_pages_compact(ff_ctx *ctx, const ff_page_pool *pool, int32_t *live);
+
 #ifdef __cplusplus
 }
 #endif

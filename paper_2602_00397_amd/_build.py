@@ -12,7 +12,8 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libfastforward.so")
 SOURCES = ["ff_api.hip", "ff_predict.hip", "ff_gemm.hip", "ff_gemv.hip", "ff_glue.hip", "ff_norm.hip", "ff_rotary.hip",
-           "ff_attention.hip", "ff_cache8.hip", "ff_select.hip"]
+           "ff_attention.hip", "ff_cache8.hip", "ff_select.hip",
+           "ff_pages.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

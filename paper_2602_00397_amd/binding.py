@@ -60,6 +60,17 @@ class Selection(C.Structure):
     _fields_ = [("query_block", C.c_int32), ("keep", C.c_int32), ("first", C.c_int32)]
 
 
+class PagePart(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("page_bytes", C.c_int64)]
+
+
+class PagePool(C.Structure):
+    """Pages shared by the rows of a table (ff_page_pool)."""
+    _fields_ = [("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_rows", C.c_int32), ("table_stride", C.c_int32),
+                ("refs", C.c_void_p), ("page_table", C.c_void_p), ("lens", C.c_void_p), ("parts", C.POINTER(PagePart)),
+                ("n_parts", C.c_int32)]
+
+
 class RotarySpec(C.Structure):
     _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32),
                 ("axis", C.POINTER(C.c_int32)), ("inv_freq", C.c_void_p)]
@@ -131,6 +142,12 @@ def load_library(build_if_missing: bool = True):
         "ff_select_pages": ([vp, P(Attention), P(Selection), i32, i32, vp, i64, vp, vp, i32, i32, vp, vp, i32, vp, vp, vp], C.c_int),
         "ff_selected_attention": ([vp, P(Attention), i32, i32, vp, i64, vp, vp, i32, P(PagedCache), P(PagedCache8), vp, i32, vp, i64,
                                    vp], C.c_int),
+        "ff_pages_workspace_bytes": ([P(PagePool), i32, P(sz)], C.c_int),
+        "ff_pages_copy": ([vp, P(PagePool), i32, vp, vp], C.c_int),
+        "ff_pages_fork": ([vp, P(PagePool), i32, vp, vp, vp], C.c_int),
+        "ff_pages_grow": ([vp, P(PagePool), i32, vp, vp, vp], C.c_int),
+        "ff_pages_free": ([vp, P(PagePool), i32, vp], C.c_int),
+        "ff_pages_compact": ([vp, P(PagePool), vp], C.c_int),
         "ff_copy": ([vp, vp, vp, sz], C.c_int),
         "ff_mfma_peak": ([vp, i32, i32, P(C.c_double)], C.c_int),
     }
@@ -146,7 +163,8 @@ EXPORTS = ["ff_create", "ff_destroy", "ff_set_stream", "ff_status_str", "ff_last
            "ff_sparse_ffn", "ff_dense_ffn", "ff_ffn_stack", "ff_rmsnorm", "ff_residual_add",
            "ff_norm_residual", "ff_rotary", "ff_attention_workspace_bytes", "ff_prompt_attention", "ff_chunk_attention",
            "ff_cache8_append", "ff_chunk_attention8", "ff_page_means", "ff_selection_blocks", "ff_selection_pages",
-           "ff_selection_workspace_bytes", "ff_select_pages", "ff_selected_attention",
+           "ff_selection_workspace_bytes", "ff_select_pages", "ff_selected_attention", "ff_pages_workspace_bytes",
+           "ff_pages_copy", "ff_pages_fork", "ff_pages_grow", "ff_pages_free", "ff_pages_compact",
            "ff_profile_enable", "ff_profile_read", "ff_copy", "ff_mfma_peak"]
 
 STAGES = ("pool", "mlp", "topk", "gemm1", "gemm2", "glue")
@@ -250,6 +268,14 @@ def selection_workspace_bytes(heads: Attention, n_blocks: int, table_stride: int
     return out.value
 
 
+def pages_workspace_bytes(pool: PagePool, n: int) -> int:
+    out = C.c_size_t()
+    st = load_library().ff_pages_workspace_bytes(C.byref(pool), int(n), C.byref(out))
+    if st:
+        raise FFError(st, "ff_pages_workspace_bytes")
+    return out.value
+
+
 # The descriptions below hold pointers; each keeps the tensors that it was made of alive.
 
 def norm(kind: str, eps: float, gain: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
@@ -290,6 +316,22 @@ def paged_cache8(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: torch.Te
                     _typed(v_scale, torch.float32, k_scale.shape), n_pages, page_size, page_size // blocks)
     c.tensors = (k_pages, v_pages, k_scale, v_scale)
     return c
+
+
+def page_pool(refs: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, page_size: int,
+              parts: Sequence[torch.Tensor]) -> PagePool:
+    """int32 [n_pages], [n_rows][table_stride] and [n_rows]; parts: tensors of any type, [n_pages] first."""
+    n_pages, (n_rows, table_stride) = refs.numel(), page_table.shape
+    each = []
+    for x in parts:
+        if x.shape[0] != n_pages:
+            raise AssertionError(f"a part of {x.shape[0]} pages in a pool of {n_pages}")
+        each.append(PagePart(_ptr(x), x.numel() * x.element_size() // max(1, n_pages)))
+    array = (PagePart * len(each))(*each)
+    pool = PagePool(n_pages, int(page_size), n_rows, table_stride, _typed(refs, torch.int32, (n_pages,)),
+                    _typed(page_table, torch.int32), _typed(lens, torch.int32, (n_rows,)), array, len(each))
+    pool.tensors = (refs, page_table, lens, list(parts), array)
+    return pool
 
 
 def _check_pages(cache, heads: Attention):
@@ -349,6 +391,10 @@ class Context:
     def ensure_selection_workspace(self, heads: Attention, n_blocks: int, table_stride: int):
         """Enough for every select_pages call of up to so many blocks over page tables of up to so many entries."""
         self._ensure(selection_workspace_bytes(heads, n_blocks, table_stride))
+
+    def ensure_pages_workspace(self, pool: PagePool, n: int):
+        """Enough for every call of up to n entries on the pool."""
+        self._ensure(pages_workspace_bytes(pool, n))
 
     def _ensure(self, need: int):
         if self._ws is None or self._ws.numel() < need:
@@ -508,6 +554,37 @@ class Context:
             _typed(block_lens, torch.int32, (n_blocks,)), max_chunk, *_either(cache),
             _typed(block_tables, torch.int32, (n_blocks, heads.n_kv_heads, block_stride)), block_stride, *_rows(o, n, qw),
             _typed(lse, torch.float32, (n, heads.n_heads)))
+        if st:
+            self._check(st)
+
+    def pages_copy(self, pool: PagePool, sources, targets):
+        n = sources.numel()
+        st = self.lib.ff_pages_copy(self._h, pool, n, _typed(sources, torch.int32, (n,)), _typed(targets, torch.int32, (n,)))
+        if st:
+            self._check(st)
+
+    def pages_fork(self, pool: PagePool, sources, targets, missing):
+        n = sources.numel()
+        st = self.lib.ff_pages_fork(self._h, pool, n, _typed(sources, torch.int32, (n,)), _typed(targets, torch.int32, (n,)),
+                                    _typed(missing, torch.int32, (1,)))
+        if st:
+            self._check(st)
+
+    def pages_grow(self, pool: PagePool, rows, new_lens, missing):
+        n = rows.numel()
+        st = self.lib.ff_pages_grow(self._h, pool, n, _typed(rows, torch.int32, (n,)), _typed(new_lens, torch.int32, (n,)),
+                                    _typed(missing, torch.int32, (1,)))
+        if st:
+            self._check(st)
+
+    def pages_free(self, pool: PagePool, rows):
+        n = rows.numel()
+        st = self.lib.ff_pages_free(self._h, pool, n, _typed(rows, torch.int32, (n,)))
+        if st:
+            self._check(st)
+
+    def pages_compact(self, pool: PagePool, live):
+        st = self.lib.ff_pages_compact(self._h, pool, _typed(live, torch.int32, (1,)))
         if st:
             self._check(st)
 

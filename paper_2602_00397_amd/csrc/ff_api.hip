@@ -11,6 +11,7 @@
 
 #include "ff_attn_plan.h"
 #include "ff_internal.h"
+#include "ff_pages.h"
 
 #include <vector>
 
@@ -581,6 +582,45 @@ ff_status check_selected(ff_ctx *ctx, const ff_attention *a) {
 ff_status check_either(ff_ctx *ctx, const ff_paged_cache *cache, const ff_paged_cache8 *cache8) {
   if ((cache != nullptr) == (cache8 != nullptr)) return fail(ctx, FF_ERR_INVALID_ARG, "one of cache and cache8 is given");
   return cache8 ? check_cache8(ctx, cache8) : check_cache(ctx, cache);
+}
+
+// `tables`: whether the call takes counts, table and lengths
+ff_status check_pool(ff_ctx *ctx, const ff_page_pool *pool, bool tables) {
+  if (!pool) return fail(ctx, FF_ERR_INVALID_ARG, "page pool is NULL");
+  if (pool->n_pages < 1 || pool->n_pages > (1 << 28) || pool->n_parts < 0 || pool->n_parts > 4096)
+    return fail(ctx, FF_ERR_SHAPE, "n_pages (%d) must be in [1, 2^28], n_parts (%d) in [0, 4096]", pool->n_pages, pool->n_parts);
+  if (pool->n_parts > 0 && !pool->parts) return fail(ctx, FF_ERR_INVALID_ARG, "parts is NULL");
+  for (int i = 0; i < pool->n_parts; ++i) {
+    if (!pool->parts[i].data) return fail(ctx, FF_ERR_INVALID_ARG, "part %d is NULL", i);
+    if (!aligned16(pool->parts[i].data)) return fail(ctx, FF_ERR_ALIGNMENT, "part %d must be 16-byte aligned", i);
+    if (pool->parts[i].page_bytes < 1 || pool->parts[i].page_bytes > (1ll << 32))
+      return fail(ctx, FF_ERR_SHAPE, "page_bytes of part %d (%lld) must be in [1, 2^32]", i, (long long)pool->parts[i].page_bytes);
+  }
+  if (!tables) return FF_OK;
+  if (!is_power(pool->page_size) || pool->page_size < 8 || pool->page_size > 4096)
+    return fail(ctx, FF_ERR_SHAPE, "page_size (%d) must be a power of two from 8 to 4096", pool->page_size);
+  if (pool->n_rows < 1 || pool->n_rows > (1 << 24) || pool->table_stride < 1 || pool->table_stride > (1 << 20))
+    return fail(ctx, FF_ERR_SHAPE, "n_rows (%d) must be in [1, 2^24], table_stride (%d) in [1, 2^20]", pool->n_rows, pool->table_stride);
+  if (!pool->refs || !pool->page_table || !pool->lens) return fail(ctx, FF_ERR_INVALID_ARG, "refs, page_table or lens is NULL");
+  if (!aligned16(pool->refs) || !aligned16(pool->page_table) || !aligned16(pool->lens))
+    return fail(ctx, FF_ERR_ALIGNMENT, "refs / page_table / lens must be 16-byte aligned");
+  return FF_OK;
+}
+// Entries of a call (b may be none), its workspace if it takes one, and what its kernels get.
+ff_status pool_params(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const int32_t *a, const int32_t *b, bool ws, PoolParams *p) {
+  if (n < 1 || n > (1 << 20)) return fail(ctx, FF_ERR_SHAPE, "n (%d) must be in [1, 2^20]", n);
+  if (!aligned16(a) || !aligned16(b)) return fail(ctx, FF_ERR_ALIGNMENT, "entries must be 16-byte aligned");
+  *p = {};
+  p->refs = pool->refs; p->table = pool->page_table; p->lens = pool->lens;
+  p->n_pages = pool->n_pages; p->n_rows = pool->n_rows; p->table_stride = pool->table_stride;
+  p->page_shift = log2_of(pool->page_size);
+  p->n = n;
+  if (!ws) return FF_OK;
+  const size_t need = ff_pages_ints(n, pool->n_pages, pool->n_rows, pool->table_stride) * sizeof(int32_t);
+  if (!ctx->ws) return fail(ctx, FF_ERR_WORKSPACE, "no workspace set (ff_set_workspace)");
+  if (ctx->ws_bytes < need) return fail(ctx, FF_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", ctx->ws_bytes, need);
+  p->ws = static_cast<int32_t *>(ctx->ws);
+  return FF_OK;
 }
 
 ff_status check_weights(ff_ctx *ctx, const ff_ffn_weights *w) {
@@ -1229,6 +1269,89 @@ ff_status ff_selected_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_to
   if ((st = check_selected(ctx, a)) != FF_OK || (st = check_either(ctx, cache, cache8)) != FF_OK) return st;
   return attend_pages(ctx, a, n_tokens, n_blocks, q, q_stride, block_starts, block_lens, max_chunk, cache, cache8, block_tables, block_stride,
                       a->n_kv_heads, o, o_stride, lse_opt);
+}
+
+ff_status ff_pages_workspace_bytes(const ff_page_pool *pool, int32_t n, size_t *bytes) {
+  if (!bytes) return FF_ERR_INVALID_ARG;
+  ff_status st = check_pool(nullptr, pool, true);
+  if (st != FF_OK) return st;
+  if (n < 1 || n > (1 << 20)) return FF_ERR_SHAPE;
+  *bytes = ff_pages_ints(n, pool->n_pages, pool->n_rows, pool->table_stride) * sizeof(int32_t);
+  return FF_OK;
+}
+
+ff_status ff_pages_copy(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const int32_t *from, const int32_t *to) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_pool(ctx, pool, false);
+  if (st != FF_OK) return st;
+  if (!from || !to || pool->n_parts < 1) return fail(ctx, FF_ERR_INVALID_ARG, "from or to is NULL, or there are no parts");
+  PoolParams p;
+  if ((st = pool_params(ctx, pool, n, from, to, false, &p)) != FF_OK) return st;
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_pages_copy(pool->parts, pool->n_parts, pool->n_pages, n, from, to, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
+}
+
+ff_status ff_pages_fork(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const int32_t *from, const int32_t *to, int32_t *missing) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_pool(ctx, pool, true);
+  if (st != FF_OK) return st;
+  if (!from || !to || !missing) return fail(ctx, FF_ERR_INVALID_ARG, "from, to or missing is NULL");
+  PoolParams p;
+  if ((st = pool_params(ctx, pool, n, from, to, true, &p)) != FF_OK) return st;
+  p.from = from; p.to = to; p.result = missing;
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_pages_fork(p, pool->parts, pool->n_parts, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
+}
+
+ff_status ff_pages_grow(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const int32_t *rows, const int32_t *new_lens, int32_t *missing) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_pool(ctx, pool, true);
+  if (st != FF_OK) return st;
+  if (!rows || !new_lens || !missing) return fail(ctx, FF_ERR_INVALID_ARG, "rows, new_lens or missing is NULL");
+  PoolParams p;
+  if ((st = pool_params(ctx, pool, n, rows, new_lens, true, &p)) != FF_OK) return st;
+  p.to = rows; p.new_lens = new_lens; p.result = missing;
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_pages_grow(p, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
+}
+
+ff_status ff_pages_free(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const int32_t *rows) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_pool(ctx, pool, true);
+  if (st != FF_OK) return st;
+  if (!rows) return fail(ctx, FF_ERR_INVALID_ARG, "rows is NULL");
+  PoolParams p;
+  if ((st = pool_params(ctx, pool, n, rows, nullptr, false, &p)) != FF_OK) return st;
+  p.to = rows;
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_pages_free(p, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
+}
+
+ff_status ff_pages_compact(ff_ctx *ctx, const ff_page_pool *pool, int32_t *live) {
+  if (!ctx) return FF_ERR_INVALID_ARG;
+  ff_status st = check_pool(ctx, pool, true);
+  if (st != FF_OK) return st;
+  if (!live) return fail(ctx, FF_ERR_INVALID_ARG, "live is NULL");
+  PoolParams p;
+  if ((st = pool_params(ctx, pool, 1, nullptr, nullptr, true, &p)) != FF_OK) return st;
+  p.result = live;
+  FF_HIP(ctx, hipSetDevice(ctx->device));
+  prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
+  FF_HIP(ctx, ff_launch_pages_compact(p, pool->parts, pool->n_parts, ctx->stream));
+  prof_end(&ctx->prof, ctx->stream);
+  return FF_OK;
 }
 
 ff_status ff_copy(ff_ctx *ctx, void *dst, const void *src, size_t bytes) {
