@@ -523,10 +523,10 @@ void set_cache8(AttnParams *p, const ff_paged_cache8 &c) {
   p->k_scale = c.k_scale; p->v_scale = c.v_scale;
   p->page_shift = log2_of(c.page_size); p->scale_shift = log2_of(c.scale_tokens); p->n_pages = c.n_pages;
 }
-// Attention over pages of either kind (one of the two is given); `tables` of page tables to a sequence.
+// Attention over pages of either kind (one of the two is given), of selected ones with a table to each key head.
 ff_status attend_pages(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs, const void *q, int64_t q_stride,
                        const int32_t *starts, const int32_t *lens, int32_t max_chunk, const ff_paged_cache *cache, const ff_paged_cache8 *cache8,
-                       const int32_t *table, int32_t table_stride, int tables, void *o, int64_t o_stride, float *lse) {
+                       const int32_t *table, int32_t table_stride, bool selected, void *o, int64_t o_stride, float *lse) {
   ff_status st = check_attention(ctx, a, n_tokens, n_seqs);
   if (st != FF_OK) return st;
   const int64_t qw = (int64_t)a->n_heads * a->head_dim;
@@ -541,7 +541,8 @@ ff_status attend_pages(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int
   p.counters = ctx->counters;
   if (cache8) set_cache8(&p, *cache8);
   else set_cache(&p, *cache);
-  set_chunks(&p, starts, lens, table, table_stride, tables);
+  set_chunks(&p, starts, lens, table, table_stride, selected ? a->n_kv_heads : 1);
+  p.selected = selected;
   const size_t need = ff_attention_need(p, a->head_dim, max_chunk);
   if (need > 0) {
     if (!ctx->ws) return fail(ctx, FF_ERR_WORKSPACE, "no workspace set (ff_set_workspace)");
@@ -1129,7 +1130,7 @@ ff_status ff_chunk_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_token
                              const int32_t *chunk_starts, const int32_t *context_lens, int32_t max_chunk, const ff_paged_cache *cache,
                              const int32_t *page_table, int32_t table_stride, void *o, int64_t o_stride, float *lse_opt) {
   if (!ctx) return FF_ERR_INVALID_ARG;
-  return attend_pages(ctx, a, n_tokens, n_seqs, q, q_stride, chunk_starts, context_lens, max_chunk, cache, nullptr, page_table, table_stride, 1,
+  return attend_pages(ctx, a, n_tokens, n_seqs, q, q_stride, chunk_starts, context_lens, max_chunk, cache, nullptr, page_table, table_stride, false,
                       o, o_stride, lse_opt);
 }
 
@@ -1163,7 +1164,7 @@ ff_status ff_chunk_attention8(ff_ctx *ctx, const ff_attention *a, int32_t n_toke
                               const int32_t *page_table, int32_t table_stride, void *o, int64_t o_stride, float *lse_opt) {
   if (!ctx) return FF_ERR_INVALID_ARG;
   if (!cache) return fail(ctx, FF_ERR_INVALID_ARG, "no cache, or one without pages or scales");
-  return attend_pages(ctx, a, n_tokens, n_seqs, q, q_stride, chunk_starts, context_lens, max_chunk, nullptr, cache, page_table, table_stride, 1,
+  return attend_pages(ctx, a, n_tokens, n_seqs, q, q_stride, chunk_starts, context_lens, max_chunk, nullptr, cache, page_table, table_stride, false,
                       o, o_stride, lse_opt);
 }
 
@@ -1268,7 +1269,7 @@ ff_status ff_selected_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_to
   if (st != FF_OK) return st;
   if ((st = check_selected(ctx, a)) != FF_OK || (st = check_either(ctx, cache, cache8)) != FF_OK) return st;
   return attend_pages(ctx, a, n_tokens, n_blocks, q, q_stride, block_starts, block_lens, max_chunk, cache, cache8, block_tables, block_stride,
-                      a->n_kv_heads, o, o_stride, lse_opt);
+                      true, o, o_stride, lse_opt);
 }
 
 ff_status ff_pages_workspace_bytes(const ff_page_pool *pool, int32_t n, size_t *bytes) {

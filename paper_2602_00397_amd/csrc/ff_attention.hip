@@ -395,32 +395,55 @@ __device__ __forceinline__ uint32_t chunk8_at(int key, int c) {
   constexpr int S = HD == 128 ? 1 : 2;            // log2 of the keys of a row
   return (uint32_t)((key >> S) * 256 + (((((key & ((1 << S) - 1)) << (4 - S)) | c) ^ swizzle8<HD>(key >> S)) << 4));
 }
-// The copies of KEYS (32 or 64) keys in 8 bits to LDS, as one wavefront makes them, 1 KB (8 or 16 keys of one page) each, and their scales, one for
-// each 8 keys.
+// The copies of KEYS (32 or 64) keys in 8 bits to LDS, as one wavefront makes them, 1 KB each, and their scales, one for each 8 keys.
+// Scalar arithmetic is what these cost (a lookup of page and scale for each KB: some 750 scalar instructions a step, 48 tokens 67 us), so keys
+// that are all there and in one page have one lookup, and others one for each 16.
 template <int HD, int KEYS>
 struct Copier8 {
-  static constexpr int KPI = 1024 / HD, NI = KEYS / KPI;
+  static constexpr int S = HD == 128 ? 1 : 2, KPI = 1024 / HD, NI = KEYS / KPI;   // log2 of the keys of a row, keys of a copy
   Source8 src;
   int end;
+  // key and offset of this lane's 16 bytes of copy i, from the copy's first key
+  static __device__ __forceinline__ int key_of(int i, int lane) { return ((i * 4 + (lane >> 4)) << S | (lane & 15) >> (4 - S)) - i * KPI; }
+  static __device__ __forceinline__ int chunk_of(int i, int lane) { return ((lane & 15) ^ swizzle8<HD>(i * 4 + (lane >> 4))) & ((1 << (4 - S)) - 1); }
   template <bool VALUES>
   __device__ __forceinline__ void copy(int j, uint32_t lds, int lane, f32x4_t (&scale)[KEYS / 32]) const {
-    const bool full = j + KEYS <= end;
+    const uint8_t *const codes = VALUES ? src.v : src.k;
+    const float *const scales = VALUES ? src.vs : src.ks;
+    if (j + KEYS <= end && (1 << src.shift) >= KEYS) {
+      int place;
+      const int page = page_of(src, j, place);
+      const uint8_t *base = codes + (size_t)page * src.page_bytes + (uint32_t)place * HD;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      constexpr int S = HD == 128 ? 1 : 2;
-      const int r = i * 4 + (lane >> 4), c = (lane & 15) ^ swizzle8<HD>(r);
-      const int in_copy = (r << S | c >> (4 - S)) - i * KPI, chunk = c & ((1 << (4 - S)) - 1);
-      const int key0 = full ? j + i * KPI : min(j + i * KPI, end - 1);
-      const int key = full ? in_copy : min(j + i * KPI + in_copy, end - 1) - key0;
+      for (int i = 0; i < NI; ++i) gload_lds16_at(base + i * 1024, (uint32_t)(key_of(i, lane) * HD + chunk_of(i, lane) * 16), lds + i * 1024);
+      const float *from = scales + (size_t)page * src.page_scales + (place >> src.scale_shift);
+      if ((1 << src.scale_shift) >= KEYS) {
+        const float one = scalar_load(from);
+#pragma unroll
+        for (int b = 0; b < KEYS / 8; ++b) scale[b >> 2][b & 3] = one;
+      } else {
+#pragma unroll
+        for (int b = 0; b < KEYS / 8; ++b) scale[b >> 2][b & 3] = scalar_load(from + (b * 8 >> src.scale_shift));
+      }
+      return;
+    }
+#pragma unroll
+    for (int g = 0; g < KEYS / 16; ++g) {
+      // (behind the end: the last key again, with some scale of its page; no row sees them)
+      const int key0 = min(j + g * 16, end - 1);
       int place;
       const int page = page_of(src, key0, place);
-      const uint8_t *base = (VALUES ? src.v : src.k) + (size_t)page * src.page_bytes + (uint32_t)place * HD;
-      gload_lds16_at(base, (uint32_t)(key * HD + chunk * 16), lds + i * 1024);
-      // (key0 is the last key where the copy's keys lie behind it, and then the copy has nothing but it)
+      const uint8_t *base = codes + (size_t)page * src.page_bytes + (uint32_t)place * HD;
 #pragma unroll
-      for (int b = 0; b < KPI / 8; ++b) {
-        const int n = i * (KPI / 8) + b;
-        scale[n >> 2][n & 3] = scale8<VALUES>(src, page, (full ? place : place & -KPI) + b * 8);
+      for (int i = g * 16 / KPI; i < (g + 1) * 16 / KPI; ++i) {
+        const int key = min(j + i * KPI + key_of(i, lane), end - 1) - key0;
+        gload_lds16_at(base, (uint32_t)(key * HD + chunk_of(i, lane) * 16), lds + i * 1024);
+      }
+      const float *from = scales + (size_t)page * src.page_scales;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int n = g * 2 + b;
+        scale[n >> 2][n & 3] = scalar_load(from + (((place & -16) + b * 8) >> src.scale_shift));
       }
     }
   }
@@ -1350,7 +1373,14 @@ hipError_t raise_limits() {
 // One token's keys go to a piece for every CU, and no more: its pieces are joined by one workgroup.  Many tokens' are cut finer, for
 // their lengths differ.  (Heads of 128, us with 256 / 512 / 1024 pieces: 8 key heads, one token over
 // 8191 keys, whose pieces were 256 / 128 / 64 keys long for it, 15.7 / 19.9 / 33.8, over 32768 28.6 / 32.0 / 44.3; 48 tokens over up to 16384 137 / 97 / 94.)
-int few_target(long tiles, int n_kv) { return tiles * n_kv < 128 ? kFewGrid / 2 : 2 * kFewGrid; }
+// Over keys in 8 bits, which come in half the time, to fewer: 48 tokens over up to 16384 with 512 / 768 / 1024 / 2048 pieces 57.6 / 55.0 / 59.6 / 70.1.
+// Selected pages are as many for every block, so blocks enough for every CU stay whole: 48 of some 2100 keys in 256 (whole) / 512 / 1024 pieces
+// 51.4 / 54.3 / 58.0 with the selection.
+int few_target(long tiles, int n_kv, bool eight, bool selected) {
+  if (selected || tiles * n_kv < 128) return kFewGrid / 2;
+  return eight ? 3 * kFewGrid / 2 : 2 * kFewGrid;
+}
+int most_few_target(long tiles, int n_kv) { return few_target(tiles, n_kv, false, false); }
 // Items that a plan can have at most: about `target` pieces and one more for each of the tiles and key heads.
 long most_items(long tiles, int n_kv, int target) { return tiles * n_kv + target + 16; }
 // (More items than counters: not split.  32768 keys among sequences of 200, 8 key heads of 128: 1400 tokens 273 us, 1600 670.)
@@ -1367,7 +1397,7 @@ struct Choice {
   size_t bytes = 0;
 };
 // `even`: a prompt's last tiles have not many more keys than the others.
-Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int max_chunk, bool paged, bool even) {
+Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int max_chunk, bool paged, bool even, bool eight, bool selected) {
   Choice c;
   const int group = n_heads / n_kv;
   const long rows = (long)n_tokens * group, chunk_rows = (long)max_chunk * group, seqs = std::min(n_seqs, n_tokens);
@@ -1385,17 +1415,19 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
   // One workgroup joins a tile's pieces where these have few rows in all; a launch more costs 1 to 3 us, and many rows several times
   // that.  (us joined by the last piece and by a launch: 8 key heads, one token of 4 rows over 8191 keys 15.4 and 16.5, 32768 28.2 and
   // 31.1; 4 key heads, one token of 7 rows over 16384 keys 24.1 and 20.5, four tokens 56 and 24.)
-  const auto joins_here = [&](long tile_rows, long tiles) { return tile_rows <= 8 && tile_rows * few_target(tiles, n_kv) <= 256 * tiles * n_kv; };
+  const auto joins_here = [&](long tile_rows, long tiles) { return tile_rows <= 8 && tile_rows * few_target(tiles, n_kv, eight, selected) <= 256 * tiles * n_kv; };
   // (the rows' own tiles and a part-filled one for each sequence; a call with more of them than are counted has longer chunks than the host
   // knows)
   if (paged && chunk_rows <= 32 && rows / 16 + seqs <= kMostItems) {
     c.nb = chunk_rows <= 16 ? 1 : 2;
     c.few_tiles = rows / (16 * c.nb) + seqs;
-    set(c.few, 16 * c.nb, c.few_tiles, 0, kAll, few_target(c.few_tiles, n_kv), 4);
+    set(c.few, 16 * c.nb, c.few_tiles, 0, kAll, few_target(c.few_tiles, n_kv, eight, selected), 4);
     c.few.join_here = joins_here(chunk_rows, c.few_tiles);
     return c;
   }
-  const bool both = paged && n_seqs > 1 && group <= 16;     // sequences that generate one token beside chunks
+  // sequences that generate one token beside chunks; blocks over selected pages that are mostly full have no more of them than a
+  // prompt's last, whose tile takes no longer than the others' (8192 tokens in blocks of 128: 4.7 us less without a launch for them)
+  const bool both = paged && n_seqs > 1 && group <= 16 && !(selected && 2l * n_tokens >= (long)n_seqs * max_chunk);
   // 256 rows, or 128 rows and two groups of keys: half as many steps for the longest tile, but twice the tiles, and steps that take 1.4
   // times as long.  256 rows where the others would be more than a tile for every CU, and where one causal prompt's longest tile takes as long as the
   // launch, where they are themselves.  (us with 128 and 256 rows, 8 key heads of 128 / 64.  One causal prompt of 2048 tokens, 256
@@ -1419,7 +1451,7 @@ Choice choose(int n_heads, int n_kv, int head_dim, int n_tokens, int n_seqs, int
   if (both) {
     c.nb = 1;
     c.few_tiles = seqs;
-    set(c.few, 16, seqs, 0, 16, few_target(seqs, n_kv), 4);
+    set(c.few, 16, seqs, 0, 16, few_target(seqs, n_kv, eight, selected), 4);
     c.few.join_here = joins_here(group, seqs);
   }
   return c;
@@ -1471,7 +1503,7 @@ size_t ff_attention_part_bytes(int n_heads, int n_kv, int head_dim, int n_tokens
   const auto bytes = [&](long tiles, int target, int tile_rows) {
     return std::min<long>(most_items(tiles, n_kv, target), kAttnCounters) * item_bytes(tile_rows, head_dim);
   };
-  const auto few = [&](long tiles, int tile_rows) { return bytes(tiles, few_target(tiles, n_kv), tile_rows); };
+  const auto few = [&](long tiles, int tile_rows) { return bytes(tiles, most_few_target(tiles, n_kv), tile_rows); };
   // tiles of 128 rows, the only ones of calls that are split, beside sequences of at most 16 rows
   const long whole = std::min(rows / 128, (few_items(n_seqs) - 1) / n_kv);
   size_t most = bytes(whole + seqs, tile_target(n_seqs, head_dim), 128) + (n_seqs > 1 && group <= 16 ? few(seqs, 16) : 0);
@@ -1482,7 +1514,7 @@ size_t ff_attention_part_bytes(int n_heads, int n_kv, int head_dim, int n_tokens
 
 static Choice choose(const AttnParams &p, int head_dim, int max_chunk) {
   const bool even = !p.causal || p.n_seqs > 1 || (p.window > 0 && p.window < p.T);
-  return choose(p.n_heads, p.n_kv, head_dim, p.T, p.n_seqs, max_chunk, p.table != nullptr, even);
+  return choose(p.n_heads, p.n_kv, head_dim, p.T, p.n_seqs, max_chunk, p.table != nullptr, even, p.k_scale != nullptr, p.selected);
 }
 
 size_t ff_attention_need(const AttnParams &p, int head_dim, int max_chunk) {

@@ -11,7 +11,7 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kBatch = 8;     // loads of a lane on their way
 
 // ---- mean keys of the pages that have new tokens ------------------------------------------------------------------------------
 // A workgroup to a page and key head: HD / 8 lanes to a key, float64 sums (of up to 4096 bf16 numbers, nearly always exact), one rounding.
@@ -91,13 +91,23 @@ __global__ __launch_bounds__(kThreads) void ff_page_scores_kernel(SelectParams a
   if (b.s < 0 || b.earlier <= a.keep || (int)blockIdx.z * 64 >= b.earlier) return;
   const int group = threadIdx.x / LPR, channel = threadIdx.x % LPR * 8;
   double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (int r = group; r < b.n * p.group; r += GROUPS) {
-    const int t = p.by_group(r);
-    const u32x4_t w = *reinterpret_cast<const u32x4_t *>(p.q + (int64_t)(b.t0 + t) * p.q_stride + (kvh * p.group + r - t * p.group) * HD + channel);
+  const int rows = b.n * p.group;
+  for (int r0 = group; r0 < rows; r0 += GROUPS * kBatch) {
+    u32x4_t w[kBatch];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      acc[2 * e] += (double)__uint_as_float(w[e] << 16);
-      acc[2 * e + 1] += (double)__uint_as_float(w[e] & 0xffff0000u);
+    for (int i = 0; i < kBatch; ++i) {
+      const int r = min(r0 + i * GROUPS, rows - 1), t = p.by_group(r);
+      w[i] = *reinterpret_cast<const u32x4_t *>(p.q + (int64_t)(b.t0 + t) * p.q_stride + (kvh * p.group + r - t * p.group) * HD + channel);
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const bool is = r0 + i * GROUPS < rows;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t v = is ? w[i][e] : 0;
+        acc[2 * e] += (double)__uint_as_float(v << 16);
+        acc[2 * e + 1] += (double)__uint_as_float(v & 0xffff0000u);
+      }
     }
   }
 #pragma unroll
@@ -134,27 +144,109 @@ __global__ __launch_bounds__(kThreads) void ff_page_scores_kernel(SelectParams a
 }
 
 // ---- the best pages, in order ---------------------------------------------------------------------------------------------------
-// A score as a whole number in the scores' order (-0 as +0; NaN by its bits), and pages that are always taken above all.
-__device__ __forceinline__ uint64_t order_of(double s) {
+// A workgroup to a block and key head: a chain of latencies.  The scores' range is cut into 1024 parts; those above the part that holds
+// the last page wanted are taken, and of that part's few the best, by counting for each how many are better.  (2047 pages of which 64
+// are kept 14.1 us by whole numbers alone, as below, 9.4 so.)
+// Where that part has too many, or scores are not finite, the scores are compared as whole numbers in their order: the range of those is
+// cut in 1024 until the part with the last one wanted has no more than are wanted of it, or is one number (then its first pages are); each
+// cut is ten bits of it, so there are at most seven.
+constexpr int kBins = 1024, kHeld = 4096, kFew = 64;     // parts; scores that are held in LDS (of more pages they are read again); candidates of a part
+__device__ __forceinline__ uint64_t order_of(double s) {      // (-0 as +0; NaN by its bits)
   const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 // (of plain min and max, mixed 64-bit types take the double one)
 __device__ __forceinline__ uint64_t lower(uint64_t a, uint64_t b) { return a < b ? a : b; }
 __device__ __forceinline__ uint64_t higher(uint64_t a, uint64_t b) { return a < b ? b : a; }
-constexpr int kBins = 1024, kHeld = 4096;     // numbers that are held in LDS; of more pages they are made again from the scores
-// A workgroup to a block and key head.  The range of the numbers that hold the last one wanted is cut in 1024 until that one's part has
-// no more than are wanted of it (or is one number: then its first pages are); each cut is ten bits of it, so there are at most seven.
+struct SelectShared {
+  double held[kHeld];
+  double extreme[2][kThreads / 64];
+  int bins[kBins], sums[kThreads / 64], sums2[kThreads / 64], odd[kThreads / 64], found[3], n_few;
+  double few[kFew], last;
+  int few_at[kFew], last_at;
+};
+// The part, counted from the highest, in which the running count reaches `want`: found = part, how many are above it, how many in it.
+__device__ __forceinline__ void find_part(SelectShared &sh, int want) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int top = kBins - 1 - 4 * (int)threadIdx.x;
+  const int c[4] = {sh.bins[top], sh.bins[top - 1], sh.bins[top - 2], sh.bins[top - 3]};
+  const int mine = c[0] + c[1] + c[2] + c[3], upto = lane_sums(mine);
+  if (lane == 63) sh.sums[wave] = upto;
+  __syncthreads();
+  int above = upto - mine;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) above += w < wave ? sh.sums[w] : 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (above < want && want <= above + c[i]) {
+      sh.found[0] = top - i;
+      sh.found[1] = above;
+      sh.found[2] = c[i];
+    }
+    above += c[i];
+  }
+  __syncthreads();
+}
+// The pages that `taken` says, in order, and of those that `tied` says the first `ties`: a run of pages to a thread.
+template <class Taken, class Tied>
+__device__ __forceinline__ void write_list(SelectShared &sh, int n, int ties, const int32_t *table, int32_t *list, Taken taken, Tied tied) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int per = (n + kThreads - 1) / kThreads, from = min(n, (int)threadIdx.x * per), to = min(n, from + per);
+  int t = 0, e = 0;
+  for (int i = from; i < to; ++i) {
+    t += taken(i);
+    e += tied(i);
+  }
+  const int t_upto = lane_sums(t), e_upto = lane_sums(e);
+  if (lane == 63) {
+    sh.sums[wave] = t_upto;
+    sh.sums2[wave] = e_upto;
+  }
+  __syncthreads();
+  int at = t_upto - t, before = e_upto - e;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    at += w < wave ? sh.sums[w] : 0;
+    before += w < wave ? sh.sums2[w] : 0;
+  }
+  for (int i = from; i < to; ++i) {
+    const bool is = taken(i), tie = tied(i);
+    if (is || (tie && before < ties)) list[at + min(before, ties)] = table[i];
+    at += is;
+    before += tie;
+  }
+}
+template <class Get>
+__device__ __forceinline__ void list_by_numbers(SelectShared &sh, int n, int kept, const int32_t *table, int32_t *list, Get number) {
+  uint64_t lo = 0, hi = ~0ull;
+  int want = kept;               // of those in [lo, hi]; all above are taken
+  for (;;) {
+    const int shift = max(0, 64 - (int)__clzll((long long)(hi - lo | 1)) - 10);
+    __syncthreads();             // (what the last use of the counts read)
+    for (int i = threadIdx.x; i < kBins; i += kThreads) sh.bins[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const uint64_t u = number(i);
+      if (u >= lo && u <= hi) atomicAdd(&sh.bins[(u - lo) >> shift], 1);
+    }
+    __syncthreads();
+    find_part(sh, want);
+    lo += (uint64_t)sh.found[0] << shift;
+    hi = lo + lower(hi - lo, ((uint64_t)1 << shift) - 1);
+    want -= sh.found[1];
+    if (shift == 0 || sh.found[2] == want) break;
+  }
+  __syncthreads();
+  write_list(sh, n, want, table, list, [&](int i) { return number(i) > hi; }, [&](int i) { const uint64_t u = number(i); return u >= lo && u <= hi; });
+}
 __global__ __launch_bounds__(kThreads) void ff_select_pages_kernel(SelectParams a) {
-  __shared__ uint64_t held[kHeld];
-  __shared__ uint64_t extreme[2][kThreads / 64];
-  __shared__ int bins[kBins], sums[kThreads / 64], found[3];
+  __shared__ SelectShared sh;
   const AttnParams &p = a.seqs;
   const int x = blockIdx.y, kvh = blockIdx.x;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const Block b = block_of(a, x);
-  const int end = attn_clamp(p.starts[p.n_seqs], 0, p.T);
   if (kvh == 0 && threadIdx.x == 0) {
+    const int end = attn_clamp(p.starts[p.n_seqs], 0, p.T);
     a.starts[x] = b.s < 0 ? end : b.t0;
     a.lens[x] = b.keys;
     if (x == a.n_blocks - 1) a.starts[a.n_blocks] = b.s < 0 ? end : b.t0 + b.n;
@@ -168,91 +260,92 @@ __global__ __launch_bounds__(kThreads) void ff_select_pages_kernel(SelectParams 
     return;
   }
   const double *scores = a.scores + ((size_t)x * p.n_kv + kvh) * p.table_stride;
-  const bool hold = n <= kHeld;
-  const auto number = [&](int i) { return i < a.first ? ~0ull : order_of(scores[i]); };
-  const auto get = [&](int i) { return hold ? held[i] : number(i); };
-  uint64_t lo = ~0ull, hi = 0;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const uint64_t u = number(i);
-    if (hold) held[i] = u;
-    lo = lower(lo, u);
-    hi = higher(hi, u);
-  }
+  const int first = a.first, want = kept - first;
+  bool by_numbers = n > kHeld;
+  double lo = INFINITY, hi = -INFINITY, scale = 0;
+  if (!by_numbers) {
+    bool odd = false;
+    for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kBatch) {
+      double s[kBatch];
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    lo = lower(lo, __shfl_xor((unsigned long long)lo, off));
-    hi = higher(hi, __shfl_xor((unsigned long long)hi, off));
-  }
-  if (lane == 0) {
-    extreme[0][wave] = lo;
-    extreme[1][wave] = hi;
-  }
-  __syncthreads();
+      for (int i = 0; i < kBatch; ++i) s[i] = scores[min(i0 + i * kThreads, n - 1)];
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    lo = lower(lo, extreme[0][w]);
-    hi = higher(hi, extreme[1][w]);
-  }
-  int want = kept;               // of those in [lo, hi]; all above are taken
-  for (;;) {
-    const int shift = max(0, 64 - (int)__clzll((long long)(hi - lo | 1)) - 10);
-    for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      const uint64_t u = get(i);
-      if (u >= lo && u <= hi) atomicAdd(&bins[(u - lo) >> shift], 1);
+      for (int i = 0; i < kBatch; ++i)
+        if (i0 + i * kThreads < n) {
+          sh.held[i0 + i * kThreads] = s[i];
+          if (i0 + i * kThreads >= first) {
+            odd = odd || !(fabs(s[i]) < INFINITY);
+            lo = fmin(lo, s[i]);
+            hi = fmax(hi, s[i]);
+          }
+        }
+    }
+    for (int i = threadIdx.x; i < kBins; i += kThreads) sh.bins[i] = 0;
+    if (threadIdx.x == 0) sh.n_few = 0;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+      lo = fmin(lo, __shfl_xor(lo, off));
+      hi = fmax(hi, __shfl_xor(hi, off));
+    }
+    const bool any_odd = __any(odd);
+    if (lane == 0) {
+      sh.extreme[0][wave] = lo;
+      sh.extreme[1][wave] = hi;
+      sh.odd[wave] = any_odd;
     }
     __syncthreads();
-    // bins in falling order, four to a thread
-    const int top = kBins - 1 - 4 * (int)threadIdx.x;
-    const int c[4] = {bins[top], bins[top - 1], bins[top - 2], bins[top - 3]};
-    const int mine = c[0] + c[1] + c[2] + c[3], upto = lane_sums(mine);
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    int above = upto - mine;
-    for (int w = 0; w < wave; ++w) above += sums[w];
+    by_numbers = want == 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (above < want && want <= above + c[i]) {
-        found[0] = top - i;
-        found[1] = above;
-        found[2] = c[i];
-      }
-      above += c[i];
+    for (int w = 0; w < kThreads / 64; ++w) {
+      lo = fmin(lo, sh.extreme[0][w]);
+      hi = fmax(hi, sh.extreme[1][w]);
+      by_numbers = by_numbers || sh.odd[w];
     }
+    const double range = hi - lo;
+    by_numbers = by_numbers || !(range > 1e-290 && range < 1e290);
+    scale = (kBins - 1) / range;
+  }
+  const auto part_of = [&](double s) { return min((int)((s - lo) * scale), kBins - 1); };       // (rounded, but never out of order)
+  int part = 0, need = 0, c = 0;
+  if (!by_numbers) {
+    for (int i = first + threadIdx.x; i < n; i += kThreads) atomicAdd(&sh.bins[part_of(sh.held[i])], 1);
     __syncthreads();
-    lo += (uint64_t)found[0] << shift;
-    hi = lo + lower(hi - lo, ((uint64_t)1 << shift) - 1);
-    want -= found[1];
-    if (shift == 0 || found[2] == want) break;
+    find_part(sh, want);
+    part = sh.found[0];
+    need = want - sh.found[1];
+    c = sh.found[2];
+    by_numbers = c > kFew;
   }
-  // a run of pages to a thread: how many are above, how many in the last part, and where its own begin
-  const int per = (n + kThreads - 1) / kThreads, from = min(n, (int)threadIdx.x * per), to = min(n, from + per);
-  int taken = 0, last = 0;
-  for (int i = from; i < to; ++i) {
-    const uint64_t u = get(i);
-    taken += u > hi;
-    last += u >= lo && u <= hi;
+  if (by_numbers) {
+    list_by_numbers(sh, n, kept, table, list, [&](int i) { return i < first ? ~0ull : order_of(n > kHeld ? scores[i] : sh.held[i]); });
+    return;
   }
-  __syncthreads();               // (found and sums have been read)
-  const int taken_upto = lane_sums(taken), last_upto = lane_sums(last);
-  if (lane == 63) {
-    sums[wave] = taken_upto;
-    bins[wave] = last_upto;
+  for (int i = first + threadIdx.x; i < n; i += kThreads)
+    if (part_of(sh.held[i]) == part) {
+      const int k = atomicAdd(&sh.n_few, 1);
+      sh.few[k] = sh.held[i];
+      sh.few_at[k] = i;
+    }
+  __syncthreads();
+  if ((int)threadIdx.x < c) {
+    const double s = sh.few[threadIdx.x];
+    const int at = sh.few_at[threadIdx.x];
+    int better = 0;
+    for (int k = 0; k < c; ++k) better += sh.few[k] > s || (sh.few[k] == s && sh.few_at[k] < at);
+    if (better == need - 1) {
+      sh.last = s;
+      sh.last_at = at;
+    }
   }
   __syncthreads();
-  int before = last_upto - last, at = taken_upto - taken;
-  for (int w = 0; w < wave; ++w) {
-    at += sums[w];
-    before += bins[w];
-  }
-  for (int i = from; i < to; ++i) {
-    const uint64_t u = get(i);
-    const bool in_last = u >= lo && u <= hi;
-    if (u > hi || (in_last && before < want)) list[at + min(before, want)] = table[i];
-    at += u > hi;
-    before += in_last;
-  }
+  const double last = sh.last;
+  const int last_at = sh.last_at;
+  const auto taken = [&](int i) {
+    const double s = sh.held[i];
+    const int its = part_of(s);
+    return i < first || its > part || (its == part && (s > last || (s == last && i <= last_at)));
+  };
+  write_list(sh, n, 0, table, list, taken, [](int) { return false; });
 }
 
 template <int HD>
