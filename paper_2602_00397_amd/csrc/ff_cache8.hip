@@ -33,41 +33,37 @@ __global__ __launch_bounds__(kThreads) void ff_append8_kernel(Append8Params a, l
   for (long id = blockIdx.x; id * UNITS < n_items; id += gridDim.x) {
     const long unit = id * UNITS + wave / W;
     // (all of a workgroup's wavefronts pass the barrier below the same number of times)
-    const int heads = 2 * p.n_kv;
-    const long run = unit / heads;
-    const int h = (int)(unit - run * heads), kvh = h >> 1;
-    const bool is_v = h & 1;
+    // k and v of a head side by side, then the heads, then the blocks (of runs and heads there are fewer than 2^31)
+    const bool is_v = unit & 1;
+    const int pair = (int)(unit >> 1), run = p.by_kv(pair), kvh = pair - run * p.n_kv;
     const Found f = unit < n_items ? find_item(p, run, [&](const Seq &q) { return runs_of(q, p.scale_shift); }) : Found{-1, 0, {0, 0, 0}};
     const int first = first_new(f.seq), block = (first >> p.scale_shift) + f.at;
     const int from = max(first, block << p.scale_shift);
     const int n = f.s < 0 ? 0 : (int)min((long)f.seq.keys, (long)(block + 1) << p.scale_shift) - from;
-    int page = -1;
-    if (f.s >= 0) page = p.table[f.s * p.seq_tables + (from >> p.page_shift)];
-    const bool here = n > 0 && (unsigned)page < (unsigned)p.n_pages;
-    // token number i of the unit is row t0 of the call + i
+    // token number i of the unit is row t0 of the call + i.  (Its values are on their way while the page is looked up.)
     const int64_t t0 = (int64_t)f.seq.t0 + (from - (f.seq.keys - f.seq.n));
     const bf16_t *src = (is_v ? a.v + t0 * a.v_stride : a.k + t0 * a.k_stride) + kvh * HD + channel;
     const int64_t stride = is_v ? a.v_stride : a.k_stride;
+    int page = -1;
+    if (f.s >= 0) page = p.table[f.s * p.seq_tables + (from >> p.page_shift)];
     u32x4_t x[PASSES];
-    float top = 0.f;
-    if (here) {
 #pragma unroll
-      for (int i = 0; i < PASSES; ++i) {
-        const int t = i * W * TPW + token;
-        x[i] = u32x4_t{0, 0, 0, 0};
-        if (i * W * TPW < n && t < n) x[i] = *reinterpret_cast<const u32x4_t *>(src + t * stride);
-      }
-#pragma unroll
-      for (int i = 0; i < PASSES; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float lo = fabsf(__uint_as_float(x[i][e] << 16)), hi = fabsf(__uint_as_float(x[i][e] & 0xffff0000u));
-          if (lo < INFINITY) top = fmaxf(top, lo);
-          if (hi < INFINITY) top = fmaxf(top, hi);
-        }
-#pragma unroll
-      for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+    for (int i = 0; i < PASSES; ++i) {
+      const int t = i * W * TPW + token;
+      x[i] = u32x4_t{0, 0, 0, 0};
+      if (i * W * TPW < n && t < n) x[i] = *reinterpret_cast<const u32x4_t *>(src + t * stride);
     }
+    const bool here = n > 0 && (unsigned)page < (unsigned)p.n_pages;
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float lo = fabsf(__uint_as_float(x[i][e] << 16)), hi = fabsf(__uint_as_float(x[i][e] & 0xffff0000u));
+        if (lo < INFINITY) top = fmaxf(top, lo);
+        if (hi < INFINITY) top = fmaxf(top, hi);
+      }
+    top = lane_max(top);
     if (W > 1) {
       if (lane == 0) top_s[wave] = top;
       __syncthreads();

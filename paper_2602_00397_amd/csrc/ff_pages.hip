@@ -61,21 +61,42 @@ __device__ __forceinline__ int sums_before(int v, int &all) {
 }
 // what another thread of the workgroup wrote, not what this CU's cache held before
 __device__ __forceinline__ int fresh(const int *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ void written() { __threadfence(); }
+__device__ __forceinline__ void put(int *at, int v) { __hip_atomic_store(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// (those stores have arrived where the loads above look: no write-back of a cache is needed, which a fence would make)
+__device__ __forceinline__ void written() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// Of several entries of one row the last counts: winner[row] = its number + 1.
-__device__ void find_winners(const PoolParams &p, const Work &w) {
-  for (int i = threadIdx.x; i < p.n; i += kPlanThreads)
-    if (is_row(p, p.to[i])) __hip_atomic_store(&w.winner[p.to[i]], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+// Of several entries of one row the last counts: every row that is listed is marked with the number of its last entry, in LDS where there is
+// room for all rows.
+constexpr int kRowsHeld = 4096;
+struct Winners {
+  int held[kRowsHeld];
+};
+__device__ __forceinline__ void find_winners(const PoolParams &p, const Work &w, Winners &in) {
+  const bool hold = p.n_rows <= kRowsHeld;
+  for (int i = threadIdx.x; i < p.n; i += kPlanThreads) {
+    const int row = p.to[i];
+    if (!is_row(p, row)) continue;
+    if (hold) in.held[row] = 0;
+    else put(&w.winner[row], 0);
+  }
   written();
   __syncthreads();
-  for (int i = threadIdx.x; i < p.n; i += kPlanThreads)
-    if (is_row(p, p.to[i])) __hip_atomic_fetch_max(&w.winner[p.to[i]], i + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int i = threadIdx.x; i < p.n; i += kPlanThreads) {
+    const int row = p.to[i];
+    if (!is_row(p, row)) continue;
+    if (hold) atomicMax(&in.held[row], i + 1);
+    else __hip_atomic_fetch_max(&w.winner[row], i + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
   written();
   __syncthreads();
 }
-// The first `want` free pages, in order, to `pages`; how many there are of them.
-__device__ int find_free(const PoolParams &p, int want, int *pages) {
+__device__ __forceinline__ bool wins(const PoolParams &p, const Work &w, const Winners &in, int i) {
+  const int row = p.to[i];
+  return (p.n_rows <= kRowsHeld ? in.held[row] : fresh(&w.winner[row])) == i + 1;
+}
+// The first `want` free pages, in order, to `sink` with their numbers; how many there are of them.
+template <class Sink>
+__device__ __forceinline__ int find_free(const PoolParams &p, int want, Sink sink) {
   int found = 0;
   for (int j0 = 0; j0 < p.n_pages && found < want; j0 += 4 * kPlanThreads) {
     const int j = j0 + 4 * (int)threadIdx.x;
@@ -94,7 +115,7 @@ __device__ int find_free(const PoolParams &p, int want, int *pages) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (r[e] <= 0) {
-        if (at < want) pages[at] = j + e;
+        if (at < want) sink(at, j + e);
         ++at;
       }
     found += all;
@@ -161,12 +182,13 @@ __global__ __launch_bounds__(kPlanThreads) void ff_pages_fork_plan_kernel(PoolPa
     }
     return;
   }
-  find_winners(p, w);
+  __shared__ Winners in;
+  find_winners(p, w, in);
   int want = 0;
   for (int i0 = 0; i0 < p.n; i0 += kPlanThreads) {
     const int i = i0 + threadIdx.x;
     int first = kSkip, needs = 0;
-    if (i < p.n && is_row(p, p.to[i]) && is_row(p, p.from[i]) && p.from[i] != p.to[i] && fresh(&w.winner[p.to[i]]) == i + 1) {
+    if (i < p.n && is_row(p, p.to[i]) && is_row(p, p.from[i]) && p.from[i] != p.to[i] && wins(p, w, in, i)) {
       const int len = clamped_len(p, p.lens[p.from[i]]), last = len >> p.page_shift;
       needs = (len & ((1 << p.page_shift) - 1)) != 0 && is_page(p, p.table[(size_t)p.from[i] * p.table_stride + last]);
       first = 0;
@@ -176,7 +198,7 @@ __global__ __launch_bounds__(kPlanThreads) void ff_pages_fork_plan_kernel(PoolPa
     if (i < p.n) w.first[i] = first == kSkip ? kSkip : needs ? want + before : -1;
     want += all;
   }
-  const int found = find_free(p, want, pages);
+  const int found = find_free(p, want, [&](int at, int page) { pages[at] = page; });
   if (threadIdx.x == 0) {
     *w.ok = found == want;
     *p.result = want - found;
@@ -216,42 +238,60 @@ __global__ __launch_bounds__(kThreads) void ff_pages_fork_kernel(PoolParams p, P
 }
 
 // ---- grow, free -------------------------------------------------------------------------------------------------------------------
+// One workgroup.  With up to 1024 entries that take up to 4096 pages the plan stays in LDS, and rows that change by a few pages, as they do
+// when tokens are generated, have a thread each (256 rows of a page at most 24.9 us with a wavefront each and fences, 5.7 so).
+constexpr int kHeldPages = 4096, kFewPages = 8;
 __global__ __launch_bounds__(kPlanThreads) void ff_pages_grow_kernel(PoolParams p) {
+  __shared__ Winners in;
+  __shared__ int firsts[kPlanThreads], held[kHeldPages];
   const Work w = work_of(p);
-  find_winners(p, w);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  find_winners(p, w, in);
   long wanted = 0;
+  bool long_change = false;
+  int first = kSkip;
   for (int i0 = 0; i0 < p.n; i0 += kPlanThreads) {
     const int i = i0 + threadIdx.x;
-    const bool is = i < p.n && is_row(p, p.to[i]) && fresh(&w.winner[p.to[i]]) == i + 1;
-    const int needs = is ? max(0, pages_of(p, p.new_lens[i]) - pages_of(p, p.lens[p.to[i]])) : 0;
+    const bool is = i < p.n && is_row(p, p.to[i]) && wins(p, w, in, i);
+    const int change = is ? pages_of(p, p.new_lens[i]) - pages_of(p, p.lens[p.to[i]]) : 0;
     int all;
-    const int before = sums_before(needs, all);            // (of 1024 rows of at most 2^20 pages)
-    if (i < p.n) w.first[i] = is ? (int)min(wanted + before, 0x7fffffffL) : kSkip;
+    const int before = sums_before(max(change, 0), all);            // (of 1024 rows of at most 2^20 pages)
+    first = is ? (int)min(wanted + before, 0x7fffffffL) : kSkip;
+    if (p.n > kPlanThreads && i < p.n) put(&w.first[i], first);
+    long_change = long_change || change > kFewPages || change < -kFewPages;
     wanted += all;
   }
+  const bool in_lds = p.n <= kPlanThreads && wanted <= kHeldPages;
+  if (p.n <= kPlanThreads) firsts[threadIdx.x] = first;
   const int want = (int)min(wanted, (long)p.n_pages + 1);
-  const int found = find_free(p, want, w.pages);
+  const int found = find_free(p, want, [&](int at, int page) {
+    if (in_lds) held[at] = page;
+    else put(&w.pages[at], page);
+  });
   if (threadIdx.x == 0) *p.result = (int)min(wanted - found, 0x7fffffffL);
   if (found < want) return;
   written();
-  __syncthreads();
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int i = wave; i < p.n; i += kPlanThreads / 64) {
-    const int first = fresh(&w.first[i]);
-    if (first == kSkip) continue;
+  const bool by_wave = __syncthreads_or(long_change) || p.n > kPlanThreads;
+  const auto apply = [&](int i, int at, int step, int begin) __attribute__((always_inline)) {
+    if (begin == kSkip) return;
     int *row = p.table + (size_t)p.to[i] * p.table_stride;
     const int len = clamped_len(p, p.new_lens[i]), had = pages_of(p, p.lens[p.to[i]]), gets = pages_of(p, len);
-    for (int j = had + lane; j < gets; j += 64) {
-      const int page = fresh(&w.pages[first + j - had]);
+    for (int j = had + at; j < gets; j += step) {
+      const int page = in_lds ? held[begin + j - had] : fresh(&w.pages[begin + j - had]);
       row[j] = page;
       p.refs[page] = 1;
     }
-    for (int j = gets + lane; j < had; j += 64) {
+    for (int j = gets + at; j < had; j += step) {
       if (is_page(p, row[j])) atomicSub(&p.refs[row[j]], 1);
       row[j] = -1;
     }
-    if (lane == 0) p.lens[p.to[i]] = len;
+    if (at == 0) p.lens[p.to[i]] = len;
+  };
+  if (!by_wave) {
+    if ((int)threadIdx.x < p.n) apply(threadIdx.x, 0, 1, first);
+    return;
   }
+  for (int i = wave; i < p.n; i += kPlanThreads / 64) apply(i, lane, 64, p.n <= kPlanThreads ? firsts[i] : fresh(&w.first[i]));
 }
 
 // (a row that is listed twice: whoever takes an entry gives its page back)
@@ -295,8 +335,8 @@ __global__ __launch_bounds__(kPlanThreads) void ff_pages_compact_plan_kernel(Poo
     // (a run of pages may have both: the two counts go together, 11 bits are enough for each)
     int both;
     const int before = sums_before((int)is_hole | (int)is_move << 12, both);
-    if (is_hole) c.holes[holes + (before & 0xfff)] = j;
-    if (is_move) c.origin[moves + (before >> 12)] = j;
+    if (is_hole) put(&c.holes[holes + (before & 0xfff)], j);
+    if (is_move) put(&c.origin[moves + (before >> 12)], j);
     if (j < p.n_pages && j >= live && !is_move) c.target[j] = -1;
     holes += both & 0xfff;
     moves += both >> 12;

@@ -22,8 +22,7 @@ __global__ __launch_bounds__(kThreads) void ff_page_means_kernel(SelectParams a,
   const AttnParams &p = a.seqs;
   const int group = threadIdx.x / LPK, channel = threadIdx.x % LPK * 8;
   for (long id = blockIdx.x; id < n_items; id += gridDim.x) {
-    const long run = id / p.n_kv;
-    const int kvh = (int)(id - run * p.n_kv);
+    const int run = p.by_kv((int)id), kvh = (int)id - run * p.n_kv;       // (fewer than 2^31)
     const Found f = find_item(p, run, [&](const Seq &q) { return runs_of(q, p.page_shift); });
     if (f.s < 0) break;
     const int number = (first_new(f.seq) >> p.page_shift) + f.at, page = p.table[f.s * p.seq_tables + number];

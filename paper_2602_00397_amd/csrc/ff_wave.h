@@ -18,6 +18,16 @@ __device__ __forceinline__ T lane_sums(T v) {
   v += dpp<0x143, 0xc>(v);     // rows 2 and 3: lane 31
   return v;
 }
+// the largest of the lanes' values, none of them below 0 (in all lanes)
+__device__ __forceinline__ float lane_max(float v) {
+  v = fmaxf(v, dpp<0x111, 0xf>(v));
+  v = fmaxf(v, dpp<0x112, 0xf>(v));
+  v = fmaxf(v, dpp<0x114, 0xf>(v));
+  v = fmaxf(v, dpp<0x118, 0xf>(v));
+  v = fmaxf(v, dpp<0x142, 0xa>(v));
+  v = fmaxf(v, dpp<0x143, 0xc>(v));
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
 __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 __device__ __forceinline__ float last_lane(float v) { return __builtin_bit_cast(float, last_lane(__builtin_bit_cast(int, v))); }
 // a wave-uniform value by a scalar load: the wait for it is not one for the copies before it

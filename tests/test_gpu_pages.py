@@ -219,6 +219,24 @@ def test_pages_in_use_by_their_thousands(ctx):  # noqa: F811
     assert p.counts_match()
 
 
+def test_more_rows_than_are_marked_in_lds(ctx):  # noqa: F811
+    """Entries of one row among few and many entries, in tables of some thousand rows; rows that change by many pages beside those by one."""
+    p = Pool(6000, 5000, 60, parts=((2, torch.float32),), seed=10)
+    p.check("grow", p.grow(ctx, [4999, 3, 4999, 7, 3], [5, 900, 40, 16, 33]))
+    p.check("fork", p.fork(ctx, [4999, 3, 7, 3], [8, 4500, 8, 9]))
+    rows = [(13 * i) % 5000 for i in range(1100)] + [(13 * i) % 5000 for i in range(50)]
+    p.check("grow many", p.grow(ctx, rows, [1 + i % 70 for i in range(1150)]))
+    p.check("fork many", p.fork(ctx, rows, [(13 * i + 1) % 5000 for i in range(1150)]))
+    p.free(ctx, rows[:600])
+    p.check("free")
+    p.check("compact", p.compact(ctx))
+    assert p.counts_match()
+    p.check("grow in LDS", p.grow(ctx, list(range(0, 1000)), [(i * 7) % 40 for i in range(1000)]))
+    p.check("long rows", p.grow(ctx, [4000, 4001, 4002], [960, 1, 500]))
+    p.check("short again", p.grow(ctx, [4000, 4001, 4002], [1, 960, 0]))
+    assert p.counts_match()
+
+
 def test_tables_that_hold_no_pages(ctx):  # noqa: F811
     """Entries out of range are not counted, not followed and not copied; lengths are cut to what a row can have."""
     p = Pool(50, 6, 6, seed=6)
