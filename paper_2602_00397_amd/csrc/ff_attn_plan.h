@@ -160,3 +160,33 @@ ATTN_FN Range row_range(const AttnParams &p, const Seq &q, int r) {
 ATTN_FN int pieces_of(const Range &r, int keys_per_piece) {
   return r.hi > r.lo ? (r.hi - r.lo - 1) / keys_per_piece + 1 : 1;
 }
+
+// ---- new tokens by the runs of positions and by the blocks that they lie in
+// They stand at the positions keys - n .. keys - 1 of their sequence, as far as these are not negative.
+ATTN_FN int first_new(const Seq &q) { return q.keys > q.n ? q.keys - q.n : 0; }
+// how many runs of 2^shift positions have new tokens
+ATTN_FN int runs_of(const Seq &q, int shift) {
+  return q.n > 0 && q.keys > 0 ? ((q.keys - 1) >> shift) - (first_new(q) >> shift) + 1 : 0;
+}
+// most runs of a call: each has a token, and all of a sequence's but two are full
+inline long most_runs(long n_tokens, long n_seqs, int shift) {
+  const long seqs = n_seqs < n_tokens ? n_seqs : n_tokens, runs = (n_tokens >> shift) + 2 * seqs;
+  return runs < n_tokens ? runs : n_tokens;
+}
+ATTN_FN int blocks_of(const Seq &q, int query_block) { return (int)(((long)q.n + query_block - 1) / query_block); }
+// Block number `at` of sequence s: its rows, how many pages lie in front of the one that its first token is in, how many from that one to the
+// last token's, and the keys of as many of the former as are kept and of the latter, up to the last token.
+struct Block { int s, t0, n, earlier, own, keys; };
+ATTN_FN Block block_at(const Seq &q, int s, int at, int query_block, int keep, int page_shift) {
+  Block b = {s, 0, 0, 0, 0, 0};
+  const int t = at * query_block;
+  b.t0 = q.t0 + t;
+  b.n = attn_min(query_block, q.n - t);
+  const int last = q.keys - q.n + t + b.n - 1;              // (below 0: its tokens see nothing)
+  if (last < 0) return b;
+  b.earlier = attn_max(last - b.n + 1, 0) >> page_shift;
+  b.own = (last >> page_shift) - b.earlier + 1;
+  // (its own pages are the last of the list, and the last of those ends with the block's last token)
+  b.keys = ((attn_min(keep, b.earlier) + b.own - 1) << page_shift) + (last & ((1 << page_shift) - 1)) + 1;
+  return b;
+}

@@ -136,6 +136,60 @@ static void part1_no_gpu(void) {
     EXPECT(ff_prompt_attention(NULL, &heads, 4, 1, FAKE(7), 4096, FAKE(8), 1024, FAKE(9), 1024, (const int32_t *)FAKE(10), FAKE(11), 4096, NULL), FF_ERR_INVALID_ARG);
     EXPECT(ff_chunk_attention(NULL, &heads, 4, 1, FAKE(7), 4096, (const int32_t *)FAKE(8), (const int32_t *)FAKE(9), 4, &cache, (const int32_t *)FAKE(10), 8, FAKE(11), 4096,
                               NULL), FF_ERR_INVALID_ARG);
+    {                                    /* caches in 8 bits, selected pages, page pools */
+      const ff_paged_cache8 c8 = {FAKE(9), FAKE(10), (float *)FAKE(11), (float *)FAKE(12), 4, 16, 8};
+      const ff_selection sel = {4, 2, 1};
+      ff_selection bad_sel = sel;
+      const ff_page_part part = {FAKE(13), 64};
+      const ff_page_pool pool = {100, 16, 8, 20, (int32_t *)FAKE(8), (int32_t *)FAKE(9), (int32_t *)FAKE(10), &part, 1};
+      ff_page_pool bad_pool = pool;
+      const int32_t *ints = (const int32_t *)FAKE(14);
+      int32_t *out = (int32_t *)FAKE(15), got = 0;
+      EXPECT(ff_cache8_append(NULL, &heads, 4, 1, FAKE(7), 4096, FAKE(7), 4096, ints, ints, &c8, ints, 8), FF_ERR_INVALID_ARG);
+      EXPECT(ff_chunk_attention8(NULL, &heads, 4, 1, FAKE(7), 4096, ints, ints, 4, &c8, ints, 8, FAKE(11), 4096, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_page_means(NULL, &heads, 4, 1, ints, ints, &cache, NULL, ints, 8, (float *)FAKE(11)), FF_ERR_INVALID_ARG);
+      EXPECT(ff_select_pages(NULL, &heads, &sel, 4, 1, FAKE(7), 4096, ints, ints, 4, 16, (float *)FAKE(11), ints, 8, out, out, out), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selected_attention(NULL, &heads, 4, 1, FAKE(7), 4096, ints, ints, 4, &cache, NULL, ints, 8, FAKE(11), 4096, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_copy(NULL, &pool, 1, ints, ints), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_fork(NULL, &pool, 1, ints, ints, out), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_grow(NULL, &pool, 1, ints, ints, out), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_free(NULL, &pool, 1, ints), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_compact(NULL, &pool, out), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selection_blocks(&sel, 9, 2, &got), FF_OK);
+      if (got != 4) ++n_fail;
+      EXPECT(ff_selection_blocks(&sel, 2147483647, 2147483647, &got), FF_OK);
+      if (got != 2147483647) ++n_fail;
+      EXPECT(ff_selection_blocks(NULL, 9, 2, &got), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selection_blocks(&sel, 0, 2, &got), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selection_blocks(&sel, 9, 2, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selection_pages(&sel, 16, &got), FF_OK);
+      if (got != 4) ++n_fail;                       /* 2 kept, 4 tokens in at most 2 pages */
+      EXPECT(ff_selection_pages(&sel, 24, &got), FF_ERR_SHAPE);
+      EXPECT(ff_selection_pages(&sel, 16, NULL), FF_ERR_INVALID_ARG);
+      bad_sel.query_block = bad_sel.keep = 1 << 20;
+      EXPECT(ff_selection_pages(&bad_sel, 8, &got), FF_OK);
+      bad_sel.keep = 0;
+      EXPECT(ff_selection_pages(&bad_sel, 16, &got), FF_ERR_SHAPE);
+      bad_sel = sel; bad_sel.first = 3;
+      EXPECT(ff_selection_blocks(&bad_sel, 9, 2, &got), FF_ERR_SHAPE);
+      EXPECT(ff_selection_workspace_bytes(&heads, 16384, 1 << 20, &bytes), FF_OK);
+      EXPECT(ff_selection_workspace_bytes(&heads, 16385, 8, &bytes), FF_ERR_SHAPE);
+      EXPECT(ff_selection_workspace_bytes(&heads, 4, 0, &bytes), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selection_workspace_bytes(NULL, 4, 8, &bytes), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selection_workspace_bytes(&heads, 4, 8, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_workspace_bytes(&pool, 1, &bytes), FF_OK);
+      EXPECT(ff_pages_workspace_bytes(&pool, 1 << 20, &more), FF_OK);
+      if (more < bytes) ++n_fail;
+      EXPECT(ff_pages_workspace_bytes(&pool, 0, &bytes), FF_ERR_SHAPE);
+      EXPECT(ff_pages_workspace_bytes(&pool, 1, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_workspace_bytes(NULL, 1, &bytes), FF_ERR_INVALID_ARG);
+      bad_pool.n_pages = 1 << 28; bad_pool.n_rows = 1 << 24; bad_pool.table_stride = 1 << 20;
+      EXPECT(ff_pages_workspace_bytes(&bad_pool, 1 << 20, &bytes), FF_OK);
+      bad_pool.n_pages = (1 << 28) + 1;
+      EXPECT(ff_pages_workspace_bytes(&bad_pool, 1, &bytes), FF_ERR_SHAPE);
+      bad_pool = pool; bad_pool.parts = NULL;
+      EXPECT(ff_pages_workspace_bytes(&bad_pool, 1, &bytes), FF_ERR_INVALID_ARG);
+    }
     EXPECT(ff_attention_workspace_bytes(NULL, 4, 1, &bytes), FF_ERR_INVALID_ARG);
     EXPECT(ff_attention_workspace_bytes(&heads, 4, 1, NULL), FF_ERR_INVALID_ARG);
     EXPECT(ff_attention_workspace_bytes(&heads, 0, 1, &bytes), FF_ERR_INVALID_ARG);
@@ -375,6 +429,121 @@ static void part2_argument_errors(ff_ctx *ctx) {
     c = ok_cache; c.v = odd;
     EXPECT(CHUNK(4, &c, pos, 4, pos), FF_ERR_ALIGNMENT);
 #undef CHUNK
+
+    /* caches in 8 bits, selected pages, page pools: each with one thing wrong */
+    {
+      const ff_paged_cache8 ok8 = {FAKE(15), FAKE(16), (float *)FAKE(18), (float *)FAKE(19), 4, 16, 8};
+      const ff_selection sel = {2, 2, 1};
+      ff_paged_cache8 c8 = ok8;
+      ff_selection bs = sel;
+      float *means = (float *)FAKE(20);
+      int32_t *out = (int32_t *)FAKE(21);
+      ff_page_part part = {FAKE(22), 64};
+      const ff_page_pool ok_pool = {100, 16, 8, 20, (int32_t *)FAKE(23), (int32_t *)FAKE(24), (int32_t *)FAKE(25), &part, 1};
+      ff_page_pool pool = ok_pool;
+      int i;
+#define APPEND(nt, ns, kk, ks, st, cc, tb, ts) ff_cache8_append(ctx, &a, nt, ns, kk, ks, y, 128, st, pos, cc, tb, ts)
+      EXPECT(APPEND(0, 1, x, 128, pos, &c8, pos, 4), FF_ERR_INVALID_ARG);
+      EXPECT(APPEND(4, 0, x, 128, pos, &c8, pos, 4), FF_ERR_INVALID_ARG);
+      EXPECT(APPEND(4, 16385, x, 128, pos, &c8, pos, 4), FF_ERR_SHAPE);
+      EXPECT(APPEND(4, 1, NULL, 128, pos, &c8, pos, 4), FF_ERR_INVALID_ARG);
+      EXPECT(APPEND(4, 1, x, 120, pos, &c8, pos, 4), FF_ERR_SHAPE);
+      EXPECT(APPEND(4, 1, x, 132, pos, &c8, pos, 4), FF_ERR_ALIGNMENT);
+      EXPECT(APPEND(4, 1, odd, 128, pos, &c8, pos, 4), FF_ERR_ALIGNMENT);
+      EXPECT(APPEND(4, 1, x, 128, NULL, &c8, pos, 4), FF_ERR_INVALID_ARG);
+      EXPECT(APPEND(4, 1, x, 128, pos, NULL, pos, 4), FF_ERR_INVALID_ARG);
+      EXPECT(APPEND(4, 1, x, 128, pos, &c8, NULL, 4), FF_ERR_INVALID_ARG);
+      EXPECT(APPEND(4, 1, x, 128, pos, &c8, pos_odd, 4), FF_ERR_ALIGNMENT);
+      EXPECT(APPEND(4, 1, x, 128, pos, &c8, pos, 0), FF_ERR_INVALID_ARG);
+#define CHUNK8(mc, cc) ff_chunk_attention8(ctx, &a, 4, 1, x, 256, pos, pos, mc, cc, pos, 4, y, 256, NULL)
+      EXPECT(CHUNK8(4, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(CHUNK8(5, &c8), FF_ERR_INVALID_ARG);
+      EXPECT(CHUNK8(4, &c8), FF_ERR_WORKSPACE);
+      for (i = 0; i < 9; ++i) {
+        static const ff_status want[9] = {FF_ERR_INVALID_ARG, FF_ERR_SHAPE,     FF_ERR_SHAPE,       FF_ERR_SHAPE,    FF_ERR_SHAPE,
+                                          FF_ERR_SHAPE,       FF_ERR_ALIGNMENT, FF_ERR_INVALID_ARG, FF_ERR_ALIGNMENT};
+        c8 = ok8;
+        if (i == 0) c8.n_pages = 0;
+        if (i == 1) c8.page_size = 8;
+        if (i == 2) c8.page_size = 8192;
+        if (i == 3) c8.scale_tokens = 4;
+        if (i == 4) c8.scale_tokens = 32;
+        if (i == 5) c8.scale_tokens = 12;
+        if (i == 6) c8.v = odd;
+        if (i == 7) c8.k_scale = NULL;
+        if (i == 8) c8.v_scale = (float *)odd;
+        EXPECT(APPEND(4, 1, x, 128, pos, &c8, pos, 4), want[i]);
+        EXPECT(CHUNK8(4, &c8), want[i]);
+        EXPECT(ff_page_means(ctx, &a, 4, 1, pos, pos, NULL, &c8, pos, 4, means), want[i]);
+        EXPECT(ff_selected_attention(ctx, &a, 4, 1, x, 256, pos, pos, 2, NULL, &c8, pos, 4, y, 256, NULL), want[i]);
+      }
+      c8 = ok8; c = ok_cache;
+#undef APPEND
+#undef CHUNK8
+      EXPECT(ff_page_means(ctx, &a, 4, 1, pos, pos, NULL, NULL, pos, 4, means), FF_ERR_INVALID_ARG);
+      EXPECT(ff_page_means(ctx, &a, 4, 1, pos, pos, &c, &c8, pos, 4, means), FF_ERR_INVALID_ARG);
+      EXPECT(ff_page_means(ctx, &a, 4, 1, pos, pos, &c, NULL, pos, 4, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_page_means(ctx, &a, 4, 1, pos, pos, &c, NULL, pos, 4, (float *)odd), FF_ERR_ALIGNMENT);
+      EXPECT(ff_page_means(ctx, &a, 4, 1, NULL, pos, &c, NULL, pos, 4, means), FF_ERR_INVALID_ARG);
+#define SELECT(sl, nt, np, ps, mm, ts, o1) ff_select_pages(ctx, &a, sl, nt, 1, x, 256, pos, pos, np, ps, mm, pos, ts, o1, out, out)
+      EXPECT(SELECT(NULL, 4, 4, 16, means, 4, out), FF_ERR_INVALID_ARG);
+      EXPECT(SELECT(&sel, 0, 4, 16, means, 4, out), FF_ERR_INVALID_ARG);
+      EXPECT(SELECT(&sel, 4, 0, 16, means, 4, out), FF_ERR_INVALID_ARG);
+      EXPECT(SELECT(&sel, 4, 4, 12, means, 4, out), FF_ERR_SHAPE);
+      EXPECT(SELECT(&sel, 4, 4, 16, NULL, 4, out), FF_ERR_INVALID_ARG);
+      EXPECT(SELECT(&sel, 4, 4, 16, (float *)odd, 4, out), FF_ERR_ALIGNMENT);
+      EXPECT(SELECT(&sel, 4, 4, 16, means, 0, out), FF_ERR_INVALID_ARG);
+      EXPECT(SELECT(&sel, 4, 4, 16, means, 4, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(SELECT(&sel, 1 << 20, 4, 16, means, 4, out), FF_ERR_SHAPE);         /* more than 16384 blocks */
+      EXPECT(SELECT(&sel, 4, 4, 16, means, 1 << 20, out), FF_ERR_WORKSPACE);
+      bs.query_block = 0;
+      EXPECT(SELECT(&bs, 4, 4, 16, means, 4, out), FF_ERR_SHAPE);
+      a.causal = 0;
+      EXPECT(SELECT(&sel, 4, 4, 16, means, 4, out), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selected_attention(ctx, &a, 4, 1, x, 256, pos, pos, 2, &c, NULL, pos, 4, y, 256, NULL), FF_ERR_INVALID_ARG);
+      a = ok_heads; a.window = 8;
+      EXPECT(SELECT(&sel, 4, 4, 16, means, 4, out), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selected_attention(ctx, &a, 4, 1, x, 256, pos, pos, 2, &c, NULL, pos, 4, y, 256, NULL), FF_ERR_INVALID_ARG);
+      a = ok_heads;
+#undef SELECT
+      EXPECT(ff_selected_attention(ctx, &a, 4, 1, x, 256, pos, pos, 2, &c, &c8, pos, 4, y, 256, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selected_attention(ctx, &a, 4, 1, x, 256, pos, pos, 2, NULL, NULL, pos, 4, y, 256, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selected_attention(ctx, &a, 4, 1, x, 256, pos, pos, 0, &c, NULL, pos, 4, y, 256, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selected_attention(ctx, &a, 4, 1, x, 256, pos, NULL, 2, &c, NULL, pos, 4, y, 256, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_selected_attention(ctx, &a, 4, 1, x, 256, pos, pos, 2, &c, NULL, pos, 4, y, 256, NULL), FF_ERR_WORKSPACE);
+#define POOL(want)                                                     \
+  EXPECT(ff_pages_fork(ctx, &pool, 1, pos, pos, out), want);           \
+  EXPECT(ff_pages_grow(ctx, &pool, 1, pos, pos, out), want);           \
+  EXPECT(ff_pages_free(ctx, &pool, 1, pos), want);                     \
+  EXPECT(ff_pages_compact(ctx, &pool, out), want)
+      pool.n_pages = 0; POOL(FF_ERR_SHAPE);
+      EXPECT(ff_pages_copy(ctx, &pool, 1, pos, pos), FF_ERR_SHAPE);
+      pool = ok_pool; pool.page_size = 24; POOL(FF_ERR_SHAPE);
+      pool = ok_pool; pool.n_rows = 0; POOL(FF_ERR_SHAPE);
+      pool = ok_pool; pool.table_stride = (1 << 20) + 1; POOL(FF_ERR_SHAPE);
+      pool = ok_pool; pool.n_parts = 4097; POOL(FF_ERR_SHAPE);
+      pool = ok_pool; pool.refs = NULL; POOL(FF_ERR_INVALID_ARG);
+      pool = ok_pool; pool.lens = (int32_t *)odd; POOL(FF_ERR_ALIGNMENT);
+      pool = ok_pool; part.data = NULL; POOL(FF_ERR_INVALID_ARG);
+      part.data = odd; POOL(FF_ERR_ALIGNMENT);
+      EXPECT(ff_pages_copy(ctx, &pool, 1, pos, pos), FF_ERR_ALIGNMENT);
+      part.data = FAKE(22); part.page_bytes = 0; POOL(FF_ERR_SHAPE);
+      part.page_bytes = 64;
+#undef POOL
+      EXPECT(ff_pages_copy(ctx, &pool, 0, pos, pos), FF_ERR_SHAPE);
+      EXPECT(ff_pages_copy(ctx, &pool, 1, NULL, pos), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_copy(ctx, &pool, 1, pos, pos_odd), FF_ERR_ALIGNMENT);
+      EXPECT(ff_pages_fork(ctx, &pool, (1 << 20) + 1, pos, pos, out), FF_ERR_SHAPE);
+      EXPECT(ff_pages_fork(ctx, &pool, 1, pos, NULL, out), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_fork(ctx, &pool, 1, pos, pos, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_fork(ctx, &pool, 1, pos_odd, pos, out), FF_ERR_ALIGNMENT);
+      EXPECT(ff_pages_fork(ctx, &pool, 1, pos, pos, out), FF_ERR_WORKSPACE);
+      EXPECT(ff_pages_grow(ctx, &pool, 1, pos, NULL, out), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_grow(ctx, &pool, 1, pos, pos, out), FF_ERR_WORKSPACE);
+      EXPECT(ff_pages_free(ctx, &pool, 1, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_compact(ctx, &pool, NULL), FF_ERR_INVALID_ARG);
+      EXPECT(ff_pages_compact(ctx, &pool, out), FF_ERR_WORKSPACE);
+    }
   }
   EXPECT(ff_copy(ctx, x, y, 0), FF_ERR_INVALID_ARG);
   EXPECT(ff_copy(ctx, x, y, 100), FF_ERR_INVALID_ARG);
@@ -391,8 +560,8 @@ static int part3_real_calls(ff_ctx *ctx) {
   const int32_t nB = 4, ks_ragged[4] = {688, 100, 344, 7}, ks[4] = {344, 344, 344, 344};
   const int32_t kl[2 * 4] = {344, 344, 344, 344, 688, 100, 344, 7};
   void *x = NULL, *wg = NULL, *wu = NULL, *wd = NULL, *w1 = NULL, *w2 = NULL, *wc1 = NULL, *wc2 = NULL, *y = NULL, *ws = NULL, *h = NULL;
-  void *ws2 = NULL;
-  int32_t *idx = NULL, *pages = NULL, *lens = NULL, host_idx[8];
+  void *ws2 = NULL, *ws3 = NULL;
+  int32_t *idx = NULL, *pages = NULL, *lens = NULL, *pool_ints = NULL, *blocks = NULL, host_idx[8];
   float *lse = NULL;
   size_t need = 0;
   double ms[FF_N_STAGES];
@@ -472,6 +641,39 @@ static int part3_real_calls(ff_ctx *ctx) {
     EXPECT(ff_chunk_attention(ctx, &a, tokens, 1, h, 256, lens, pages, tokens, &c, pages, 64, y, 256, lse), FF_OK);
     EXPECT(ff_chunk_attention(ctx, &a, tokens, 1, h, 256, lens, pages, 1, &c, pages, 64, y, 256, NULL), FF_OK);
     EXPECT(ff_set_option(ctx, "validate", 0), FF_OK);
+    {                                   /* pages in 8 bits, selected ones and a pool of them; everything is zeros, lens 0 and 230 */
+      const ff_paged_cache8 c8 = {wg, wu, (float *)wc1, (float *)wc2, 16, 16, 8};
+      const ff_selection sel = {16, 2, 1};
+      const ff_page_part parts[4] = {{wg, 2 * 16 * 64}, {wu, 2 * 16 * 64}, {wc1, 16}, {wc2, 16}};
+      ff_page_pool p = {16, 16, 2, 20, NULL, NULL, NULL, parts, 4};
+      int32_t n_blocks = 0, block_stride = 0;
+      size_t need3 = 0, need4 = 0, need5 = 0;
+      EXPECT(ff_selection_blocks(&sel, tokens, 1, &n_blocks), FF_OK);
+      EXPECT(ff_selection_pages(&sel, 16, &block_stride), FF_OK);
+      EXPECT(ff_attention_workspace_bytes(&a, tokens, n_blocks, &need3), FF_OK);
+      EXPECT(ff_selection_workspace_bytes(&a, n_blocks, 64, &need4), FF_OK);
+      DEVBUF(pool_ints, 256 * 4); DEVBUF(blocks, 4096 * 4);
+      p.refs = pool_ints; p.page_table = pool_ints + 64; p.lens = pool_ints + 128;
+      EXPECT(ff_pages_workspace_bytes(&p, 2, &need5), FF_OK);
+      need3 = need3 > need4 ? need3 : need4;
+      need3 = need3 > need5 ? need3 : need5;
+      DEVBUF(ws3, need3);
+      EXPECT(ff_set_workspace(ctx, ws3, need3), FF_OK);
+      {
+        EXPECT(ff_cache8_append(ctx, &a, tokens, 1, x, 256, x, 256, lens, pages, &c8, pages, 64), FF_OK);
+        EXPECT(ff_chunk_attention8(ctx, &a, tokens, 1, h, 256, lens, pages, tokens, &c8, pages, 64, y, 256, lse), FF_OK);
+        EXPECT(ff_page_means(ctx, &a, tokens, 1, lens, pages, NULL, &c8, pages, 64, (float *)w1), FF_OK);
+        EXPECT(ff_page_means(ctx, &a, tokens, 1, lens, pages, &c, NULL, pages, 64, (float *)w1), FF_OK);
+        EXPECT(ff_select_pages(ctx, &a, &sel, tokens, 1, h, 256, lens, pages, 16, 16, (float *)w1, pages, 64, blocks, blocks + 256, blocks + 512), FF_OK);
+        EXPECT(ff_selected_attention(ctx, &a, tokens, n_blocks, h, 256, blocks, blocks + 256, 16, NULL, &c8, blocks + 512, block_stride, y, 256, NULL), FF_OK);
+        EXPECT(ff_selected_attention(ctx, &a, tokens, n_blocks, h, 256, blocks, blocks + 256, 16, &c, NULL, blocks + 512, block_stride, y, 256, lse), FF_OK);
+        EXPECT(ff_pages_grow(ctx, &p, 2, pages, lens, blocks), FF_OK);
+        EXPECT(ff_pages_fork(ctx, &p, 2, pages, pool_ints + 32, blocks), FF_OK);
+        EXPECT(ff_pages_copy(ctx, &p, 2, pages, lens), FF_OK);
+        EXPECT(ff_pages_free(ctx, &p, 2, pages), FF_OK);
+        EXPECT(ff_pages_compact(ctx, &p, blocks), FF_OK);
+      }
+    }
   }
   if (hipDeviceSynchronize() != hipSuccess) { rc = 1; goto done; }
   if (hipMemcpy(host_idx, idx, sizeof(host_idx), hipMemcpyDeviceToHost) != hipSuccess) { rc = 1; goto done; }
@@ -481,7 +683,7 @@ done:
   (void)ff_set_workspace(ctx, NULL, 0);
   (void)hipDeviceSynchronize();
   hipFree(x); hipFree(h); hipFree(wg); hipFree(wu); hipFree(wd); hipFree(w1); hipFree(w2); hipFree(wc1); hipFree(wc2);
-  hipFree(y); hipFree(idx); hipFree(ws); hipFree(ws2); hipFree(pages); hipFree(lens); hipFree(lse);
+  hipFree(y); hipFree(idx); hipFree(ws); hipFree(ws2); hipFree(ws3); hipFree(pool_ints); hipFree(blocks); hipFree(pages); hipFree(lens); hipFree(lse);
   return rc;
 }
 

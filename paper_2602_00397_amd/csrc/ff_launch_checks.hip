@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "ff_attn_plan.h"
+#include "ff_pages.h"
 #include "ff_internal.h"
 
 struct Launch {
@@ -657,6 +658,181 @@ static void check_most_rows() {
   g_attn = false;
 }
 
+// Attention over pages in 8 bits and over selected ones: their plans fit into the same workspace, every row is covered by one kernel, and
+// the items fit into the launch.
+static void check_other_pages() {
+  uint32_t rnd = 777;
+  const auto below = [&](int n) { rnd = rnd * 1664525u + 1013904223u; return (int)((rnd >> 8) % (unsigned)n); };
+  static float room[1];
+  g_attn = true;
+  for (int round = 0; round < 6000; ++round) {
+    static const int groups[] = {1, 3, 4, 7, 8, 20, 33};
+    const int group = groups[below(7)], n_kv = 1 + below(8), n_seqs = 1 + below(round % 5 == 0 ? 300 : 9), hd = below(2) ? 64 : 128;
+    std::vector<int32_t> starts(n_seqs + 1), lens(n_seqs);
+    AttnParams p = {};
+    p.k_scale = below(3) ? room : nullptr;
+    p.selected = below(3) != 0;
+    p.page_shift = 4 + below(6);
+    p.table_stride = 1 + below(60);
+    p.head_tables = p.selected ? p.table_stride : 0;
+    p.seq_tables = (int64_t)(p.selected ? n_kv : 1) * p.table_stride;
+    const int most = 1 << (1 + below(9));
+    int t = 0, longest = 1;
+    for (int s = 0; s < n_seqs; ++s) {
+      starts[s] = t;
+      const int n = below(4) == 0 ? below(3) : round % 2 ? most : below(most);
+      t += n;
+      longest = std::max(longest, n);
+      lens[s] = below((p.table_stride << p.page_shift) + 1);
+    }
+    starts[n_seqs] = t;
+    p.T = std::max(1, t);
+    p.starts = starts.data(); p.lens = lens.data(); p.table = starts.data();          // (never read: there is one)
+    p.n_seqs = n_seqs; p.n_kv = n_kv; p.group = group; p.n_heads = n_kv * group; p.n_pages = 10;
+    p.by_group = fast_div(group); p.by_kv = fast_div(n_kv);
+    p.causal = 1;
+    p.part = room;
+    p.part_bytes = ff_attention_part_bytes(p.n_heads, n_kv, hd, p.T, n_seqs);
+    const int hint = below(3) ? std::min(longest, p.T) : 1 + below(p.T);
+    CHECK(ff_attention_need(p, hd, hint) <= p.part_bytes, "round %d: %zu", round, p.part_bytes);
+    g_log.clear();
+    ++g_calls;
+    CHECK(ff_launch_attention(p, hd, hint, nullptr) == hipSuccess && !g_log.empty(), "round %d", round);
+    std::vector<long> covered(n_seqs, 0);
+    int before = -1;
+    for (const Launch &l : g_log) {
+      const AttnPlan &pl = l.plan;
+      if (before == pl.tile_rows) continue;                                             // (joins the pieces of the launch before)
+      before = pl.tile_rows;
+      float steps = 0.f;
+      for (int s = 0; s < n_seqs; ++s) steps += price_of(p, pl, seq_of(p, s));
+      const int kpp = pl.target > 0 ? piece_keys_for(p, pl, steps) : kUnsplit;
+      long items = 0;
+      for (int s = 0; s < n_seqs; ++s) {
+        const Seq q = seq_of(p, s);
+        items += (long)tiles_of(p, pl, q.n) * seq_pieces(p, pl, q, kpp);
+        covered[s] += (long)tiles_of(p, pl, q.n) * pl.tile_rows;
+      }
+      CHECK(l.lds <= kLds && items * n_kv <= pl.max_items, "round %d: %ld items, %d workgroups", round, items * n_kv, pl.max_items);
+      CHECK(pl.target == 0 || (pl.part_at + (size_t)pl.max_items * pl.tile_rows * (hd + 2)) * sizeof(float) <= p.part_bytes, "round %d: room", round);
+    }
+    for (int s = 0; s < n_seqs; ++s) {
+      const long rows = (long)seq_of(p, s).n * group;
+      CHECK(covered[s] >= rows && covered[s] < rows + 256 && (rows > 0 || covered[s] == 0), "round %d sequence %d: %ld rows of %ld", round, s, covered[s], rows);
+    }
+  }
+  g_attn = false;
+}
+
+// Runs of positions that the write in 8 bits and the means take, and blocks that select pages: as many as their launches have, and within the
+// sequence's rows, positions and tables, also where starts and lengths are anything.
+static void check_runs_and_blocks() {
+  uint32_t rnd = 4711;
+  const auto below = [&](int n) { rnd = rnd * 1664525u + 1013904223u; return (int)((rnd >> 8) % (unsigned)n); };
+  for (int round = 0; round < 20000; ++round) {
+    const bool valid = round % 3 != 0;
+    const int n_seqs = 1 + below(round % 7 == 0 ? 200 : 6), shift = 3 + below(5), keep = 1 + below(40), qb = 1 + below(1 << below(9));
+    std::vector<int32_t> starts(n_seqs + 1), lens(n_seqs);
+    AttnParams p = {};
+    p.page_shift = shift + below(4);
+    p.table_stride = 1 + below(60);
+    int t = 0;
+    for (int s = 0; s < n_seqs; ++s) {
+      starts[s] = t;
+      t += below(3) == 0 ? below(3) : below(1 << (1 + below(9)));
+      lens[s] = below((p.table_stride << p.page_shift) + 1);
+    }
+    starts[n_seqs] = t;
+    p.T = std::max(1, t + below(3));
+    if (!valid)
+      for (int i = 0; i < 1 + n_seqs / 2; ++i) {
+        static const int odd[] = {-1, -2147483647 - 1, 2147483647, 1 << 30, 77};
+        starts[below(n_seqs + 1)] = odd[below(5)];
+        lens[below(n_seqs)] = odd[below(5)];
+      }
+    p.starts = starts.data(); p.lens = lens.data(); p.n_seqs = n_seqs;
+    ++g_calls;
+    long runs = 0, blocks = 0;
+    for (int s = 0; s < n_seqs; ++s) {
+      const Seq q = seq_of(p, s);
+      const int n = runs_of(q, shift), first = first_new(q);
+      long tokens = 0;
+      for (int at = 0; at < n; ++at) {
+        const long run = (first >> shift) + at, from = std::max<long>(first, run << shift), to = std::min<long>(q.keys, (run + 1) << shift);
+        CHECK(from < to && to <= q.keys && from >> p.page_shift < p.table_stride, "round %d sequence %d run %d", round, s, at);
+        tokens += to - from;
+      }
+      CHECK(tokens == std::min(q.n, q.keys), "round %d sequence %d: %ld tokens of %d", round, s, tokens, q.n);
+      runs += n;
+      const int nb = blocks_of(q, qb);
+      long rows = 0;
+      for (int at = 0; at < nb; ++at) {
+        const Block b = block_at(q, s, at, qb, keep, p.page_shift);
+        rows += b.n;
+        CHECK(b.n >= 1 && b.n <= qb && b.t0 >= q.t0 && b.t0 + (long)b.n <= q.t0 + (long)q.n, "round %d block %d", round, at);
+        CHECK(b.earlier >= 0 && b.own >= 0 && b.earlier + (long)b.own <= p.table_stride && b.own <= (qb + (1 << p.page_shift) - 2) / (1 << p.page_shift) + 1, "round %d block %d: %d, %d pages",
+              round, at, b.earlier, b.own);
+        CHECK(b.keys >= 0 && b.keys <= (long)(std::min(keep, b.earlier) + b.own) << p.page_shift && (b.own == 0) == (b.keys == 0), "round %d block %d: %d keys", round, at, b.keys);
+      }
+      CHECK(rows == q.n, "round %d sequence %d: %ld rows of %d", round, s, rows, q.n);
+      blocks += nb;
+    }
+    CHECK(!valid || (runs <= most_runs(p.T, n_seqs, shift) && blocks <= std::min<long>(p.T, (long)(p.T / qb) + n_seqs)), "round %d: %ld runs, %ld blocks", round, runs, blocks);
+  }
+}
+
+// Launches of the write in 8 bits, the selection and the page calls at their limits: dimensions and threads that a launch can have, and
+// workspaces that hold what the arrays in them take.
+static void check_page_launches() {
+  g_few = true;
+  const auto sane = [&](const char *what) {
+    for (const Launch &l : g_log)
+      CHECK(l.dims.x >= 1 && l.dims.y >= 1 && l.dims.y <= 65535 && l.dims.z >= 1 && l.dims.z <= 65535 && (unsigned long)l.dims.x * l.threads < 1ul << 32 && l.threads <= 1024, "%s: %u x %u x %u", what,
+            l.dims.x, l.dims.y, l.dims.z);
+  };
+  for (int n_kv : {1, 8, 1024})
+    for (int T : {1, 48, 9001, 1 << 20, 1 << 30})
+      for (int n_seqs : {1, 48, 16384})
+        for (int hd : {64, 128}) {
+          if ((long)T * n_kv > 0x7fff0000L) continue;
+          AttnParams p = {};
+          p.T = T; p.n_seqs = n_seqs; p.n_kv = n_kv; p.by_kv = fast_div(n_kv); p.page_shift = 4; p.table_stride = 4096;
+          for (int shift : {3, 4, 5, 6, 7}) {
+            Append8Params a = {};
+            a.seqs = p;
+            a.seqs.scale_shift = shift;
+            g_log.clear();
+            ++g_calls;
+            CHECK(ff_launch_append8(a, hd, nullptr) == hipSuccess && g_log.size() == 1, "%d tokens", T);
+            sane("append");
+          }
+          SelectParams q = {};
+          q.seqs = p;
+          q.keep = 16; q.query_block = 128;
+          q.n_blocks = std::min({T, T / 128 + n_seqs, 16384});
+          g_log.clear();
+          ++g_calls;
+          CHECK(ff_launch_page_means(q, hd, nullptr) == hipSuccess && ff_launch_select_pages(q, hd, nullptr) == hipSuccess && g_log.size() == 3, "%d tokens", T);
+          sane("select");
+        }
+  for (int parts : {0, 1, 64, 65, 4096})
+    for (int n : {1, 1000, 1 << 20})
+      for (int n_pages : {1, 3000, 1 << 28}) {
+        std::vector<ff_page_part> part(parts, ff_page_part{nullptr, 1ll << 32});
+        PoolParams p = {};
+        p.n_pages = n_pages; p.n_rows = 1 << 24; p.table_stride = 1 << 20; p.n = n; p.page_shift = 4;
+        g_log.clear();
+        ++g_calls;
+        CHECK(ff_launch_pages_fork(p, part.data(), parts, nullptr) == hipSuccess && (int)g_log.size() == 1 + std::max(1, (parts + 63) / 64), "%d parts", parts);
+        CHECK(ff_launch_pages_grow(p, nullptr) == hipSuccess && ff_launch_pages_free(p, nullptr) == hipSuccess, "%d entries", n);
+        CHECK(ff_launch_pages_compact(p, part.data(), parts, nullptr) == hipSuccess, "%d parts", parts);
+        if (parts) CHECK(ff_launch_pages_copy(part.data(), parts, n_pages, n, nullptr, nullptr, nullptr) == hipSuccess, "%d parts", parts);
+        sane("pages");
+        CHECK(ff_pages_ints(n, n_pages, p.n_rows, p.table_stride) <= ff_pages_ints(n + 1, n_pages, p.n_rows, p.table_stride), "%d entries", n);
+      }
+  g_few = false;
+}
+
 int main() {
   if (ff_gemm_init(kLds) != hipSuccess) return 1;
   for (int T : {9, 70, 300, 700, 2000, 8192})
@@ -679,6 +855,9 @@ int main() {
   check_pooling();
   check_topk_map();
   check_attention();
+  check_other_pages();
+  check_runs_and_blocks();
+  check_page_launches();
   check_far_contexts();
   check_most_rows();
   printf("launch checks: %d calls, %d wrong\n", g_calls, g_fail);

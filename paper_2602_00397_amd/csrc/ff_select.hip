@@ -59,22 +59,9 @@ __global__ __launch_bounds__(kThreads) void ff_page_means_kernel(SelectParams a,
 }
 
 // ---- blocks of new tokens -----------------------------------------------------------------------------------------------------
-struct Block { int s, t0, n, earlier, own, keys; };   // rows; pages in front of its own, its own, and keys of the kept pages and its own
 __device__ __forceinline__ Block block_of(const SelectParams &a, int x) {
-  const AttnParams &p = a.seqs;
-  const Found f = find_item(p, x, [&](const Seq &q) { return (int)(((long)q.n + a.query_block - 1) / a.query_block); });
-  Block b = {f.s, 0, 0, 0, 0, 0};
-  if (f.s < 0) return b;
-  const int at = f.at * a.query_block;
-  b.t0 = f.seq.t0 + at;
-  b.n = min(a.query_block, f.seq.n - at);
-  const int last = f.seq.keys - f.seq.n + at + b.n - 1;     // (below 0: its tokens see nothing)
-  if (last < 0) return b;
-  b.earlier = max(last - b.n + 1, 0) >> p.page_shift;
-  b.own = (last >> p.page_shift) - b.earlier + 1;
-  // (its own pages are the last of the list, and the last of those ends with the block's last token)
-  b.keys = ((min(a.keep, b.earlier) + b.own - 1) << p.page_shift) + (last & ((1 << p.page_shift) - 1)) + 1;
-  return b;
+  const Found f = find_item(a.seqs, x, [&](const Seq &q) { return blocks_of(q, a.query_block); });
+  return f.s < 0 ? Block{-1, 0, 0, 0, 0, 0} : block_at(f.seq, f.s, f.at, a.query_block, a.keep, a.seqs.page_shift);
 }
 
 // A workgroup to 64 pages, or several times that, of a block and key head: the queries' sum once, then four lanes to a page.  Blocks with

@@ -59,15 +59,3 @@ __device__ __forceinline__ Found find_item(const AttnParams &p, long x, Count co
   }
   return f;
 }
-
-// New tokens of a sequence stand at the positions keys - n .. keys - 1 of its cache, as far as these are not negative.
-__device__ __forceinline__ int first_new(const Seq &q) { return q.keys > q.n ? q.keys - q.n : 0; }
-// how many runs of 2^shift positions have new tokens
-__device__ __forceinline__ int runs_of(const Seq &q, int shift) {
-  return q.n > 0 && q.keys > 0 ? ((q.keys - 1) >> shift) - (first_new(q) >> shift) + 1 : 0;
-}
-// most runs of a call: each has a token, and all of a sequence's but two are full
-inline long most_runs(long n_tokens, long n_seqs, int shift) {
-  const long seqs = n_seqs < n_tokens ? n_seqs : n_tokens, runs = (n_tokens >> shift) + 2 * seqs;
-  return runs < n_tokens ? runs : n_tokens;
-}
