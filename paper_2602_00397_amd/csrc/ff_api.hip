@@ -1241,6 +1241,7 @@ ff_status ff_select_pages(ff_ctx *ctx, const ff_attention *a, const ff_selection
   p.seqs.q = static_cast<const bf16_t *>(q);
   p.seqs.q_stride = q_stride;
   p.seqs.n_pages = n_pages;
+  p.seqs.counters = ctx->counters;
   p.seqs.page_shift = log2_of(page_size);
   set_chunks(&p.seqs, chunk_starts, context_lens, page_table, table_stride, 1);
   p.means = const_cast<float *>(means);

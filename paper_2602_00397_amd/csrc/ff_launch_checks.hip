@@ -812,8 +812,9 @@ static void check_page_launches() {
           q.n_blocks = std::min({T, T / 128 + n_seqs, 16384});
           g_log.clear();
           ++g_calls;
-          CHECK(ff_launch_page_means(q, hd, nullptr) == hipSuccess && ff_launch_select_pages(q, hd, nullptr) == hipSuccess && g_log.size() == 3, "%d tokens", T);
+          CHECK(ff_launch_page_means(q, hd, nullptr) == hipSuccess && ff_launch_select_pages(q, hd, nullptr) == hipSuccess && g_log.size() == 2, "%d tokens", T);
           sane("select");
+          CHECK(g_log[1].dims.z == 1 || (long)q.n_blocks * n_kv <= kAttnCounters, "%d blocks", q.n_blocks);
         }
   for (int parts : {0, 1, 64, 65, 4096})
     for (int n : {1, 1000, 1 << 20})

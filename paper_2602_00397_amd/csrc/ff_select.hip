@@ -64,20 +64,146 @@ __device__ __forceinline__ Block block_of(const SelectParams &a, int x) {
   return f.s < 0 ? Block{-1, 0, 0, 0, 0, 0} : block_at(f.seq, f.s, f.at, a.query_block, a.keep, a.seqs.page_shift);
 }
 
-// A workgroup to 64 pages, or several times that, of a block and key head: the queries' sum once, then four lanes to a page.  Blocks with
-// no more earlier pages than are kept need no scores.
+// ---- the best pages, in order ---------------------------------------------------------------------------------------------------
+// A workgroup to a block and key head scores the earlier pages and lists the best; where there are few blocks, several score and the last
+// of them to end lists.  It is a chain of latencies (one token over 2047 pages, 48 over up to 512, 8192 in blocks of 128 take
+// 12.0, 10.4 and 17.4 us with 512 threads, 13.8, 13.3 and 16.1 with 256; as two launches, scores and lists, 15.3, 16.1 and 24.0).  Blocks with no more earlier pages than are kept need no scores.
+//
+// The list: the scores' range is cut into 1024 parts; those above the part that holds
+// the last page wanted are taken, and of that part's few the best, by counting for each how many are better.  (2047 pages of which 64
+// are kept 14.1 us by whole numbers alone, as below, 9.4 so.)
+// Where that part has too many, or scores are not finite, the scores are compared as whole numbers in their order: the range of those is
+// cut in 1024 until the part with the last one wanted has no more than are wanted of it, or is one number (then its first pages are); each
+// cut is ten bits of it, so there are at most seven.
+constexpr int kSelectThreads = 512;
+constexpr int kBins = 1024, kHeld = 4096, kFew = 64;     // parts; scores that are held in LDS (of more pages they are read again); candidates of a part
+__device__ __forceinline__ uint64_t order_of(double s) {      // (-0 as +0; NaN by its bits)
+  const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
+  return u >> 63 ? ~u : u | 1ull << 63;
+}
+// (of plain min and max, mixed 64-bit types take the double one)
+__device__ __forceinline__ uint64_t lower(uint64_t a, uint64_t b) { return a < b ? a : b; }
+__device__ __forceinline__ uint64_t higher(uint64_t a, uint64_t b) { return a < b ? b : a; }
+struct SelectShared {
+  double held[kHeld];
+  double extreme[2][kSelectThreads / 64];
+  int bins[kBins], sums[kSelectThreads / 64], sums2[kSelectThreads / 64], odd[kSelectThreads / 64], found[3], n_few;
+  double few[kFew], last;
+  int few_at[kFew], last_at;
+};
+// The part, counted from the highest, in which the running count reaches `want`: found = part, how many are above it, how many in it.
+__device__ __forceinline__ void find_part(SelectShared &sh, int want) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  constexpr int PER = kBins / kSelectThreads;
+  const int top = kBins - 1 - PER * (int)threadIdx.x;
+  int c[PER], mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    c[i] = sh.bins[top - i];
+    mine += c[i];
+  }
+  const int upto = lane_sums(mine);
+  if (lane == 63) sh.sums[wave] = upto;
+  __syncthreads();
+  int above = upto - mine;
+#pragma unroll
+  for (int w = 0; w < kSelectThreads / 64; ++w) above += w < wave ? sh.sums[w] : 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (above < want && want <= above + c[i]) {
+      sh.found[0] = top - i;
+      sh.found[1] = above;
+      sh.found[2] = c[i];
+    }
+    above += c[i];
+  }
+  __syncthreads();
+}
+// The pages that `taken` says, in order, and of those that `tied` says the first `ties`: a run of pages to a thread.
+template <class Taken, class Tied>
+__device__ __forceinline__ void write_list(SelectShared &sh, int n, int ties, const int32_t *table, int32_t *list, Taken taken, Tied tied) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int per = (n + kSelectThreads - 1) / kSelectThreads, from = min(n, (int)threadIdx.x * per), to = min(n, from + per);
+  int t = 0, e = 0;
+  for (int i = from; i < to; ++i) {
+    t += taken(i);
+    e += tied(i);
+  }
+  const int t_upto = lane_sums(t), e_upto = lane_sums(e);
+  if (lane == 63) {
+    sh.sums[wave] = t_upto;
+    sh.sums2[wave] = e_upto;
+  }
+  __syncthreads();
+  int at = t_upto - t, before = e_upto - e;
+#pragma unroll
+  for (int w = 0; w < kSelectThreads / 64; ++w) {
+    at += w < wave ? sh.sums[w] : 0;
+    before += w < wave ? sh.sums2[w] : 0;
+  }
+  for (int i = from; i < to; ++i) {
+    const bool is = taken(i), tie = tied(i);
+    if (is || (tie && before < ties)) list[at + min(before, ties)] = table[i];
+    at += is;
+    before += tie;
+  }
+}
+template <class Get>
+__device__ __forceinline__ void list_by_numbers(SelectShared &sh, int n, int kept, const int32_t *table, int32_t *list, Get number) {
+  uint64_t lo = 0, hi = ~0ull;
+  int want = kept;               // of those in [lo, hi]; all above are taken
+  for (;;) {
+    const int shift = max(0, 64 - (int)__clzll((long long)(hi - lo | 1)) - 10);
+    __syncthreads();             // (what the last use of the counts read)
+    for (int i = threadIdx.x; i < kBins; i += kSelectThreads) sh.bins[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kSelectThreads) {
+      const uint64_t u = number(i);
+      if (u >= lo && u <= hi) atomicAdd(&sh.bins[(u - lo) >> shift], 1);
+    }
+    __syncthreads();
+    find_part(sh, want);
+    lo += (uint64_t)sh.found[0] << shift;
+    hi = lo + lower(hi - lo, ((uint64_t)1 << shift) - 1);
+    want -= sh.found[1];
+    if (shift == 0 || sh.found[2] == want) break;
+  }
+  __syncthreads();
+  write_list(sh, n, want, table, list, [&](int i) { return number(i) > hi; }, [&](int i) { const uint64_t u = number(i); return u >= lo && u <= hi; });
+}
+__device__ __forceinline__ void score_store(double *at, double v) { __hip_atomic_store(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ double score_load(const double *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+constexpr int kRun = kSelectThreads / 2;        // pages that a workgroup scores at a time, four lanes to two of them
 template <int HD>
-__global__ __launch_bounds__(kThreads) void ff_page_scores_kernel(SelectParams a) {
-  constexpr int LPR = HD / 8, GROUPS = kThreads / LPR;
-  __shared__ double part[GROUPS][HD + 2];
+__global__ __launch_bounds__(kSelectThreads) void ff_select_pages_kernel(SelectParams a) {
+  constexpr int LPR = HD / 8, GROUPS = kSelectThreads / LPR;
+  static_assert(GROUPS * HD <= kHeld, "the groups' sums lie where the scores come afterwards");
+  __shared__ SelectShared sh;
   __shared__ double sum[HD];
   const AttnParams &p = a.seqs;
-  const int x = blockIdx.y, kvh = blockIdx.x;
+  const int x = blockIdx.y, kvh = blockIdx.x, piece = blockIdx.z;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const Block b = block_of(a, x);
-  if (b.s < 0 || b.earlier <= a.keep || (int)blockIdx.z * 64 >= b.earlier) return;
-  const int group = threadIdx.x / LPR, channel = threadIdx.x % LPR * 8;
+  int32_t *list = a.tables + ((size_t)x * p.n_kv + kvh) * a.width;
+  const int32_t *table = p.table + (b.s < 0 ? 0 : b.s * p.seq_tables);
+  const int n = b.earlier, kept = min(a.keep, n);
+  if (piece == 0) {
+    if (kvh == 0 && threadIdx.x == 0) {
+      const int end = attn_clamp(p.starts[p.n_seqs], 0, p.T);
+      a.starts[x] = b.s < 0 ? end : b.t0;
+      a.lens[x] = b.keys;
+      if (x == a.n_blocks - 1) a.starts[a.n_blocks] = b.s < 0 ? end : b.t0 + b.n;
+    }
+    for (int i = kept + threadIdx.x; i < a.width; i += kSelectThreads) list[i] = i < kept + b.own ? table[n + i - kept] : -1;
+    if (n <= a.keep)
+      for (int i = threadIdx.x; i < n; i += kSelectThreads) list[i] = table[i];
+  }
+  const int pieces = min((int)gridDim.z, (n + kRun - 1) / kRun);
+  if (n <= a.keep || piece >= pieces) return;
+
+  // the block's queries of the key head, summed
+  const int group = threadIdx.x / LPR, channel = threadIdx.x % LPR * 8, rows = b.n * p.group;
   double acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  const int rows = b.n * p.group;
   for (int r0 = group; r0 < rows; r0 += GROUPS * kBatch) {
     u32x4_t w[kBatch];
 #pragma unroll
@@ -97,177 +223,85 @@ __global__ __launch_bounds__(kThreads) void ff_page_scores_kernel(SelectParams a
     }
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) part[group][channel + e] = acc[e];
+  for (int e = 0; e < 8; ++e) sh.held[group * HD + channel + e] = acc[e];
   __syncthreads();
   if (threadIdx.x < HD) {
     double s = 0;
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) s += part[g][threadIdx.x];
+    for (int g = 0; g < GROUPS; ++g) s += sh.held[g * HD + threadIdx.x];
     sum[threadIdx.x] = s;
   }
+  for (int i = threadIdx.x; i < kBins; i += kSelectThreads) sh.bins[i] = 0;
+  if (threadIdx.x == 0) sh.n_few = 0;
   __syncthreads();
-  const int quarter = threadIdx.x & 3;
-  const int32_t *table = p.table + b.s * p.seq_tables;
-  double *scores = a.scores + ((size_t)x * p.n_kv + kvh) * p.table_stride;
-  for (int j0 = blockIdx.z * 64; j0 < b.earlier; j0 += gridDim.z * 64) {
-    const int j = j0 + (threadIdx.x >> 2);
-    int page = table[min(j, b.earlier - 1)];
-    page = (unsigned)page < (unsigned)p.n_pages ? page : 0;
-    const float *mean = a.means + ((size_t)page * p.n_kv + kvh) * HD;
-    float4 m[HD / 16];
-#pragma unroll
-    for (int i = 0; i < HD / 16; ++i) m[i] = *reinterpret_cast<const float4 *>(mean + i * 16 + quarter * 4);
-    double s = 0;
-#pragma unroll
-    for (int i = 0; i < HD / 16; ++i) {
-      const double *q = sum + i * 16 + quarter * 4;
-      s += (double)m[i].x * q[0] + (double)m[i].y * q[1] + (double)m[i].z * q[2] + (double)m[i].w * q[3];
-    }
-    s += __shfl_xor(s, 1);
-    s += __shfl_xor(s, 2);
-    if (quarter == 0 && j < b.earlier) scores[j] = s;
-  }
-}
 
-// ---- the best pages, in order ---------------------------------------------------------------------------------------------------
-// A workgroup to a block and key head: a chain of latencies.  The scores' range is cut into 1024 parts; those above the part that holds
-// the last page wanted are taken, and of that part's few the best, by counting for each how many are better.  (2047 pages of which 64
-// are kept 14.1 us by whole numbers alone, as below, 9.4 so.)
-// Where that part has too many, or scores are not finite, the scores are compared as whole numbers in their order: the range of those is
-// cut in 1024 until the part with the last one wanted has no more than are wanted of it, or is one number (then its first pages are); each
-// cut is ten bits of it, so there are at most seven.
-constexpr int kBins = 1024, kHeld = 4096, kFew = 64;     // parts; scores that are held in LDS (of more pages they are read again); candidates of a part
-__device__ __forceinline__ uint64_t order_of(double s) {      // (-0 as +0; NaN by its bits)
-  const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
-  return u >> 63 ? ~u : u | 1ull << 63;
-}
-// (of plain min and max, mixed 64-bit types take the double one)
-__device__ __forceinline__ uint64_t lower(uint64_t a, uint64_t b) { return a < b ? a : b; }
-__device__ __forceinline__ uint64_t higher(uint64_t a, uint64_t b) { return a < b ? b : a; }
-struct SelectShared {
-  double held[kHeld];
-  double extreme[2][kThreads / 64];
-  int bins[kBins], sums[kThreads / 64], sums2[kThreads / 64], odd[kThreads / 64], found[3], n_few;
-  double few[kFew], last;
-  int few_at[kFew], last_at;
-};
-// The part, counted from the highest, in which the running count reaches `want`: found = part, how many are above it, how many in it.
-__device__ __forceinline__ void find_part(SelectShared &sh, int want) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int top = kBins - 1 - 4 * (int)threadIdx.x;
-  const int c[4] = {sh.bins[top], sh.bins[top - 1], sh.bins[top - 2], sh.bins[top - 3]};
-  const int mine = c[0] + c[1] + c[2] + c[3], upto = lane_sums(mine);
-  if (lane == 63) sh.sums[wave] = upto;
-  __syncthreads();
-  int above = upto - mine;
+  // scores
+  const bool hold = n <= kHeld, alone = pieces == 1;
+  double *scores = a.scores + ((size_t)x * p.n_kv + kvh) * p.table_stride;
+  const int quarter = threadIdx.x & 3;
+  for (int j0 = piece * kRun; j0 < n; j0 += pieces * kRun) {
+    float4 m[2][HD / 16];
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) above += w < wave ? sh.sums[w] : 0;
+    for (int u = 0; u < 2; ++u) {
+      int page = table[min(j0 + u * (kRun / 2) + (int)(threadIdx.x >> 2), n - 1)];
+      page = (unsigned)page < (unsigned)p.n_pages ? page : 0;
+      const float *mean = a.means + ((size_t)page * p.n_kv + kvh) * HD + quarter * 4;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (above < want && want <= above + c[i]) {
-      sh.found[0] = top - i;
-      sh.found[1] = above;
-      sh.found[2] = c[i];
+      for (int i = 0; i < HD / 16; ++i) m[u][i] = *reinterpret_cast<const float4 *>(mean + i * 16);
     }
-    above += c[i];
-  }
-  __syncthreads();
-}
-// The pages that `taken` says, in order, and of those that `tied` says the first `ties`: a run of pages to a thread.
-template <class Taken, class Tied>
-__device__ __forceinline__ void write_list(SelectShared &sh, int n, int ties, const int32_t *table, int32_t *list, Taken taken, Tied tied) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int per = (n + kThreads - 1) / kThreads, from = min(n, (int)threadIdx.x * per), to = min(n, from + per);
-  int t = 0, e = 0;
-  for (int i = from; i < to; ++i) {
-    t += taken(i);
-    e += tied(i);
-  }
-  const int t_upto = lane_sums(t), e_upto = lane_sums(e);
-  if (lane == 63) {
-    sh.sums[wave] = t_upto;
-    sh.sums2[wave] = e_upto;
-  }
-  __syncthreads();
-  int at = t_upto - t, before = e_upto - e;
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    at += w < wave ? sh.sums[w] : 0;
-    before += w < wave ? sh.sums2[w] : 0;
+    for (int u = 0; u < 2; ++u) {
+      const int j = j0 + u * (kRun / 2) + (threadIdx.x >> 2);
+      double s = 0;
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) {
+        const double *q = sum + i * 16 + quarter * 4;
+        s += (double)m[u][i].x * q[0] + (double)m[u][i].y * q[1] + (double)m[u][i].z * q[2] + (double)m[u][i].w * q[3];
+      }
+      s += __shfl_xor(s, 1);
+      s += __shfl_xor(s, 2);
+      if (quarter == 0 && j < n) {
+        if (alone && hold) sh.held[j] = s;
+        else score_store(scores + j, s);
+      }
+    }
   }
-  for (int i = from; i < to; ++i) {
-    const bool is = taken(i), tie = tied(i);
-    if (is || (tie && before < ties)) list[at + min(before, ties)] = table[i];
-    at += is;
-    before += tie;
-  }
-}
-template <class Get>
-__device__ __forceinline__ void list_by_numbers(SelectShared &sh, int n, int kept, const int32_t *table, int32_t *list, Get number) {
-  uint64_t lo = 0, hi = ~0ull;
-  int want = kept;               // of those in [lo, hi]; all above are taken
-  for (;;) {
-    const int shift = max(0, 64 - (int)__clzll((long long)(hi - lo | 1)) - 10);
-    __syncthreads();             // (what the last use of the counts read)
-    for (int i = threadIdx.x; i < kBins; i += kThreads) sh.bins[i] = 0;
+  if (!alone) {
+    // the last workgroup of the block and key head to end goes on
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // this wavefront's scores have arrived
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      const uint64_t u = number(i);
-      if (u >= lo && u <= hi) atomicAdd(&sh.bins[(u - lo) >> shift], 1);
+    int *counter = p.counters + x * p.n_kv + kvh;
+    if (threadIdx.x == 0) {
+      sh.found[0] = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pieces - 1;
+      if (sh.found[0]) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // as the next call expects it
     }
     __syncthreads();
-    find_part(sh, want);
-    lo += (uint64_t)sh.found[0] << shift;
-    hi = lo + lower(hi - lo, ((uint64_t)1 << shift) - 1);
-    want -= sh.found[1];
-    if (shift == 0 || sh.found[2] == want) break;
+    if (!sh.found[0]) return;
+  } else if (!hold) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
-  __syncthreads();
-  write_list(sh, n, want, table, list, [&](int i) { return number(i) > hi; }, [&](int i) { const uint64_t u = number(i); return u >= lo && u <= hi; });
-}
-__global__ __launch_bounds__(kThreads) void ff_select_pages_kernel(SelectParams a) {
-  __shared__ SelectShared sh;
-  const AttnParams &p = a.seqs;
-  const int x = blockIdx.y, kvh = blockIdx.x;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const Block b = block_of(a, x);
-  if (kvh == 0 && threadIdx.x == 0) {
-    const int end = attn_clamp(p.starts[p.n_seqs], 0, p.T);
-    a.starts[x] = b.s < 0 ? end : b.t0;
-    a.lens[x] = b.keys;
-    if (x == a.n_blocks - 1) a.starts[a.n_blocks] = b.s < 0 ? end : b.t0 + b.n;
-  }
-  int32_t *list = a.tables + ((size_t)x * p.n_kv + kvh) * a.width;
-  const int32_t *table = p.table + (b.s < 0 ? 0 : b.s * p.seq_tables);
-  const int n = b.earlier, kept = min(a.keep, n);
-  for (int i = kept + threadIdx.x; i < a.width; i += kThreads) list[i] = i < kept + b.own ? table[n + i - kept] : -1;
-  if (n <= a.keep) {
-    for (int i = threadIdx.x; i < n; i += kThreads) list[i] = table[i];
-    return;
-  }
-  const double *scores = a.scores + ((size_t)x * p.n_kv + kvh) * p.table_stride;
-  const int first = a.first, want = kept - first;
-  bool by_numbers = n > kHeld;
-  double lo = INFINITY, hi = -INFINITY, scale = 0;
-  if (!by_numbers) {
-    bool odd = false;
-    for (int i0 = threadIdx.x; i0 < n; i0 += kThreads * kBatch) {
+  if (hold && !alone) {
+    for (int i0 = threadIdx.x; i0 < n; i0 += kSelectThreads * kBatch) {
       double s[kBatch];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) s[i] = scores[min(i0 + i * kThreads, n - 1)];
+      for (int i = 0; i < kBatch; ++i) s[i] = score_load(scores + min(i0 + i * kSelectThreads, n - 1));
 #pragma unroll
       for (int i = 0; i < kBatch; ++i)
-        if (i0 + i * kThreads < n) {
-          sh.held[i0 + i * kThreads] = s[i];
-          if (i0 + i * kThreads >= first) {
-            odd = odd || !(fabs(s[i]) < INFINITY);
-            lo = fmin(lo, s[i]);
-            hi = fmax(hi, s[i]);
-          }
-        }
+        if (i0 + i * kSelectThreads < n) sh.held[i0 + i * kSelectThreads] = s[i];
     }
-    for (int i = threadIdx.x; i < kBins; i += kThreads) sh.bins[i] = 0;
-    if (threadIdx.x == 0) sh.n_few = 0;
+  }
+  __syncthreads();
+  const int first = a.first, want = kept - first;
+  bool by_numbers = !hold;
+  double lo = INFINITY, hi = -INFINITY, scale = 0;
+  if (hold) {
+    bool odd = false;
+    for (int i = first + threadIdx.x; i < n; i += kSelectThreads) {
+      const double s = sh.held[i];
+      odd = odd || !(fabs(s) < INFINITY);
+      lo = fmin(lo, s);
+      hi = fmax(hi, s);
+    }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
       lo = fmin(lo, __shfl_xor(lo, off));
@@ -282,7 +316,7 @@ __global__ __launch_bounds__(kThreads) void ff_select_pages_kernel(SelectParams 
     __syncthreads();
     by_numbers = want == 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < kSelectThreads / 64; ++w) {
       lo = fmin(lo, sh.extreme[0][w]);
       hi = fmax(hi, sh.extreme[1][w]);
       by_numbers = by_numbers || sh.odd[w];
@@ -294,7 +328,7 @@ __global__ __launch_bounds__(kThreads) void ff_select_pages_kernel(SelectParams 
   const auto part_of = [&](double s) { return min((int)((s - lo) * scale), kBins - 1); };       // (rounded, but never out of order)
   int part = 0, need = 0, c = 0;
   if (!by_numbers) {
-    for (int i = first + threadIdx.x; i < n; i += kThreads) atomicAdd(&sh.bins[part_of(sh.held[i])], 1);
+    for (int i = first + threadIdx.x; i < n; i += kSelectThreads) atomicAdd(&sh.bins[part_of(sh.held[i])], 1);
     __syncthreads();
     find_part(sh, want);
     part = sh.found[0];
@@ -303,10 +337,10 @@ __global__ __launch_bounds__(kThreads) void ff_select_pages_kernel(SelectParams 
     by_numbers = c > kFew;
   }
   if (by_numbers) {
-    list_by_numbers(sh, n, kept, table, list, [&](int i) { return i < first ? ~0ull : order_of(n > kHeld ? scores[i] : sh.held[i]); });
+    list_by_numbers(sh, n, kept, table, list, [&](int i) { return i < first ? ~0ull : order_of(hold ? sh.held[i] : score_load(scores + i)); });
     return;
   }
-  for (int i = first + threadIdx.x; i < n; i += kThreads)
+  for (int i = first + threadIdx.x; i < n; i += kSelectThreads)
     if (part_of(sh.held[i]) == part) {
       const int k = atomicAdd(&sh.n_few, 1);
       sh.few[k] = sh.held[i];
@@ -351,13 +385,11 @@ hipError_t ff_launch_page_means(const SelectParams &a, int head_dim, hipStream_t
 
 hipError_t ff_launch_select_pages(const SelectParams &a, int head_dim, hipStream_t s) {
   const AttnParams &p = a.seqs;
-  if (p.table_stride > a.keep) {
-    // (a sequence's pages are shared out where there are few blocks)
-    const long units = (long)a.n_blocks * p.n_kv;
-    const dim3 grid(p.n_kv, a.n_blocks, (unsigned)std::max(1l, std::min((p.table_stride + 63l) / 64, 1024 / units)));
-    if (head_dim == 128) hipLaunchKernelGGL((ff_page_scores_kernel<128>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((ff_page_scores_kernel<64>), grid, dim3(kThreads), 0, s, a);
-  }
-  hipLaunchKernelGGL(ff_select_pages_kernel, dim3(p.n_kv, a.n_blocks), dim3(kThreads), 0, s, a);
+  // (a sequence's pages are shared out where there are few blocks; then there are counters for all of them)
+  const long units = (long)a.n_blocks * p.n_kv;
+  const long pieces = std::max(1l, std::min((p.table_stride + kRun - 1l) / kRun, 512 / units));
+  const dim3 grid(p.n_kv, a.n_blocks, (unsigned)pieces);
+  if (head_dim == 128) hipLaunchKernelGGL((ff_select_pages_kernel<128>), grid, dim3(kSelectThreads), 0, s, a);
+  else hipLaunchKernelGGL((ff_select_pages_kernel<64>), grid, dim3(kSelectThreads), 0, s, a);
   return hipGetLastError();
 }
