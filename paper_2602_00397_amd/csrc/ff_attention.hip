@@ -397,26 +397,34 @@ __device__ __forceinline__ uint32_t chunk8_at(int key, int c) {
 }
 // The copies of KEYS (32 or 64) keys in 8 bits to LDS, as one wavefront makes them, 1 KB each, and their scales, one for each 8 keys.
 // Scalar arithmetic is what these cost (a lookup of page and scale for each KB: some 750 scalar instructions a step, 48 tokens 67 us), so keys
-// that are all there and in one page have one lookup, and others one for each 16.
+// that are all there and in one page have one lookup, and others one for each 16; the values lie where their keys do.
 template <int HD, int KEYS>
 struct Copier8 {
   static constexpr int S = HD == 128 ? 1 : 2, KPI = 1024 / HD, NI = KEYS / KPI;   // log2 of the keys of a row, keys of a copy
   Source8 src;
   int end;
+  // of the last keys that were asked for, from page 0 of the head's codes and scales on
+  uint64_t codes_at[KEYS / 16], scales_at[KEYS / 16];
   // key and offset of this lane's 16 bytes of copy i, from the copy's first key
   static __device__ __forceinline__ int key_of(int i, int lane) { return ((i * 4 + (lane >> 4)) << S | (lane & 15) >> (4 - S)) - i * KPI; }
   static __device__ __forceinline__ int chunk_of(int i, int lane) { return ((lane & 15) ^ swizzle8<HD>(i * 4 + (lane >> 4))) & ((1 << (4 - S)) - 1); }
+  __device__ __forceinline__ void look(int g, int key) {
+    int place;
+    const int page = page_of(src, key, place);
+    codes_at[g] = (uint64_t)page * src.page_bytes + (uint32_t)place * HD;
+    scales_at[g] = (uint64_t)page * src.page_scales + (uint32_t)((place & -16) >> src.scale_shift);
+  }
+  // keys, or the values of the keys that were asked for last
   template <bool VALUES>
-  __device__ __forceinline__ void copy(int j, uint32_t lds, int lane, f32x4_t (&scale)[KEYS / 32]) const {
+  __device__ __forceinline__ void copy(int j, uint32_t lds, int lane, f32x4_t (&scale)[KEYS / 32]) {
     const uint8_t *const codes = VALUES ? src.v : src.k;
     const float *const scales = VALUES ? src.vs : src.ks;
     if (j + KEYS <= end && (1 << src.shift) >= KEYS) {
-      int place;
-      const int page = page_of(src, j, place);
-      const uint8_t *base = codes + (size_t)page * src.page_bytes + (uint32_t)place * HD;
+      if (!VALUES) look(0, j);
+      const uint8_t *base = codes + codes_at[0];
 #pragma unroll
       for (int i = 0; i < NI; ++i) gload_lds16_at(base + i * 1024, (uint32_t)(key_of(i, lane) * HD + chunk_of(i, lane) * 16), lds + i * 1024);
-      const float *from = scales + (size_t)page * src.page_scales + (place >> src.scale_shift);
+      const float *from = scales + scales_at[0];
       if ((1 << src.scale_shift) >= KEYS) {
         const float one = scalar_load(from);
 #pragma unroll
@@ -431,43 +439,62 @@ struct Copier8 {
     for (int g = 0; g < KEYS / 16; ++g) {
       // (behind the end: the last key again, with some scale of its page; no row sees them)
       const int key0 = min(j + g * 16, end - 1);
-      int place;
-      const int page = page_of(src, key0, place);
-      const uint8_t *base = codes + (size_t)page * src.page_bytes + (uint32_t)place * HD;
+      if (!VALUES) look(g, key0);
+      const uint8_t *base = codes + codes_at[g];
 #pragma unroll
       for (int i = g * 16 / KPI; i < (g + 1) * 16 / KPI; ++i) {
         const int key = min(j + i * KPI + key_of(i, lane), end - 1) - key0;
         gload_lds16_at(base, (uint32_t)(key * HD + chunk_of(i, lane) * 16), lds + i * 1024);
       }
-      const float *from = scales + (size_t)page * src.page_scales;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int n = g * 2 + b;
-        scale[n >> 2][n & 3] = scalar_load(from + (((place & -16) + b * 8) >> src.scale_shift));
-      }
+      const float *from = scales + scales_at[g];
+      scale[g >> 1][g % 2 * 2] = scalar_load(from);
+      scale[g >> 1][g % 2 * 2 + 1] = scalar_load(from + (8 >> src.scale_shift));
     }
   }
 };
-// The keys and values of a tile of 64 on their way from pages in 8 bits to bf16 in LDS, as one of RW wavefronts brings them: NU times 8
-// channels of a key to a lane, 4 or 8 keys at a time, which share a page and a scale.
+// The keys and values of a tile of 64 on their way from pages in 8 bits to bf16 in LDS, as one of RW wavefronts brings them: NU times 16
+// channels of a key to a lane (8 of head_dim 64), 8 keys at a time, which share a page and a scale.  Pages are looked up a tile ahead, and
+// the values' are those that the keys had, so that no wavefront waits for a table where its matrix instructions could start.
 template <int HD, int RW>
 struct Stager8 {
-  static constexpr int NU = HD / (8 * RW), KPC = 512 / HD;
+  static constexpr int CPL = HD == 128 ? 16 : 8, NU = HD / (CPL * RW), KPC = 64 * CPL / HD, W = CPL / 8;
   Source8 src;
-  int first, end;
-  u32x2_t code[2][NU];
+  int first, end, step;                       // tiles from one to the next of the same wavefronts: `step` keys
+  uint32_t code[2][NU][CPL / 4];
   float scale[2][NU];
-  template <bool VALUES>
-  __device__ __forceinline__ void load(int j, int lane) {
+  int next[NU], keys[NU], values[NU];         // pages of the next tile, of the last keys that were asked for, of the values that are next
+  __device__ __forceinline__ int key0(int j, int i) const { return min(j + (first + i) * KPC, end - 1); }
+  __device__ __forceinline__ void look(int j) {
+#pragma unroll
+    for (int i = 0; i < NU; ++i) next[i] = scalar_load(src.table + (key0(j, i) >> src.shift));
+  }
+  // (`look` has been called for j)
+  __device__ __forceinline__ void load_keys(int j, int lane) {
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-      const int at = j + (first + i) * KPC, key0 = min(at, end - 1);
-      const int key = min(at + lane / (HD / 8), end - 1) - key0;
-      int place;
-      const int page = page_of(src, key0, place);
-      scale[VALUES][i] = scale8<VALUES>(src, page, place);
-      const uint8_t *base = (VALUES ? src.v : src.k) + (size_t)page * src.page_bytes + (uint32_t)place * HD;
-      code[VALUES][i] = *reinterpret_cast<const u32x2_t *>(base + (uint32_t)(key * HD + lane % (HD / 8) * 8));
+      values[i] = keys[i];
+      keys[i] = __builtin_amdgcn_readfirstlane((unsigned)next[i] < (unsigned)src.n_pages ? next[i] : 0);
+    }
+    load<false>(j, lane, keys);
+    if (j + step < end) look(j + step);
+  }
+  // `after`: the next tile's keys have been asked for in between
+  __device__ __forceinline__ void load_values(int j, int lane, bool after) {
+#pragma unroll
+    for (int i = 0; i < NU; ++i)
+      if (!after) values[i] = keys[i];
+    load<true>(j, lane, values);
+  }
+  template <bool VALUES>
+  __device__ __forceinline__ void load(int j, int lane, const int (&pages)[NU]) {
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int from = key0(j, i), key = min(j + (first + i) * KPC + lane / (HD / CPL), end - 1) - from, place = from & ((1 << src.shift) - 1);
+      const uint8_t *base = (VALUES ? src.v : src.k) + (size_t)pages[i] * src.page_bytes + (uint32_t)place * HD;
+      const uint8_t *at = base + (uint32_t)(key * HD + lane % (HD / CPL) * CPL);
+      if constexpr (CPL == 16) __builtin_memcpy(code[VALUES][i], __builtin_assume_aligned(at, 16), 16);
+      else __builtin_memcpy(code[VALUES][i], __builtin_assume_aligned(at, 8), 8);
+      scale[VALUES][i] = scale8<VALUES>(src, pages[i], place);
     }
   }
   // `edge`: infinities and NaN become 0; returns whether there were some
@@ -475,14 +502,16 @@ struct Stager8 {
   __device__ __forceinline__ bool store(uint32_t lds, int lane, bool edge) const {
     uint32_t odd = 0;
 #pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      u32x4_t w = decode8(code[VALUES][i][0], code[VALUES][i][1], scale[VALUES][i]);
-      if (edge)
+    for (int i = 0; i < NU; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = finite_pair(w[e], odd);
-      const int key = (first + i) * KPC + lane / (HD / 8);
-      *reinterpret_cast<__attribute__((address_space(3))) u32x4_t *>(lds + chunk_at<HD>(key, lane % (HD / 8))) = w;
-    }
+      for (int h = 0; h < W; ++h) {
+        u32x4_t w = decode8(code[VALUES][i][2 * h], code[VALUES][i][2 * h + 1], scale[VALUES][i]);
+        if (edge)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = finite_pair(w[e], odd);
+        const int key = (first + i) * KPC + lane / (HD / CPL);
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4_t *>(lds + chunk_at<HD>(key, lane % (HD / CPL) * W + h)) = w;
+      }
     return odd != 0;
   }
 };
@@ -571,8 +600,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void ff_attn_few_kernel(AttnPara
     const int n_pieces = pieces_of(range, cut.keys);
     if (it.piece >= n_pieces) continue;
     const int beg = range.lo + it.piece * cut.keys, end = range.hi - beg > cut.keys ? beg + cut.keys : range.hi;
-    std::conditional_t<EIGHT, Copier8<HD, KEYS>, Copier<HD, true, NI, 32>> copier = [&] {
-      if constexpr (EIGHT) return Copier8<HD, KEYS>{source8<HD>(p, it), end};
+    std::conditional_t<EIGHT, Copier8<HD, KEYS>, const Copier<HD, true, NI, 32>> copier = [&] {
+      if constexpr (EIGHT) return Copier8<HD, KEYS>{source8<HD>(p, it), end, {}, {}};
       else return Copier<HD, true, NI, 32>(key_source<HD, true>(p, it), 0, end, lane);
     }();
     [[maybe_unused]] f32x4_t k_scale[SETS], v_scale[SETS];        // of each eight keys on their way
@@ -909,21 +938,32 @@ __global__ __launch_bounds__(RW * KW * 64, HD == 64 && (SRC != kRows || KW == 1)
   if (it.piece >= n_pieces) return;
   const int beg = range.lo + it.piece * kpp, end = range.hi - beg > kpp ? beg + kpp : range.hi;
   std::conditional_t<EIGHT, Stager8<HD, RW>, const Copier<HD, PAGED, NI, kTileKeys>> copier = [&] {
-    if constexpr (EIGHT) return Stager8<HD, RW>{source8<HD>(p, it), wave * (HD / (8 * RW)), end};
+    if constexpr (EIGHT) {
+      Stager8<HD, RW> s8;
+      s8.src = source8<HD>(p, it);
+      s8.first = wave * Stager8<HD, RW>::NU;
+      s8.end = end;
+      s8.step = kStep;
+      return s8;
+    }
     else return Copier<HD, PAGED, NI, kTileKeys>(key_source<HD, PAGED>(p, it), wave * NI, end, lane);
   }();
   const auto copy_k = [&](int j, uint32_t to) __attribute__((always_inline)) {
-    if constexpr (EIGHT) copier.template load<false>(j, lane);
+    if constexpr (EIGHT) copier.load_keys(j, lane);
     else copier.template copy<false>(j, to, lane);
   };
+  // (in 8 bits: behind the next tile's keys, if there is one)
   const auto copy_v = [&](int j, uint32_t to) __attribute__((always_inline)) {
-    if constexpr (EIGHT) copier.template load<true>(j, lane);
+    if constexpr (EIGHT) copier.load_values(j, lane, j + kStep < end);
     else copier.template copy<true>(j, to, lane);
   };
   const uint32_t ring_k = lds_addr_of(lds) + kw * 4 * kHalf, ring_v = ring_k + 2 * kHalf;
 
   // (out before the rows' own arithmetic and loads)
-  if (beg + kw * kTileKeys < end) copy_k(beg + kw * kTileKeys, ring_k);
+  if (beg + kw * kTileKeys < end) {
+    if constexpr (EIGHT) copier.look(beg + kw * kTileKeys);
+    copy_k(beg + kw * kTileKeys, ring_k);
+  }
   Range see;
   u32x4_t q[KS];
   {
@@ -1463,7 +1503,10 @@ hipError_t launch(const AttnParams &p, Choice &c, hipStream_t s) {
   c.few.part = p.part + c.few.part_at;
   c.tile.part = p.part + c.tile.part_at;
   if (c.nb) {
-    const dim3 grid((unsigned)std::min(c.few.max_items, kFewGrid)), block(64 * kFewWaves);
+    // (four workgroups of narrow heads in 8 bits on a CU, which have half the bytes on their way that the others have: 48 tokens of 8 key heads of
+    // 64 over up to 16384 keys in pages of 16 / 64 47.3 / 33.4 us with two, 32.6 / 28.5 with four)
+    const int most = HD == 64 && p.k_scale ? 2 * kFewGrid : kFewGrid;
+    const dim3 grid((unsigned)std::min(c.few.max_items, most)), block(64 * kFewWaves);
     const size_t lds = few_lds(HD, c.nb);
     const auto few = [&](auto eight) {
       if (c.nb == 1) hipLaunchKernelGGL((ff_attn_few_kernel<HD, 1, eight()>), grid, block, lds, s, p, c.few);
