@@ -124,7 +124,8 @@ __device__ __forceinline__ int find_free(const PoolParams &p, int want, Sink sin
 }
 
 // ---- copies -----------------------------------------------------------------------------------------------------------------------
-// HBM-bound: 16 KB of a page's part to a workgroup at a time, four loads of a lane on their way.
+// HBM-bound: 16 KB of a page's part to a workgroup at a time, four loads of a lane on their way.  (2.2 GB of pages read and written: 452 us, 4.9
+// TB/s; with 4096 workgroups 460; 4 KB at a time 457, 64 KB with the next 16 KB on their way 456.)
 constexpr int kPiece = 16384;
 struct Parts {
   int n, pieces;                       // pieces of a page in all parts
@@ -386,7 +387,7 @@ Parts parts_of(const ff_page_part *parts, int n) {
   }
   return q;
 }
-constexpr long kCopyGrid = 4096;
+constexpr long kCopyGrid = 16384;
 int copy_grid(const Parts &q, long moves) { return (int)std::min<long>(moves * q.pieces, kCopyGrid); }
 
 }  // namespace
