@@ -441,7 +441,8 @@ ff_status ff_chunk_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_token
  *   chunk_starts, context_lens, page_table, table_stride   as for ff_chunk_attention:
  *                 sequence s's new tokens are the last of its context_lens[s] keys.
  *                 Tokens whose position would be negative, or whose page is outside
- *                 [0, n_pages), are not written
+ *                 [0, n_pages), are not written; with starts that do not ascend it is
+ *                 open which tokens are
  * A block of scale_tokens tokens whose first place is written gets the least scale
  * for which its largest value stays within 448 (2^-110 at least, 2^80 at most);
  * one that is added to keeps the larger of its scale and that of the new tokens,

@@ -168,10 +168,14 @@ ATTN_FN int first_new(const Seq &q) { return q.keys > q.n ? q.keys - q.n : 0; }
 ATTN_FN int runs_of(const Seq &q, int shift) {
   return q.n > 0 && q.keys > 0 ? ((q.keys - 1) >> shift) - (first_new(q) >> shift) + 1 : 0;
 }
-// most runs of a call: each has a token, and all of a sequence's but two are full
+// A call's runs are numbered so that the sequence of a number is found from the starts alone: those of sequence s from run_base on, with a gap
+// up to run_base of the next.  A run has a token, and all of a sequence's but two are full; where there are fewer tokens than that makes,
+// the numbers are the tokens'.
+ATTN_FN bool runs_by_token(long n_tokens, long n_seqs, int shift) { return n_tokens <= (n_tokens >> shift) + 2 * n_seqs; }
+ATTN_FN int run_base(int t0, int s, int shift, bool by_token) { return by_token ? t0 : (t0 >> shift) + 2 * s; }
+// how many numbers there are
 inline long most_runs(long n_tokens, long n_seqs, int shift) {
-  const long seqs = n_seqs < n_tokens ? n_seqs : n_tokens, runs = (n_tokens >> shift) + 2 * seqs;
-  return runs < n_tokens ? runs : n_tokens;
+  return runs_by_token(n_tokens, n_seqs, shift) ? n_tokens : (n_tokens >> shift) + 2 * n_seqs;
 }
 ATTN_FN int blocks_of(const Seq &q, int query_block) { return (int)(((long)q.n + query_block - 1) / query_block); }
 // Block number `at` of sequence s: its rows, how many pages lie in front of the one that its first token is in, how many from that one to the

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(kThreads) void ff_append8_kernel(Append8Params a, l
     // k and v of a head side by side, then the heads, then the blocks (of runs and heads there are fewer than 2^31)
     const bool is_v = unit & 1;
     const int pair = (int)(unit >> 1), run = p.by_kv(pair), kvh = pair - run * p.n_kv;
-    const Found f = unit < n_items ? find_item(p, run, [&](const Seq &q) { return runs_of(q, p.scale_shift); }) : Found{-1, 0, {0, 0, 0}};
+    const Found f = unit < n_items ? find_run(p, run, p.scale_shift) : Found{-1, 0, {0, 0, 0}};
     const int first = first_new(f.seq), block = (first >> p.scale_shift) + f.at;
     const int from = max(first, block << p.scale_shift);
     const int n = f.s < 0 ? 0 : (int)min((long)f.seq.keys, (long)(block + 1) << p.scale_shift) - from;

@@ -763,6 +763,9 @@ static void check_runs_and_blocks() {
         tokens += to - from;
       }
       CHECK(tokens == std::min(q.n, q.keys), "round %d sequence %d: %ld tokens of %d", round, s, tokens, q.n);
+      const bool by_token = runs_by_token(p.T, n_seqs, shift);
+      const long end = s + 1 < n_seqs ? run_base(seq_of(p, s + 1).t0, s + 1, shift, by_token) : most_runs(p.T, n_seqs, shift);
+      CHECK(!valid || run_base(q.t0, s, shift, by_token) + (long)n <= end, "round %d sequence %d: %d runs up to %ld", round, s, n, end);
       runs += n;
       const int nb = blocks_of(q, qb);
       long rows = 0;

@@ -23,8 +23,8 @@ __global__ __launch_bounds__(kThreads) void ff_page_means_kernel(SelectParams a,
   const int group = threadIdx.x / LPK, channel = threadIdx.x % LPK * 8;
   for (long id = blockIdx.x; id < n_items; id += gridDim.x) {
     const int run = p.by_kv((int)id), kvh = (int)id - run * p.n_kv;       // (fewer than 2^31)
-    const Found f = find_item(p, run, [&](const Seq &q) { return runs_of(q, p.page_shift); });
-    if (f.s < 0) break;
+    const Found f = find_run(p, run, p.page_shift);
+    if (f.s < 0) continue;
     const int number = (first_new(f.seq) >> p.page_shift) + f.at, page = p.table[f.s * p.seq_tables + number];
     if ((unsigned)page >= (unsigned)p.n_pages) continue;
     const int live = (int)min((long)f.seq.keys - ((long)number << p.page_shift), 1L << p.page_shift);

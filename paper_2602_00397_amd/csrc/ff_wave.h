@@ -59,3 +59,25 @@ __device__ __forceinline__ Found find_item(const AttnParams &p, long x, Count co
   }
   return f;
 }
+// The same for runs of 2^shift positions (runs_of), of which a call of more than 64 sequences has numbers with gaps: then the last sequence that
+// begins at or before number x is found by steps of 64th parts, three looks at most, where counting looks at all.  (1024 and 16384 single
+// tokens of 8 key heads are written in 24 and 344 us, in 35 and 3390 by counting.)
+__device__ __forceinline__ Found find_run(const AttnParams &p, int x, int shift) {
+  if (p.n_seqs <= 64) return find_item(p, x, [&](const Seq &q) { return runs_of(q, shift); });
+  const Found none = {-1, 0, {0, 0, 0}};
+  const int lane = threadIdx.x & 63;
+  const bool by_token = runs_by_token(p.T, p.n_seqs, shift);
+  int s = 0, to = p.n_seqs, step;
+  do {
+    step = (to - s + 63) >> 6;
+    const int at = s + lane * step;
+    const unsigned long long hit = __ballot(at < to && run_base(attn_clamp(p.starts[attn_min(at, to - 1)], 0, p.T), at, shift, by_token) <= x);
+    if (!hit) return none;
+    s += (63 - __builtin_clzll(hit)) * step;
+    to = attn_min(to, s + step);
+  } while (step > 1);
+  const Seq q = seq_of(p, s);
+  const int at = x - run_base(q.t0, s, shift, by_token);
+  if (at < 0 || at >= runs_of(q, shift)) return none;
+  return {s, at, q};
+}

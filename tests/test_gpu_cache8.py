@@ -437,6 +437,47 @@ def test_append_to_many_sequences(ctx):  # noqa: F811
         assert not codes.view(torch.uint8)[:, :, 1:].any() and not scale[:, :, 1].any()
 
 
+@pytest.mark.parametrize("n_seqs", [64, 65, 300, 4100])
+@pytest.mark.parametrize("most", [2, 40])
+def test_append_to_many_ragged_sequences(ctx, n_seqs, most):  # noqa: F811
+    """One call against calls of 50 sequences, to the bit: few tokens to a sequence and many, with empty sequences throughout."""
+    new = [(i * i * 7 + i // 64) % (most + 1) for i in range(n_seqs)]
+    a = Append(TINY, new, [n + (37 * i) % 30 for i, n in enumerate(new)], page_size=16, scale_tokens=8, seed=17, behind=2)
+    a.starts += 1                                  # (a row in front of the first sequence's)
+    before = a.held()
+    for s in range(0, n_seqs, 50):
+        e = min(n_seqs, s + 50)
+        ctx.cache8_append(a.c.h, a.k, a.v, a.starts[s:e + 1].clone(), a.lens[s:e].clone(), a.c.cache, a.c.table[s:e].clone())
+    want = a.held()
+    assert any(not torch.equal(x, y) for x, y in zip(before, want))
+    for x, held in zip((a.c.k_pages.view(torch.uint8), a.c.v_pages.view(torch.uint8), a.c.k_scale, a.c.v_scale), before):
+        x.copy_(held)
+    a.run(ctx)
+    for x, y in zip(a.held(), want):
+        assert torch.equal(x.nan_to_num(-1.0), y.nan_to_num(-1.0)) if x.is_floating_point() else torch.equal(x, y)
+
+
+def test_append_to_many_sequences_whose_starts_do_not_ascend(ctx):  # noqa: F811
+    """What is written is of the call's tokens, at its places: nothing else changes."""
+    new = [3] * 200
+    for what, change in (("one", lambda a: a.starts[100].fill_(-9)), ("far", lambda a: a.starts[30:40].fill_(1 << 30)), ("none", lambda a: a.starts.fill_(-1)),
+                         ("all", lambda a: a.starts.copy_(a.starts.flip(0)))):
+        a = Append(TINY, new, [3 + (37 * i) % 60 for i in range(200)], page_size=16, scale_tokens=8, seed=18)
+        change(a)
+        before = a.held()
+        a.run(ctx)
+        rows = a.starts.tolist()
+        may = torch.zeros(before[0].shape[0], 16, dtype=torch.bool, device=DEV)
+        for s in range(200):
+            t0, t1 = _clamped(rows, s, 600)
+            for j in range(max(0, int(a.lens[s]) - (t1 - t0)) // 8 * 8 if t1 > t0 else int(a.lens[s]), int(a.lens[s])):
+                may[int(a.c.table[s, j // 16]), j % 16] = True
+        for x, y in zip(a.held()[:2], before[:2]):
+            assert not ((x != y).any(dim=3).any(dim=1) & ~may).any(), what
+        for x, y in zip(a.held()[2:], before[2:]):
+            assert not ((x.nan_to_num(-1.0) != y.nan_to_num(-1.0)).any(dim=1) & ~may.unflatten(1, (2, 8)).any(dim=2)).any(), what
+
+
 def test_append_beyond_32_bit_offsets(ctx):  # noqa: F811
     a = Append(H8B, [3, 40], [130, 40], seed=9)
     big = Cache8(_heads(H8B), [130, 40], 64, 32, _gen(9), far=66000)

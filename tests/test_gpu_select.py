@@ -173,6 +173,23 @@ def test_means_of_the_pages_with_new_tokens(ctx, h, eight):  # noqa: F811
         assert torch.equal(s.means, want), f"{h} pages of {ps}"
 
 
+@pytest.mark.parametrize("n_seqs", [64, 65, 300, 4100])
+@pytest.mark.parametrize("most", [1, 40])
+def test_means_of_many_ragged_sequences(ctx, n_seqs, most):  # noqa: F811
+    """One call against calls of 50 sequences, to the bit, with empty sequences throughout."""
+    new = [(i * i * 7 + i // 64) % (most + 1) for i in range(n_seqs)]
+    s = Step(_heads(TINY), new, [n + (37 * i) % 30 for i, n in enumerate(new)], 1, 1, page_size=16, behind=2)
+    s.starts += 1                                  # (a row in front of the first sequence's)
+    before = s.means.clone()
+    for a in range(0, n_seqs, 50):
+        e = min(n_seqs, a + 50)
+        ctx.page_means(s.h, s.q.shape[0], s.starts[a:e + 1].clone(), s.lens[a:e].clone(), s.c.cache, s.table[a:e].clone(), s.means)
+    want = s.means.clone()
+    s.means.copy_(before)
+    s.update(ctx)
+    assert torch.equal(s.means, want) and not torch.equal(want, before)
+
+
 @pytest.mark.parametrize("eight", [False, True], ids=["bf16", "8 bits"])
 @pytest.mark.parametrize("h", [H8B, H7B, H1B, TINY, MHA, MQA], ids=lambda h: "%d_%d_%d" % h)
 @pytest.mark.parametrize("query_block,keep,first", [(1, 4, 1), (16, 8, 0), (7, 3, 3), (64, 1, 0), (200, 40, 2)])
