@@ -582,7 +582,8 @@ ff_status ff_pages_copy(ff_ctx *ctx, const ff_page_pool *pool, int32_t n,
  * that goes on with some beams in the place of others): full pages are shared, a
  * part-filled last page is copied to a free one, so that both rows may be added to.
  * What row to[i] held is given back (and may be taken by the next call, not by this one).  from[i] ==
- * to[i] leaves the row alone.
+ * to[i] gives the row a part-filled last page of its own if another row holds it too,
+ * and leaves it alone else.
  *   from, to   dev int32 [n] each
  *   missing    dev int32 [1] out: 0, or by how many the free pages fell short; then
  *              nothing is changed */
@@ -590,7 +591,9 @@ ff_status ff_pages_fork(ff_ctx *ctx, const ff_page_pool *pool, int32_t n,
                         const int32_t *from, const int32_t *to, int32_t *missing);
 
 /* Row rows[i] gets the pages for new_lens[i] tokens (free ones, whose contents are
- * what they were), or gives back those that it has beyond them; lens follow.
+ * what they were), or gives back those that it has beyond them; lens follow.  A row
+ * that is cut inside a page that other rows hold (tokens taken back behind a fork)
+ * still shares it: fork it onto itself before it is added to.
  * missing as above (pages that are given back serve the next call, not this one). */
 ff_status ff_pages_grow(ff_ctx *ctx, const ff_page_pool *pool, int32_t n,
                         const int32_t *rows, const int32_t *new_lens,

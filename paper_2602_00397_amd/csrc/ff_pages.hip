@@ -189,10 +189,14 @@ __global__ __launch_bounds__(kPlanThreads) void ff_pages_fork_plan_kernel(PoolPa
   for (int i0 = 0; i0 < p.n; i0 += kPlanThreads) {
     const int i = i0 + threadIdx.x;
     int first = kSkip, needs = 0;
-    if (i < p.n && is_row(p, p.to[i]) && is_row(p, p.from[i]) && p.from[i] != p.to[i] && wins(p, w, in, i)) {
-      const int len = clamped_len(p, p.lens[p.from[i]]), last = len >> p.page_shift;
-      needs = (len & ((1 << p.page_shift) - 1)) != 0 && is_page(p, p.table[(size_t)p.from[i] * p.table_stride + last]);
-      first = 0;
+    if (i < p.n && is_row(p, p.to[i]) && is_row(p, p.from[i]) && wins(p, w, in, i)) {
+      const int len = clamped_len(p, p.lens[p.from[i]]);
+      if ((len & ((1 << p.page_shift) - 1)) != 0) {
+        const int last = p.table[(size_t)p.from[i] * p.table_stride + (len >> p.page_shift)];
+        // (a row that stays where it is keeps its last page unless others hold it)
+        needs = is_page(p, last) && (p.from[i] != p.to[i] || p.refs[last] > 1);
+      }
+      if (needs || p.from[i] != p.to[i]) first = 0;
     }
     int all;
     const int before = sums_before(needs, all);

@@ -48,10 +48,13 @@ class Pool:
         win, ps = self.winners(targets), self.page_size
         free, rows, moves = [p for p in range(self.n_pages) if self.m_refs[p] == 0], {}, []
         for i, (a, b) in enumerate(zip(sources, targets)):
-            if self.is_row(a) and self.is_row(b) and a != b and win[b] == i:
+            if self.is_row(a) and self.is_row(b) and win[b] == i:
                 n = min(max(self.m_lens[a], 0), self.stride * ps)
                 row, last = self.m_table[a][:self.pages(n)], n // ps
-                if n % ps and self.is_page(row[last]):
+                own = n % ps and self.is_page(row[last]) and (a != b or self.m_refs[row[last]] > 1)
+                if a == b and not own:
+                    continue
+                if own:
                     moves.append((row[last], len(moves)))
                     row = row[:last] + [("new", len(moves) - 1)]
                 rows[b] = (row, n)
@@ -150,6 +153,26 @@ def test_a_search(ctx):  # noqa: F811
     p.check("compact", p.compact(ctx))
     assert p.counts_match() and all(n > 0 for n in p.m_refs[:int(p.result)])
     p.check("compact again", p.compact(ctx))
+
+
+def test_rows_that_are_cut_inside_a_shared_page(ctx):  # noqa: F811
+    """Tokens taken back behind a fork: the row shares the page that it was cut in until it is forked onto itself."""
+    p = Pool(30, 6, 8, seed=11)
+    for step in [lambda: p.grow(ctx, [0], [64]), lambda: p.fork(ctx, [0, 0, 0], [1, 2, 3]), lambda: p.grow(ctx, [1, 2, 3], [41, 48, 60])]:
+        p.check("shared", step())
+    assert p.m_table[1][2] == p.m_table[0][2] == p.m_table[2][2] and p.m_table[3][3] == p.m_table[0][3]
+    p.check("own", p.fork(ctx, [1, 2, 3, 0, 4], [1, 2, 3, 0, 4]))
+    assert p.m_table[1][2] != p.m_table[0][2] and p.m_table[2][2] == p.m_table[0][2] and p.m_table[3][3] != p.m_table[0][3] and p.counts_match()
+    held = p.table.clone()
+    p.check("own already", p.fork(ctx, [1, 3], [1, 3]))
+    assert torch.equal(held, p.table)
+    # the last two that hold a page, both forked; one forked onto itself and into another row; too few pages
+    for step in [lambda: p.grow(ctx, [4], [16]), lambda: p.fork(ctx, [4], [5]), lambda: p.grow(ctx, [4, 5], [9, 5]), lambda: p.fork(ctx, [4, 5], [4, 5]),
+                 lambda: p.fork(ctx, [4], [5]), lambda: p.grow(ctx, [4, 5], [16, 16]), lambda: p.fork(ctx, [4], [5]), lambda: p.grow(ctx, [4], [3]),
+                 lambda: p.fork(ctx, [4, 4], [4, 1]), lambda: p.grow(ctx, [1, 4], [16 * (2 + sum(n == 0 for n in p.m_refs)), 16]), lambda: p.fork(ctx, [1], [4]),
+                 lambda: p.grow(ctx, [1], [10]), lambda: p.grow(ctx, [4], [12])]:
+        p.check("again", step())
+        assert p.counts_match()
 
 
 @pytest.mark.parametrize("parts", [(), ((1, torch.uint8),), ((7, torch.uint8), (6, torch.uint8)), (((2, 16, 64), torch.bfloat16),) * 3,
