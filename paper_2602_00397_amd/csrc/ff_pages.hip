@@ -124,8 +124,10 @@ __device__ __forceinline__ int find_free(const PoolParams &p, int want, Sink sin
 }
 
 // ---- copies -----------------------------------------------------------------------------------------------------------------------
-// HBM-bound: 16 KB of a page's part to a workgroup at a time, four loads of a lane on their way.  (2.2 GB of pages read and written: 452 us, 4.9
-// TB/s; with 4096 workgroups 460; 4 KB at a time 457, 64 KB with the next 16 KB on their way 456.)
+// HBM-bound: 16 KB of a page's part to a workgroup at a time, four loads of a lane on their way.  What is written goes past the
+// caches, and so does what is read if it is read once (2.2 GB of pages read and written 437 us, 5.1 TB/s; both through the caches 454, reads
+// alone 446; 64 pages' sequences each in three more 66, through the caches 75, with reads past them 74).  (With 4096 workgroups 453, a million 462;
+// 8 KB at a time 435 but the 64 sequences 76, 32 KB 435 and 71.)
 constexpr int kPiece = 16384;
 struct Parts {
   int n, pieces;                       // pieces of a page in all parts
@@ -133,7 +135,8 @@ struct Parts {
   int64_t bytes[kPartsAtOnce];
   int upto[kPartsAtOnce];              // pieces of a page in this part and those before it
 };
-template <class T>
+// ONCE: no page is read twice.
+template <bool ONCE, class T>
 __device__ __forceinline__ void copy_as(uint8_t *to, const uint8_t *from, int bytes) {
   const int n = bytes / (int)sizeof(T);
   const T *src = reinterpret_cast<const T *>(from);
@@ -142,13 +145,14 @@ __device__ __forceinline__ void copy_as(uint8_t *to, const uint8_t *from, int by
     T v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (i + e * kThreads < n) v[e] = src[i + e * kThreads];
+      if (i + e * kThreads < n) v[e] = ONCE ? __builtin_nontemporal_load(src + i + e * kThreads) : src[i + e * kThreads];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (i + e * kThreads < n) dst[i + e * kThreads] = v[e];
+      if (i + e * kThreads < n) __builtin_nontemporal_store(v[e], dst + i + e * kThreads);
   }
 }
 // piece number x of a page
+template <bool ONCE>
 __device__ void copy_piece(const Parts &parts, int x, int64_t from, int64_t to) {
   // (a lane to a part)
   const int lane = threadIdx.x & 63;
@@ -157,14 +161,14 @@ __device__ void copy_piece(const Parts &parts, int x, int64_t from, int64_t to) 
   const int n = (int)(bytes - at < kPiece ? bytes - at : kPiece);
   const uint8_t *src = parts.data[k] + from * bytes + at;
   uint8_t *dst = parts.data[k] + to * bytes + at;
-  if (bytes % 16 == 0) copy_as<u32x4_t>(dst, src, n);
-  else if (bytes % 4 == 0) copy_as<uint32_t>(dst, src, n);
-  else copy_as<uint8_t>(dst, src, n);
+  if (bytes % 16 == 0) copy_as<ONCE, u32x4_t>(dst, src, n);
+  else if (bytes % 4 == 0) copy_as<ONCE, uint32_t>(dst, src, n);
+  else copy_as<ONCE, uint8_t>(dst, src, n);
 }
 __global__ __launch_bounds__(kThreads) void ff_pages_copy_kernel(Parts parts, int n_pages, int n, const int32_t *from, const int32_t *to) {
   for (long id = blockIdx.x; id < (long)n * parts.pieces; id += gridDim.x) {
     const int i = (int)(id / parts.pieces), a = from[i], b = to[i];
-    if (a != b && (unsigned)a < (unsigned)n_pages && (unsigned)b < (unsigned)n_pages) copy_piece(parts, (int)(id - (long)i * parts.pieces), a, b);
+    if (a != b && (unsigned)a < (unsigned)n_pages && (unsigned)b < (unsigned)n_pages) copy_piece<false>(parts, (int)(id - (long)i * parts.pieces), a, b);
   }
 }
 
@@ -220,7 +224,7 @@ __global__ __launch_bounds__(kThreads) void ff_pages_fork_kernel(PoolParams p, P
       const int i = (int)(id / parts.pieces), first = w.first[i];
       if (first < 0) continue;
       const int page = w.rows[(size_t)i * p.table_stride + (w.lens[i] >> p.page_shift)];
-      copy_piece(parts, (int)(id - (long)i * parts.pieces), page, pages[first]);
+      copy_piece<false>(parts, (int)(id - (long)i * parts.pieces), page, pages[first]);
     }
     return;
   }
@@ -366,7 +370,7 @@ __global__ __launch_bounds__(kThreads) void ff_pages_compact_kernel(PoolParams p
     const int n_copy = gridDim.x - n_apply;
     for (long id = blockIdx.x - n_apply; id < (long)moves * parts.pieces; id += n_copy) {
       const int k = (int)(id / parts.pieces);
-      copy_piece(parts, (int)(id - (long)k * parts.pieces), c.origin[k], c.holes[k]);
+      copy_piece<true>(parts, (int)(id - (long)k * parts.pieces), c.origin[k], c.holes[k]);
     }
     return;
   }
