@@ -125,7 +125,7 @@ __device__ __forceinline__ int find_free(const PoolParams &p, int want, Sink sin
 
 // ---- copies -----------------------------------------------------------------------------------------------------------------------
 // HBM-bound: 16 KB of a page's part to a workgroup at a time, four loads of a lane on their way.  What is written goes past the
-// caches, and so does what is read if it is read once (2.2 GB of pages read and written 437 us, 5.1 TB/s; both through the caches 454, reads
+// caches, and so does what is read if it is read once (2.2 GB of pages read and written 434 us, 5.1 TB/s; both through the caches 454, reads
 // alone 446; 64 pages' sequences each in three more 66, through the caches 75, with reads past them 74).  (With 4096 workgroups 453, a million 462;
 // 8 KB at a time 435 but the 64 sequences 76, 32 KB 435 and 71.)
 constexpr int kPiece = 16384;
