@@ -440,9 +440,13 @@ ff_status ff_chunk_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_token
  *                 count)
  *   chunk_starts, context_lens, page_table, table_stride   as for ff_chunk_attention:
  *                 sequence s's new tokens are the last of its context_lens[s] keys.
- *                 Tokens whose position would be negative, or whose page is outside
- *                 [0, n_pages), are not written; with starts that do not ascend it is
- *                 open which tokens are
+ *                 Tokens whose position would be negative, or behind the table's
+ *                 table_stride * page_size, or whose page is outside [0, n_pages), are
+ *                 not written (a length from 2^30 on, which no sequence has, is cut to
+ *                 the table first); with starts that do not ascend it is open which
+ *                 tokens are.  So with the lengths that were asked of ff_pages_grow, not
+ *                 those that the rows got, no token comes to the place of an earlier one
+ *                 where a row or the pool is full
  * A block of scale_tokens tokens whose first place is written gets the least scale
  * for which its largest value stays within 448 (2^-110 at least, 2^80 at most);
  * one that is added to keeps the larger of its scale and that of the new tokens,
@@ -478,7 +482,8 @@ ff_status ff_chunk_attention8(ff_ctx *ctx, const ff_attention *a, int32_t n_toke
 /* Means of the keys of pages that have new tokens, over the page's keys so far:
  *   means         dev f32 [n_pages][n_kv_heads][head_dim]; of other pages as they were
  *   the rest      as for ff_cache8_append (n_tokens new tokens in all; their keys are
- *                 in the cache).  A page outside [0, n_pages) is passed over
+ *                 in the cache).  A page outside [0, n_pages) is passed over, and so are
+ *                 tokens that have no place in the table
  * Sums are float64, rounded once. */
 ff_status ff_page_means(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens,
                         int32_t n_seqs, const int32_t *chunk_starts,
@@ -591,7 +596,9 @@ ff_status ff_pages_fork(ff_ctx *ctx, const ff_page_pool *pool, int32_t n,
                         const int32_t *from, const int32_t *to, int32_t *missing);
 
 /* Row rows[i] gets the pages for new_lens[i] tokens (free ones, whose contents are
- * what they were), or gives back those that it has beyond them; lens follow.  A row
+ * what they were), or gives back those that it has beyond them; lens follow.  More
+ * tokens than a row's entries have pages for are cut to these, and missing does not count
+ * them: the row's length is then below new_lens[i].  A row
  * that is cut inside a page that other rows hold (tokens taken back behind a fork)
  * still shares it: fork it onto itself before it is added to.
  * missing as above (pages that are given back serve the next call, not this one). */

@@ -163,6 +163,14 @@ ATTN_FN int pieces_of(const Range &r, int keys_per_piece) {
 
 // ---- new tokens by the runs of positions and by the blocks that they lie in
 // They stand at the positions keys - n .. keys - 1 of their sequence, as far as these are not negative.
+// The sequence as the calls see it that write something for new tokens: those behind the table's end have no place and are left out, so that none
+// stands on an earlier token's (which other rows may share).  (Lengths from 2^30 on, which no sequence has, are cut as everywhere.)
+ATTN_FN Seq placed_seq(const AttnParams &p, int s) {
+  Seq q = seq_of(p, s);
+  const int keys = p.lens[s];
+  if (keys > q.keys && keys < kMaxKeys) q.n = attn_max(0, q.n - (keys - q.keys));
+  return q;
+}
 ATTN_FN int first_new(const Seq &q) { return q.keys > q.n ? q.keys - q.n : 0; }
 // how many runs of 2^shift positions have new tokens
 ATTN_FN int runs_of(const Seq &q, int shift) {

@@ -784,6 +784,37 @@ static void check_runs_and_blocks() {
   }
 }
 
+// New tokens of sequences that outgrow their tables: those with a place keep it, the others have none.
+static void check_placed_tokens() {
+  uint32_t rnd = 99;
+  const auto below = [&](int n) { rnd = rnd * 1664525u + 1013904223u; return (int)((rnd >> 8) % (unsigned)n); };
+  for (int round = 0; round < 20000; ++round) {
+    AttnParams p = {};
+    p.page_shift = 3 + below(5);
+    p.table_stride = 1 + below(20);
+    const int most = p.table_stride << p.page_shift, far[] = {-2147483647 - 1, -1, kMaxKeys - 1, kMaxKeys, 2147483647};
+    int32_t starts[2] = {below(5), 0}, lens = round % 4 ? below(2 * most + 40) : far[below(5)];
+    starts[1] = starts[0] + below(most + 60);
+    p.T = starts[1] + below(3);
+    p.starts = starts; p.lens = &lens; p.n_seqs = 1;
+    const Seq q = seq_of(p, 0), w = placed_seq(p, 0);
+    ++g_calls;
+    CHECK(w.t0 == q.t0 && w.keys == q.keys && w.n >= 0 && w.n <= q.n, "round %d", round);
+    if (lens >= kMaxKeys) {
+      CHECK(w.n == q.n, "round %d: length %d", round, lens);
+      continue;
+    }
+    // token t stands at len - n + t
+    int last = -1;
+    for (int t = 0; t < q.n; ++t) {
+      const long at = (long)attn_max(lens, 0) - q.n + t;
+      if (at < most) last = t;
+      if (t < w.n) CHECK((long)w.keys - w.n + t == at && at < most, "round %d token %d of %d: length %d of %d", round, t, q.n, lens, most);
+    }
+    CHECK(w.n == last + 1, "round %d: %d tokens of %d, length %d of %d", round, w.n, q.n, lens, most);
+  }
+}
+
 // Launches of the write in 8 bits, the selection and the page calls at their limits: dimensions and threads that a launch can have, and
 // workspaces that hold what the arrays in them take.
 static void check_page_launches() {
@@ -861,6 +892,7 @@ int main() {
   check_attention();
   check_other_pages();
   check_runs_and_blocks();
+  check_placed_tokens();
   check_page_launches();
   check_far_contexts();
   check_most_rows();

@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kThreads) void ff_page_means_kernel(SelectParams a,
 
 // ---- blocks of new tokens -----------------------------------------------------------------------------------------------------
 __device__ __forceinline__ Block block_of(const SelectParams &a, int x) {
-  const Found f = find_item(a.seqs, x, [&](const Seq &q) { return blocks_of(q, a.query_block); });
+  const Found f = find_item(a.seqs, x, seq_of, [&](const Seq &q) { return blocks_of(q, a.query_block); });
   return f.s < 0 ? Block{-1, 0, 0, 0, 0, 0} : block_at(f.seq, f.s, f.at, a.query_block, a.keep, a.seqs.page_shift);
 }
 

@@ -36,15 +36,15 @@ __device__ __forceinline__ T scalar_load(const T *at) {
   return *reinterpret_cast<const __attribute__((address_space(4))) T *>(reinterpret_cast<uintptr_t>(at));
 }
 
-// Items are counted over the sequences: `count` gives a sequence's.  Item number x (the same in all lanes) is number `at` of sequence s;
+// Items are counted over the sequences: `get` gives a sequence, `count` its items.  Item number x (the same in all lanes) is number `at` of sequence s;
 // s < 0: there are fewer.  64 sequences are looked at together, so a call of up to 64 takes one look.
 struct Found { int s, at; Seq seq; };
-template <class Count>
-__device__ __forceinline__ Found find_item(const AttnParams &p, long x, Count count) {
+template <class Get, class Count>
+__device__ __forceinline__ Found find_item(const AttnParams &p, long x, Get get, Count count) {
   const int lane = threadIdx.x & 63;
   Found f = {-1, 0, {0, 0, 0}};
   for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
-    const Seq q = s0 + lane < p.n_seqs ? seq_of(p, s0 + lane) : Seq{0, 0, 0};
+    const Seq q = s0 + lane < p.n_seqs ? get(p, s0 + lane) : Seq{0, 0, 0};
     // (a call's tokens keep the sums in 32 bits; starts that do not ascend may not: nothing is found then, or another item)
     const int mine = count(q), upto = lane_sums(mine);
     const unsigned long long hit = __ballot(x < (long)(unsigned)upto);
@@ -59,11 +59,11 @@ __device__ __forceinline__ Found find_item(const AttnParams &p, long x, Count co
   }
   return f;
 }
-// The same for runs of 2^shift positions (runs_of), of which a call of more than 64 sequences has numbers with gaps: then the last sequence that
-// begins at or before number x is found by steps of 64th parts, three looks at most, where counting looks at all.  (1024 and 16384 single
-// tokens of 8 key heads are written in 24 and 344 us, in 35 and 3390 by counting.)
+// The same for runs of 2^shift positions that new tokens have a place in (runs_of, placed_seq), of which a call of more than 64 sequences has
+// numbers with gaps: then the last sequence that begins at or before number x is found by steps of 64th parts, three looks at most, where
+// counting looks at all.  (1024 and 16384 single tokens of 8 key heads are written in 24 and 344 us, in 35 and 3390 by counting.)
 __device__ __forceinline__ Found find_run(const AttnParams &p, int x, int shift) {
-  if (p.n_seqs <= 64) return find_item(p, x, [&](const Seq &q) { return runs_of(q, shift); });
+  if (p.n_seqs <= 64) return find_item(p, x, placed_seq, [&](const Seq &q) { return runs_of(q, shift); });
   const Found none = {-1, 0, {0, 0, 0}};
   const int lane = threadIdx.x & 63;
   const bool by_token = runs_by_token(p.T, p.n_seqs, shift);
@@ -76,7 +76,7 @@ __device__ __forceinline__ Found find_run(const AttnParams &p, int x, int shift)
     s += (63 - __builtin_clzll(hit)) * step;
     to = attn_min(to, s + step);
   } while (step > 1);
-  const Seq q = seq_of(p, s);
+  const Seq q = placed_seq(p, s);
   const int at = x - run_base(q.t0, s, shift, by_token);
   if (at < 0 || at >= runs_of(q, shift)) return none;
   return {s, at, q};

@@ -621,3 +621,46 @@ def test_the_validate_option(ctx):  # noqa: F811
         _refused(4, c.run, ctx)
     finally:
         ctx.set_option("validate", 0)
+
+
+# ------------------------------------------------------------------ sequences that outgrow their page table
+
+def _placed(new, lens, most):
+    """How many of each sequence's new tokens have a place in a table of `most` keys: the first ones."""
+    return [min(n, max(0, n - max(0, keys - most))) for n, keys in zip(new, lens)]
+
+
+def _placed_model(c, k, v, starts, lens, held):
+    """The write of the tokens that have a place, as if the others were not in the call."""
+    most, new = c.table.shape[1] * c.page_size, [b - a for a, b in zip(starts, starts[1:])]
+    n = _placed(new, lens, most)
+    rows = torch.tensor([t for a, m in zip(starts, n) for t in range(a, a + m)], dtype=torch.long, device=DEV)
+    return _append_model(c, k[rows], v[rows], _starts(n), [min(x, most) for x in lens], held)
+
+
+@pytest.mark.parametrize("h", [H8B, H1B], ids=lambda h: "%d_%d_%d" % h)
+@pytest.mark.parametrize("n_seqs", [6, 64, 65, 200])
+def test_append_behind_the_end_of_the_table(ctx, h, n_seqs):  # noqa: F811
+    """Tokens that the table has no place for are not written, and nor is any earlier key or scale changed; up to there they are."""
+    most = 6 * 16
+    over = [(1, 97), (5, 98), (5, 101), (5, 102), (40, 130), (3, 96), (0, 97), (1, 500), (9, (1 << 30) - 1), (2, 95), (20, 110)]
+    new, lens = ([over[i % len(over)][j] for i in range(n_seqs)] for j in (0, 1))
+    a = Append(h, new, [min(n, most - 1) for n in lens], page_size=16, scale_tokens=8, seed=n_seqs, behind=2)
+    # a full table: each row has its pages and no column more
+    c = a.c
+    c.table = torch.randperm(c.k_pages.shape[0], device=DEV, generator=_gen(3))[:n_seqs * 6].to(torch.int32).view(n_seqs, 6).contiguous()
+    for x in (c.k_pages, c.v_pages):
+        codes = x.view(torch.uint8)
+        codes.copy_(torch.randint(0, 127, codes.shape, device=DEV, generator=_gen(4)))
+    for x in (c.k_scale, c.v_scale):
+        x.copy_(torch.exp2(torch.randint(-9, -5, x.shape, device=DEV, generator=_gen(5)).float()))
+    a.lens = _int32(lens)
+    held = a.held()
+    a.run(ctx)
+    want = _placed_model(c, a.k, a.v, a.starts.tolist(), lens, held)
+    for x, y in zip(a.held(), want):
+        assert torch.equal(x, y)
+    # of a token behind a full row there is no trace
+    full = [i for i in range(n_seqs) if lens[i] - new[i] >= most]
+    pages = c.table[full].long().flatten()
+    assert full and all(torch.equal(x[pages], y[pages]) for x, y in zip(a.held(), held))

@@ -113,3 +113,53 @@ def test_append_on_another_stream_than_the_current_one():
         torch.cuda.synchronize()
         a.close()
         b.close()
+
+
+def test_rows_that_outgrow_their_table_or_the_pool(ctx):  # noqa: F811
+    """A step's lengths as the program wants them, whatever the pool could give: tokens without a page are dropped, and what is cached stays,
+    of the row and of the rows that share its pages."""
+    h, ps = _heads((8, 2, 64)), 16
+    n_pages, stride, kw = 8, 3, 128
+    k, v = (torch.zeros((n_pages, 2, ps, 64), dtype=torch.uint8, device=DEV).view(E4M3) for _ in range(2))
+    ks, vs = (torch.ones((n_pages, 2, 2), device=DEV) for _ in range(2))
+    refs, lens, table = torch.zeros(n_pages, dtype=torch.int32, device=DEV), _int32([0] * 3), torch.full((3, stride), -1, dtype=torch.int32, device=DEV)
+    cache, pool, missing = B.paged_cache8(k, v, ks, vs), B.page_pool(refs, table, lens, ps, [k, v, ks, vs]), _int32([0])
+    ctx.ensure_pages_workspace(pool, 3)
+    gen, rows = _gen(9), _int32([0, 1, 2])
+    x, y = _bf16(gen, 100, kw), _bf16(gen, 100, kw)
+
+    def step(new, wanted):
+        wanted = _int32(wanted)
+        ctx.pages_grow(pool, rows, wanted, missing)
+        ctx.cache8_append(h, x[:sum(new)], y[:sum(new)], _int32(_starts(new)), wanted, cache, table)
+
+    def held():
+        return [t.clone() for t in (k.view(torch.uint8), v.view(torch.uint8), ks, vs)]
+
+    step([48, 0, 5], [48, 0, 5])
+    ctx.pages_fork(pool, _int32([0]), _int32([1]), missing)
+    assert lens.tolist() == [48, 48, 5] and refs.tolist()[:4] == [2, 2, 2, 1] and int(missing) == 0
+    before = held()
+    # a token behind the full row 0, then another: row 1 shares its pages, and nothing of them changes
+    for n in (49, 50):
+        step([1, 0, 0], [n, 48, 5])
+        assert lens.tolist() == [48, 48, 5] and int(missing) == 0
+        assert all(torch.equal(a, b) for a, b in zip(held(), before))
+    # three tokens for row 2 that has a place for one of them
+    step([0, 0, 42], [48, 48, 47])
+    before = held()
+    step([0, 0, 3], [48, 48, 50])
+    after, last = held(), int(table[2, 2])
+    same = torch.ones((n_pages, ps), dtype=torch.bool, device=DEV)
+    same[last, 8:] = False                                    # (the block of the token, whose scale may have grown)
+    for a, b in zip(after[:2], before[:2]):
+        assert torch.equal(a.transpose(1, 2)[same], b.transpose(1, 2)[same]) and bool((a[last, :, 15] != b[last, :, 15]).any())
+    # too few pages: nothing is grown, and the tokens of the pages that are missing are dropped
+    refs[refs == 0] = 1
+    ctx.pages_free(pool, _int32([2]))
+    ctx.pages_grow(pool, _int32([2]), _int32([16]), missing)
+    refs[refs == 0] = 1
+    before, tables = held(), table.clone()
+    step([0, 0, 20], [48, 48, 36])
+    assert int(missing) == 2 and torch.equal(table, tables) and lens.tolist() == [48, 48, 16]
+    assert all(torch.equal(a, b) for a, b in zip(held(), before))

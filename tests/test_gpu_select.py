@@ -443,3 +443,20 @@ def test_refusals(ctx):  # noqa: F811
         _refused(4, s.attend, ctx)
     finally:
         ctx.set_option("validate", 0)
+
+
+@pytest.mark.parametrize("n_seqs", [5, 70])
+def test_means_behind_the_end_of_the_table(ctx, n_seqs):  # noqa: F811
+    """New tokens that the table has no place for change no mean: only pages with tokens in front of its end are made anew."""
+    over = [(1, 97), (5, 98), (40, 130), (3, 96), (9, (1 << 30) - 1)]
+    new, lens = ([over[i % len(over)][j] for i in range(n_seqs)] for j in (0, 1))
+    s = Step(_heads(TINY), new, [96] * n_seqs, 1, 1, page_size=16, seed=n_seqs)
+    s.table = s.table[:, :6].contiguous()
+    s.lens = _int32(lens)
+    want = s.means.clone()
+    for i in range(n_seqs):
+        for j in range(max(0, min(lens[i] - new[i], 96)) // 16, 6 if lens[i] - new[i] < 96 else 0):
+            page = int(s.table[i, j])
+            want[page] = s.c.values("k", page).mean(dim=1).float()
+    s.update(ctx)
+    assert torch.equal(s.means, want)
