@@ -573,7 +573,10 @@ typedef struct {
   int32_t n_parts;
 } ff_page_pool;
 
-/* Workspace of the calls below for up to n entries; more entries never take less. */
+/* Workspace of any of the calls below for up to n entries; more entries never take less.
+ * ff_pages_fork asks for all of it, which is mostly 4 n table_stride bytes; ff_pages_grow and
+ * ff_pages_compact (n = 1) for what a program that does not fork may set instead, 4 max(n_rows +
+ * 3 n + 64, n_pages + n_rows + 2 n + 65, 3 n_pages + 64) bytes. */
 ff_status ff_pages_workspace_bytes(const ff_page_pool *pool, int32_t n, size_t *bytes);
 
 /* Copies page from[i] of every part to page to[i] (dev int32 [n] each; i with a page

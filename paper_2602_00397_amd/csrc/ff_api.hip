@@ -607,8 +607,9 @@ ff_status check_pool(ff_ctx *ctx, const ff_page_pool *pool, bool tables) {
     return fail(ctx, FF_ERR_ALIGNMENT, "refs / page_table / lens must be 16-byte aligned");
   return FF_OK;
 }
-// Entries of a call (b may be none), its workspace if it takes one, and what its kernels get.
-ff_status pool_params(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const int32_t *a, const int32_t *b, bool ws, PoolParams *p) {
+// Entries of a call (b may be none), its workspace if it takes one (with or without the pages of rows), and what its kernels get.
+enum PoolRoom { kNoRoom, kRoom, kRoomForRows };
+ff_status pool_params(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const int32_t *a, const int32_t *b, PoolRoom room, PoolParams *p) {
   if (n < 1 || n > (1 << 20)) return fail(ctx, FF_ERR_SHAPE, "n (%d) must be in [1, 2^20]", n);
   if (!aligned16(a) || !aligned16(b)) return fail(ctx, FF_ERR_ALIGNMENT, "entries must be 16-byte aligned");
   *p = {};
@@ -616,8 +617,8 @@ ff_status pool_params(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const in
   p->n_pages = pool->n_pages; p->n_rows = pool->n_rows; p->table_stride = pool->table_stride;
   p->page_shift = log2_of(pool->page_size);
   p->n = n;
-  if (!ws) return FF_OK;
-  const size_t need = ff_pages_ints(n, pool->n_pages, pool->n_rows, pool->table_stride) * sizeof(int32_t);
+  if (room == kNoRoom) return FF_OK;
+  const size_t need = ff_pages_ints(n, pool->n_pages, pool->n_rows, room == kRoomForRows ? pool->table_stride : 0) * sizeof(int32_t);
   if (!ctx->ws) return fail(ctx, FF_ERR_WORKSPACE, "no workspace set (ff_set_workspace)");
   if (ctx->ws_bytes < need) return fail(ctx, FF_ERR_WORKSPACE, "workspace has %zu bytes, this call needs %zu", ctx->ws_bytes, need);
   p->ws = static_cast<int32_t *>(ctx->ws);
@@ -1288,7 +1289,7 @@ ff_status ff_pages_copy(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const 
   if (st != FF_OK) return st;
   if (!from || !to || pool->n_parts < 1) return fail(ctx, FF_ERR_INVALID_ARG, "from or to is NULL, or there are no parts");
   PoolParams p;
-  if ((st = pool_params(ctx, pool, n, from, to, false, &p)) != FF_OK) return st;
+  if ((st = pool_params(ctx, pool, n, from, to, kNoRoom, &p)) != FF_OK) return st;
   FF_HIP(ctx, hipSetDevice(ctx->device));
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
   FF_HIP(ctx, ff_launch_pages_copy(pool->parts, pool->n_parts, pool->n_pages, n, from, to, ctx->stream));
@@ -1302,7 +1303,7 @@ ff_status ff_pages_fork(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const 
   if (st != FF_OK) return st;
   if (!from || !to || !missing) return fail(ctx, FF_ERR_INVALID_ARG, "from, to or missing is NULL");
   PoolParams p;
-  if ((st = pool_params(ctx, pool, n, from, to, true, &p)) != FF_OK) return st;
+  if ((st = pool_params(ctx, pool, n, from, to, kRoomForRows, &p)) != FF_OK) return st;
   p.from = from; p.to = to; p.result = missing;
   FF_HIP(ctx, hipSetDevice(ctx->device));
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
@@ -1317,7 +1318,7 @@ ff_status ff_pages_grow(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const 
   if (st != FF_OK) return st;
   if (!rows || !new_lens || !missing) return fail(ctx, FF_ERR_INVALID_ARG, "rows, new_lens or missing is NULL");
   PoolParams p;
-  if ((st = pool_params(ctx, pool, n, rows, new_lens, true, &p)) != FF_OK) return st;
+  if ((st = pool_params(ctx, pool, n, rows, new_lens, kRoom, &p)) != FF_OK) return st;
   p.to = rows; p.new_lens = new_lens; p.result = missing;
   FF_HIP(ctx, hipSetDevice(ctx->device));
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
@@ -1332,7 +1333,7 @@ ff_status ff_pages_free(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const 
   if (st != FF_OK) return st;
   if (!rows) return fail(ctx, FF_ERR_INVALID_ARG, "rows is NULL");
   PoolParams p;
-  if ((st = pool_params(ctx, pool, n, rows, nullptr, false, &p)) != FF_OK) return st;
+  if ((st = pool_params(ctx, pool, n, rows, nullptr, kNoRoom, &p)) != FF_OK) return st;
   p.to = rows;
   FF_HIP(ctx, hipSetDevice(ctx->device));
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
@@ -1347,7 +1348,7 @@ ff_status ff_pages_compact(ff_ctx *ctx, const ff_page_pool *pool, int32_t *live)
   if (st != FF_OK) return st;
   if (!live) return fail(ctx, FF_ERR_INVALID_ARG, "live is NULL");
   PoolParams p;
-  if ((st = pool_params(ctx, pool, 1, nullptr, nullptr, true, &p)) != FF_OK) return st;
+  if ((st = pool_params(ctx, pool, 1, nullptr, nullptr, kRoom, &p)) != FF_OK) return st;
   p.result = live;
   FF_HIP(ctx, hipSetDevice(ctx->device));
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);

@@ -17,7 +17,7 @@ struct PoolParams {
   int32_t *result;               // pages that were missing, or pages in use
   int32_t *ws;                   // see ff_pages_ints
 };
-// 32-bit numbers of workspace that a call with n entries takes at most
+// 32-bit numbers of workspace that a call with n entries takes at most; grow and compact, which keep no row's pages, with a table_stride of 0
 size_t ff_pages_ints(int64_t n, int32_t n_pages, int32_t n_rows, int32_t table_stride);
 
 hipError_t ff_launch_pages_copy(const ff_page_part *parts, int n_parts, int32_t n_pages, int32_t n, const int32_t *from, const int32_t *to, hipStream_t s);

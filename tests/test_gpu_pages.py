@@ -418,3 +418,63 @@ def test_refusals(ctx):  # noqa: F811
     finally:
         fresh.close()
     p.check("after refusals")
+
+
+def _room(pool, n):
+    """What grow asks for with n entries, and compact with 1."""
+    return 4 * max(pool.n_rows + 3 * n + 64, pool.n_pages + pool.n_rows + 2 * n + 65, 3 * pool.n_pages + 64)
+
+
+@pytest.mark.parametrize("n_rows,stride,page_size", [(40, 300, 8), (5000, 70, 16)])
+def test_calls_that_keep_no_rows_need_no_room_for_them(ctx, n_rows, stride, page_size):  # noqa: F811
+    """Exactly what the header says is enough for each call, nothing behind it is written, and a byte less is refused."""
+    p = Pool(3000, n_rows, stride, page_size=page_size, seed=12)
+    n = 300
+    most = B.pages_workspace_bytes(p.pool, n)
+    buf = torch.full((most + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    need = {"grow": _room(p.pool, n), "fork": most, "compact": _room(p.pool, 1)}
+    assert max(need["grow"], need["compact"]) < most
+    own = B.Context(0)  # noqa: F811
+    try:
+        own.ensure_pages_workspace = lambda pool, entries: None
+        rows = [(i * 7) % n_rows for i in range(n)]
+        for name, call in (("grow", lambda: p.grow(own, rows, [1 + (i * 31) % 140 for i in range(n)])),
+                           ("fork", lambda: p.fork(own, rows, [(r + 1) % n_rows for r in rows])),
+                           ("compact", lambda: p.compact(own))):
+            size = need[name]
+            own.set_workspace(buf[:size - 1])
+            one = _int32([0] * n)
+            _refused(5, *((own.pages_compact, p.pool, p.result) if name == "compact" else (getattr(own, "pages_" + name), p.pool, one, one, p.result)))
+            p.check("refused")
+            buf.fill_(0x5a)
+            own.set_workspace(buf[:size])
+            p.check(name, call())
+            assert bool((buf[size:] == 0x5a).all()), f"{name} wrote behind its workspace"
+            assert p.counts_match()
+    finally:
+        torch.cuda.synchronize()
+        own.close()
+
+
+def test_a_pool_at_the_limits_grows(ctx):  # noqa: F811
+    """Entries and tables for which a fork would take tebibytes: the calls that keep no rows are not refused."""
+    stride, n = 1 << 20, 1 << 20
+    refs, lens = torch.zeros(64, dtype=torch.int32, device=DEV), _int32([0] * 4)
+    table = torch.full((4, stride), -1, dtype=torch.int32, device=DEV)
+    pool, missing = B.page_pool(refs, table, lens, 16, []), _int32([-1])
+    rows = torch.full((n,), -1, dtype=torch.int32, device=DEV)
+    rows[77], rows[n - 1] = 2, 3
+    new = torch.full((n,), 40, dtype=torch.int32, device=DEV)
+    own = B.Context(0)  # noqa: F811
+    try:
+        assert B.pages_workspace_bytes(pool, n) > 1 << 42
+        own.set_workspace(torch.zeros(_room(pool, n), dtype=torch.uint8, device=DEV))
+        own.pages_grow(pool, rows, new, missing)
+        assert int(missing) == 0 and lens.tolist() == [0, 0, 40, 40] and table[2:, :4].tolist() == [[0, 1, 2, -1], [3, 4, 5, -1]]
+        _refused(5, own.pages_fork, pool, rows, new, missing)
+        own.pages_free(pool, _int32([2]))
+        own.pages_compact(pool, missing)
+        assert int(missing) == 3 and table[3, :4].tolist() == [0, 1, 2, -1] and refs[:4].tolist() == [1, 1, 1, 0]
+    finally:
+        torch.cuda.synchronize()
+        own.close()
