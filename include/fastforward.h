@@ -581,8 +581,8 @@ ff_status ff_pages_workspace_bytes(const ff_page_pool *pool, int32_t n, size_t *
 
 /* Copies page from[i] of every part to page to[i] (dev int32 [n] each; i with a page
  * out of range, or onto itself, is passed over).  A page that is both read and
- * written, or written twice, ends with either's contents, in part.  Counts and tables stay as they are;
- * no workspace. */
+ * written, or written twice, ends with either's contents, in part.  Of the pool only n_pages and the
+ * parts count; counts and tables stay as they are; no workspace. */
 ff_status ff_pages_copy(ff_ctx *ctx, const ff_page_pool *pool, int32_t n,
                         const int32_t *from, const int32_t *to);
 

@@ -489,7 +489,7 @@ ff_status check_norm(ff_ctx *ctx, const ff_norm *n, NormSpec *out) {
 }
 int log2_of(int v) {
   int s = 0;
-  while ((1 << s) < v) ++s;
+  while ((1ll << s) < v) ++s;
   return s;
 }
 AttnParams attn_params(const ff_attention &a, int32_t n_tokens, int32_t n_seqs) {

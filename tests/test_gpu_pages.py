@@ -478,3 +478,12 @@ def test_a_pool_at_the_limits_grows(ctx):  # noqa: F811
     finally:
         torch.cuda.synchronize()
         own.close()
+
+
+@pytest.mark.parametrize("page_size", [0, -1, -(1 << 31), 24, (1 << 30) + 1, (1 << 31) - 1])
+def test_copies_of_pages_of_any_size(ctx, page_size):  # noqa: F811
+    """A copy takes the parts alone: what else the pool says does not matter to it."""
+    p = Pool(20, 2, 3, seed=13)
+    p.pool.page_size, p.pool.n_rows, p.pool.table_stride, p.pool.refs, p.pool.page_table, p.pool.lens = page_size, 0, -1, None, None, None
+    p.copy(ctx, [3, 0, 19, 7], [4, 1, 18, 7])
+    p.check(f"pages of {page_size}")
