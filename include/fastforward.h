@@ -142,8 +142,12 @@ ff_status ff_set_workspace(ff_ctx *ctx, void *dev_ptr, size_t bytes);
 /* Options: "validate" (0/1, default 0): ff_sparse_ffn first checks on the GPU
  * that every index row is ascending, in range and -1 padded, synchronises,
  * and returns FF_ERR_INDEX instead of launching if not (while the stream is
- * capturing a HIP graph the call returns FF_ERR_INVALID_ARG); ff_chunk_attention
- * checks its starts, lengths and pages in the same way.  "small_path" (0/1,
+ * capturing a HIP graph the call returns FF_ERR_INVALID_ARG); in the same way
+ * ff_chunk_attention, ff_chunk_attention8 and ff_selected_attention check their
+ * starts, lengths and pages, ff_cache8_append, ff_page_means and ff_select_pages
+ * their starts and lengths (pages out of range they pass over), and ff_pages_grow
+ * the lengths of rows that are there.  The other calls check none of what lies on
+ * the GPU.  "small_path" (0/1,
  * default 1): calls with at most 8 tokens in total (the generation-time
  * regime) use gather-GEMV kernels, which read every selected weight row once
  * at HBM speed, instead of the MFMA tiles; 0 forces the tiles.
@@ -601,7 +605,8 @@ ff_status ff_pages_fork(ff_ctx *ctx, const ff_page_pool *pool, int32_t n,
 /* Row rows[i] gets the pages for new_lens[i] tokens (free ones, whose contents are
  * what they were), or gives back those that it has beyond them; lens follow.  More
  * tokens than a row's entries have pages for are cut to these, and missing does not count
- * them: the row's length is then below new_lens[i].  A row
+ * them: the row's length is then below new_lens[i] (with the option "validate":
+ * FF_ERR_INDEX, and nothing is changed).  A row
  * that is cut inside a page that other rows hold (tokens taken back behind a fork)
  * still shares it: fork it onto itself before it is added to.
  * missing as above (pages that are given back serve the next call, not this one). */

@@ -523,6 +523,18 @@ void set_cache8(AttnParams *p, const ff_paged_cache8 &c) {
   p->k_scale = c.k_scale; p->v_scale = c.v_scale;
   p->page_shift = log2_of(c.page_size); p->scale_shift = log2_of(c.scale_tokens); p->n_pages = c.n_pages;
 }
+// The option "validate": starts and lengths, and for attention the pages that it reads (the other calls pass over pages out of range).
+ff_status validate_chunks(ff_ctx *ctx, AttnParams p, bool pages) {
+  if (!ctx->validate) return FF_OK;
+  if (!pages) p.table = nullptr;
+  ff_status st = begin_validate(ctx);
+  if (st != FF_OK) return st;
+  FF_HIP(ctx, ff_launch_validate_pages(p, ctx->flag_dev, ctx->stream));
+  if ((st = read_flag(ctx)) != FF_OK) return st;
+  if (ctx->flag_host[0] != 0)
+    return fail(ctx, FF_ERR_INDEX, "sequence %d has a chunk%s out of range", ctx->flag_host[0] - 1, pages ? ", a length or a page" : " or a length");
+  return FF_OK;
+}
 // Attention over pages of either kind (one of the two is given), of selected ones with a table to each key head.
 ff_status attend_pages(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int32_t n_seqs, const void *q, int64_t q_stride,
                        const int32_t *starts, const int32_t *lens, int32_t max_chunk, const ff_paged_cache *cache, const ff_paged_cache8 *cache8,
@@ -551,13 +563,7 @@ ff_status attend_pages(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, int
     p.part_bytes = ctx->ws_bytes;
   }
   FF_HIP(ctx, hipSetDevice(ctx->device));
-  if (ctx->validate) {
-    if ((st = begin_validate(ctx)) != FF_OK) return st;
-    FF_HIP(ctx, ff_launch_validate_pages(p, ctx->flag_dev, ctx->stream));
-    if ((st = read_flag(ctx)) != FF_OK) return st;
-    if (ctx->flag_host[0] != 0)
-      return fail(ctx, FF_ERR_INDEX, "sequence %d has a chunk, a length or a page out of range", ctx->flag_host[0] - 1);
-  }
+  if ((st = validate_chunks(ctx, p, true)) != FF_OK) return st;
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
   FF_HIP(ctx, ff_launch_attention(p, a->head_dim, max_chunk, ctx->stream));
   prof_end(&ctx->prof, ctx->stream);
@@ -1154,6 +1160,7 @@ ff_status ff_cache8_append(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens,
   p.k_codes = static_cast<uint8_t *>(cache->k); p.v_codes = static_cast<uint8_t *>(cache->v);
   p.k_scale = cache->k_scale; p.v_scale = cache->v_scale;
   FF_HIP(ctx, hipSetDevice(ctx->device));
+  if ((st = validate_chunks(ctx, p.seqs, false)) != FF_OK) return st;
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
   FF_HIP(ctx, ff_launch_append8(p, a->head_dim, ctx->stream));
   prof_end(&ctx->prof, ctx->stream);
@@ -1186,6 +1193,7 @@ ff_status ff_page_means(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens, in
   set_chunks(&p.seqs, chunk_starts, context_lens, page_table, table_stride, 1);
   p.means = means;
   FF_HIP(ctx, hipSetDevice(ctx->device));
+  if ((st = validate_chunks(ctx, p.seqs, false)) != FF_OK) return st;
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
   FF_HIP(ctx, ff_launch_page_means(p, a->head_dim, ctx->stream));
   prof_end(&ctx->prof, ctx->stream);
@@ -1256,6 +1264,7 @@ ff_status ff_select_pages(ff_ctx *ctx, const ff_attention *a, const ff_selection
     p.scores = static_cast<double *>(ctx->ws);
   }
   FF_HIP(ctx, hipSetDevice(ctx->device));
+  if ((st = validate_chunks(ctx, p.seqs, false)) != FF_OK) return st;
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
   FF_HIP(ctx, ff_launch_select_pages(p, a->head_dim, ctx->stream));
   prof_end(&ctx->prof, ctx->stream);
@@ -1321,6 +1330,12 @@ ff_status ff_pages_grow(ff_ctx *ctx, const ff_page_pool *pool, int32_t n, const 
   if ((st = pool_params(ctx, pool, n, rows, new_lens, kRoom, &p)) != FF_OK) return st;
   p.to = rows; p.new_lens = new_lens; p.result = missing;
   FF_HIP(ctx, hipSetDevice(ctx->device));
+  if (ctx->validate) {
+    if ((st = begin_validate(ctx)) != FF_OK) return st;
+    FF_HIP(ctx, ff_launch_validate_grow(p, ctx->flag_dev, ctx->stream));
+    if ((st = read_flag(ctx)) != FF_OK) return st;
+    if (ctx->flag_host[0] != 0) return fail(ctx, FF_ERR_INDEX, "entry %d has a length that its row cannot have", ctx->flag_host[0] - 1);
+  }
   prof_begin(&ctx->prof, FF_STAGE_GLUE, ctx->stream);
   FF_HIP(ctx, ff_launch_pages_grow(p, ctx->stream));
   prof_end(&ctx->prof, ctx->stream);

@@ -1364,14 +1364,13 @@ __global__ __launch_bounds__(256) void ff_attn_join_rows_kernel(AttnParams p, At
 // one wavefront per sequence and table
 __global__ __launch_bounds__(64) void ff_attn_validate_kernel(AttnParams p, int32_t *flag) {
   const int s = blockIdx.x, lane = threadIdx.x;
-  const int32_t *table = p.table + s * p.seq_tables + (size_t)blockIdx.y * p.head_tables;
   const int a = p.starts[s], b = p.starts[s + 1];
   bool bad = a < 0 || b < a || b > p.T || p.lens[s] < 0 || p.lens[s] > most_keys(p);
   const Seq q = seq_of(p, s);
   const int first = p.window > 0 ? max(0, q.keys - q.n + 1 - min(p.window, kMaxKeys)) >> p.page_shift : 0;
-  const int pages = q.n > 0 ? (int)(((long)q.keys + (1 << p.page_shift) - 1) >> p.page_shift) : 0;
+  const int pages = p.table && q.n > 0 ? (int)(((long)q.keys + (1 << p.page_shift) - 1) >> p.page_shift) : 0;
   for (int i = first + lane; i < pages; i += 64) {
-    const int page = table[i];
+    const int page = p.table[s * p.seq_tables + (size_t)blockIdx.y * p.head_tables + i];
     bad = bad || page < 0 || page >= p.n_pages;
   }
   if (__any(bad) && lane == 0) atomicMax(flag, s + 1);

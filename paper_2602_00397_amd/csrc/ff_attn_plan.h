@@ -65,7 +65,7 @@ size_t ff_attention_part_bytes(int n_heads, int n_kv, int head_dim, int n_tokens
 size_t ff_attention_need(const AttnParams &p, int head_dim, int max_chunk);   // what this call takes
 hipError_t ff_attention_init();   // raises the kernels' dynamic-LDS limits
 hipError_t ff_launch_attention(const AttnParams &p, int head_dim, int max_chunk, hipStream_t s);
-// flag[0] is set to 1 + a sequence whose start, length or page is out of range.  The caller zeroes flag[0] first.
+// flag[0] is set to 1 + a sequence whose start, length or (if there is a table) page is out of range.  The caller zeroes flag[0] first.
 hipError_t ff_launch_validate_pages(const AttnParams &p, int32_t *flag, hipStream_t s);
 
 // The write of new tokens into pages in 8 bits: seqs has starts, lens, tables and the pages' shape (scale_shift with it).

@@ -23,5 +23,7 @@ size_t ff_pages_ints(int64_t n, int32_t n_pages, int32_t n_rows, int32_t table_s
 hipError_t ff_launch_pages_copy(const ff_page_part *parts, int n_parts, int32_t n_pages, int32_t n, const int32_t *from, const int32_t *to, hipStream_t s);
 hipError_t ff_launch_pages_fork(const PoolParams &p, const ff_page_part *parts, int n_parts, hipStream_t s);
 hipError_t ff_launch_pages_grow(const PoolParams &p, hipStream_t s);
+// flag[0] is set to 1 + an entry of a grow whose length its row cannot have.  The caller zeroes flag[0] first.
+hipError_t ff_launch_validate_grow(const PoolParams &p, int32_t *flag, hipStream_t s);
 hipError_t ff_launch_pages_free(const PoolParams &p, hipStream_t s);
 hipError_t ff_launch_pages_compact(const PoolParams &p, const ff_page_part *parts, int n_parts, hipStream_t s);

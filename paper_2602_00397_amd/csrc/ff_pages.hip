@@ -303,6 +303,11 @@ __global__ __launch_bounds__(kPlanThreads) void ff_pages_grow_kernel(PoolParams 
   for (int i = wave; i < p.n; i += kPlanThreads / 64) apply(i, lane, 64, p.n <= kPlanThreads ? firsts[i] : fresh(&w.first[i]));
 }
 
+__global__ __launch_bounds__(kThreads) void ff_pages_validate_kernel(PoolParams p, int32_t *flag) {
+  const int i = blockIdx.x * kThreads + threadIdx.x;
+  if (i < p.n && is_row(p, p.to[i]) && p.new_lens[i] != clamped_len(p, p.new_lens[i])) atomicMax(flag, i + 1);
+}
+
 // (a row that is listed twice: whoever takes an entry gives its page back)
 __global__ __launch_bounds__(kThreads) void ff_pages_free_kernel(PoolParams p) {
   for (int i = blockIdx.x; i < p.n; i += gridDim.x) {
@@ -430,6 +435,11 @@ hipError_t ff_launch_pages_fork(const PoolParams &p, const ff_page_part *parts, 
 
 hipError_t ff_launch_pages_grow(const PoolParams &p, hipStream_t s) {
   hipLaunchKernelGGL(ff_pages_grow_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+hipError_t ff_launch_validate_grow(const PoolParams &p, int32_t *flag, hipStream_t s) {
+  hipLaunchKernelGGL(ff_pages_validate_kernel, dim3((p.n + kThreads - 1) / kThreads), dim3(kThreads), 0, s, p, flag);
   return hipGetLastError();
 }
 

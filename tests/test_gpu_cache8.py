@@ -664,3 +664,27 @@ def test_append_behind_the_end_of_the_table(ctx, h, n_seqs):  # noqa: F811
     full = [i for i in range(n_seqs) if lens[i] - new[i] >= most]
     pages = c.table[full].long().flatten()
     assert full and all(torch.equal(x[pages], y[pages]) for x, y in zip(a.held(), held))
+
+
+def test_the_validate_option_of_the_write(ctx):  # noqa: F811
+    """Starts and lengths out of range are refused and nothing is written; pages out of range are passed over as without it."""
+    ctx.set_option("validate", 1)
+    try:
+        a = Append(H8B, [40, 30], [100, 80], page_size=16, scale_tokens=8, seed=6, behind=3)
+        most = a.c.table.shape[1] * 16
+        for what, change in (("longer than the table", lambda: a.lens[0].fill_(most + 1)), ("negative length", lambda: a.lens[1].fill_(-3)),
+                             ("end", lambda: a.starts[2].fill_(74)), ("descending starts", lambda: a.starts[1].fill_(-9))):
+            starts, lens, held = a.starts.clone(), a.lens.clone(), a.held()
+            change()
+            _refused(4, a.run, ctx)
+            assert all(torch.equal(x.nan_to_num(-1.0), y.nan_to_num(-1.0)) if x.is_floating_point() else torch.equal(x, y) for x, y in zip(a.held(), held)), what
+            a.starts.copy_(starts)
+            a.lens.copy_(lens)
+        a.run_and_check(ctx, "validated")
+        a.lens[0] = most
+        a.run_and_check(ctx, "a full table")
+        a.c.table[1, 0] = 1 << 30
+        a.c.table[0, 6] = -5
+        a.run_and_check(ctx, "pages passed over")
+    finally:
+        ctx.set_option("validate", 0)

@@ -487,3 +487,20 @@ def test_copies_of_pages_of_any_size(ctx, page_size):  # noqa: F811
     p.pool.page_size, p.pool.n_rows, p.pool.table_stride, p.pool.refs, p.pool.page_table, p.pool.lens = page_size, 0, -1, None, None, None
     p.copy(ctx, [3, 0, 19, 7], [4, 1, 18, 7])
     p.check(f"pages of {page_size}")
+
+
+def test_the_validate_option(ctx):  # noqa: F811
+    """Lengths that a row cannot have are refused before anything is changed; rows that are not there are passed over."""
+    p = Pool(40, 5, 6, seed=14)
+    ctx.ensure_pages_workspace(p.pool, 300)
+    ctx.set_option("validate", 1)
+    try:
+        p.check("grow", p.grow(ctx, [0, 1, -1, 5], [96, 3, 1 << 30, -1]))
+        for rows, lens in (([0, 1, 2], [96, 97, 5]), ([3], [-1]), ([3], [2147483647]), (list(range(-295, 5)), [7] * 299 + [97])):
+            _refused(4, ctx.pages_grow, p.pool, _int32(rows), _int32(lens), p.result)
+            p.check("refused")
+        p.check("fork", p.fork(ctx, [0, 1], [2, 3]))
+        p.check("longest", p.grow(ctx, [0, 1, 2, 3], [96, 96, 0, 96]))
+    finally:
+        ctx.set_option("validate", 0)
+    p.check("cut", p.grow(ctx, [4], [97]))

@@ -460,3 +460,29 @@ def test_means_behind_the_end_of_the_table(ctx, n_seqs):  # noqa: F811
             want[page] = s.c.values("k", page).mean(dim=1).float()
     s.update(ctx)
     assert torch.equal(s.means, want)
+
+
+def test_the_validate_option_of_means_and_selection(ctx):  # noqa: F811
+    s = Step(_heads(TINY), [3, 20], [400, 90], 2, 2)
+    s.all_means()
+    s.run(ctx)
+    most = s.table.shape[1] * 16
+    ctx.set_option("validate", 1)
+    try:
+        for what, change in (("longer than the table", lambda: s.lens[0].fill_(most + 1)), ("negative length", lambda: s.lens[1].fill_(-1)),
+                             ("end", lambda: s.starts[2].fill_(24)), ("descending starts", lambda: s.starts[1].fill_(-1))):
+            starts, lens, means, tables = s.starts.clone(), s.lens.clone(), s.means.clone(), s.tables.clone()
+            change()
+            _refused(4, s.update, ctx)
+            _refused(4, s.select, ctx)
+            assert torch.equal(s.means, means) and torch.equal(s.tables, tables), what
+            s.starts.copy_(starts)
+            s.lens.copy_(lens)
+        s.run(ctx)
+        s.check("validated")
+        s.table[1, 1] = -5                                      # (passed over by the means, scored as page 0, listed as it is)
+        s.update(ctx)
+        s.select(ctx)
+        s.check_selection("a page out of range")
+    finally:
+        ctx.set_option("validate", 0)
