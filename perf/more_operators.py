@@ -361,6 +361,7 @@ def _prepare_own(c, s):
     ctx = s["ctx"] = B.Context(0)
     if c["op"] in ("fork", "compact"):
         s["pool"] = B.page_pool(s["refs"], s["table"], s["lens"], c["page_size"], s["parts"])
+        s["grow_missing"] = _int32([-1])
         ctx.ensure_pages_workspace(s["pool"], s["rows"].numel())
         return
     n_tokens, n_seqs = s["q"].shape[0], c["n_seqs"]
@@ -421,8 +422,10 @@ def _run_own(c, s):
                                s["block_tables"], s["o"])
         return {x: s[x] for x in ("o", "means", "block_starts", "block_lens", "block_tables")}
     if c["op"] == "fork":
+        # (each call says how many pages it was short of; a program looks at both)
         ctx.pages_fork(s["pool"], s["sources"], s["targets"], s["missing"])
-        ctx.pages_grow(s["pool"], s["rows"], s["grown"], s["missing"])
+        ctx.pages_grow(s["pool"], s["rows"], s["grown"], s["grow_missing"])
+        s["missing"].add_(s["grow_missing"])
         return _pool_of(s)
     ctx.pages_free(s["pool"], s["rows"])
     ctx.pages_compact(s["pool"], s["live"])
