@@ -450,7 +450,8 @@ ff_status ff_chunk_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_token
  *                 the table first); with starts that do not ascend it is open which
  *                 tokens are.  So with the lengths that were asked of ff_pages_grow, not
  *                 those that the rows got, no token comes to the place of an earlier one
- *                 where a row or the pool is full
+ *                 where a row or the pool is full (in a table that began with -1
+ *                 everywhere: the page calls leave -1 behind a row's pages)
  * A block of scale_tokens tokens whose first place is written gets the least scale
  * for which its largest value stays within 448 (2^-110 at least, 2^80 at most);
  * one that is added to keeps the larger of its scale and that of the new tokens,
@@ -498,7 +499,7 @@ ff_status ff_page_means(ff_ctx *ctx, const ff_attention *a, int32_t n_tokens,
 /* Host arithmetic: most blocks that n_tokens tokens of n_seqs sequences are cut into
  * (min(n_tokens, n_tokens / query_block + n_seqs)), entries of a block's page table
  * (keep, and the most pages that a block's own tokens lie in), and the workspace that
- * ff_select_pages needs for so many blocks. */
+ * ff_select_pages needs for so many blocks (none where table_stride is at most keep). */
 ff_status ff_selection_blocks(const ff_selection *sel, int32_t n_tokens,
                               int32_t n_seqs, int32_t *n_blocks);
 ff_status ff_selection_pages(const ff_selection *sel, int32_t page_size,
@@ -510,7 +511,8 @@ ff_status ff_selection_workspace_bytes(const ff_attention *a, int32_t n_blocks,
  *   q, chunk_starts, context_lens, page_table, table_stride   as for ff_chunk_attention
  *                 (a->causal is 1, a->window 0; the scale does not matter)
  *   n_pages, page_size, means   of the cache; means as ff_page_means keeps them
- *   block_starts  dev int32 [n_blocks + 1] out, n_blocks of ff_selection_blocks: block
+ *   block_starts  dev int32 [n_blocks + 1] out, n_blocks of ff_selection_blocks (at most
+ *                 16384, FF_ERR_SHAPE: blocks are ff_selected_attention's sequences): block
  *                 b is rows [block_starts[b], block_starts[b + 1]); blocks behind the
  *                 last have none
  *   block_lens    dev int32 [n_blocks] out: keys of the block's pages, up to its last token's own
@@ -552,13 +554,14 @@ ff_status ff_selected_attention(ff_ctx *ctx, const ff_attention *a, int32_t n_to
  * Who holds which pages, on the GPU: row r of the table (a sequence, a beam) has
  * lens[r] tokens, and its first ceil(lens[r] / page_size) entries are pages; entries
  * behind those are not looked at.  refs[p] counts the entries that hold page p; 0:
- * the page is free.  The caller begins with zeros (and lens all 0), and from then on these
+ * the page is free.  The caller begins with zeros (lens all 0, the table best -1), and from then on these
  * calls keep the three together.  Everything about a page lies in the pool's parts: k
  * and v of every layer, scales, means.  Free pages are taken in ascending order, entries of
  * a call are served in theirs, and nothing depends on timing: the same call on the same state gives
  * the same tables.  Rows out of range are passed over, lengths are cut to [0,
  * table_stride * page_size], entries that are no page are not counted and not followed.
- * Calls that take entries of the same row twice: the last one counts. */
+ * Calls that take entries of the same row twice: the last one counts (of a fork also one
+ * whose from is out of range: the row then stays as it is). */
 typedef struct {
   void *data;            /* dev: page p is the page_bytes bytes from p * page_bytes on */
   int64_t page_bytes;    /* 1 to 2^32; quickest as a multiple of 16 */

@@ -1412,9 +1412,13 @@ hipError_t raise_limits() {
 // One token's keys go to a piece for every CU, and no more: its pieces are joined by one workgroup.  Many tokens' are cut finer, for
 // their lengths differ.  (Heads of 128, us with 256 / 512 / 1024 pieces: 8 key heads, one token over
 // 8191 keys, whose pieces were 256 / 128 / 64 keys long for it, 15.7 / 19.9 / 33.8, over 32768 28.6 / 32.0 / 44.3; 48 tokens over up to 16384 137 / 97 / 94.)
-// Over keys in 8 bits, which come in half the time, to fewer: 48 tokens over up to 16384 with 512 / 768 / 1024 / 2048 pieces 57.6 / 55.0 / 59.6 / 70.1.
-// Selected pages are as many for every block, so blocks enough for every CU stay whole: 48 of some 2100 keys in 256 (whole) / 512 / 1024 pieces
-// 51.4 / 54.3 / 58.0 with the selection.
+// Over keys in 8 bits, which come in half the time, to fewer: with 512 / 768 / 1024 pieces 8 key heads of 128, 48 tokens over up to 16384 keys
+// 49.7 / 46.5 / 50.4, all over 16384 303 / 281 / 291, 96 over up to 8192 60.9 / 53.6 / 52.3, 200 over up to 2000 49.5 / 52.2 / 52.0; 4 key heads, 48
+// tokens 40.2 / 38.4 / 46.7; heads of 64 27.3 / 28.2 / 31.2.
+// Selected pages are few for every token, long context or short, so they are not cut finer than for one token.  256 / 512 / 1024 pieces over 8 bits: 8
+// key heads of 128, 48 tokens with 32 pages of 64 kept, all of which have 2112 keys, 39.0 / 48.9 / 46.2, of contexts of up to 32768 (15 have some
+// 2100 keys, 22 fewer than 256) 26.3 / 29.7 / 32.8; 100 tokens with 16 kept, equal 44.8 / 44.8 / 63.0, ragged 31.4 / 29.5 / 35.7; 4 key heads, 48
+// equal 35.9 / 37.7 / 33.8, ragged 20.6 / 26.9 / 25.8; heads of 64 23.6 / 27.4 / 29.9, ragged 20.0 / 17.7 / 19.8.
 int few_target(long tiles, int n_kv, bool eight, bool selected) {
   if (selected || tiles * n_kv < 128) return kFewGrid / 2;
   return eight ? 3 * kFewGrid / 2 : 2 * kFewGrid;

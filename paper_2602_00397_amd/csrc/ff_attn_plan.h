@@ -48,7 +48,7 @@ struct AttnParams {
   // pages in 8 bits: k and v are codes, with a scale for every 2^scale_shift keys of a page and head; nullptr: bf16
   const float *k_scale = nullptr, *v_scale = nullptr;
   int32_t scale_shift = 0;
-  int32_t selected = 0;          // the tables are of selected pages: about as many keys for every sequence
+  int32_t selected = 0;          // the tables are of selected pages: no sequence has many keys
 };
 constexpr int kAttnCounters = 16384, kAttnSeqs = 16384;   // most sequences of a call
 constexpr int kMostItems = 1 << 24;      // a sequence's (tile, piece), and all of a call's, are counted up to this number

@@ -66,15 +66,17 @@ __device__ __forceinline__ Block block_of(const SelectParams &a, int x) {
 
 // ---- the best pages, in order ---------------------------------------------------------------------------------------------------
 // A workgroup to a block and key head scores the earlier pages and lists the best; where there are few blocks, several score and the last
-// of them to end lists.  It is a chain of latencies (one token over 2047 pages, 48 over up to 512, 8192 in blocks of 128 take
-// 12.0, 10.4 and 17.4 us with 512 threads, 13.8, 13.3 and 16.1 with 256; as two launches, scores and lists, 15.3, 16.1 and 24.0).  Blocks with no more earlier pages than are kept need no scores.
+// of them to end lists.  It is a chain of latencies (one token over 2047 pages, 48 over up to 512, 8192 in blocks of 128, each call repeated on one
+// state: 12.0, 10.5 and 17.3 us with 512 threads, 13.8, 13.3 and 16.1 with 256; as two launches, scores and lists, 15.3, 16.1 and 24.0; on three
+// states in turn, as traced, 13.6, 15.1 and 22.5).  Blocks with no more earlier pages than are kept need no scores.
 //
 // The list: the scores' range is cut into 1024 parts; those above the part that holds
 // the last page wanted are taken, and of that part's few the best, by counting for each how many are better.  (2047 pages of which 64
 // are kept 14.1 us by whole numbers alone, as below, 9.4 so.)
 // Where that part has too many, or scores are not finite, the scores are compared as whole numbers in their order: the range of those is
 // cut in 1024 until the part with the last one wanted has no more than are wanted of it, or is one number (then its first pages are); each
-// cut is ten bits of it, so there are at most seven.
+// cut is ten bits of it, so there are at most seven.  So are scores of more pages than are held, which are read again for each cut (one token over 4096
+// pages 15 us, 8192 44, 65536 272).
 constexpr int kSelectThreads = 512;
 constexpr int kBins = 1024, kHeld = 4096, kFew = 64;     // parts; scores that are held in LDS (of more pages they are read again); candidates of a part
 __device__ __forceinline__ uint64_t order_of(double s) {      // (-0 as +0; NaN by its bits)
